@@ -312,6 +312,113 @@ int mixkv_decode_attention(const void* K_cache, const void* V_cache,
                            int32_t head_dim, float softmax_scale, int32_t max_rows, float* out,
                            void* stream);
 
+/* A paged KV cache held in 4 bits: where decoding puts the rows of new tokens, and what it attends over when nothing,
+ * or not everything, is compressed away (no counterpart in the paper, whose caches stop growing at the end of
+ * prefill).  A page holds page_rows rows of K and V of ONE KV head, because compression leaves the heads of a sequence with
+ * different numbers of rows.
+ *
+ * Format.  The 128 values of a row are eight blocks of 16.  A value is a 4-bit code (a sign and one of 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6; the sign is the top bit) times the scale of its block (e4m3) times k_scale or v_scale.  A page is a run of
+ * tiles of 16 rows, MIXKV_PAGE_TILE_BYTES each, laid out as the matrix fragments of a warp take them; row
+ * 4 a + 2 j + b of a tile (a < 4; j, b < 2) has
+ *   K codes    at 512 j + 64 (2 a + b): 64 bytes, dimension 2 i in the low half of byte i
+ *   V codes    of block g at 1024 + 512 j + 64 g + 16 a + 8 b: 8 bytes, likewise
+ *   K scales   of blocks 2 t, 2 t + 1 at 2048 + 16 (2 a + b) + 4 t + 2 j
+ *   V scales   of block g at 2176 + 16 g + 4 a + 2 j + b
+ * code * scale has at most six significant bits: it is exact in fp16 and bf16. */
+enum { MIXKV_TYPE_BF16 = 0, MIXKV_TYPE_FP16 = 1 };
+#define MIXKV_PAGE_TILE_BYTES 2304
+#define MIXKV_PAGE_MAX_ROWS 256
+#define MIXKV_PAGES_MAX 32768      /* columns of a page table that a page selection takes */
+#define MIXKV_PAGED_MAX_QUERIES 128  /* q_tokens * gqa_ratio */
+
+typedef struct mixkv_pages {
+  void* pool;            /* device, 16-byte aligned: page p at p * mixkv_paged_page_bytes */
+  void* bounds_opt;      /* device fp16 [num_pages, 2, 128], 16-byte aligned, or NULL: elementwise minimum and maximum of
+                            the K values of a page, without k_scale (exact) */
+  const int32_t* table;  /* device [batch, kv_heads, max_pages]: page of a head's rows p * page_rows .. */
+  const int32_t* rows;   /* device [batch, kv_heads]: rows of every head, those that a call appends included */
+  int64_t num_pages;     /* pages in the pool */
+  int32_t max_pages;     /* columns of the table */
+  int32_t page_rows;     /* a multiple of 16, at most 256 */
+  int32_t batch, kv_heads;
+  int32_t head_dim;      /* 128 */
+  float k_scale, v_scale; /* > 0: a third factor of all values, for caches whose blocks are far from the range of e4m3
+                            (largest magnitudes of 0.1 to 2000 need none) */
+} mixkv_pages;
+
+/* Bytes of a page.  Host-only. */
+int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
+
+/* Appends rows to the cache: the last n rows of every head, where the n new rows of sequence b are tokens
+ * offsets[b] .. offsets[b + 1] - 1 of k and v (n = rows after the call minus rows before it: the caller counts them into
+ * c->rows first).  K is rotated by the tokens' positions on the way.
+ *   k, v            device, type `type`: head h of token i at i * row_stride + h * head_stride elements (both multiples of
+ *                   8; 16-byte aligned), num_tokens tokens
+ *   offsets_opt     device int32 [batch + 1], ascending; NULL: one token per sequence.  offsets_per_head != 0:
+ *                   [batch * kv_heads + 1], every head its own range of rows, head_stride is not used: K_out, V_out and
+ *                   out_row_offsets of a compressed layer as they are
+ *   max_new         upper bound on n; of more, a head's last max_new are written
+ *   cos_opt, sin_opt  device fp32 [table_len, rot_dim / 2], 16-byte aligned; both NULL: no rotation.  Dimension i of a
+ *                   pair becomes x cos - y sin, its partner y cos + x sin, in fp32; pairs are (i, i + rot_dim / 2), or
+ *                   with interleaved != 0 (2 i, 2 i + 1), below rot_dim (a multiple of 16, at most 128)
+ *   positions_opt   device int32 [num_tokens], needed with cos_opt: row of the tables.  It is not the row in the cache: a
+ *                   compressed cache has fewer rows than its sequence has tokens
+ * Rounding: the scale of a block is e4m3(min(max |x| / (6 k_scale), 448)), nearest even; a code is the nearest to
+ * x / (scale k_scale), ties to the even code, largest magnitude 6; a block of zeros, or one that is too small for e4m3,
+ * is zero; one that holds a NaN is NaN.  Every operation is rounded by itself, so codes are the same wherever
+ * they are computed.
+ * Bounds (if there are any) of a page that begins with a new row are set, those of a page that had rows are widened.
+ * Pages are written by one call at a time.  A token whose page (table entry outside the pool, row beyond the table or
+ * below zero), position or place in k lies outside gives MIXKV_ERR_INVALID_ARG in *status_dev and is not written. */
+int mixkv_paged_append(const mixkv_pages* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
+                       int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
+                       const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, const float* cos_opt,
+                       const float* sin_opt, int32_t table_len, int32_t rot_dim, int32_t interleaved,
+                       const int32_t* positions_opt, int32_t* status_dev, void* stream);
+
+/* The last n rows of every head back as dense rows: what mixkv_paged_append was given, rounded (and rotated).  offsets_opt,
+ * offsets_per_head and max_new as there (n = the number of rows reads the whole head).
+ *   k_out, v_out    device, type `type`, 16-byte aligned: [num_tokens, kv_heads, 128], or [num_tokens, 128] with
+ *                   offsets_per_head; rows that do not exist are not written */
+int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
+                     const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, void* stream);
+
+/* Pages of every (sequence, KV head) that a query would miss most: a page's score is the largest, over the query rows
+ * of the head, of sum_d max(q_d lo_d, q_d hi_d), with lo and hi its bounds: no key of the page has a larger product with q.
+ * The 128 terms are summed as neighbouring pairs, seven times over, in fp32 (the products are exact): the same scores
+ * wherever they are computed.  The first keep_first and the last keep_last pages go first, then NaN, then by score; ties go to the
+ * lower page.
+ *   q               device, type `type`: [batch, q_tokens, kv_heads * gqa_ratio, 128], strides in elements of the first
+ *                   two dimensions (multiples of 8), 16-byte aligned
+ *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call
+ *   top             pages to list
+ *   page_list       out, int32 [batch, kv_heads, top]: ascending columns of the page table, -1 behind the last
+ *   counts          out, int32 [batch, kv_heads]: min(top, pages of the head)
+ * Needs c->bounds_opt; at most MIXKV_PAGES_MAX pages per head (of max_rows), else MIXKV_ERR_UNSUPPORTED. */
+int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t type, int64_t q_batch_stride,
+                       int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows, int32_t top,
+                       int32_t keep_first, int32_t keep_last, int32_t* page_list, int32_t* counts, void* stream);
+
+/* Workspace of mixkv_paged_attention (any max_rows, with or without a list).  Asks the device for its SMs. */
+int mixkv_paged_workspace_size(const mixkv_pages* c, int32_t q_tokens, int32_t gqa_ratio, size_t* bytes);
+
+/* softmax(q K^T scale) V over the cache: q_tokens new tokens per sequence, the last of its rows (append theirs first).
+ * Token t attends to rows 0 .. rows - q_tokens + t of its KV head; a token that has no row gets zeros.
+ *   q               as in mixkv_paged_select; q_tokens * gqa_ratio <= MIXKV_PAGED_MAX_QUERIES
+ *   page_list_opt   device int32 [batch, kv_heads, top], counts_opt [batch, kv_heads]: attend to the rows of these
+ *                   pages only (ascending, as mixkv_paged_select lists them); NULL, NULL, 0: to all
+ *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call.  It steers how the rows of a head are
+ *                   split
+ *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned
+ * Logits, softmax statistics and sums are fp32, the weights enter the value sum as fp16.  softmax_scale 0 means
+ * 1 / sqrt(128).  A page outside the pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that
+ * sees a NaN, is NaN, and so is what a wait inside the kernel ran out on (there is no status word). */
+int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_t type, int64_t q_batch_stride,
+                          int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
+                          int32_t max_rows, const int32_t* page_list_opt, const int32_t* counts_opt, int32_t top,
+                          void* workspace, size_t workspace_bytes, void* out, void* stream);
+
 /* Number of kernels one mixkv_compress_layer[s] call WITH events enqueues, and the name of the
  * i-th of them (NULL when i is out of range), for the measurement hook.  The route depends on the
  * shape: fixed budgets take three kernels (pass1, pass2, tail; max pooling adds poolsum) while

@@ -42,7 +42,8 @@ EXPORTS = ("mixkv_default_params", "mixkv_workspace_size", "mixkv_scores", "mixk
            "mixkv_compress_layers_budgeted", "mixkv_layer_budget_schedule",
            "mixkv_similarity_workspace_size", "mixkv_similarity_map", "mixkv_decode_attention",
            "mixkv_selftest_bounded_wait", "mixkv_launches_for", "mixkv_stage_name_for",
-           "mixkv_device_check")
+           "mixkv_device_check", "mixkv_paged_page_bytes", "mixkv_paged_append", "mixkv_paged_read",
+           "mixkv_paged_select", "mixkv_paged_workspace_size", "mixkv_paged_attention")
 
 
 class MixKVError(RuntimeError):
@@ -57,6 +58,13 @@ class _CParams(C.Structure):
                 ("use_vnorm", C.c_int32), ("mix_mode", C.c_int32), ("budget_mode", C.c_int32),
                 ("budget", C.c_int32), ("ada_floor", C.c_float), ("eps", C.c_float),
                 ("softmax_scale", C.c_float)]
+
+
+class _CPages(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("bounds_opt", C.c_void_p), ("table", C.c_void_p), ("rows", C.c_void_p),
+                ("num_pages", C.c_int64), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
+                ("batch", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("k_scale", C.c_float), ("v_scale", C.c_float)]
 
 
 @dataclass
@@ -81,6 +89,21 @@ class Params:
                         self.pool_kernel, self.pool_mode, self.use_vnorm, self.mix_mode,
                         self.budget_mode, self.budget, self.ada_floor, self.eps,
                         self.softmax_scale)
+
+
+@dataclass
+class Pages:
+    """A paged 4-bit KV cache (``mixkv_pages`` in include/mixkv.h, which gives the format): pool [pages, bytes of a
+    page] uint8, table [batch, kv_heads, columns] int32, rows [batch, kv_heads] int32 (those that a call appends
+    included), bounds [pages, 2, 128] fp16 or None (page selection needs them).  The tensors are the caller's, which
+    gives pages out and counts rows; :func:`new_pages` makes them for a cache whose heads own their pages from the start."""
+    pool: torch.Tensor
+    table: torch.Tensor
+    rows: torch.Tensor
+    page_rows: int
+    bounds: Optional[torch.Tensor] = None
+    k_scale: float = 1.0
+    v_scale: float = 1.0
 
 
 _lib: Optional[C.CDLL] = None
@@ -133,6 +156,14 @@ def load_library() -> C.CDLL:
         lib.mixkv_similarity_map.argtypes = [vp, i32, i32, i32, i32, vp, sz, vp, vp, vp]
         lib.mixkv_decode_attention.argtypes = [vp, vp, vp, C.c_int64, vp, i32, i32, i32, i32, i32,
                                                C.c_float, i32, vp, vp]
+        lib.mixkv_paged_page_bytes.argtypes = [i32, C.POINTER(sz)]
+        lib.mixkv_paged_append.argtypes = [C.POINTER(_CPages), vp, vp, i32] + [C.c_int64] * 5 + [
+            vp, i32, i32, vp, vp, i32, i32, i32, vp, vp, vp]
+        lib.mixkv_paged_read.argtypes = [C.POINTER(_CPages), vp, vp, i32, C.c_int64, vp, i32, i32, vp]
+        lib.mixkv_paged_select.argtypes = [C.POINTER(_CPages), vp, i32, C.c_int64, C.c_int64] + [i32] * 6 + [vp, vp, vp]
+        lib.mixkv_paged_workspace_size.argtypes = [C.POINTER(_CPages), i32, i32, C.POINTER(sz)]
+        lib.mixkv_paged_attention.argtypes = [C.POINTER(_CPages), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float, i32,
+                                              vp, vp, i32, vp, sz, vp, vp]
         lib.mixkv_selftest_bounded_wait.argtypes = [vp, vp, vp]
         lib.mixkv_stage_name.restype = C.c_char_p
         lib.mixkv_stage_name.argtypes = [C.POINTER(_CParams), i32]
@@ -314,6 +345,87 @@ def decode_attention(K_cache: torch.Tensor, V_cache: torch.Tensor, out_row_offse
     [n_layers, batch, H*G, 128] fp32."""
     return (_host_module or _host()).decode_attention(K_cache, V_cache, out_row_offsets, q, kv_heads,
                                                       gqa_ratio, max_rows, softmax_scale, stream)
+
+
+def page_bytes(page_rows: int) -> int:
+    """mixkv_paged_page_bytes: bytes of a page of so many rows (a multiple of 16) of one KV head."""
+    out = C.c_size_t(0)
+    rc = load_library().mixkv_paged_page_bytes(page_rows, C.byref(out))
+    if rc != 0:
+        raise MixKVError(rc, "mixkv_paged_page_bytes")
+    return int(out.value)
+
+
+def new_pages(batch: int, kv_heads: int, max_rows: int, page_rows: int = 64, bounds: bool = False,
+              k_scale: float = 1.0, v_scale: float = 1.0, device="cuda") -> Pages:
+    """An empty cache with room for max_rows rows of every head.  The pages of a head follow one another in the pool;
+    a program that shares a pool between sequences fills its own table instead."""
+    n = -(-max_rows // page_rows)
+    total = batch * kv_heads * n
+    return Pages(pool=torch.empty((total, page_bytes(page_rows)), dtype=torch.uint8, device=device),
+                 table=torch.arange(total, dtype=torch.int32, device=device).view(batch, kv_heads, n),
+                 rows=torch.zeros((batch, kv_heads), dtype=torch.int32, device=device), page_rows=page_rows,
+                 bounds=torch.empty((total, 2, 128), dtype=torch.float16, device=device) if bounds else None,
+                 k_scale=k_scale, v_scale=v_scale)
+
+
+def paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+                 max_new: int = 1, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                 positions: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """mixkv_paged_append: writes the last rows of every head (count them into ``pages.rows`` first), rounded to 4 bits.
+    k, v [tokens, kv_heads, 128] bf16 or fp16 (tokens and heads may be strided): sequence b's are ``offsets[b] ..
+    offsets[b + 1] - 1`` (int32 device tensor), at most ``max_new`` of them; without offsets one per sequence.  Or compact
+    rows [rows, 128] with an offset per (sequence, head): ``K_out``, ``V_out`` and ``out_row_offsets`` of
+    :func:`compress_layer`.  With ``cos`` and ``sin`` [length, rot_dim / 2] fp32, K is rotated by the tables' rows
+    ``positions`` (int32, one per token).  ``status``: an int32 device word, zeroed by the caller, that receives
+    MIXKV_ERR_INVALID_ARG for rows without a place."""
+    (_host_module or _host()).paged_append(pages, k, v, offsets, max_new, cos, sin, positions, interleaved, status, stream)
+
+
+def paged_read(pages: Pages, tokens: int, dtype: torch.dtype = torch.bfloat16,
+               offsets: Optional[torch.Tensor] = None, max_new: int = 1, compact: bool = False, stream=None):
+    """mixkv_paged_read: the last rows of every head as dense K, V [tokens, kv_heads, 128] (``compact``: [tokens, 128],
+    with an offset per (sequence, head)); offsets and max_new as in :func:`paged_append`.  Rows that do not exist are
+    left as they come from the allocator."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("paged_read gives bf16 or fp16")
+    return (_host_module or _host()).paged_read(pages, tokens, dtype == torch.float16, offsets, max_new, compact, stream)
+
+
+def paged_workspace(pages: Pages, q: torch.Tensor, max_rows: Optional[int] = None) -> torch.Tensor:
+    """A workspace for :func:`paged_attention` and :func:`paged_sparse_attention` calls with such pages and queries, of
+    any ``max_rows``; it belongs to one call at a time."""
+    return torch.empty((_host_module or _host()).paged_workspace_size(pages, q), dtype=torch.uint8, device=q.device)
+
+
+def _seen_rows(pages: Pages, max_rows: Optional[int]) -> int:
+    return pages.table.size(2) * pages.page_rows if max_rows is None else max_rows
+
+
+def paged_select(pages: Pages, q: torch.Tensor, top: int, max_rows: Optional[int] = None, keep_first: int = 1,
+                 keep_last: int = 1, stream=None):
+    """mixkv_paged_select: (page_list [batch, kv_heads, top], counts [batch, kv_heads]) int32, the pages whose bounds
+    promise the largest products with the queries q [batch, tokens, kv_heads * gqa_ratio, 128]."""
+    return (_host_module or _host()).paged_select(pages, q, top, _seen_rows(pages, max_rows), keep_first, keep_last, stream)
+
+
+def paged_attention(pages: Pages, q: torch.Tensor, max_rows: Optional[int] = None,
+                    page_list: Optional[torch.Tensor] = None, counts: Optional[torch.Tensor] = None,
+                    softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """mixkv_paged_attention: q [batch, tokens, kv_heads * gqa_ratio, 128] bf16 or fp16, the newest tokens of every
+    sequence (append theirs first) -> the same shape and type.  ``max_rows``: upper bound on ``pages.rows`` (default:
+    what the table has room for).  With a page list only its pages are read."""
+    return (_host_module or _host()).paged_attention(pages, q, _seen_rows(pages, max_rows), page_list, counts,
+                                                     softmax_scale, workspace, stream)
+
+
+def paged_sparse_attention(pages: Pages, q: torch.Tensor, top: int, max_rows: Optional[int] = None,
+                           keep_first: int = 1, keep_last: int = 1, softmax_scale: float = 0.0,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """:func:`paged_select`, then :func:`paged_attention` over what it lists, in one call -> (out, page_list, counts)."""
+    return (_host_module or _host()).paged_sparse_attention(pages, q, top, _seen_rows(pages, max_rows), keep_first,
+                                                            keep_last, softmax_scale, workspace, stream)
 
 
 def selftest_bounded_wait(stream=None):

@@ -44,6 +44,11 @@ struct Api {
   decltype(&mixkv_similarity_workspace_size) sim_ws_size;
   decltype(&mixkv_similarity_map) sim_map;
   decltype(&mixkv_decode_attention) decode;
+  decltype(&mixkv_paged_append) paged_append;
+  decltype(&mixkv_paged_read) paged_read;
+  decltype(&mixkv_paged_select) paged_select;
+  decltype(&mixkv_paged_workspace_size) paged_ws_size;
+  decltype(&mixkv_paged_attention) paged_attention;
 } api;
 PyObject* g_error = nullptr;   // binding.MixKVError
 
@@ -53,6 +58,7 @@ struct Names {
       *budget_mode, *budget, *ada_floor, *eps, *softmax_scale, *cuda_stream;
   PyObject *s_comp, *s_ex, *s_div, *rbar, *status, *idx, *counts, *idx_offsets, *K_out, *V_out,
       *out_row_offsets;
+  PyObject *pool, *table, *rows, *page_rows, *bounds, *k_scale, *v_scale;
 } nm;
 
 // A Python exception is set; unwinds to the entry point.
@@ -415,6 +421,7 @@ PyObject* compress_outputs(PyObject* given, PyObject* aux, const int64_t lead, c
 struct Ref {   // an owned reference
   PyObject* o;
   explicit Ref(PyObject* x) : o(x) {}
+  Ref(Ref&& x) noexcept : o(x.release()) {}
   ~Ref() { Py_XDECREF(o); }
   PyObject* release() {
     PyObject* r = o;
@@ -593,6 +600,289 @@ PyObject* py_decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- the paged 4-bit cache
+void want(const bool ok, const char* what) {
+  if (!ok) fail(PyExc_AssertionError, what);
+}
+// A mixkv_pages from a binding.Pages; `pool` and the other tensors stay alive through the attributes they are held by.
+struct PagesArg {
+  mixkv_pages c;
+  std::vector<Ref> held;
+  at::Tensor pool;
+  const at::Tensor& attr(PyObject* o, PyObject* name, const bool optional = false) {
+    PyObject* v = PyObject_GetAttr(o, name);
+    if (!v) throw Raised();
+    held.emplace_back(v);
+    static const at::Tensor none;
+    return optional && v == Py_None ? none : tensor(v);
+  }
+  explicit PagesArg(PyObject* o) {
+    if (!api.paged_append || !api.paged_read || !api.paged_select || !api.paged_ws_size || !api.paged_attention)
+      fail(PyExc_OSError, "the library has no paged cache");
+    held.reserve(4);
+    pool = attr(o, nm.pool);
+    const at::Tensor table = attr(o, nm.table), rows = attr(o, nm.rows), bounds = attr(o, nm.bounds, true);
+    want(pool.is_cuda() && pool.dim() == 2 && pool.is_contiguous() && pool.element_size() == 1,
+         "pool must be a contiguous CUDA tensor of bytes [pages, bytes of a page]");
+    want(table.scalar_type() == at::kInt && table.dim() == 3 && table.is_contiguous() && table.device() == pool.device(),
+         "table must be a contiguous int32 tensor [batch, kv_heads, pages] on the pool's device");
+    want(rows.scalar_type() == at::kInt && rows.dim() == 2 && rows.is_contiguous() && rows.size(0) == table.size(0) &&
+             rows.size(1) == table.size(1) && rows.device() == pool.device(),
+         "rows must be a contiguous int32 tensor [batch, kv_heads] on the pool's device");
+    c.page_rows = attr_int(o, nm.page_rows);
+    want(c.page_rows > 0 && pool.size(1) * 16 == (int64_t)c.page_rows * MIXKV_PAGE_TILE_BYTES,
+         "a page of the pool must have page_rows / 16 tiles");
+    if (bounds.defined())
+      want(bounds.scalar_type() == at::kHalf && bounds.is_contiguous() && bounds.dim() == 3 &&
+               bounds.size(0) == pool.size(0) && bounds.size(1) == 2 && bounds.size(2) == 128 &&
+               bounds.device() == pool.device(),
+           "bounds must be a contiguous fp16 tensor [pages, 2, 128] on the pool's device");
+    c.pool = pool.data_ptr();
+    c.bounds_opt = bounds.defined() ? bounds.data_ptr() : nullptr;
+    c.table = ip(table), c.rows = ip(rows);
+    c.num_pages = pool.size(0);
+    c.max_pages = int32(table.size(2), "mixkv_pages"), c.batch = int32(table.size(0), "mixkv_pages");
+    c.kv_heads = int32(table.size(1), "mixkv_pages"), c.head_dim = 128;
+    c.k_scale = attr_float(o, nm.k_scale), c.v_scale = attr_float(o, nm.v_scale);
+  }
+};
+int32_t paged_type(const at::ScalarType t) {
+  want(t == at::kBFloat16 || t == at::kHalf, "bf16 or fp16 is expected");
+  return t == at::kBFloat16 ? MIXKV_TYPE_BF16 : MIXKV_TYPE_FP16;
+}
+// Offsets of the new rows: None or an int32 tensor of n + 1 words.
+const int32_t* row_offsets(PyObject* o, const int64_t n, const PagesArg& pages) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  want(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n + 1 && t.device() == pages.pool.device(),
+       "offsets must be a contiguous int32 tensor [batch + 1] (compact rows: [batch * kv_heads + 1]) on the pool's device");
+  return ip(t);
+}
+
+// paged_append(pages, k, v, offsets, max_new, cos, sin, positions, interleaved, status, stream)
+PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 11, [&]() -> PyObject* {
+    const char* what = "mixkv_paged_append";
+    const PagesArg pages(a[0]);
+    const mixkv_pages& c = pages.c;
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]);
+    const bool compact = k.dim() == 2;
+    want((compact || (k.dim() == 3 && k.size(1) == c.kv_heads)) && k.sizes() == v.sizes() && k.size(-1) == 128 &&
+             k.stride(-1) == 1 && v.stride(-1) == 1 && k.device() == pages.pool.device() && v.device() == k.device() &&
+             k.scalar_type() == v.scalar_type(),
+         "k and v must be of one type and shape, [tokens, kv_heads, 128] or compact rows [rows, 128], on the pool's device");
+    const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), pages);
+    want(!compact || offsets, "compact rows need offsets");
+    want(offsets || k.size(0) == c.batch, "without offsets there is one token per sequence");
+    const int32_t max_new = int32(a[4], what);
+    const float *cosv = nullptr, *sinv = nullptr;
+    const int32_t* positions = nullptr;
+    int32_t table_len = 0, rot = 0;
+    if (a[5] != Py_None) {
+      const at::Tensor &cs = tensor(a[5]), &sn = tensor(a[6]), &pos = tensor(a[7]);
+      want(cs.scalar_type() == at::kFloat && cs.dim() == 2 && cs.is_contiguous() && sn.scalar_type() == at::kFloat &&
+               sn.is_contiguous() && sn.sizes() == cs.sizes() && cs.device() == k.device() && sn.device() == k.device(),
+           "cos and sin must be contiguous fp32 tensors [positions, rot_dim / 2] on the pool's device");
+      want(pos.scalar_type() == at::kInt && pos.is_contiguous() && pos.numel() == k.size(0) && pos.device() == k.device(),
+           "positions must be a contiguous int32 tensor, one for every token, on the pool's device");
+      cosv = fp(cs), sinv = fp(sn), positions = ip(pos);
+      table_len = int32(cs.size(0), what), rot = int32(2 * cs.size(1), what);
+    } else {
+      want(a[6] == Py_None, "sin without cos");
+    }
+    const bool interleaved = truth(a[8]);
+    int32_t* status = nullptr;
+    if (a[9] != Py_None) {
+      const at::Tensor& t = tensor(a[9]);
+      want(t.scalar_type() == at::kInt && t.is_cuda() && t.numel() >= 1, "status must be an int32 CUDA tensor");
+      status = ip(t);
+    }
+    const CallStream stream(a[10], k);
+    const int32_t type = paged_type(k.scalar_type());
+    int rc = MIXKV_OK;
+    if (k.size(0) > 0) {
+      const Unlocked u;
+      rc = api.paged_append(&c, k.data_ptr(), v.data_ptr(), type, k.size(0), k.stride(0), compact ? 0 : k.stride(1),
+                            v.stride(0), compact ? 0 : v.stride(1), offsets, compact, max_new, cosv, sinv, table_len, rot,
+                            interleaved, positions, status, stream.handle);
+    }
+    check_status(rc, what);
+    Py_RETURN_NONE;
+  });
+}
+
+// paged_read(pages, tokens, fp16, offsets, max_new, compact, stream) -> (k, v)
+PyObject* py_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const char* what = "mixkv_paged_read";
+    const PagesArg pages(a[0]);
+    const mixkv_pages& c = pages.c;
+    const int64_t tokens = int32(a[1], what);
+    const bool half = truth(a[2]), compact = truth(a[5]);
+    const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), pages);
+    want(tokens >= 0 && (!compact || offsets), "compact rows need offsets");
+    const int32_t max_new = int32(a[4], what);
+    const CallStream stream(a[6], pages.pool);
+    at::Tensor k, v;
+    int rc = MIXKV_OK;
+    {
+      const Unlocked u;
+      const at::ScalarType type = half ? at::kHalf : at::kBFloat16;
+      std::vector<int64_t> size = {tokens, c.kv_heads, 128};
+      if (compact) size.erase(size.begin() + 1);
+      k = empty(size, type, pages.pool), v = empty(size, type, pages.pool);
+      if (tokens > 0)
+        rc = api.paged_read(&c, k.data_ptr(), v.data_ptr(), half ? MIXKV_TYPE_FP16 : MIXKV_TYPE_BF16, tokens, offsets,
+                            compact, max_new, stream.handle);
+    }
+    check_status(rc, what);
+    Ref kr(THPVariable_Wrap(k)), vr(THPVariable_Wrap(v));
+    if (!kr.o || !vr.o) throw Raised();
+    return PyTuple_Pack(2, kr.o, vr.o);
+  });
+}
+
+// q [batch, tokens, kv_heads * gqa, 128] of a paged call.
+struct PagedQuery {
+  const at::Tensor& q;
+  int32_t type, tokens, gqa;
+  PagedQuery(PyObject* o, const PagesArg& pages) : q(tensor(o)) {
+    want(q.dim() == 4 && q.size(0) == pages.c.batch && q.size(2) % pages.c.kv_heads == 0 && q.size(3) == 128 &&
+             (q.size(2) <= 1 || q.stride(2) == 128) && q.stride(3) == 1 && q.device() == pages.pool.device(),
+         "q must be [batch, tokens, kv_heads * gqa_ratio, 128], a token's heads packed, on the pool's device");
+    type = paged_type(q.scalar_type());
+    tokens = int32(q.size(1), "q"), gqa = int32(q.size(2) / pages.c.kv_heads, "q");
+  }
+};
+size_t paged_space(const PagesArg& pages, const PagedQuery& q) {
+  size_t need = 0;
+  check_status(api.paged_ws_size(&pages.c, q.tokens, q.gqa, &need), "mixkv_paged_workspace_size");
+  return need;
+}
+// paged_workspace_size(pages, q)
+PyObject* py_paged_workspace_size(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 2, [&]() -> PyObject* {
+    const PagesArg pages(a[0]);
+    return PyLong_FromSize_t(paged_space(pages, PagedQuery(a[1], pages)));
+  });
+}
+struct PagedSpace {   // the caller's workspace or one of the call's own
+  at::Tensor own;
+  void* data = nullptr;
+  size_t bytes = 0;
+  PagedSpace(PyObject* o, const PagesArg& pages, const PagedQuery& q) {
+    if (o != Py_None) {
+      const at::Tensor& t = tensor(o);
+      want(t.is_cuda() && t.is_contiguous() && t.device() == pages.pool.device(),
+           "workspace must be a contiguous tensor on the pool's device");
+      data = t.data_ptr(), bytes = t.nbytes();
+    } else {
+      bytes = paged_space(pages, q);
+    }
+  }
+  void fill(const PagesArg& pages) {   // (without the interpreter lock)
+    if (!data) own = empty({(int64_t)bytes}, at::kByte, pages.pool), data = own.data_ptr();
+  }
+};
+
+// paged_select(pages, q, top, max_rows, keep_first, keep_last, stream) -> (list, counts)
+PyObject* py_paged_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const char* what = "mixkv_paged_select";
+    const PagesArg pages(a[0]);
+    const PagedQuery q(a[1], pages);
+    const int32_t top = int32(a[2], what), rows = int32(a[3], what), first = int32(a[4], what), last = int32(a[5], what);
+    if (top < 1) check_status(MIXKV_ERR_INVALID_ARG, what);
+    const CallStream stream(a[6], pages.pool);
+    at::Tensor list, counts;
+    int rc;
+    {
+      const Unlocked u;
+      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool);
+      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool);
+      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
+                            last, ip(list), ip(counts), stream.handle);
+    }
+    check_status(rc, what);
+    Ref l(THPVariable_Wrap(list)), c(THPVariable_Wrap(counts));
+    if (!l.o || !c.o) throw Raised();
+    return PyTuple_Pack(2, l.o, c.o);
+  });
+}
+
+// paged_attention(pages, q, max_rows, list, counts, softmax_scale, workspace, stream)
+PyObject* py_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> PyObject* {
+    const char* what = "mixkv_paged_attention";
+    const PagesArg pages(a[0]);
+    const PagedQuery q(a[1], pages);
+    const int32_t rows = int32(a[2], what);
+    const int32_t *list = nullptr, *counts = nullptr;
+    int32_t top = 0;
+    if (a[3] != Py_None) {
+      const at::Tensor &l = tensor(a[3]), &c = tensor(a[4]);
+      want(l.scalar_type() == at::kInt && l.dim() == 3 && l.is_contiguous() && l.size(0) == pages.c.batch &&
+               l.size(1) == pages.c.kv_heads && c.scalar_type() == at::kInt && c.is_contiguous() &&
+               c.numel() == (int64_t)pages.c.batch * pages.c.kv_heads && l.device() == pages.pool.device() &&
+               c.device() == pages.pool.device(),
+           "page lists and counts must be contiguous int32 tensors [batch, kv_heads, top] and [batch, kv_heads]");
+      list = ip(l), counts = ip(c), top = int32(l.size(2), what);
+    }
+    const double scale = PyFloat_AsDouble(a[5]);
+    if (PyErr_Occurred()) throw Raised();
+    const CallStream stream(a[7], pages.pool);
+    PagedSpace ws(a[6], pages, q);
+    at::Tensor out;
+    int rc;
+    {
+      const Unlocked u;
+      ws.fill(pages);
+      out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
+      rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, (float)scale,
+                               rows, list, counts, top, ws.data, ws.bytes, out.data_ptr(), stream.handle);
+    }
+    check_status(rc, what);
+    return THPVariable_Wrap(out);
+  });
+}
+
+// paged_sparse_attention(pages, q, top, max_rows, keep_first, keep_last, softmax_scale, workspace, stream)
+//   -> (out, list, counts)
+PyObject* py_paged_sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const PagesArg pages(a[0]);
+    const PagedQuery q(a[1], pages);
+    const char* what = "mixkv_paged_select";
+    const int32_t top = int32(a[2], what), rows = int32(a[3], what), first = int32(a[4], what), last = int32(a[5], what);
+    if (top < 1) check_status(MIXKV_ERR_INVALID_ARG, what);
+    const double scale = PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) throw Raised();
+    const CallStream stream(a[8], pages.pool);
+    PagedSpace ws(a[7], pages, q);
+    at::Tensor list, counts, out;
+    int rc;
+    {
+      const Unlocked u;
+      ws.fill(pages);
+      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool);
+      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool);
+      out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
+      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
+                            last, ip(list), ip(counts), stream.handle);
+      if (rc == MIXKV_OK) {
+        what = "mixkv_paged_attention";
+        rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa,
+                                 (float)scale, rows, ip(list), ip(counts), top, ws.data, ws.bytes, out.data_ptr(),
+                                 stream.handle);
+      }
+    }
+    check_status(rc, what);
+    Ref o(THPVariable_Wrap(out)), l(THPVariable_Wrap(list)), c(THPVariable_Wrap(counts));
+    if (!o.o || !l.o || !c.o) throw Raised();
+    return PyTuple_Pack(3, o.o, l.o, c.o);
+  });
+}
+
 // setup(path of libmixkv.so, error class): resolves the library's entry points.
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject* {
@@ -604,6 +894,9 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
       fn = reinterpret_cast<std::decay_t<decltype(fn)>>(dlsym(lib, name));
       if (!fn) fail(PyExc_OSError, name);
     };
+    auto find = [&](auto& fn, const char* name) {   // (a library without the paged cache: the first call on one says so)
+      fn = reinterpret_cast<std::decay_t<decltype(fn)>>(dlsym(lib, name));
+    };
     get(api.scores, "mixkv_internal_scores");
     get(api.select, "mixkv_internal_select");
     get(api.layer, "mixkv_compress_layer_traced");
@@ -613,6 +906,11 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     get(api.sim_ws_size, "mixkv_similarity_workspace_size");
     get(api.sim_map, "mixkv_similarity_map");
     get(api.decode, "mixkv_decode_attention");
+    find(api.paged_append, "mixkv_paged_append");
+    find(api.paged_read, "mixkv_paged_read");
+    find(api.paged_select, "mixkv_paged_select");
+    find(api.paged_ws_size, "mixkv_paged_workspace_size");
+    find(api.paged_attention, "mixkv_paged_attention");
     Py_XSETREF(g_error, Py_NewRef(a[1]));
     Py_RETURN_NONE;
   });
@@ -626,6 +924,12 @@ PyMethodDef methods[] = {{"setup", FAST(py_setup)},
                          {"compress_layers", FAST(py_compress_layers)},
                          {"similarity_map", FAST(py_similarity_map)},
                          {"decode_attention", FAST(py_decode_attention)},
+                         {"paged_append", FAST(py_paged_append)},
+                         {"paged_read", FAST(py_paged_read)},
+                         {"paged_workspace_size", FAST(py_paged_workspace_size)},
+                         {"paged_select", FAST(py_paged_select)},
+                         {"paged_attention", FAST(py_paged_attention)},
+                         {"paged_sparse_attention", FAST(py_paged_sparse_attention)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mixkv_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -636,7 +940,8 @@ PyMODINIT_FUNC PyInit__mixkv_host() {
   NAME(kv_heads), NAME(gqa_ratio), NAME(head_dim), NAME(window), NAME(pool_kernel), NAME(pool_mode),
       NAME(use_vnorm), NAME(mix_mode), NAME(budget_mode), NAME(budget), NAME(ada_floor), NAME(eps),
       NAME(softmax_scale), NAME(cuda_stream), NAME(s_comp), NAME(s_ex), NAME(s_div), NAME(rbar), NAME(status),
-      NAME(idx), NAME(counts), NAME(idx_offsets), NAME(K_out), NAME(V_out), NAME(out_row_offsets);
+      NAME(idx), NAME(counts), NAME(idx_offsets), NAME(K_out), NAME(V_out), NAME(out_row_offsets),
+      NAME(pool), NAME(table), NAME(rows), NAME(page_rows), NAME(bounds), NAME(k_scale), NAME(v_scale);
 #undef NAME
   return PyModule_Create(&module);
 }

@@ -1,0 +1,109 @@
+// The paged 4-bit cache (format: include/mixkv.h): where things lie, and the small conversions its kernels share.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "internal_api.h"
+#include "tc_common.cuh"
+
+namespace mixkv {
+
+constexpr int kPageTile = 16;                                // rows of a tile
+constexpr int kTileBytes = MIXKV_PAGE_TILE_BYTES;
+constexpr int kTileV = 1024, kTileKs = 2048, kTileVs = 2176;  // V codes, K scales, V scales inside a tile
+static_assert(kTileBytes == kTileVs + 128, "a tile");
+
+// What kernels take of a mixkv_pages.
+struct PagePool {
+  unsigned char* pool;
+  __half* bounds;
+  const int* table;
+  const int* rows;
+  long long num_pages;
+  int max_pages, page_rows, tiles;   // tiles of a page
+  int H;
+  float k_scale, v_scale;
+};
+
+inline int check_pages(const mixkv_pages* c, PagePool* p) {
+  if (!c || !c->pool || !c->table || !c->rows) return MIXKV_ERR_INVALID_ARG;
+  if (c->num_pages < 1 || c->max_pages < 1 || c->batch < 1 || c->kv_heads < 1 || !(c->k_scale > 0.f) ||
+      !(c->v_scale > 0.f) || c->k_scale > 3e38f || c->v_scale > 3e38f)
+    return MIXKV_ERR_INVALID_ARG;
+  if (c->page_rows < kPageTile || c->page_rows % kPageTile || c->page_rows > MIXKV_PAGE_MAX_ROWS)
+    return MIXKV_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(c->pool) & 15u) || (reinterpret_cast<uintptr_t>(c->bounds_opt) & 15u) ||
+      (reinterpret_cast<uintptr_t>(c->table) & 3u) || (reinterpret_cast<uintptr_t>(c->rows) & 3u))
+    return MIXKV_ERR_INVALID_ARG;
+  if (c->head_dim != kHeadDim) return MIXKV_ERR_UNSUPPORTED;
+  if ((long long)c->batch * c->kv_heads > (1 << 24) || (long long)c->max_pages * c->page_rows > (1ll << 30) ||
+      c->num_pages > 0x7fffffffll)
+    return MIXKV_ERR_UNSUPPORTED;
+  *p = PagePool{static_cast<unsigned char*>(c->pool), static_cast<__half*>(c->bounds_opt), c->table, c->rows,
+                c->num_pages, c->max_pages, c->page_rows, c->page_rows / kPageTile, c->kv_heads, c->k_scale, c->v_scale};
+  return MIXKV_OK;
+}
+
+// First byte of tile `t` of page `id` (offsets pass 32 bits: a pool of 2^31 bytes is 14.9 million rows).
+__device__ __forceinline__ unsigned char* tile_ptr(const PagePool& p, const int id, const int t) {
+  return p.pool + ((long long)id * p.tiles + t) * kTileBytes;
+}
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T x);
+template <>
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <>
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
+
+// Two adjacent 16-bit values of a word, widened.
+template <typename T>
+__device__ __forceinline__ float2 widen2(uint32_t w);
+template <>
+__device__ __forceinline__ float2 widen2<__nv_bfloat16>(uint32_t w) {
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 widen2<__half>(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t narrow2(float x, float y);   // x in the low half
+template <>
+__device__ __forceinline__ uint32_t narrow2<__nv_bfloat16>(float x, float y) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t narrow2<__half>(float x, float y) {
+  const __half2 v = __floats2half2_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The four bytes of a word, two codes each, as four fp16 pairs (low code in the low half).
+__device__ __forceinline__ void codes_to_f16(const uint32_t w, uint32_t (&r)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+      : "r"(w));
+}
+// Two scales (the halves of a 16-bit word) as an fp16 pair.
+__device__ __forceinline__ uint32_t scales_to_f16(const uint32_t w16) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)w16));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(const uint32_t a, const uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+}  // namespace mixkv

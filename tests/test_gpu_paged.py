@@ -1,0 +1,479 @@
+"""GPU parity of the paged 4-bit cache (append, read back, page selection, attention) against its plain definition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_plain as plain
+from paper_2510_20707_b200 import binding
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def f32(t):
+    return t.float().cpu().numpy()
+
+
+class Cache:
+    """A cache of `lens` [batch][heads] rows behind a shuffled page table; every byte starts as 0xff (scales of NaN)."""
+
+    def __init__(self, lens, page=32, bounds=False, ks=1.0, vs=1.0, seed=0, spare=2, room=0):
+        lens = np.asarray(lens)
+        rng = np.random.default_rng(seed)
+        count = -(-np.maximum(lens, room) // page)
+        cols, total = max(1, int(count.max())), int(count.sum())
+        table = np.full((*lens.shape, cols), -1, np.int32)
+        table[np.arange(cols) < count[..., None]] = rng.permutation(total + spare)[:total]
+        self.lens, self.table, self.page = lens, table, page
+        n = total + spare
+        self.pages = binding.Pages(
+            pool=torch.full((n, binding.page_bytes(page)), 0xFF, dtype=torch.uint8, device="cuda"),
+            table=torch.from_numpy(table).cuda(), rows=torch.from_numpy(lens.astype(np.int32)).cuda(), page_rows=page,
+            bounds=torch.full((n, 2, 128), 7.0, dtype=torch.float16, device="cuda") if bounds else None,
+            k_scale=ks, v_scale=vs)
+
+    def pool(self):
+        return self.pages.pool.cpu().numpy()
+
+    def rows_of(self, b, h):
+        k, v = plain.get_rows(self.pool(), self.table[b, h], self.page, int(self.lens[b, h]))
+        return k * self.pages.k_scale, v * self.pages.v_scale
+
+    def fill(self, seed=1, k_gain=1.0, dtype=torch.bfloat16, positions=None):
+        """Random rows everywhere, one offset per (sequence, head)."""
+        flat = self.lens.reshape(-1)
+        off = torch.from_numpy(np.concatenate([[0], flat.cumsum()]).astype(np.int32)).cuda()
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        n = int(flat.sum())
+        k, v = (torch.randn((max(n, 1), 128), generator=gen, device="cuda") for _ in range(2))
+        k[:, 3::31] *= 3.0
+        k, v = (k * k_gain).to(dtype)[:n], v.to(dtype)[:n]
+        binding.paged_append(self.pages, k, v, offsets=off, max_new=max(1, int(flat.max())))
+        return k, v, off
+
+
+def expect_rows(cache, token_rows, kx, vx):
+    """The bytes that fp32 rows kx, vx [n, 128] leave: token_rows [n] of (b, h, row)."""
+    want = np.full(cache.pages.pool.shape, 0xFF, np.uint8)
+    tiles = want.reshape(-1, plain.TILE_BYTES)
+    kc, ks = plain.quantise(kx, cache.pages.k_scale)
+    vc, vs = plain.quantise(vx, cache.pages.v_scale)
+    per = cache.page // 16
+    for i, (b, h, r) in enumerate(token_rows):
+        t = int(cache.table[b, h, r // cache.page]) * per + r % cache.page // 16
+        plain.put_row(tiles[t], r % 16, kc[i], ks[i], vc[i], vs[i])
+    return want, plain.values(kc, ks), plain.values(vc, vs)
+
+
+def expect_bounds(cache, token_rows, kv, start):
+    """Bounds of pages, by fp64 minima and maxima of all rows a page has; kv[(b, h, r)] -> values."""
+    want = np.full((cache.pages.pool.shape[0], 2, 128), 7.0)
+    pages = {}
+    for i, (b, h, r) in enumerate(token_rows):
+        pages.setdefault((b, h, r // cache.page), []).append(kv[i])
+    for (b, h, p), rows in pages.items():
+        x = np.stack(rows)
+        want[cache.table[b, h, p]] = x.min(0), x.max(0)
+    return want
+
+
+def rope_tables(n, rot, seed=0):
+    a = np.arange(n)[:, None] * 10000.0 ** (-np.arange(rot // 2) / (rot // 2))[None]
+    return np.cos(a).astype(np.float32), np.sin(a).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype,page,rot,inter,H", [
+    ("bf16", 16, 128, False, 3), ("fp16", 32, 64, True, 1), ("bf16", 64, 32, False, 2), ("fp16", 128, 16, True, 4),
+    ("bf16", 256, 0, False, 2), ("fp16", 48, 96, False, 5)])
+def test_append_and_read_back(dtype, page, rot, inter, H):
+    # new rows of several sequences (none, one, a page and more) behind rows that are there, K and V slices of one tensor
+    new, old = np.array([0, 1, 17, 2 * page + 5, 15]), np.array([3, page - 1, 2, page // 2 + 1, 0])
+    B, N = len(new), int(new.sum())
+    c = Cache((old + new)[:, None].repeat(H, 1), page, ks=0.5, vs=2.0, bounds=True, seed=page)
+    off = np.concatenate([[0], new.cumsum()]).astype(np.int32)
+    gen = torch.Generator(device="cuda").manual_seed(page)
+    qkv = torch.randn((N, 3 * H, 128), generator=gen, device="cuda").to(TYPES[dtype])
+    k, v = qkv[:, H:2 * H], qkv[:, 2 * H:]
+    pos = np.random.default_rng(1).integers(0, 5000, N).astype(np.int32)
+    cos, sin = rope_tables(5000, rot) if rot else (None, None)
+    dev = lambda a: None if a is None else torch.from_numpy(a).cuda()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    kw = dict(offsets=dev(off), max_new=int(new.max()))
+    binding.paged_append(c.pages, k, v, cos=dev(cos), sin=dev(sin), positions=dev(pos) if rot else None,
+                         interleaved=inter, status=status, **kw)
+    assert status.item() == 0
+    kx, vx = f32(k), f32(v)
+    if rot:
+        kx = np.stack([plain.rotate(kx[:, h], cos[pos], sin[pos], inter) for h in range(H)], 1)
+    where = [(b, h, int(old[b]) + i) for b in range(B) for i in range(new[b]) for h in range(H)]
+    want, kv, vv = expect_rows(c, where, kx.reshape(-1, 128), vx.reshape(-1, 128))
+    assert np.array_equal(c.pool(), want)
+    # pages that had rows keep what was in their bounds (7.0 here), those that begin with a new row are set
+    got = c.pages.bounds.double().cpu().numpy()
+    bounds = expect_bounds(c, where, kv, old)
+    for b in range(B):
+        if new[b] and old[b] % page:
+            ids = c.table[b, :, old[b] // page]
+            bounds[ids, 0], bounds[ids, 1] = np.minimum(bounds[ids, 0], 7.0), np.maximum(bounds[ids, 1], 7.0)
+    assert np.array_equal(got, bounds)
+    kr, vr = binding.paged_read(c.pages, N, TYPES[dtype], **kw)
+    back = lambda x, s: torch.from_numpy((x * s).reshape(N, H, 128)).to(TYPES[dtype])
+    assert torch.equal(kr.cpu(), back(kv, 0.5)) and torch.equal(vr.cpu(), back(vv, 2.0))
+
+
+def test_tokens_one_by_one_leave_what_one_call_leaves():
+    B, H, page, n = 3, 2, 16, 37
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((B, n, H, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    whole, steps = (Cache(np.full((B, H), n), page, bounds=True, seed=5) for _ in range(2))
+    off = torch.arange(0, B * n + 1, n, dtype=torch.int32, device="cuda")
+    binding.paged_append(whole.pages, k.reshape(-1, H, 128), v.reshape(-1, H, 128), offsets=off, max_new=n)
+    steps.pages.rows.zero_()
+    for i in range(n):
+        steps.pages.rows += 1
+        binding.paged_append(steps.pages, k[:, i], v[:, i])     # (strided: a token of every sequence)
+    assert torch.equal(whole.pages.pool, steps.pages.pool)
+    used = torch.from_numpy(np.unique(whole.table[whole.table >= 0])).cuda()
+    assert torch.equal(whole.pages.bounds[used], steps.pages.bounds[used])
+
+
+def test_compact_rows_of_a_compressed_layer():
+    # what compress_layer leaves (heads of different lengths) goes into pages as it is
+    lens = np.array([[40, 7, 0], [129, 64, 1]])
+    c = Cache(lens, 64, bounds=True, seed=2)
+    k, v, off = c.fill()
+    where = [(b, h, r) for b in range(2) for h in range(3) for r in range(lens[b, h])]
+    want, kv, vv = expect_rows(c, where, f32(k), f32(v))
+    assert np.array_equal(c.pool(), want)
+    kr, vr = binding.paged_read(c.pages, k.shape[0], offsets=off, max_new=129, compact=True)
+    assert torch.equal(kr.cpu(), torch.from_numpy(kv).bfloat16()) and torch.equal(vr.cpu(), torch.from_numpy(vv).bfloat16())
+
+
+def test_rounding_of_special_values():
+    rows = np.zeros((12, 128), np.float32)
+    rows[1] = np.linspace(-6, 6, 128)                      # ties among them
+    rows[2] = np.repeat([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0], 16) * np.tile([1, -1], 64)
+    rows[2, 15::16] = 6.0                                  # scale 1: every tie goes to the even code
+    rows[3] = 1e-4                                         # a scale below the smallest e4m3 number
+    rows[4] = 0.004
+    rows[5] = 30000.0                                      # beyond 6 * 448: saturates
+    rows[6, 5], rows[7, 20], rows[8, 127] = np.inf, -np.inf, np.nan
+    rows[6, :16] += 1.0
+    rows[9] = -0.0
+    rows[10] = np.random.default_rng(0).standard_normal(128)
+    rows[11, ::16] = 448.0
+    x = torch.from_numpy(rows).cuda().half()
+    c = Cache([[12]], 16, bounds=True)
+    off = torch.tensor([0, 12], dtype=torch.int32, device="cuda")
+    binding.paged_append(c.pages, x, x, offsets=off, max_new=12)
+    kc, ks = plain.quantise(f32(x))
+    got, _ = plain.get_rows(c.pool(), c.table[0, 0], 16, 12)
+    assert np.array_equal(got, plain.values(kc, ks), equal_nan=True)
+    assert np.isnan(got[8, 112:]).all() and np.isfinite(np.delete(got, 8, 0)).all() and got[5, 0] == 2688.0
+    lo, hi = c.pages.bounds[int(c.table[0, 0, 0])].double().cpu().numpy()
+    assert np.array_equal(lo, got.min(0), equal_nan=True) and np.array_equal(hi, got.max(0), equal_nan=True)
+
+
+def test_rows_without_a_place_are_reported_and_not_written():
+    k = torch.ones((4, 1, 128), device="cuda").bfloat16()
+    cos, sin = (torch.from_numpy(x).cuda() for x in rope_tables(8, 128))
+
+    def run(change, tokens=4, **kw):
+        c = Cache([[4], [5], [6], [7]], 16)
+        change(c)
+        before = c.pages.pool.clone()
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        binding.paged_append(c.pages, k[:tokens], k[:tokens], status=status, **kw)
+        ids = [int(x) for x in c.table[:, 0, 0]]
+        return status.item(), [not torch.equal(c.pages.pool[i], before[i]) for i in ids]
+
+    pos = lambda *p: dict(cos=cos, sin=sin, positions=torch.tensor(p, dtype=torch.int32, device="cuda"))
+    assert run(lambda c: None, **pos(0, 7, 1, 2)) == (0, [True] * 4)
+    assert run(lambda c: None, **pos(0, 8, -1, 2)) == (-1, [True, False, False, True])
+    assert run(lambda c: c.pages.table[1].fill_(c.pages.pool.shape[0])) == (-1, [True, False, True, True])
+    assert run(lambda c: c.pages.table[2].fill_(-5)) == (-1, [True, True, False, True])
+    assert run(lambda c: c.pages.rows[0].fill_(17)) == (-1, [False, True, True, True])       # beyond the table
+    assert run(lambda c: c.pages.rows[0].fill_(0)) == (-1, [False, True, True, True])        # a token more than rows
+    off = dict(offsets=torch.tensor([0, 1, 2, 3, 5], dtype=torch.int32, device="cuda"), max_new=2)   # one past the input
+    assert run(lambda c: None, **off) == (-1, [True] * 4)
+
+
+def check_attention(c, q, out, T, G, ctx=""):
+    """out against fp64.  A value may be off by the output's rounding, by the weights' (fp16, 2^-11 each, and 2^-25 of the
+    smallest next to a largest of 2^6 at least), and by what the logits' fp32 sums (128 products, their terms 2^-23 of the
+    largest partial sum each) do to the weights."""
+    unit = 2.0 ** -8 if q.dtype == torch.bfloat16 else 2.0 ** -11
+    got, qf = out.double().cpu().numpy(), q.double().cpu().numpy()
+    pool = c.pool()
+    for b in range(c.lens.shape[0]):
+        for h in range(c.lens.shape[1]):
+            n = int(c.lens[b, h])
+            K, V = plain.get_rows(pool, c.table[b, h], c.page, n)
+            K, V = K * c.pages.k_scale, V * c.pages.v_scale
+            want, mass, size = plain.attention(qf[b, :, h * G:(h + 1) * G], K, V, T, 1 / np.sqrt(128))
+            most = np.abs(V).max() if n else 0.0
+            off = 2.0 ** -23 * 128 * size[..., None] + 2.0 ** -20
+            tol = unit * np.abs(want) + mass * (2.0 ** -11 + 2 * off) + n * 2.0 ** -31 * most + 2.0 ** -24 * (unit < 2.0 ** -10)
+            bad = np.abs(got[b, :, h * G:(h + 1) * G] - want) > tol
+            assert not bad.any(), (ctx, b, h, n, int(bad.sum()))
+
+
+def queries(B, T, HG, dtype, seed=0, gain=1.5):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn((B, T, HG, 128), generator=gen, device="cuda") * gain).to(TYPES[dtype])
+
+
+@pytest.mark.parametrize("G,T,dtype,page", [
+    (1, 1, "bf16", 16), (7, 1, "fp16", 32), (8, 1, "bf16", 64), (9, 1, "bf16", 128), (16, 1, "fp16", 48),
+    (4, 2, "bf16", 16), (7, 5, "fp16", 64), (5, 3, "bf16", 256), (16, 8, "bf16", 32), (3, 11, "fp16", 16)])
+def test_lengths_at_the_edges_of_tiles_and_pages(G, T, dtype, page):
+    # no row, fewer than the tokens, one, a tile, a page, one more and one less; heads of their own lengths; what was
+    # never written holds scales of NaN
+    lens = np.array([[0, 1, 2], [15, 16, 17], [page - 1, page, page + 1], [2 * page + 3, 33, 5]])
+    c = Cache(lens, page, ks=0.5, vs=0.25, seed=G)
+    c.fill()
+    q = queries(4, T, 3 * G, dtype, G)
+    out = binding.paged_attention(c.pages, q)
+    assert out.dtype == q.dtype
+    check_attention(c, q, out, T, G)
+    assert (out[0, :, :G] == 0).all()
+
+
+@pytest.mark.parametrize("lens,G,T,page", [
+    ([[20000, 513], [4097, 1]], 4, 1, 64), ([[9000] * 8], 7, 1, 32), ([[70000]], 8, 2, 64), ([[6000], [33], [0]], 16, 3, 16)])
+def test_long_rows_split_over_many_ctas(lens, G, T, page):
+    lens = np.array(lens)
+    c = Cache(lens, page, seed=3)
+    c.fill()
+    q = queries(lens.shape[0], T, lens.shape[1] * G, "bf16", 1)
+    ws = binding.paged_workspace(c.pages, q)
+    ws.fill_(0xFF)       # nothing of it is read before it is written
+    out = binding.paged_attention(c.pages, q, workspace=ws)
+    check_attention(c, q, out, T, G)
+    for _ in range(5):
+        assert torch.equal(out, binding.paged_attention(c.pages, q, workspace=ws))
+
+
+@pytest.mark.parametrize("B,H,G,lo,hi", [(75, 8, 7, 0, 40), (37, 4, 16, 1, 300), (149, 1, 4, 100, 140), (19, 3, 12, 1, 700),
+                                         (300, 4, 4, 1, 90), (64, 8, 4, 10, 2000)])
+def test_many_units(B, H, G, lo, hi):
+    rng = np.random.default_rng(B)
+    lens = rng.integers(lo, hi + 1, (B, H))
+    lens[0, 0], lens[-1, -1] = lo, hi
+    c = Cache(lens, 16, seed=B)
+    c.fill()
+    q = queries(B, 1, H * G, "bf16", B)
+    out = binding.paged_attention(c.pages, q, max_rows=hi)
+    check_attention(c, q, out, 1, G)
+    assert torch.equal(out, binding.paged_attention(c.pages, q, max_rows=hi))
+
+
+def test_sharp_and_flat_rows():
+    # a row far above the rest late in a long head (the running reference moves), all rows alike (the weights of thousands),
+    # logits that fall steadily and rise steadily
+    n, G = 5000, 4
+    c = Cache([[n, n, n, n]], 64)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    base = torch.randn(128, generator=gen, device="cuda")
+    k = torch.randn((4, n, 128), generator=gen, device="cuda")
+    k[0, n - 700] = 8 * base
+    k[1] = base
+    ramp = torch.linspace(-6, 6, n, device="cuda").unsqueeze(1)
+    k[2], k[3] = ramp * base, -ramp * base
+    v = torch.randn((4, n, 128), generator=gen, device="cuda")
+    off = torch.arange(0, 4 * n + 1, n, dtype=torch.int32, device="cuda")
+    binding.paged_append(c.pages, k.reshape(-1, 128).bfloat16(), v.reshape(-1, 128).bfloat16(), offsets=off, max_new=n)
+    q = (base * torch.tensor([0.2, 1.0, 3.0, -1.0], device="cuda").repeat(4).unsqueeze(1)).view(1, 1, 16, 128).bfloat16()
+    check_attention(c, q, binding.paged_attention(c.pages, q), 1, G)
+
+
+@pytest.mark.parametrize("gain", [1e-30, 1e-6, 1e3, 1e20])
+def test_queries_of_any_size(gain):
+    c = Cache([[300]], 32)
+    c.fill(k_gain=0.0 if gain > 1e10 else 1.0)     # (logits of 1e20 would leave one row: keys of zero keep it even)
+    q = queries(1, 1, 3, "bf16", 0, gain)
+    check_attention(c, q, binding.paged_attention(c.pages, q), 1, 3)
+
+
+def test_not_a_number():
+    n, G, T = 100, 2, 3
+    c = Cache([[n, n, n]], 16)
+    k, v, off = c.fill()
+    k, v = k.view(3, n, 128), v.view(3, n, 128)
+    v[0, n - 1, 40] = float("nan")     # the last token's value: its own output alone, in that block
+    k[1, n - 2, 3] = float("nan")      # the last token but one's key: its own and the last one's
+    binding.paged_append(c.pages, k.reshape(-1, 128), v.reshape(-1, 128), offsets=off, max_new=n)
+    q = queries(1, T, 3 * G, "bf16")
+    q[0, 1, 2 * G, 7] = float("inf")   # a query: its own row
+    nan = torch.isnan(binding.paged_attention(c.pages, q)).cpu()
+    want = torch.zeros_like(nan)
+    want[0, 2, :G, 32:48] = True
+    want[0, 1:, G:2 * G] = True
+    want[0, 1, 2 * G] = True
+    assert torch.equal(nan, want)
+
+
+def test_a_page_outside_the_pool_counts_as_empty():
+    n, page, G = 100, 16, 4
+    for bad in (-1, 10 ** 6):
+        c = Cache([[n]], page)
+        c.fill()
+        keep = np.r_[0:32, 48:n]
+        K, V = c.rows_of(0, 0)
+        c.pages.table[0, 0, 2] = bad
+        q = queries(1, 1, G, "bf16")
+        want, mass, _ = plain.attention(q[0].double().cpu().numpy(), K[keep], V[keep], 1, 1 / np.sqrt(128))
+        got = binding.paged_attention(c.pages, q)[0].double().cpu().numpy()
+        assert (np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + mass * 2.0 ** -10).all()
+
+
+def test_strided_queries_streams_and_capture():
+    c = Cache([[3000, 20], [700, 701]], 32, bounds=True)
+    c.fill()
+    big = queries(2, 4, 10, "bf16")
+    q = big[:, 1:3, 2:8]            # two of four tokens, six of ten heads
+    want = binding.paged_attention(c.pages, q.contiguous())
+    assert torch.equal(binding.paged_attention(c.pages, q), want)
+    swant = binding.paged_sparse_attention(c.pages, q.contiguous(), 5)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = binding.paged_attention(c.pages, q, stream=side)
+    sout = binding.paged_sparse_attention(c.pages, q, 5, stream=side)
+    side.synchronize()
+    assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(sout, swant))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = binding.paged_attention(c.pages, q)
+        sout = binding.paged_sparse_attention(c.pages, q, 5)
+    out.zero_(), sout[0].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(sout, swant))
+
+
+def test_a_pool_beyond_four_gigabytes():
+    page, total = 64, 500_000         # 4.6 GB; the pages in use are the last ones
+    pool = torch.empty((total, binding.page_bytes(page)), dtype=torch.uint8, device="cuda")
+    c = Cache([[200, 130]], page, bounds=True)
+    pool[-16:] = 0xFF
+    c.table = np.where(c.table >= 0, total - 1 - c.table, -1).astype(np.int32)
+    c.pages.pool, c.pages.table = pool, torch.from_numpy(c.table).cuda()
+    c.pages.bounds = torch.zeros((total, 2, 128), dtype=torch.float16, device="cuda")
+    c.pool = lambda: torch.cat([torch.zeros((1, pool.shape[1]), dtype=torch.uint8), pool[-16:].cpu()]).numpy()
+    k, v, off = c.fill()
+    kr, vr = binding.paged_read(c.pages, 330, offsets=off, max_new=200, compact=True)
+    kc, ks = plain.quantise(f32(k))
+    assert torch.equal(kr.cpu(), torch.from_numpy(plain.values(kc, ks)).bfloat16())
+    real = c.table
+    c.table = np.where(real >= 0, real - (total - 17), -1)
+    q = queries(1, 1, 8, "bf16")
+    check_attention(c, q, binding.paged_attention(c.pages, q), 1, 4)
+    lists, counts = binding.paged_select(c.pages, q, 2)
+    out = binding.paged_attention(c.pages, q, page_list=lists, counts=counts)
+    assert torch.isfinite(out).all() and counts.tolist() == [[2, 2]]
+
+
+def oracle_select(c, q, T, G, top, first, last):
+    lists = np.full((*c.lens.shape, top), -1, np.int32)
+    bounds = f32(c.pages.bounds)
+    for b in range(c.lens.shape[0]):
+        for h in range(c.lens.shape[1]):
+            n = -(-int(c.lens[b, h]) // c.page)
+            ids = c.table[b, h, :n]
+            s = plain.scores(f32(q[b, :, h * G:(h + 1) * G]).reshape(-1, 128), bounds[ids, 0], bounds[ids, 1])
+            picked = plain.select(s, top, first, last)
+            lists[b, h, :len(picked)] = picked
+    return lists
+
+
+@pytest.mark.parametrize("B,H,G,T,page,top,first,last,hi,dtype", [
+    (2, 2, 7, 1, 16, 5, 1, 1, 700, "bf16"), (3, 1, 1, 1, 32, 1, 0, 0, 900, "fp16"), (1, 4, 4, 2, 16, 64, 0, 2, 20000, "bf16"),
+    (2, 3, 16, 1, 64, 7, 2, 3, 5000, "fp16"), (1, 1, 9, 4, 16, 3, 5, 5, 1000, "bf16"), (40, 8, 4, 1, 16, 9, 1, 1, 400, "bf16"),
+    (1, 2, 16, 8, 128, 200, 1, 1, 9000, "bf16")])
+def test_selected_pages(B, H, G, T, page, top, first, last, hi, dtype):
+    rng = np.random.default_rng(top)
+    lens = rng.integers(0, hi + 1, (B, H))
+    lens[0, 0], lens[-1, -1] = hi, rng.integers(0, page)
+    c = Cache(lens, page, bounds=True, seed=top)
+    c.fill()
+    q = queries(B, T, H * G, dtype, top)
+    lists, counts = binding.paged_select(c.pages, q, top, keep_first=first, keep_last=last)
+    want = oracle_select(c, q, T, G, top, first, last)
+    assert np.array_equal(lists.cpu().numpy(), want)
+    assert np.array_equal(counts.cpu().numpy(), (want >= 0).sum(-1))
+    out, lists2, counts2 = binding.paged_sparse_attention(c.pages, q, top, keep_first=first, keep_last=last)
+    assert torch.equal(lists, lists2) and torch.equal(counts, counts2)
+    assert torch.equal(out, binding.paged_attention(c.pages, q, page_list=lists, counts=counts))
+    # what is attended to: the rows of the listed pages
+    for b, h in [(0, 0), (B - 1, H - 1), (B // 2, H // 2)]:
+        K, V = c.rows_of(b, h)
+        rows = [r for p in want[b, h] if p >= 0 for r in range(p * page, min((p + 1) * page, lens[b, h]))]
+        qf = q[b, :, h * G:(h + 1) * G].double().cpu().numpy()
+        for t in range(T):
+            seen = [r for r in rows if r <= lens[b, h] - T + t]
+            ref, mass, size = plain.attention(qf[t:t + 1], K[seen], V[seen], 1, 1 / np.sqrt(128))
+            got = out[b, t, h * G:(h + 1) * G].double().cpu().numpy()
+            unit = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -11
+            tol = unit * np.abs(ref[0]) + mass[0] * (2.0 ** -11 + 2.0 ** -15 * size[0][:, None] + 2.0 ** -19) + 2.0 ** -24
+            assert (np.abs(got - ref[0]) <= tol).all(), (b, h, t)
+
+
+def test_equal_scores_go_to_the_lower_page_and_nan_goes_first():
+    c = Cache([[16 * 40]], 16, bounds=True)
+    c.fill()
+    ids = c.table[0, 0]
+    q = queries(1, 1, 2, "bf16")
+    c.pages.bounds.fill_(1.0)           # one score for all
+    assert binding.paged_select(c.pages, q, 6, keep_first=0, keep_last=0)[0].tolist() == [[[0, 1, 2, 3, 4, 5]]]
+    assert binding.paged_select(c.pages, q, 6, keep_first=1, keep_last=2)[0].tolist() == [[[0, 1, 2, 3, 38, 39]]]
+    c.pages.bounds[int(ids[17])] = float("nan")
+    assert binding.paged_select(c.pages, q, 3, keep_first=0, keep_last=0)[0].tolist() == [[[0, 1, 17]]]
+    assert binding.paged_select(c.pages, q, 1, keep_first=0, keep_last=1)[0].tolist() == [[[39]]]
+    c.pages.bounds.zero_()              # scores of 0 and -0 are equal
+    q[0, 0, :, ::2] *= -1
+    assert binding.paged_select(c.pages, q, 4, keep_first=0, keep_last=0)[0].tolist() == [[[0, 1, 2, 3]]]
+    assert binding.paged_select(c.pages, q, 50, keep_first=0, keep_last=0)[0][0, 0].tolist() == list(range(40)) + [-1] * 10
+
+
+def test_refusals():
+    c = Cache([[40, 40]], 16, bounds=True)
+    c.fill()
+    q = queries(1, 1, 4, "bf16")
+    k = torch.zeros((1, 2, 128), dtype=torch.bfloat16, device="cuda")
+    P = binding.Pages
+    change = lambda **kw: P(**{**c.pages.__dict__, **kw})
+
+    def _status(f):
+        with pytest.raises(binding.MixKVError) as e:
+            f()
+        return e.value.status
+
+    assert _status(lambda: binding.paged_attention(change(k_scale=0.0), q)) == -1
+    assert _status(lambda: binding.paged_attention(change(v_scale=float("nan")), q)) == -1
+    assert _status(lambda: binding.paged_attention(c.pages, q, max_rows=0)) == -1
+    assert _status(lambda: binding.paged_attention(c.pages, q, softmax_scale=-1.0)) == -1
+    assert _status(lambda: binding.paged_attention(c.pages, q, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))) == -3
+    assert _status(lambda: binding.paged_attention(c.pages, queries(1, 33, 8, "bf16"))) == -2        # 132 query rows
+    assert _status(lambda: binding.paged_select(change(bounds=None), q, 3)) == -1
+    assert _status(lambda: binding.paged_select(c.pages, q, 0)) == -1
+    assert _status(lambda: binding.paged_select(c.pages, q, 3, keep_first=-1)) == -1
+    assert _status(lambda: binding.paged_append(c.pages, k, k, max_new=0)) == -1
+    table = lambda n: torch.zeros((4, n), device="cuda")
+    pos = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert _status(lambda: binding.paged_append(c.pages, k, k, cos=table(4), sin=table(4), positions=pos)) == -2   # 8 dimensions
+    assert _status(lambda: binding.paged_append(c.pages, k, k, cos=table(72), sin=table(72), positions=pos)) == -1
+    for bad in (dict(table=c.pages.table.long()), dict(rows=c.pages.rows[:, :1]), dict(page_rows=32),
+                dict(bounds=c.pages.bounds.float()), dict(pool=c.pages.pool.cpu())):
+        with pytest.raises(AssertionError):
+            binding.paged_attention(change(**bad), q)
+    for bad in (q[..., :64], q[:, :, :3], q.float(), q.cpu(), q[0], queries(1, 1, 8, "bf16")[:, :, ::2]):
+        with pytest.raises(AssertionError):
+            binding.paged_attention(c.pages, bad)
+    with pytest.raises(AssertionError):
+        binding.paged_append(c.pages, k.view(2, 128), k.view(2, 128))       # compact rows without offsets
+    with pytest.raises(AssertionError):
+        binding.paged_append(c.pages, k, k.half())
+    with pytest.raises(AssertionError):
+        binding.paged_append(c.pages, torch.cat([k, k]), torch.cat([k, k]))     # two tokens, one sequence, no offsets
+    with pytest.raises(TypeError):
+        binding.paged_read(c.pages, 1, torch.float32)
