@@ -37,16 +37,16 @@ inline int check_pages(const mixkv_pages* c, PagePool* p) {
     return MIXKV_ERR_INVALID_ARG;
   if (c->head_dim != kHeadDim) return MIXKV_ERR_UNSUPPORTED;
   if ((long long)c->batch * c->kv_heads > (1 << 24) || (long long)c->max_pages * c->page_rows > (1ll << 30) ||
-      c->num_pages > 0x7fffffffll)
+      c->num_pages > 0x7fffffffll / (c->page_rows / kPageTile))
     return MIXKV_ERR_UNSUPPORTED;
   *p = PagePool{static_cast<unsigned char*>(c->pool), static_cast<__half*>(c->bounds_opt), c->table, c->rows,
                 c->num_pages, c->max_pages, c->page_rows, c->page_rows / kPageTile, c->kv_heads, c->k_scale, c->v_scale};
   return MIXKV_OK;
 }
 
-// First byte of tile `t` of page `id` (offsets pass 32 bits: a pool of 2^31 bytes is 14.9 million rows).
+// First byte of tile `t` of page `id` (a pool has at most 2^31 tiles, 2^42 bytes).
 __device__ __forceinline__ unsigned char* tile_ptr(const PagePool& p, const int id, const int t) {
-  return p.pool + ((long long)id * p.tiles + t) * kTileBytes;
+  return p.pool + (long long)(id * p.tiles + t) * kTileBytes;
 }
 
 template <typename T>

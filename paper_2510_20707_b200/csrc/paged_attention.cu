@@ -1,6 +1,6 @@
 // Attention of the newest tokens over the paged 4-bit cache (format: include/mixkv.h).
 //
-// A warp takes a tile of 16 cache rows per step: 2304 contiguous bytes, brought by one bulk copy into a ring of its own.
+// A warp takes two tiles of 16 cache rows per step, 2304 contiguous bytes each, brought by bulk copies into a ring of its own.
 // The codes are widened to fp16 by the hardware's conversion and multiplied by their scale: exact.  The products
 // run as m16n8k16 with the CACHE on the sixteen-row side and the query rows (tokens x heads of the group) on the
 // eight-column side: with up to eight query rows (one token of seven heads) nothing is padded but the eighth, where
@@ -22,18 +22,22 @@ namespace mixkv {
 namespace {
 
 constexpr int kAttWarps = 4, kAttThreads = kAttWarps * 32;
-constexpr int kAttDepth = 4;                   // tiles of a warp on their way or in work
-constexpr int kAttPitch = kHeadDim + 4;        // floats between the query rows of a warp's sums
+constexpr int kAttDepth = 2;                   // steps of a warp on their way or in work
+constexpr int kAttPair = 1;                    // up to so many groups of eight query rows a softmax step is two tiles, else one
+constexpr int kStepBytes = 2 * kTileBytes;
+constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is not there: beyond all
+constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
+constexpr int kAttUnits = 1024;                // most units whose steps are dealt out evenly
+constexpr int kAttSteps = 5;                   // steps of a warp above which a join pays
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
+constexpr float kNoRef = -1e30f;               // reference before the first row: below any, and finite
 
-__host__ __device__ constexpr size_t att_warp_bytes(int NT) {
-  return (size_t)(kAttDepth * kTileBytes > 8 * NT * kAttPitch * 4 ? kAttDepth * kTileBytes : 8 * NT * kAttPitch * 4);
-}
-// rings / sums of the warps; the CTA's sums; references and sums of the warps, the CTA, the cluster; barriers
+// rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
+// the cluster; barriers and rows of the rings
 __host__ __device__ constexpr size_t att_smem(int NT) {
-  return kAttWarps * att_warp_bytes(NT) + 8 * NT * kHeadDim * 4 + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
-         kAttWarps * kAttDepth * 8 + 16;
+  return kAttWarps * (kAttDepth * kStepBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
+         kAttWarps * kAttDepth * 16 + 16;
 }
 __host__ __device__ constexpr int att_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 
@@ -45,16 +49,18 @@ struct AttArgs {
   int max_rows;
   const int *list, *counts;  // nullptr: all pages
   int top;
-  int chunk, chunks;         // tiles of a work item and items of a unit; chunks == 1: a cluster has the unit
+  int units;
+  int ctas;                  // that share all steps evenly; 0: a cluster has a unit
   float scale_log2e;         // k_scale included
-  float* part;               // [unit][chunk][R][128] sums, then [unit][chunk][R][2] (reference, sum)
-  float* part_mz;
+  int* starts;               // [units + 1]: first step of every unit, units one after the other
+  float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
+  float2* part_mz;           // [2 ctas][R]: (reference, sum)
   void* out;
 };
 
-// Tiles of a unit, and its rows that the call sees.
+// Steps (pairs of tiles) of a unit, and its rows that the call sees.
 struct UnitTiles {
-  int n, tiles, pages;
+  int n, tiles, steps;
 };
 __device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
   UnitTiles r;
@@ -62,8 +68,8 @@ __device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
   n = min(n, a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
   r.n = max(n, 0);
-  r.pages = a.list ? max(0, min(a.counts[u], a.top)) : (r.n + a.p.page_rows - 1) / a.p.page_rows;
-  r.tiles = a.list ? r.pages * a.p.tiles : (r.n + kPageTile - 1) / kPageTile;
+  r.tiles = a.list ? max(0, min(a.counts[u], a.top)) * a.p.tiles : (r.n + kPageTile - 1) / kPageTile;
+  r.steps = (r.tiles + 1) >> 1;
   return r;
 }
 
@@ -96,22 +102,25 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, const uint
                : "memory");
 }
 
-// Page of the pool and first row of tile `t` of a unit (id -1: none).
+// Place in the pool and first row of tile `t` of a unit (-1, kNoRow: none).
 struct TileAt {
-  int id, row;
+  int tile, row;
 };
 __device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const UnitTiles& ut, const int t) {
-  TileAt r = {-1, 0};
+  TileAt r = {-1, kNoRow};
   if (t >= ut.tiles) return r;
-  const int slot = t / a.p.tiles;
+  const int slot = t / a.p.tiles, in = t - slot * a.p.tiles;
   const int page = a.list ? a.list[(long long)u * a.top + slot] : slot;
   if (page < 0 || page >= a.p.max_pages) return r;
-  r.row = page * a.p.page_rows + (t - slot * a.p.tiles) * kPageTile;
-  if (r.row >= ut.n) return r;
+  const int row = page * a.p.page_rows + in * kPageTile;
+  if (row >= ut.n) return r;
   const int id = a.p.table[(long long)u * a.p.max_pages + page];
-  if (id >= 0 && id < a.p.num_pages) r.id = id;
+  if (id >= 0 && id < a.p.num_pages) r.tile = id * a.p.tiles + in, r.row = row;
   return r;
 }
+
+// Steps of a CTA when `ctas` of them share `total`: CTA c has those from c * share on, the last ones may have none.
+__device__ __forceinline__ int share_of(const int total, const int ctas) { return (total + ctas - 1) / ctas; }
 
 // The first `keep` of the four scales of a word, zeros for the others.
 __device__ __forceinline__ uint32_t keep_scales(const uint32_t w, const int keep) {
@@ -136,16 +145,15 @@ __device__ __forceinline__ void values(const uint4 (&v)[2], const uint32_t vs, c
       f(4 * i + e, mul_f16x2(e0[e], s0), mul_f16x2(o0[e], s0), mul_f16x2(e1[e], s1), mul_f16x2(o1[e], s1));
   }
 }
-struct Tokens {   // of the CTA's query rows
-  int n, T, G, R, first;
-};
+// Token of query row r of a unit (rows of the padding: the last).
+__device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return min(r, a.R - 1) / a.G; }
 
 template <typename T, int NT>
 struct AttState {
   uint32_t q[NT][8][2];     // B fragments: query row g, dimensions 32 t + 4 s .. + 3
   float f[NT][2];           // logits to log2 units: query rows 2 t, 2 t + 1
   float acc[NT][8][4];      // dimensions 16 g + 2 m (0, 1), 16 g + 2 m + 1 (2, 3) of query rows 2 t, 2 t + 1
-  float m[NT][2], z[NT][2];
+  float ref[NT][2], z[NT][2];   // weights are 2^(logit - ref)
 
   // Query rows first .. first + 8 NT - 1 of a unit.  bf16 rows are divided by a power of two that brings their largest
   // magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it; the power goes into f.
@@ -198,7 +206,7 @@ struct AttState {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         f[nt][c] = __shfl_sync(0xffffffffu, up, 4 * (2 * t + c)) * a.scale_log2e;
-        m[nt][c] = -INFINITY, z[nt][c] = 0.f;
+        ref[nt][c] = kNoRef, z[nt][c] = 0.f;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -208,122 +216,164 @@ struct AttState {
   }
   static constexpr bool IsBf16 = std::is_same<T, __nv_bfloat16>::value;
 
-  // One tile.  k: codes of the lane's two K rows; ks: their scales; v, vs likewise.  EDGE: rows from `row` on may lie
-  // beyond what a query row sees; limit[nt][c] rows it sees, `left` rows of the tile exist.
-  template <bool EDGE>
-  __device__ __forceinline__ void tile(const uint4 (&k)[2], const uint32_t ks, const uint4 (&v)[2], uint32_t vs,
-                                       const int row, const int (&limit)[NT][2], const int left, const Tokens& tokens,
-                                       const int g, const int t) {
-    float s[NT][4];
+  // s[2 j + c] += products of row 4 (g / 2) + 2 j + g % 2 of the tile and query row 8 nt + 2 t + c
+  __device__ __forceinline__ void logits(const unsigned char* tile, const int lane, float (&s)[NT][4]) const {
+    const uint4 k[2] = {*reinterpret_cast<const uint4*>(tile + 16 * lane), *reinterpret_cast<const uint4*>(tile + 512 + 16 * lane)};
+    const uint32_t ks = *reinterpret_cast<const uint32_t*>(tile + kTileKs + 4 * lane);
+    const uint32_t s0 = scales_to_f16(ks & 0xffffu), s1 = scales_to_f16(ks >> 16);   // (block 2 t, block 2 t + 1) of row j
+    const uint32_t sc[2][2] = {{__byte_perm(s0, 0, 0x1010), __byte_perm(s0, 0, 0x3232)},
+                               {__byte_perm(s1, 0, 0x1010), __byte_perm(s1, 0, 0x3232)}};
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x[4], y[4];
+      codes_to_f16(i == 0 ? k[0].x : i == 1 ? k[0].y : i == 2 ? k[0].z : k[0].w, x);
+      codes_to_f16(i == 0 ? k[1].x : i == 1 ? k[1].y : i == 2 ? k[1].z : k[1].w, y);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[nt][c] = 0.f;
-    {
-      const uint32_t s0 = scales_to_f16(ks & 0xffffu), s1 = scales_to_f16(ks >> 16);   // (block 2 t, block 2 t + 1) of row j
-      const uint32_t sc[2][2] = {{__byte_perm(s0, 0, 0x1010), __byte_perm(s0, 0, 0x3232)},
-                                 {__byte_perm(s1, 0, 0x1010), __byte_perm(s1, 0, 0x3232)}};
+      for (int e = 0; e < 4; ++e) x[e] = mul_f16x2(x[e], sc[0][i >> 1]), y[e] = mul_f16x2(y[e], sc[1][i >> 1]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t x[4], y[4];
-        codes_to_f16(i == 0 ? k[0].x : i == 1 ? k[0].y : i == 2 ? k[0].z : k[0].w, x);
-        codes_to_f16(i == 0 ? k[1].x : i == 1 ? k[1].y : i == 2 ? k[1].z : k[1].w, y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = mul_f16x2(x[e], sc[0][i >> 1]), y[e] = mul_f16x2(y[e], sc[1][i >> 1]);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          mma_f16(s[nt], x[0], y[0], x[1], y[1], q[nt][2 * i][0], q[nt][2 * i][1]);
-          mma_f16(s[nt], x[2], y[2], x[3], y[3], q[nt][2 * i + 1][0], q[nt][2 * i + 1][1]);
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        mma_f16(s[nt], x[0], y[0], x[1], y[1], q[nt][2 * i][0], q[nt][2 * i][1]);
+        mma_f16(s[nt], x[2], y[2], x[3], y[3], q[nt][2 * i + 1][0], q[nt][2 * i + 1][1]);
       }
     }
-    // s[nt][2 j + c]: row 4 (g / 2) + 2 j + g % 2 of the tile, query row 8 nt + 2 t + c
+  }
+
+  // HN tiles (one softmax step), whose first rows are row[], of a unit of n rows; `first`: the CTA's first query row.  EDGE: rows may lie
+  // beyond what a query row sees.
+  template <bool EDGE, int HN>
+  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tiles, const int (&row)[HN], const int n,
+                                       const int first, const int lane) {
+    const int g = lane >> 2, t = lane & 3;
+    float s[HN][NT][4];
+#pragma unroll
+    for (int h = 0; h < HN; ++h) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[h][nt][i] = 0.f;
+      logits(tiles + h * kTileBytes, lane, s[h]);
+    }
     bool above = false;
+    uint32_t out = 0;     // EDGE: logits of rows that their query row does not see
+    if (EDGE) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[nt][i] *= f[nt][i & 1];
-        if (EDGE && row + 4 * (g >> 1) + 2 * (i >> 1) + (g & 1) >= limit[nt][i & 1]) s[nt][i] = -INFINITY;
-        above |= s[nt][i] > m[nt][i & 1] + kLag;
-      }
+        for (int c = 0; c < 2; ++c) {
+          const int sees = n - a.T + 1 + token_of(a, first + 8 * nt + 2 * t + c) - 4 * (g >> 1) - (g & 1);
+#pragma unroll
+          for (int h = 0; h < HN; ++h)
+#pragma unroll
+            for (int i = c; i < 4; i += 2)
+              if (row[h] + 2 * (i >> 1) >= sees) out |= 1u << ((h * NT + nt) * 4 + i);
+        }
+    }
+    auto gone = [&](const int h, const int nt, const int i) { return EDGE && (out >> ((h * NT + nt) * 4 + i) & 1u); };
+    float y[HN][NT][4];
+#pragma unroll
+    for (int h = 0; h < HN; ++h)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          y[h][nt][i] = gone(h, nt, i) ? -INFINITY : fmaf(s[h][nt][i], f[nt][i & 1], -ref[nt][i & 1]);
+          above |= y[h][nt][i] > kLag + kLift;
+        }
     if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const float mx = fmaxf(m[nt][c], column_max(fmaxf(s[nt][c], s[nt][2 + c])));
-          const float shrink = mx == -INFINITY ? 1.f : ex2(m[nt][c] - mx);
-          m[nt][c] = mx, z[nt][c] *= shrink;
+          float mx = -INFINITY;
+#pragma unroll
+          for (int h = 0; h < HN; ++h)
+#pragma unroll
+            for (int i = c; i < 4; i += 2) {
+              y[h][nt][i] = gone(h, nt, i) ? -INFINITY : s[h][nt][i] * f[nt][c];
+              mx = fmaxf(mx, y[h][nt][i]);
+            }
+          const float to = fmaxf(ref[nt][c], column_max(mx) - kLift);
+          const float shrink = ex2(ref[nt][c] - to);
+          ref[nt][c] = to, z[nt][c] *= shrink;
+#pragma unroll
+          for (int h = 0; h < HN; ++h)
+#pragma unroll
+            for (int i = c; i < 4; i += 2) y[h][nt][i] -= to;
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }
     }
-    uint32_t p[NT][2];   // B fragments: query row g, tile rows 4 t, 4 t + 1 and 4 t + 2, 4 t + 3
+    uint32_t p[HN][NT][2];   // B fragments: query row g, tile rows 4 t, 4 t + 1 and 4 t + 2, 4 t + 3
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      float w[4];
+    for (int h = 0; h < HN; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float ref = m[nt][i & 1] == -INFINITY ? 0.f : m[nt][i & 1] - kLift;
-        w[i] = ex2(s[nt][i] - ref);
-        z[nt][i & 1] += w[i];
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[h][nt][i] = ex2(y[h][nt][i]), z[nt][i & 1] += y[h][nt][i];
+        p[h][nt][0] = transpose8x8(narrow2<__half>(y[h][nt][0], y[h][nt][1]));
+        p[h][nt][1] = transpose8x8(narrow2<__half>(y[h][nt][2], y[h][nt][3]));
       }
-      p[nt][0] = transpose8x8(narrow2<__half>(w[0], w[1]));
-      p[nt][1] = transpose8x8(narrow2<__half>(w[2], w[3]));
-    }
-    // Rows that were never written can hold anything, a scale of NaN as well: their scales become zero.  A NaN in a row that
-    // some of the query rows see must not reach the others through a weight of zero: such a tile is taken once per
-    // token, with the rows that this token sees, and added to its own query rows alone.
-    if (EDGE) {
-      vs = keep_scales(vs, left - 4 * t);
-      const bool nan = ((((vs & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) != 0;   // a byte of 0x7f
-      if (tokens.T > 1 && __any_sync(0xffffffffu, nan)) {
-        for (int token = 0; token < tokens.T; ++token) {
-          const uint32_t seen = keep_scales(vs, tokens.n - tokens.T + 1 + token - row - 4 * t);
-          values(v, seen, [&](const int m, const uint32_t x0, const uint32_t x1, const uint32_t x2, const uint32_t x3) {
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              float d[4] = {0.f, 0.f, 0.f, 0.f};
-              mma_f16(d, x0, x1, x2, x3, p[nt][0], p[nt][1]);
+    for (int h = 0; h < HN; ++h) {
+      const unsigned char* tile = tiles + h * kTileBytes;
+      const uint4 v[2] = {*reinterpret_cast<const uint4*>(tile + kTileV + 16 * lane),
+                          *reinterpret_cast<const uint4*>(tile + kTileV + 512 + 16 * lane)};
+      uint32_t vs = *reinterpret_cast<const uint32_t*>(tile + kTileVs + 4 * lane);
+      // Rows that were never written can hold anything, a scale of NaN as well: their scales become zero.  A NaN in a row
+      // that some of the query rows see must not reach the others through a weight of zero: such a tile is taken once per
+      // token, with the rows that this token sees, and added to its own query rows alone.
+      if (EDGE) {
+        vs = keep_scales(vs, n - row[h] - 4 * t);
+        const bool nan = ((((vs & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) != 0;   // a byte of 0x7f
+        if (a.T > 1 && __any_sync(0xffffffffu, nan)) {
+          for (int token = 0; token < a.T; ++token) {
+            const uint32_t seen = keep_scales(vs, n - a.T + 1 + token - row[h] - 4 * t);
+            values(v, seen, [&](const int m, const uint32_t x0, const uint32_t x1, const uint32_t x2, const uint32_t x3) {
 #pragma unroll
-              for (int c = 0; c < 4; ++c)
-                if (min(tokens.first + 8 * nt + 2 * t + (c & 1), tokens.R - 1) / tokens.G == token) acc[nt][m][c] += d[c];
-            }
-          });
+              for (int nt = 0; nt < NT; ++nt) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(d, x0, x1, x2, x3, p[h][nt][0], p[h][nt][1]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                  if (token_of(a, first + 8 * nt + 2 * t + (c & 1)) == token) acc[nt][m][c] += d[c];
+              }
+            });
+          }
+          continue;
         }
-        return;
       }
-    }
-    values(v, vs, [&](const int m, const uint32_t x0, const uint32_t x1, const uint32_t x2, const uint32_t x3) {
+      values(v, vs, [&](const int m, const uint32_t x0, const uint32_t x1, const uint32_t x2, const uint32_t x3) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt][m], x0, x1, x2, x3, p[nt][0], p[nt][1]);
-    });
+        for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt][m], x0, x1, x2, x3, p[h][nt][0], p[h][nt][1]);
+      });
+    }
   }
 };
 
-// grid.x: units * S in clusters of S (chunks == 1), or units * chunks; grid.y: groups of 8 NT query rows
+// grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
 template <typename T, int NT>
 __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention(const AttArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int Q = 8 * NT;
-  constexpr size_t kWarpBytes = att_warp_bytes(NT);
-  float* xo = reinterpret_cast<float*>(smem + kAttWarps * kWarpBytes);   // [Q][128]
-  float* wm = xo + Q * kHeadDim;             // [warps][Q]
+  constexpr int Q = 8 * NT, kSums = Q * kAttPitch;
+  float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its sums where its rings were
+  static_assert(Q * kHeadDim * 4 <= kAttWarps * kAttDepth * kStepBytes, "sums of a CTA fit the rings");
+  float* sums = reinterpret_cast<float*>(smem + kAttWarps * kAttDepth * kStepBytes);   // [warps][Q][pitch]
+  float* wm = sums + kAttWarps * kSums;      // [warps][Q]
   float* wz = wm + kAttWarps * Q;            // [warps][Q]
   float* xm = wz + kAttWarps * Q;            // [Q]
   float* xz = xm + Q;                        // [Q]
   float* allm = xz + Q;                      // [8][Q]
   float* allz = allm + kMaxCluster * Q;      // [8][Q]
   uint64_t* bars = reinterpret_cast<uint64_t*>(allz + kMaxCluster * Q);   // [warps][depth]
-  int* abort = reinterpret_cast<int*>(bars + kAttWarps * kAttDepth);
+  int2* rows = reinterpret_cast<int2*>(bars + kAttWarps * kAttDepth);   // [warps][depth]: first rows of a step's tiles
+  int* abort = reinterpret_cast<int*>(rows + kAttWarps * kAttDepth);
+  __shared__ int starts[kAttUnits + 1];      // first step of every unit
+  __shared__ int warp_total[kAttWarps];
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const bool split = a.chunks > 1;
-  const int S = split ? 1 : (int)cluster.num_blocks(), crank = split ? 0 : (int)cluster.block_rank();
-  const int u = split ? blockIdx.x / a.chunks : blockIdx.x / S;
-  const int item = split ? blockIdx.x % a.chunks : 0;
-  const int first = blockIdx.y * Q;
+  const bool shares = a.ctas > 0;
+  const int S = shares ? 1 : (int)cluster.num_blocks(), crank = shares ? 0 : (int)cluster.block_rank();
+  const int first = blockIdx.y * Q, live = min(Q, a.R - first);
   uint64_t* bar = bars + warp * kAttDepth;
   if (lane == 0) {
     for (int d = 0; d < kAttDepth; ++d) mbar_init(&bar[d], 1);
@@ -333,176 +383,271 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
   __syncthreads();
   pdl_launch_dependents();
   pdl_wait();
-  const UnitTiles ut = unit_tiles(a, u);
-  const int t0 = item * a.chunk, t1 = split ? min(ut.tiles, t0 + a.chunk) : ut.tiles;
-  if (split && t0 >= t1 && (item > 0 || ut.tiles > 0)) return;   // (a unit without rows leaves its first item)
-  const int stride = S * kAttWarps, begin = t0 + crank * kAttWarps + warp;
-  const int count = begin < t1 ? (t1 - begin + stride - 1) / stride : 0;   // tiles of this warp
-  unsigned char* ring = smem + warp * kWarpBytes;
 
-  // lane l knows tile 32 n + l of the warp; `next` are those of n + 1
-  TileAt now = tile_at(a, u, ut, lane < count ? begin + lane * stride : ut.tiles);
-  auto issue = [&](const int i, const TileAt& from) {   // the copy of the warp's tile i
-    const int id = __shfl_sync(0xffffffffu, from.id, i & 31), row = __shfl_sync(0xffffffffu, from.row, i & 31);
-    if (lane == 0) {
-      uint64_t* full = &bar[i % kAttDepth];
-      if (id >= 0) {
-        mbar_expect_tx(full, kTileBytes);
-        bulk_load(ring + (i % kAttDepth) * kTileBytes, tile_ptr(a.p, id, row % a.p.page_rows / kPageTile), kTileBytes, full);
+  // steps lo .. hi - 1: of a cluster's unit, or of all units one after the other
+  int u = shares ? 0 : blockIdx.x / S, lo = crank * kAttWarps, hi;
+  if (shares) {
+    // first steps of all units: a thread takes consecutive ones
+    constexpr int kEach = kAttUnits / kAttThreads;
+    int mine[kEach], sum = 0;
+    const int u0 = tid * kEach;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine[i] = u0 + i < a.units ? unit_tiles(a, u0 + i).steps : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += mine[i];
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_total[warp] = upto;
+    __syncthreads();
+    int at = upto - sum, total = 0;
+    for (int w = 0; w < kAttWarps; ++w) {
+      if (w < warp) at += warp_total[w];
+      total += warp_total[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (u0 + i < a.units) starts[u0 + i] = at;
+      at += mine[i];
+    }
+    if (tid == 0) starts[a.units] = total;
+    __syncthreads();
+    if (blockIdx.x == 0 && blockIdx.y == 0)
+      for (int i = tid; i <= a.units; i += kAttThreads) a.starts[i] = starts[i];
+    const int share = share_of(total, a.ctas);
+    lo = blockIdx.x * share, hi = min(lo + share, total);
+    if (lo >= hi) return;
+    int x = 0, y = a.units;     // the last unit that begins at or before lo
+    while (y - x > 1) {
+      const int m = (x + y) >> 1;
+      (starts[m] <= lo ? x : y) = m;
+    }
+    u = x;
+  } else {
+    hi = unit_tiles(a, u).steps;
+  }
+  const int stride = S * kAttWarps, begin = lo + warp;
+  const int count = begin < hi ? (hi - begin + stride - 1) / stride : 0;   // steps of this warp
+  unsigned char* ring = smem + warp * kAttDepth * kStepBytes;
+  int2* ring_rows = rows + warp * kAttDepth;
+
+  TileAt ahead[2];      // lane l knows the tiles of step 32 n + l of the warp, 32 n the last multiple at or before `sent`
+  auto locate = [&](const int i) {
+    ahead[0] = ahead[1] = TileAt{-1, kNoRow};
+    if (i >= count) return;
+    int f = begin + i * stride, v = u;
+    if (shares) {
+      int y = a.units;
+      while (y - v > 1) {
+        const int m = (v + y) >> 1;
+        (starts[m] <= f ? v : y) = m;
+      }
+      f -= starts[v];
+    }
+    const UnitTiles ut = unit_tiles(a, v);
+    ahead[0] = tile_at(a, v, ut, 2 * f), ahead[1] = tile_at(a, v, ut, 2 * f + 1);
+  };
+  locate(lane);
+  int sent = 0, slot_out = 0;
+  auto send = [&]() {   // the copies of the warp's step `sent`
+    if ((sent & 31) == 0 && sent) locate(sent + lane);
+    if (lane == (sent & 31)) {
+      uint64_t* full = &bar[slot_out];
+      unsigned char* to = ring + slot_out * kStepBytes;
+      ring_rows[slot_out] = make_int2(ahead[0].row, ahead[1].row);
+      const uint32_t bytes = (ahead[0].tile >= 0 ? kTileBytes : 0) + (ahead[1].tile >= 0 ? kTileBytes : 0);
+      if (bytes) mbar_expect_tx(full, bytes);
+      else mbar_arrive(full);    // nothing to come
+      if (ahead[0].tile >= 0) bulk_load(to, a.p.pool + (long long)ahead[0].tile * kTileBytes, kTileBytes, full);
+      if (ahead[1].tile >= 0) bulk_load(to + kTileBytes, a.p.pool + (long long)ahead[1].tile * kTileBytes, kTileBytes, full);
+    }
+    ++sent, slot_out = slot_out + 1 == kAttDepth ? 0 : slot_out + 1;
+  };
+  while (sent < min(count, kAttDepth)) send();
+  int slot = 0;
+  uint32_t parity = 0;
+  bool lost = false;
+
+  for (int f = begin;;) {     // one unit after the other
+    int end = hi;
+    if (shares) {
+      while (starts[u + 1] <= max(lo, starts[u])) ++u;    // (units without tiles)
+      end = min(hi, starts[u + 1]);
+    }
+    AttState<T, NT> st;
+    st.start(a, u, first, g, t);
+    const int n = unit_tiles(a, u).n;
+    const int clear = n - a.T + 1;   // rows below are seen by all
+    for (; f < end && !lost; f += stride) {
+      if (!mbar_wait(&bar[slot], parity, abort)) {
+        lost = true;
+        break;
+      }
+      const int2 at = ring_rows[slot];
+      const unsigned char* tiles = ring + slot * kStepBytes;
+      const bool inside = max(at.x, at.y) + kPageTile <= clear;
+      if constexpr (NT <= kAttPair) {
+        const int row[2] = {at.x, at.y};
+        if (inside) st.template step<false, 2>(a, tiles, row, n, first, lane);
+        else st.template step<true, 2>(a, tiles, row, n, first, lane);
       } else {
-        mbar_arrive(full);    // nothing to come
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const int row[1] = {h ? at.y : at.x};
+          if (inside) st.template step<false, 1>(a, tiles + h * kTileBytes, row, n, first, lane);
+          else st.template step<true, 1>(a, tiles + h * kTileBytes, row, n, first, lane);
+        }
+      }
+      __syncwarp();     // every lane has read the slot
+      if (sent < count) send();
+      ++slot;
+      if (slot == kAttDepth) slot = 0, parity ^= 1;
+    }
+    if (lost && lane == 0) drain_ring(bar, kAttDepth, sent);
+
+    // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others
+    float* own = sums + warp * kSums;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float z = column_sum(st.z[nt][c]);
+        const int r = 8 * nt + 2 * t + c;
+        if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
+      }
+    const int b = u / a.p.H, h = u % a.p.H;
+    auto out_at = [&](const int row) {
+      return ((long long)b * a.T + row / a.G) * ((long long)a.p.H * a.G) + (long long)h * a.G + row % a.G;
+    };
+    const bool whole = shares && lo <= starts[u] && end == starts[u + 1];
+    const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            *reinterpret_cast<float2*>(own + (8 * nt + 2 * t + c) * kAttPitch + 8 * g + 2 * m) =
+                make_float2(st.acc[nt][4 * half + m][c], st.acc[nt][4 * half + m][2 + c]);
+      __syncthreads();
+      for (int e = tid; e < live * (kHeadDim / 4); e += kAttThreads) {
+        const int r = e / (kHeadDim / 4), x = 2 * (e % (kHeadDim / 4)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
+        float M = kNoRef;
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, wm[w * Q + r]);
+        float2 num = make_float2(0.f, 0.f);
+        float den = 0.f;
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) {
+          const float sc = ex2(wm[w * Q + r] - M);
+          const float2 v = *reinterpret_cast<const float2*>(sums + w * kSums + r * kAttPitch + x);
+          num.x = fmaf(v.x, sc, num.x), num.y = fmaf(v.y, sc, num.y);
+          den = fmaf(wz[w * Q + r], sc, den);
+        }
+        if (whole) {
+          const float by = den == 0.f ? 0.f : a.p.v_scale / den;
+          *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + out_at(first + r) * kHeadDim + dim) = narrow2<T>(num.x * by, num.y * by);
+        } else if (shares) {
+          const long long at = (long long)share * a.R + first + r;
+          *reinterpret_cast<float2*>(a.part + at * kHeadDim + dim) = num;
+          if (dim == 0) a.part_mz[at] = make_float2(M, den);
+        } else {
+          *reinterpret_cast<float2*>(xo + r * kHeadDim + dim) = num;
+          if (dim == 0) xm[r] = M, xz[r] = den;
+        }
       }
     }
-  };
-  for (int i = 0; i < min(count, kAttDepth); ++i) issue(i, now);
-  AttState<T, NT> st;
-  st.start(a, u, first, g, t);
-  int limit[NT][2];     // rows that a query row sees
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) limit[nt][c] = ut.n - a.T + 1 + min(first + 8 * nt + 2 * t + c, a.R - 1) / a.G;
-  const int clear = ut.n - a.T + 1;   // rows below are seen by all
-  const Tokens tokens = {ut.n, a.T, a.G, a.R, first};
-  bool lost = false;
-  int sent = min(count, kAttDepth);
-  TileAt next = tile_at(a, u, ut, 32 + lane < count ? begin + (32 + lane) * stride : ut.tiles);
-  for (int i = 0; i < count; ++i) {
-    if (!mbar_wait(&bar[i % kAttDepth], (i / kAttDepth) & 1, abort)) {
-      lost = true;
-      break;
+    if (shares) {
+      if (end == hi) return;
+      __syncthreads();
+      ++u;
+      continue;
     }
-    const int id = __shfl_sync(0xffffffffu, now.id, i & 31), row = __shfl_sync(0xffffffffu, now.row, i & 31);
-    const unsigned char* slot = ring + (i % kAttDepth) * kTileBytes;
-    const uint4 k[2] = {*reinterpret_cast<const uint4*>(slot + 16 * lane), *reinterpret_cast<const uint4*>(slot + 512 + 16 * lane)};
-    const uint4 v[2] = {*reinterpret_cast<const uint4*>(slot + kTileV + 16 * lane),
-                        *reinterpret_cast<const uint4*>(slot + kTileV + 512 + 16 * lane)};
-    const uint32_t ks = *reinterpret_cast<const uint32_t*>(slot + kTileKs + 4 * lane);
-    const uint32_t vs = *reinterpret_cast<const uint32_t*>(slot + kTileVs + 4 * lane);
-    __syncwarp();     // every lane has read the slot
-    if (sent < count) issue(sent++, (i & 31) + kAttDepth < 32 ? now : next);
-    if (id >= 0) {
-      if (row + kPageTile <= clear) st.template tile<false>(k, ks, v, vs, row, limit, kPageTile, tokens, g, t);
-      else st.template tile<true>(k, ks, v, vs, row, limit, ut.n - row, tokens, g, t);
-    }
-    if ((i & 31) == 31) {
-      now = next;
-      const int ahead = i + 1 + 32 + lane;
-      next = tile_at(a, u, ut, ahead < count ? begin + ahead * stride : ut.tiles);
-    }
-  }
-  if (lost && lane == 0) drain_ring(bar, kAttDepth, sent);
-  __syncwarp();
 
-  // ---- the warps merge through shared memory
-  float* mine = reinterpret_cast<float*>(ring);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      const float z = column_sum(st.z[nt][c]);
-      const int r = 8 * nt + 2 * t + c;
-#pragma unroll
-      for (int m = 0; m < 8; ++m)
-        *reinterpret_cast<float2*>(mine + r * kAttPitch + 16 * g + 2 * m) = make_float2(st.acc[nt][m][c], st.acc[nt][m][2 + c]);
-      if (g == 0) wm[warp * Q + r] = st.m[nt][c], wz[warp * Q + r] = lost ? NAN : z;
+    // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
+    cluster.sync();
+    for (int e = tid; e < S * live; e += kAttThreads) {
+      const int k = e / live, r = e % live;
+      allm[k * Q + r] = *cluster.map_shared_rank(&xm[r], k);
+      allz[k * Q + r] = *cluster.map_shared_rank(&xz[r], k);
     }
-  }
-  __syncthreads();
-  const int live = min(Q, a.R - first);
-  for (int e = tid; e < live * kHeadDim; e += kAttThreads) {
-    const int r = e / kHeadDim, dim = e % kHeadDim;
-    float M = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, wm[w * Q + r]);
-    float num = 0.f, den = 0.f;
-#pragma unroll
-    for (int w = 0; w < kAttWarps; ++w) {
-      const float mw = wm[w * Q + r];
-      const float sc = mw == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : ex2(mw - M);
-      num = fmaf(reinterpret_cast<const float*>(smem + w * kWarpBytes)[r * kAttPitch + dim], sc, num);
-      den = fmaf(wz[w * Q + r], sc, den);
+    __syncthreads();
+    const int per = (live * kHeadDim + S - 1) / S;
+    for (int e = crank * per + tid; e < min((crank + 1) * per, live * kHeadDim); e += kAttThreads) {
+      const int r = e / kHeadDim, dim = e % kHeadDim;
+      float M = kNoRef;
+      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+      float num = 0.f, den = 0.f;
+      for (int k = 0; k < S; ++k) {
+        const float sc = ex2(allm[k * Q + r] - M);
+        num = fmaf(*cluster.map_shared_rank(&xo[e], k), sc, num);
+        den = fmaf(allz[k * Q + r], sc, den);
+      }
+      const float by = den == 0.f ? 0.f : a.p.v_scale / den;
+      static_cast<T*>(a.out)[out_at(first + r) * kHeadDim + dim] = from_f32<T>(num * by);
     }
-    if (split) {
-      const long long at = ((long long)u * a.chunks + item) * a.R + first + r;
-      a.part[at * kHeadDim + dim] = num;
-      if (dim == 0) a.part_mz[2 * at] = M, a.part_mz[2 * at + 1] = den;
-    } else {
-      xo[e] = num;
-      if (dim == 0) xm[r] = M, xz[r] = den;
-    }
+    cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
+    return;
   }
-  if (split) return;
-
-  // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
-  cluster.sync();
-  for (int e = tid; e < S * live; e += kAttThreads) {
-    const int k = e / live, r = e % live;
-    allm[k * Q + r] = *cluster.map_shared_rank(&xm[r], k);
-    allz[k * Q + r] = *cluster.map_shared_rank(&xz[r], k);
-  }
-  __syncthreads();
-  const int per = (live * kHeadDim + S - 1) / S;
-  const int b = u / a.p.H, h = u % a.p.H;
-  for (int e = crank * per + tid; e < min((crank + 1) * per, live * kHeadDim); e += kAttThreads) {
-    const int r = e / kHeadDim;
-    float M = -INFINITY;
-    for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
-    float num = 0.f, den = 0.f;
-    for (int k = 0; k < S; ++k) {
-      const float mk = allm[k * Q + r];
-      const float sc = mk == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : ex2(mk - M);
-      num = fmaf(*cluster.map_shared_rank(&xo[e], k), sc, num);
-      den = fmaf(allz[k * Q + r], sc, den);
-    }
-    const int row = first + r;
-    const long long at = ((long long)b * a.T + row / a.G) * ((long long)a.p.H * a.G) + (long long)h * a.G + row % a.G;
-    static_cast<T*>(a.out)[at * kHeadDim + e % kHeadDim] = from_f32<T>(den == 0.f ? 0.f : num / den * a.p.v_scale);
-  }
-  cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
 }
 
-// Joins the items of split units: one CTA per (unit, query row).
-constexpr int kJoinWarps = 4;
+// Joins the shares of units that several CTAs had a part of, and writes zeros for units without rows.  per_row warps (a power
+// of two) take the shares of a query row in turn.
+constexpr int kJoinWarps = 8;
 template <typename T>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a) {
+__global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a, const int per_row) {
   __shared__ float4 sums[kJoinWarps][32];
-  __shared__ float stat[kJoinWarps][2];
+  __shared__ float stat[kJoinWarps];
   pdl_launch_dependents();
   pdl_wait();
-  const int u = blockIdx.x / a.R, row = blockIdx.x % a.R;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const UnitTiles ut = unit_tiles(a, u);
-  const int items = max(1, min(a.chunks, (ut.tiles + a.chunk - 1) / a.chunk));
-  const long long base = (long long)u * a.chunks * a.R + row;
-  float M = -INFINITY;
-  for (int i = lane; i < items; i += 32) M = fmaxf(M, a.part_mz[2 * (base + (long long)i * a.R)]);
+  const int at_once = kJoinWarps / per_row, blocks = (a.R + at_once - 1) / at_once;   // rows of a CTA, CTAs of a unit
+  const int u = blockIdx.x / blocks, row = (blockIdx.x % blocks) * at_once + warp / per_row, part = warp % per_row;
+  const int from = a.starts[u], to = a.starts[u + 1], total = a.starts[a.units];
+  int c0 = 0, c1 = -1;
+  const int share = max(1, share_of(total, a.ctas));
+  if (from < to) {
+    c0 = from / share, c1 = (to - 1) / share;
+    if (c0 == c1) return;     // written by that CTA
+  }
+  const bool on = row < a.R;
+  auto part_of = [&](const int c) { return (2LL * c + (c * share < from)) * a.R + (on ? row : 0); };
+  float M = kNoRef;
+  for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, a.part_mz[part_of(c)].x);
   M = warp_max(M);
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
   float den = 0.f;
 #pragma unroll 4
-  for (int i = warp; i < items; i += kJoinWarps) {
-    const long long at = base + (long long)i * a.R;
-    const float2 mz = *reinterpret_cast<const float2*>(a.part_mz + 2 * at);
+  for (int c = c0 + part; c <= c1; c += per_row) {
+    const long long at = part_of(c);
+    const float2 mz = a.part_mz[at];
     const float4 x = *(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
-    const float sc = mz.x == -INFINITY ? (M == -INFINITY ? 1.f : 0.f) : ex2(mz.x - M);
+    const float sc = ex2(mz.x - M);
     num.x = fmaf(x.x, sc, num.x), num.y = fmaf(x.y, sc, num.y), num.z = fmaf(x.z, sc, num.z), num.w = fmaf(x.w, sc, num.w);
     den = fmaf(mz.y, sc, den);
   }
-  sums[warp][lane] = num;
-  if (lane == 0) stat[warp][0] = den;
-  __syncthreads();
-  if (warp == 0) {
-    for (int w = 1; w < kJoinWarps; ++w) {
+  if (per_row > 1) {
+    sums[warp][lane] = num;
+    if (lane == 0) stat[warp] = den;
+    __syncthreads();
+    for (int w = warp + 1; part == 0 && w < warp + per_row; ++w) {
       const float4 x = sums[w][lane];
       num.x += x.x, num.y += x.y, num.z += x.z, num.w += x.w;
-      den += stat[w][0];
+      den += stat[w];
     }
-    const float inv = den == 0.f ? 0.f : a.p.v_scale / den;
+  }
+  if (part == 0 && on) {
+    const float by = den == 0.f ? 0.f : a.p.v_scale / den;
     const int b = u / a.p.H, h = u % a.p.H;
     const long long at = ((long long)b * a.T + row / a.G) * ((long long)a.p.H * a.G) + (long long)h * a.G + row % a.G;
     uint2 o;
-    o.x = narrow2<T>(num.x * inv, num.y * inv), o.y = narrow2<T>(num.z * inv, num.w * inv);
+    o.x = narrow2<T>(num.x * by, num.y * by), o.y = narrow2<T>(num.z * by, num.w * by);
     *(reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * kHeadDim) + lane) = o;
   }
 }
@@ -518,32 +663,21 @@ AttKernel att_kernel(const int NT) {
   }
 }
 
-// How the rows of a unit are split.  units: (sequence, head) pairs times groups of query rows; tiles: of the longest.
+// How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit.
 struct AttShape {
-  int S, chunk, chunks;
+  int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all steps
 };
-constexpr int kAttItems = 2;        // work items per resident CTA, of split units
-long long att_slots(const int NT, const int sms) { return (long long)att_per_sm(NT) * sms; }
-int att_most_chunks(const long long units, const int NT, const int sms) {
-  const long long n = (kAttItems * att_slots(NT, sms) + units - 1) / units;
-  return (int)(n < 1 ? 1 : n);
-}
+int att_slots(const int NT, const int sms) { return att_per_sm(NT) * sms; }
 template <typename Fit>
-AttShape att_shape(const long long units, const long long tiles, const int NT, const int sms, const Fit& fit) {
-  const long long slots = att_slots(NT, sms);
-  int S = (int)(slots / units < kMaxCluster ? slots / units : kMaxCluster);
-  if (S > tiles / kAttWarps) S = (int)(tiles / kAttWarps);
+AttShape att_shape(const long long units, const int groups, const long long steps, const int NT, const int sms, const Fit& fit) {
+  const long long slots = att_slots(NT, sms), all = units * groups;
+  int S = (int)(slots / all < kMaxCluster ? slots / all : kMaxCluster);
+  if (S > steps / kAttWarps) S = (int)(steps / kAttWarps);
   if (S < 1) S = 1;
-  while (S > 1 && units > fit(S)) --S;
-  // Split over items that no cluster holds together once a warp has more steps than the join costs
-  if (tiles > (long long)S * kAttWarps * 8) {
-    int chunks = att_most_chunks(units, NT, sms);
-    long long chunk = (tiles + chunks - 1) / chunks;
-    if (chunk < 4 * kAttWarps) chunk = 4 * kAttWarps;
-    chunks = (int)((tiles + chunk - 1) / chunk);
-    if (chunks > 1) return {1, (int)chunk, chunks};
-  }
-  return {S, 0, 1};
+  while (S > 1 && all > fit(S)) --S;
+  if (units <= kAttUnits && steps > (long long)S * kAttWarps * kAttSteps && groups < slots)
+    return {1, (int)(slots / groups)};
+  return {S, 0};
 }
 
 int queries_of(const mixkv_pages* c, const int32_t q_tokens, const int32_t gqa, int* groups, int* NT) {
@@ -556,8 +690,10 @@ int queries_of(const mixkv_pages* c, const int32_t q_tokens, const int32_t gqa, 
   if ((long long)c->batch * c->kv_heads * *groups > 1 << 24) return MIXKV_ERR_UNSUPPORTED;
   return MIXKV_OK;
 }
-size_t part_bytes(const long long units, const int chunks, const long long R) {
-  return (size_t)(units * chunks * R) * (kHeadDim + 2) * 4;
+// Workspace: part, part_mz, starts.
+size_t part_bytes(const int ctas, const long long R) { return (size_t)ctas * 2 * R * (kHeadDim + 2) * 4; }
+size_t att_workspace(const int NT, const int sms, const long long R) {
+  return part_bytes(att_slots(NT, sms), R) + (kAttUnits + 1) * sizeof(int);
 }
 
 }  // namespace
@@ -571,8 +707,7 @@ extern "C" int mixkv_paged_workspace_size(const mixkv_pages* c, int32_t q_tokens
   if (rc != MIXKV_OK) return rc;
   if (!bytes) return MIXKV_ERR_INVALID_ARG;
   if ((rc = queries_of(c, q_tokens, gqa_ratio, &groups, &NT)) != MIXKV_OK) return rc;
-  const long long units = (long long)c->batch * c->kv_heads;
-  *bytes = part_bytes(units, att_most_chunks(units * groups, NT, device_sm_count()), (long long)q_tokens * gqa_ratio);
+  *bytes = att_workspace(NT, device_sm_count(), (long long)q_tokens * gqa_ratio);
   return MIXKV_OK;
 }
 
@@ -593,8 +728,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   if ((rc = queries_of(c, q_tokens, gqa_ratio, &groups, &NT)) != MIXKV_OK) return rc;
   const long long units = (long long)c->batch * c->kv_heads;
   const int R = q_tokens * gqa_ratio, sms = device_sm_count();
-  if (workspace_bytes < part_bytes(units, att_most_chunks(units * groups, NT, sms), R))
-    return MIXKV_ERR_WORKSPACE_TOO_SMALL;
+  if (workspace_bytes < att_workspace(NT, sms, R)) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
   if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
   const long long seen = max_rows < (long long)c->max_pages * c->page_rows ? max_rows : (long long)c->max_pages * c->page_rows;
   long long tiles = (seen + kPageTile - 1) / kPageTile;
@@ -607,22 +741,27 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   const AttKernel kernel = bf16 ? att_kernel<__nv_bfloat16>(NT) : att_kernel<__half>(NT);
   const size_t smem = att_smem(NT);
   if (ensure_smem(kernel, smem, done[variant], dev) != cudaSuccess) return MIXKV_ERR_CUDA;
-  const AttShape shape = att_shape(units * groups, tiles, NT, sms, [&](const int size) {
+  const AttShape shape = att_shape(units, groups, (tiles + 1) / 2, NT, sms, [&](const int size) {
     return fits[variant].ask(kernel, kAttThreads, smem, size, dev);
   });
   a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride;
   a.T = q_tokens, a.G = gqa_ratio, a.R = R, a.max_rows = max_rows;
   a.list = page_list_opt, a.counts = counts_opt, a.top = top;
-  a.chunk = shape.chunk, a.chunks = shape.chunks;
+  a.units = (int)units, a.ctas = shape.ctas;
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e * c->k_scale;
   a.part = static_cast<float*>(workspace);
-  a.part_mz = a.part + units * shape.chunks * R * kHeadDim;
+  a.part_mz = reinterpret_cast<float2*>(a.part + (size_t)shape.ctas * 2 * R * kHeadDim);
+  a.starts = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + part_bytes(shape.ctas, R));
   a.out = out;
-  const unsigned per_unit = shape.chunks > 1 ? shape.chunks : shape.S;
-  cudaError_t e = launch_pdl(kernel, dim3((unsigned)units * per_unit, groups), dim3(kAttThreads), smem, (cudaStream_t)stream,
-                             shape.S, a);
-  if (e == cudaSuccess && shape.chunks > 1)
-    e = launch_pdl(bf16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>, dim3((unsigned)(units * R)),
-                   dim3(kJoinWarps * 32), 0, (cudaStream_t)stream, 1, a);
+  const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
+  cudaError_t e = launch_pdl(kernel, dim3(grid, groups), dim3(kAttThreads), smem, (cudaStream_t)stream, shape.S, a);
+  if (e == cudaSuccess && shape.ctas) {
+    int per_row = 1;      // warps that go through the shares of one query row
+    while (per_row < kJoinWarps && per_row * 4 * units < shape.ctas) per_row *= 2;
+    const int at_once = kJoinWarps / per_row;
+    e = launch_pdl(bf16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>,
+                   dim3((unsigned)(units * ((R + at_once - 1) / at_once))), dim3(kJoinWarps * 32), 0, (cudaStream_t)stream, 1,
+                   a, per_row);
+  }
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }
