@@ -1,6 +1,6 @@
 // Which pages of the paged cache a query attends to (score and order: include/mixkv.h).
 //
-// A cluster has one (sequence, KV head): its warps score the pages four at a time, the scores go as order-preserving
+// A cluster has one (sequence, KV head): its warps score runs of pages, four at a time, the scores go as order-preserving
 // words into the first CTA's shared memory, and that CTA lists the `top` largest.
 //
 // Score.  Lane l holds dimensions 4 l .. 4 l + 3 of the pages' bounds; of q max(q, 0) and min(q, 0) lie in shared memory, so a
@@ -16,9 +16,10 @@ namespace cg = cooperative_groups;
 namespace mixkv {
 namespace {
 
-constexpr int kSelThreads = 256, kSelWarps = kSelThreads / 32;
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
+constexpr int kSelBins = 2 * kSelThreads;
 constexpr int kSelPages = 4, kSelRows = 8;   // pages of a warp at a time; query rows at a time
-constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;
+constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;   // (no number has either)
 
 struct SelArgs {
   PagePool p;
@@ -50,8 +51,34 @@ __device__ __forceinline__ float sum_each(float (&v)[32], const int lane) {
   return v[0];
 }
 
+// Bounds of four pages, as they lie in memory: dimensions 4 lane .. + 3.
+struct PageBounds {
+  uint2 lo[kSelPages], hi[kSelPages];
+};
+
+// Sum of x over the CTA's threads before this one (exclusive); *total: of all.  sums: a word per warp.
+__device__ __forceinline__ uint32_t block_before(const uint32_t x, uint32_t* sums, uint32_t* total, const int lane, const int warp) {
+  uint32_t upto = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) sums[warp] = upto;
+  __syncthreads();
+  const uint32_t other = lane < kSelWarps ? sums[lane] : 0u;
+  uint32_t before = lane < warp ? other : 0u, all = other;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+  }
+  *total = all;
+  return before + upto - x;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(kSelThreads) k_paged_select(const SelArgs a) {
+__global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a) {
   extern __shared__ __align__(16) unsigned char sm[];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), crank = (int)cluster.block_rank(), u = blockIdx.x / S;
@@ -59,14 +86,33 @@ __global__ void __launch_bounds__(kSelThreads) k_paged_select(const SelArgs a) {
   const int b = u / a.p.H, h = u % a.p.H, rows_pad = (a.R + kSelRows - 1) / kSelRows * kSelRows;
   float4* qs = reinterpret_cast<float4*>(sm);                    // [R padded][2][32]: max(q, 0), min(q, 0)
   uint32_t* keys = reinterpret_cast<uint32_t*>(qs + rows_pad * 64);   // [pages], the first CTA's
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t warp_sum_s[kSelWarps];
+  __shared__ uint32_t hist[kSelBins];
+  __shared__ uint32_t sums[2][kSelWarps];
   __shared__ uint32_t found[2];
   pdl_launch_dependents();
   pdl_wait();
   int n = min(a.p.rows[u], a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
   const int pages = n <= 0 ? 0 : min((n + a.p.page_rows - 1) / a.p.page_rows, a.pages);
+  // a warp takes a run of pages, four at a time; the next four's bounds are on their way meanwhile
+  const int share = (pages + S * kSelWarps - 1) / (S * kSelWarps), run = (share + kSelPages - 1) / kSelPages * kSelPages;
+  const int begin = (crank * kSelWarps + warp) * run, end = min(begin + run, pages);
+  const int* table = a.p.table + (long long)u * a.p.max_pages;
+  int ids = begin + lane < end ? __ldg(table + begin + lane) : -1;     // of 32 pages from the last multiple of 32
+  auto fetch = [&](const int p0) {
+    PageBounds r;
+#pragma unroll
+    for (int i = 0; i < kSelPages; ++i) {
+      const int id = __shfl_sync(0xffffffffu, ids, (p0 - begin + i) & 31);
+      r.lo[i] = r.hi[i] = make_uint2(0, 0);    // (a page outside the pool scores zero)
+      if (p0 + i < end && id >= 0 && id < a.p.num_pages) {
+        const __half* src = a.p.bounds + (long long)id * 2 * kHeadDim + 4 * lane;
+        r.lo[i] = __ldg(reinterpret_cast<const uint2*>(src)), r.hi[i] = __ldg(reinterpret_cast<const uint2*>(src + kHeadDim));
+      }
+    }
+    return r;
+  };
+  PageBounds next = fetch(begin);
   for (int e = tid; e < rows_pad * 32; e += kSelThreads) {
     const int r = min(e >> 5, a.R - 1);      // (the rows of the padding repeat the last: a maximum does not mind)
     const T* src = static_cast<const T*>(a.q) + b * a.q_batch + (r / a.G) * a.q_token +
@@ -79,34 +125,28 @@ __global__ void __launch_bounds__(kSelThreads) k_paged_select(const SelArgs a) {
     qs[(e >> 5) * 64 + (e & 31)] = make_float4(up(x.x), up(x.y), up(y.x), up(y.y));
     qs[(e >> 5) * 64 + 32 + (e & 31)] = make_float4(down(x.x), down(x.y), down(y.x), down(y.y));
   }
-  __syncthreads();
   uint32_t* keys0 = cluster.map_shared_rank(keys, 0);
-  const int* table = a.p.table + (long long)u * a.p.max_pages;
   if (S > 1) cluster.sync();     // the first CTA runs
-  for (int p0 = (crank * kSelWarps + warp) * kSelPages; p0 < pages; p0 += S * kSelWarps * kSelPages) {
-    float lo[kSelPages][4], hi[kSelPages][4];
-#pragma unroll
-    for (int i = 0; i < kSelPages; ++i) {
-      const int p = min(p0 + i, pages - 1), id = __ldg(table + p);
-      uint2 wl = make_uint2(0, 0), wh = wl;    // (a page outside the pool scores zero)
-      if (id >= 0 && id < a.p.num_pages) {
-        const __half* src = a.p.bounds + (long long)id * 2 * kHeadDim + 4 * lane;
-        wl = __ldg(reinterpret_cast<const uint2*>(src)), wh = __ldg(reinterpret_cast<const uint2*>(src + kHeadDim));
-      }
-      const float2 l0 = widen2<__half>(wl.x), l1 = widen2<__half>(wl.y), h0 = widen2<__half>(wh.x), h1 = widen2<__half>(wh.y);
-      lo[i][0] = l0.x, lo[i][1] = l0.y, lo[i][2] = l1.x, lo[i][3] = l1.y;
-      hi[i][0] = h0.x, hi[i][1] = h0.y, hi[i][2] = h1.x, hi[i][3] = h1.y;
+  else __syncthreads();
+  for (int p0 = begin; p0 < end; p0 += kSelPages) {
+    const PageBounds now = next;
+    if (p0 + kSelPages < end) {
+      if ((p0 + kSelPages - begin) % 32 == 0) ids = p0 + kSelPages + lane < end ? __ldg(table + p0 + kSelPages + lane) : -1;
+      next = fetch(p0 + kSelPages);
     }
     uint32_t best = 0;
+#pragma unroll 1
     for (int r0 = 0; r0 < rows_pad; r0 += kSelRows) {
       float v[32];
 #pragma unroll
-      for (int r = 0; r < kSelRows; ++r) {
-        const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
+      for (int i = 0; i < kSelPages; ++i) {
+        const float2 l0 = widen2<__half>(now.lo[i].x), l1 = widen2<__half>(now.lo[i].y);
+        const float2 h0 = widen2<__half>(now.hi[i].x), h1 = widen2<__half>(now.hi[i].y);
 #pragma unroll
-        for (int i = 0; i < kSelPages; ++i) {
-          const float x0 = fmaf(up.x, hi[i][0], __fmul_rn(dn.x, lo[i][0])), x1 = fmaf(up.y, hi[i][1], __fmul_rn(dn.y, lo[i][1]));
-          const float x2 = fmaf(up.z, hi[i][2], __fmul_rn(dn.z, lo[i][2])), x3 = fmaf(up.w, hi[i][3], __fmul_rn(dn.w, lo[i][3]));
+        for (int r = 0; r < kSelRows; ++r) {
+          const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
+          const float x0 = fmaf(up.x, h0.x, __fmul_rn(dn.x, l0.x)), x1 = fmaf(up.y, h0.y, __fmul_rn(dn.y, l0.y));
+          const float x2 = fmaf(up.z, h1.x, __fmul_rn(dn.z, l1.x)), x3 = fmaf(up.w, h1.y, __fmul_rn(dn.w, l1.y));
           v[kSelRows * i + r] = __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
         }
       }
@@ -117,73 +157,67 @@ __global__ void __launch_bounds__(kSelThreads) k_paged_select(const SelArgs a) {
       best = max(best, k);
     }
     const int p = p0 + (__brev(lane) >> 30);
-    if (lane < 4 && p < pages) keys0[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
+    if (lane < 4 && p < end) keys0[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
   }
   if (S > 1) cluster.sync();
   else __syncthreads();
   if (crank) return;
 
-  // The `top`-th largest word, eight bits at a time; ties to the lower page
-  const int take = min(a.top, pages);
-  uint32_t prefix = 0, mask = 0;
-  int want = take;       // among words with this prefix
-  if (take < pages) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < pages; i += kSelThreads) {
-        const uint32_t k = keys[i];
-        if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      // bin 255 - tid: how many lie in it and above
-      uint32_t c = hist[255 - tid], s = c;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t x = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += x;
-      }
-      if (lane == 31) warp_sum_s[warp] = s;
-      __syncthreads();
-      for (int w = 0; w < warp; ++w) s += warp_sum_s[w];
-      if (s >= (uint32_t)want && s - c < (uint32_t)want) found[0] = 255 - tid, found[1] = s - c;
-      __syncthreads();
-      prefix |= found[0] << shift, mask |= 255u << shift;
-      want -= (int)found[1];
+  // The `top`-th largest word: keys between `low` and `high` are counted in bins, the bin that holds it is taken apart next, until
+  // a bin's lower end separates as many as are wanted, or the bin is one word.  A thread has a run of pages.
+  const int take = min(a.top, pages), each = (pages + kSelThreads - 1) / kSelThreads;
+  const int p0 = min(tid * each, pages), p1 = min(p0 + each, pages);
+  uint32_t low = 0xffffffffu, high = 0;       // of all keys
+  for (int p = p0; p < p1; ++p) low = min(low, keys[p]), high = max(high, keys[p]);
+  low = __reduce_min_sync(0xffffffffu, low), high = __reduce_max_sync(0xffffffffu, high);
+  if (lane == 0) sums[0][warp] = low, sums[1][warp] = high;
+  __syncthreads();
+  low = __reduce_min_sync(0xffffffffu, lane < kSelWarps ? sums[0][lane] : 0xffffffffu);
+  high = __reduce_max_sync(0xffffffffu, lane < kSelWarps ? sums[1][lane] : 0u);
+  uint32_t want = take;     // of the words low .. high
+  bool exact = take == pages;       // all words from `low` on are taken
+  while (!exact && low < high) {
+    const int shift = max(0, 32 - __clz((high - low) / kSelBins));   // ((high - low) >> shift < kSelBins)
+    hist[tid] = hist[tid + kSelThreads] = 0;
+    __syncthreads();
+    for (int p = p0; p < p1; ++p) {
+      const uint32_t k = keys[p];
+      if (k >= low && k <= high) atomicAdd(&hist[(k - low) >> shift], 1u);
     }
+    __syncthreads();
+    // bins from the top: how many lie above a thread's two
+    const int top_bin = kSelBins - 1 - 2 * tid;
+    const uint32_t c1 = hist[top_bin], c0 = hist[top_bin - 1];
+    uint32_t total;
+    const uint32_t above = block_before(c1 + c0, sums[0], &total, lane, warp);
+    if (above < want && above + c1 >= want) found[0] = top_bin, found[1] = above;
+    else if (above + c1 < want && above + c1 + c0 >= want) found[0] = top_bin - 1, found[1] = above + c1;
+    __syncthreads();
+    const uint32_t bin = found[0], more = want - found[1];      // of the bin's
+    exact = hist[bin] == more;
+    low += bin << shift;
+    high = low + min(high - low, (1u << shift) - 1u);
+    if (!exact) want = more;
+    __syncthreads();     // hist and found are written again
   }
-  // all above `prefix`, and the first `want` equal to it
-  int *list = a.list + (long long)u * a.top;
-  int listed = 0, equal = 0;
-  for (int base = 0; base < pages; base += kSelThreads) {
-    const int p = base + tid;
-    const uint32_t k = p < pages ? keys[p] : 0u;
-    const bool in = p < pages, all = take == pages, same = in && !all && k == prefix;
-    const uint32_t eq = __ballot_sync(0xffffffffu, same);
-    __syncthreads();
-    if (lane == 0) warp_sum_s[warp] = __popc(eq);
-    __syncthreads();
-    int before = equal, total = 0;
-    for (int w = 0; w < kSelWarps; ++w) {
-      if (w < warp) before += warp_sum_s[w];
-      total += warp_sum_s[w];
-    }
-    before += __popc(eq & ((1u << lane) - 1u));
-    equal += total;
-    const bool on = in && (all || k > prefix || (same && before < want));
-    const uint32_t yes = __ballot_sync(0xffffffffu, on);
-    __syncthreads();
-    if (lane == 0) warp_sum_s[warp] = __popc(yes);
-    __syncthreads();
-    int at = listed;
-    total = 0;
-    for (int w = 0; w < kSelWarps; ++w) {
-      if (w < warp) at += warp_sum_s[w];
-      total += warp_sum_s[w];
-    }
-    at += __popc(yes & ((1u << lane) - 1u));
-    listed += total;
-    if (on) list[at] = p;
+  // listed: all words above `high`, and of those from low to high either all (exact) or, being one word, the first `want`
+  uint32_t above = 0, equal = 0;
+  for (int p = p0; p < p1; ++p) {
+    const uint32_t k = keys[p];
+    above += exact ? k >= low : k > low;
+    equal += !exact && k == low;
+  }
+  uint32_t total, skip;
+  uint32_t before_eq = block_before(equal, sums[0], &total, lane, warp);
+  const uint32_t room = before_eq < want ? min(equal, want - before_eq) : 0u;      // of this thread's equal words
+  uint32_t at = block_before(above + (exact ? 0u : room), sums[1], &skip, lane, warp);
+  int* list = a.list + (long long)u * a.top;
+  uint32_t left = room;
+  for (int p = p0; p < p1; ++p) {
+    const uint32_t k = keys[p];
+    bool on = exact ? k >= low : k > low;
+    if (!exact && k == low && left) on = true, --left;
+    if (on) list[at++] = p;
   }
   for (int i = take + tid; i < a.top; i += kSelThreads) list[i] = -1;
   if (tid == 0) a.counts[u] = take;
@@ -214,7 +248,7 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   const long long pages = (seen + c->page_rows - 1) / c->page_rows;
   const long long units = (long long)c->batch * c->kv_heads;
   if (R > MIXKV_PAGED_MAX_QUERIES || pages > MIXKV_PAGES_MAX) return MIXKV_ERR_UNSUPPORTED;
-  const size_t smem = select_smem((int)R, (int)pages), most = 227 * 1024 - 2048;
+  const size_t smem = select_smem((int)R, (int)pages), most = 227 * 1024 - 8192;
   if (smem > most) return MIXKV_ERR_UNSUPPORTED;
   if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
   a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride, a.T = q_tokens, a.G = gqa_ratio, a.R = (int)R;
@@ -224,8 +258,8 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   void (*kernel)(SelArgs) = bf16 ? k_paged_select<__nv_bfloat16> : k_paged_select<__half>;
   static std::atomic<bool> done[2][kMaxDevices];
   if (ensure_smem(kernel, most, done[bf16]) != cudaSuccess) return MIXKV_ERR_CUDA;
-  // as many CTAs as keep a round of pages for every warp, while they fit the GPU
-  int S = (int)(2LL * device_sm_count() / units < kMaxCluster ? 2LL * device_sm_count() / units : kMaxCluster);
+  // as many CTAs as keep four pages for every warp, while they fit the GPU
+  int S = (int)(device_sm_count() / units < kMaxCluster ? device_sm_count() / units : kMaxCluster);
   const long long rounds = (pages + kSelWarps * kSelPages - 1) / (kSelWarps * kSelPages);
   if (S > rounds) S = (int)rounds;
   if (S < 1) S = 1;
