@@ -361,11 +361,12 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  *   max_new         upper bound on n; of more, a head's last max_new are written
  *   cos_opt, sin_opt  device fp32 [table_len, rot_dim / 2], 16-byte aligned; both NULL: no rotation.  Dimension i of a
  *                   pair becomes x cos - y sin, its partner y cos + x sin, in fp32; pairs are (i, i + rot_dim / 2), or
- *                   with interleaved != 0 (2 i, 2 i + 1), below rot_dim (a multiple of 16, at most 128)
+ *                   with interleaved != 0 (2 i, 2 i + 1), below rot_dim (at most 128; a multiple of 32,
+ *                   interleaved of 16)
  *   positions_opt   device int32 [num_tokens], needed with cos_opt: row of the tables.  It is not the row in the cache: a
  *                   compressed cache has fewer rows than its sequence has tokens
  * Rounding: the scale of a block is e4m3(min(max |x| / (6 k_scale), 448)), nearest even; a code is the nearest to
- * x / (scale k_scale), ties to the even code, largest magnitude 6; a block of zeros, or one that is too small for e4m3,
+ * x / (scale k_scale), ties to the even code, largest magnitude 6 (the sign of a code of zero is not defined); a block of zeros, or one that is too small for e4m3,
  * is zero; one that holds a NaN is NaN.  Every operation is rounded by itself, so codes are the same wherever
  * they are computed.
  * Bounds (if there are any) of a page that begins with a new row are set, those of a page that had rows are widened.

@@ -1,15 +1,17 @@
 // Rows into the paged 4-bit cache and back (format and rounding: include/mixkv.h).
 //
-// Append.  One CTA has one page of one head, so a page's bounds have one owner and need no atomics.  Half of its warps
-// take K, half V; a warp takes two rows at a time, sixteen lanes each, a lane eight dimensions (16 bytes in, one word of
-// codes out): a block of 16 is two lanes, and the largest magnitude of a block one exchange.  The rotation's partner
-// dimensions lie rot_dim / 2 on, in another lane's registers.
+// One CTA has one page of one head, so a page's bounds have one owner and need no atomics.  A warp takes four rows at a
+// time, eight lanes each, a lane one block of 16 dimensions: the largest magnitude, the scale and the codes of a block are
+// one lane's (32 bytes in, 8 out).  The rotation's partner dimensions lie rot_dim / 2 on, in another lane's registers.
+// (Two rows at a time, half a block per lane and K and V in warps of their own took 262 instructions a row instead of
+// about 80, and half of the warps waited for the others.)
 #include "paged.cuh"
 
 namespace mixkv {
 namespace {
 
-constexpr int kRowThreads = 256;   // of a CTA that may get many rows of a page; one row per head: 64
+constexpr int kRowThreads = 256;   // of a CTA that reads many rows of a page; one row per head: 64
+constexpr int kAppThreads = 128, kAppPerSm = 4;   // of a CTA that may get many rows, and such CTAs per SM
 
 struct RowArgs {
   PagePool p;
@@ -26,21 +28,22 @@ struct RowArgs {
 // The new rows of a unit (head h of sequence b) that lie on the CTA's page.
 struct PageSpan {
   int u, h, page;          // unit, its head, column of the page table
-  int lo, hi;              // rows of the page, lo < hi
-  long long token;         // token (or row of the input) of row `lo`
-  int id;                  // page of the pool, -1: none
-  bool bad;                // a new row that has no place
+  int lo, hi;              // rows of the page
+  int first, last;         // those of them whose token is in the input
+  long long token;         // token (or row of the input) of row 0 of the page; there may be none
+  int id;                  // what the table says, -1 beyond it
+  bool bad;                // a new row below row zero
 };
-__device__ __forceinline__ PageSpan page_span(const RowArgs& a) {
+__device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) {
   PageSpan s;
-  s.u = blockIdx.x / a.slots;
-  const int slot = blockIdx.x % a.slots, b = s.u / a.p.H;
+  s.u = task / a.slots;
+  const int slot = task % a.slots, b = s.u / a.p.H;
   s.h = s.u % a.p.H;
-  const int rows = a.p.rows[s.u];
+  const int rows = __ldg(a.p.rows + s.u);
   long long first = b, n = 1;
   if (a.offsets) {
     const int i = a.per_head ? s.u : b;
-    first = a.offsets[i], n = a.offsets[i + 1] - first;
+    first = __ldg(a.offsets + i), n = __ldg(a.offsets + i + 1) - first;
   }
   if (n > a.max_new) first += n - a.max_new, n = a.max_new;
   long long r0 = (long long)rows - n;      // row of the first new token
@@ -50,256 +53,328 @@ __device__ __forceinline__ PageSpan page_span(const RowArgs& a) {
   const long long begin = (long long)s.page * a.p.page_rows;
   const long long lo = r0 > begin ? r0 : begin, end = begin + a.p.page_rows;
   const long long hi = (long long)rows < end ? rows : end;
-  s.lo = (int)(lo - begin), s.hi = (int)(hi - begin), s.token = first + (lo - r0), s.id = -1;
-  if (n <= 0 || s.lo >= s.hi) {
-    s.lo = s.hi = 0;
-  } else if (s.page >= a.p.max_pages) {
-    s.bad = true;
-  } else {
-    const int id = a.p.table[(long long)s.u * a.p.max_pages + s.page];
-    if (id >= 0 && id < a.p.num_pages) s.id = id;
-    else s.bad = true;
-  }
+  s.lo = (int)(lo - begin), s.hi = n > 0 && hi > lo ? (int)(hi - begin) : s.lo;
+  s.token = first + (begin - r0);
+  // (rows r of the page with 0 <= token + r < num_tokens)
+  const long long from = -s.token, to = a.num_tokens - s.token;
+  s.first = from > s.lo ? (int)(from < s.hi ? from : s.hi) : s.lo;
+  s.last = to < s.hi ? (int)(to > s.lo ? to : s.lo) : s.hi;
+  s.id = s.lo < s.hi && s.page < a.p.max_pages ? __ldg(a.p.table + (long long)s.u * a.p.max_pages + s.page) : -1;
   return s;
 }
-// Rows of the page, among s.lo .. s.hi - 1, whose token is in the input.
-struct PageRows {
-  int lo, hi;
-};
-__device__ __forceinline__ PageRows rows_in(const RowArgs& a, const PageSpan& s) {
-  const long long left = a.num_tokens - s.token;     // of the input, from row s.lo on
-  PageRows r = {s.lo, s.hi};
-  if (s.token < 0) r.lo = s.token < s.lo - s.hi ? s.hi : s.lo - (int)s.token;
-  if (left < s.hi - s.lo) r.hi = left < 0 ? s.lo : s.lo + (int)left;
+
+__device__ __forceinline__ float max3_nan(const float x, const float y, const float z) {   // NaN if one is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
+}
+__device__ __forceinline__ f32x2 mul2(const f32x2 a, const f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
 }
 
-__device__ __forceinline__ float max_nan(const float x, const float y) {   // NaN if either is
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
-  return r;
+// Of every scale byte: scale * third and its rounded reciprocal.
+__device__ __forceinline__ void fill_divisors(float2* table, const float third) {
+  for (int i = threadIdx.x; i < 128; i += blockDim.x) {
+    const uint32_t wide = scales_to_f16(i);
+    const float d = __fmul_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)), third);
+    table[i] = make_float2(d, __frcp_rn(d));
+  }
 }
-// Eight values of a lane (half a block; the other half is in the neighbouring lane) -> their codes; *scale: the block's.
-__device__ __forceinline__ uint32_t quantise8(const float (&x)[8], const float inv6, const float third, uint32_t* scale) {
+
+// A block of 16 values -> its codes, and *scale.
+//
+// x / d is rounded to nearest by Markstein's correction of x times the rounded reciprocal: the remainder of that first quotient is
+// exact, and one step with it rounds correctly while nothing over- or underflows.  Blocks of infinities and of extreme scales
+// are divided.  (A code of zero has either sign.)
+__device__ __forceinline__ uint2 quantise16(const f32x2 (&x)[8], const float inv6, const float2* divisors, uint32_t* scale) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max_nan(m, fabsf(x[i]));
-  m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, 1));
+  for (int i = 0; i < 8; ++i) {
+    float a, b;
+    unpack2(x[i], a, b);
+    m = max3_nan(m, fabsf(a), fabsf(b));
+  }
   unsigned short s;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(0.f), "f"(__fmul_rn(m, inv6)));
-  *scale = s & 0xffu;
-  const uint32_t wide = scales_to_f16(*scale);
-  const float d = __fmul_rn(__low2float(*reinterpret_cast<const __half2*>(&wide)), third);
-  // x / d, rounded to nearest, by Markstein's correction of x times the rounded reciprocal: the remainder of the first
-  // quotient is exact, and one step with it rounds correctly while nothing over- or underflows (8 divisions: 110 instructions
-  // of 300).  Blocks of infinities and of extreme scales are divided.
-  const float by = __frcp_rn(d);
-  const bool plain = m < 1e30f && d > 1e-30f;     // (false for NaN, and for d == 0)
-  uint32_t w = 0;
+  *scale = s & 0x7fu;
+  const float2 div = divisors[s & 0x7fu];
+  const f32x2 by = pack2(div.y, div.y), d = pack2(-div.x, -div.x);
+  f32x2 q[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float q[2];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float first = __fmul_rn(x[2 * i + e], by);
-      q[e] = __fmaf_rn(__fmaf_rn(-first, d, x[2 * i + e]), by, first);
-    }
-    if (!plain) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) q[e] = d == 0.f ? 0.f : __fdiv_rn(x[2 * i + e], d);
-    }
-    uint32_t c;
-    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(c) : "f"(q[1]), "f"(q[0]));
-    w |= c << (8 * i);
+  for (int i = 0; i < 8; ++i) {
+    const f32x2 first = mul2(x[i], by);
+    q[i] = fma2(fma2(first, d, x[i]), by, first);
   }
-  return w;
+  if (!(m < 1e30f && div.x > 1e-30f)) {     // (NaN, and d == 0, too)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float a, b;
+      unpack2(x[i], a, b);
+      q[i] = div.x == 0.f ? 0ull : pack2(__fdiv_rn(a, div.x), __fdiv_rn(b, div.x));
+    }
+  }
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) unpack2(q[4 * i + e], v[2 * e], v[2 * e + 1]);
+    // (packed by shifts: with the four bytes packed by one move, the two upper ones came out wrong where the codes are widened
+    // again for the bounds)
+    w[i] = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t c;
+      asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}"
+          : "=r"(c)
+          : "f"(v[2 * e + 1]), "f"(v[2 * e]));
+      w[i] |= c << (8 * e);
+    }
+  }
+  return make_uint2(w[0], w[1]);
 }
 
-// Where the codes of row r, dimensions 8 c .. 8 c + 7, and the scale of block g lie inside a tile.
-__device__ __forceinline__ int k_code_at(const int r, const int c) {
-  return 512 * ((r >> 1) & 1) + 64 * ((r >> 2) * 2 + (r & 1)) + 4 * c;
+// Where the codes and the scale of block g of row r lie inside a tile.
+__device__ __forceinline__ int k_codes_at(const int r, const int g) {
+  return 512 * ((r >> 1) & 1) + 64 * ((r >> 2) * 2 + (r & 1)) + 8 * g;
 }
-__device__ __forceinline__ int v_code_at(const int r, const int c) {
-  return kTileV + 512 * ((r >> 1) & 1) + 64 * (c >> 1) + 16 * (r >> 2) + 8 * (r & 1) + 4 * (c & 1);
+__device__ __forceinline__ int v_codes_at(const int r, const int g) {
+  return kTileV + 512 * ((r >> 1) & 1) + 64 * g + 16 * (r >> 2) + 8 * (r & 1);
 }
 __device__ __forceinline__ int k_scale_at(const int r, const int g) {
   return kTileKs + 16 * ((r >> 2) * 2 + (r & 1)) + 4 * (g >> 1) + 2 * ((r >> 1) & 1) + (g & 1);
 }
 __device__ __forceinline__ int v_scale_at(const int r, const int g) { return kTileVs + 16 * g + r; }
 
+struct Raw16 {   // 16 values of 16 bits
+  uint4 a, b;
+};
+__device__ __forceinline__ uint32_t word16(const Raw16& r, const int i) {
+  return i == 0 ? r.a.x : i == 1 ? r.a.y : i == 2 ? r.a.z : i == 3 ? r.a.w : i == 4 ? r.b.x : i == 5 ? r.b.y : i == 6 ? r.b.z : r.b.w;
+}
 template <typename T>
-__device__ __forceinline__ void widen8(const uint4& raw, float (&x)[8]) {
-  const float2 a = widen2<T>(raw.x), b = widen2<T>(raw.y), c = widen2<T>(raw.z), d = widen2<T>(raw.w);
-  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y, x[4] = c.x, x[5] = c.y, x[6] = d.x, x[7] = d.y;
+__device__ __forceinline__ Raw16 load16(const T* src, const bool on) {
+  Raw16 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+  if (on) r.a = __ldg(reinterpret_cast<const uint4*>(src)), r.b = __ldg(reinterpret_cast<const uint4*>(src) + 1);
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ f32x2 wide2(const uint32_t w) {
+  const float2 v = widen2<T>(w);
+  return pack2(v.x, v.y);
+}
+template <>
+__device__ __forceinline__ f32x2 wide2<__nv_bfloat16>(const uint32_t w) { return bf16x2_wide(w); }
+
+// What a lane's block g is rotated by: cosines and sines of its pairs (ROPE 2: eight of each), from the token's row of the tables.
+// ROPE 1: pairs (i, i + rot / 2), 2: (2 i, 2 i + 1).
+template <int ROPE>
+struct Turn {
+  float4 cs[ROPE == 1 ? 4 : 2], sn[ROPE == 1 ? 4 : 2];
+};
+template <int ROPE>
+__device__ __forceinline__ Turn<ROPE> load_turn(const RowArgs& a, const int pos, const int g) {
+  Turn<ROPE> t;
+  const int half = a.rot >> 1;
+  const int at = ROPE == 2 ? 8 * g : 16 * g < half ? 16 * g : 16 * g - half;
+  const long long from = (long long)pos * half + (16 * g < a.rot ? at : 0);
+#pragma unroll
+  for (int i = 0; i < (ROPE == 1 ? 4 : 2); ++i)
+    t.cs[i] = __ldg(reinterpret_cast<const float4*>(a.cosv + from) + i), t.sn[i] = __ldg(reinterpret_cast<const float4*>(a.sinv + from) + i);
+  return t;
 }
 
-// Rotation of a lane's eight dimensions 8 c ..; products and differences are rounded one by one.
-// ROPE 1: pairs (i, i + rot / 2); 2: (2 i, 2 i + 1).  All lanes of the warp take part.
+// The rotation; products and sums are rounded one by one.  All lanes of the warp take part.
 template <typename T, int ROPE>
-__device__ __forceinline__ void rotate8(const uint4& raw, float (&x)[8], const int c, const int rot, const float* cosv,
-                                        const float* sinv) {
-  const int half = rot >> 1;
-  const bool inside = 8 * c < rot;
+__device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const int g, const int rot, const Turn<ROPE>& turn) {
+  const int half = rot >> 1, lane = threadIdx.x & 31;
+  const bool inside = 16 * g < rot;
   if constexpr (ROPE == 1) {
-    const int away = half >> 3;
-    const bool low = 8 * c < half;
-    const int lane = threadIdx.x & 31;
-    const int from = !inside ? lane : low ? lane + away : lane - away;
-    uint4 other;
-    other.x = __shfl_sync(0xffffffffu, raw.x, from), other.y = __shfl_sync(0xffffffffu, raw.y, from);
-    other.z = __shfl_sync(0xffffffffu, raw.z, from), other.w = __shfl_sync(0xffffffffu, raw.w, from);
-    if (!inside || !cosv) return;
-    float y[8], cs[8], sn[8];
-    widen8<T>(other, y);
-    const int at = low ? 8 * c : 8 * c - half;
+    const bool low = 16 * g < half;
+    const int from = !inside ? lane : low ? lane + (half >> 4) : lane - (half >> 4);
+    const uint32_t flip = low ? 0x80008000u : 0u;     // x cos - y sin is x cos + (-y) sin
+    uint32_t y[8];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      *reinterpret_cast<float4*>(&cs[4 * i]) = __ldg(reinterpret_cast<const float4*>(cosv + at) + i);
-      *reinterpret_cast<float4*>(&sn[4 * i]) = __ldg(reinterpret_cast<const float4*>(sinv + at) + i);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float own = __fmul_rn(x[i], cs[i]), cross = __fmul_rn(y[i], sn[i]);
-      x[i] = low ? __fsub_rn(own, cross) : __fadd_rn(own, cross);
-    }
-  } else if (ROPE == 2 && inside && cosv) {
-    const float4 cs = __ldg(reinterpret_cast<const float4*>(cosv + 4 * c)), sn = __ldg(reinterpret_cast<const float4*>(sinv + 4 * c));
-    const float cc[4] = {cs.x, cs.y, cs.z, cs.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
+    for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, word16(raw, i), from) ^ flip;
+    if (!inside) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = x[2 * i], b = x[2 * i + 1];
-      x[2 * i] = __fsub_rn(__fmul_rn(a, cc[i]), __fmul_rn(b, ss[i]));
-      x[2 * i + 1] = __fadd_rn(__fmul_rn(b, cc[i]), __fmul_rn(a, ss[i]));
+      const float4 cs = turn.cs[i], sn = turn.sn[i];
+      x[2 * i] = add2(mul2(x[2 * i], pack2(cs.x, cs.y)), mul2(wide2<T>(y[2 * i]), pack2(sn.x, sn.y)));
+      x[2 * i + 1] = add2(mul2(x[2 * i + 1], pack2(cs.z, cs.w)), mul2(wide2<T>(y[2 * i + 1]), pack2(sn.z, sn.w)));
+    }
+  } else if (ROPE == 2 && inside) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float4 cs = turn.cs[i], sn = turn.sn[i];
+      const float cc[4] = {cs.x, cs.y, cs.z, cs.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float p, q;
+        unpack2(x[4 * i + e], p, q);
+        x[4 * i + e] = add2(mul2(x[4 * i + e], pack2(cc[e], cc[e])), mul2(pack2(-q, p), pack2(ss[e], ss[e])));
+      }
     }
   }
 }
 
+// A CTA of two warps has one page, K and V of one row each; one of four warps has a run of pages (of a head mostly: what the next
+// page needs of the tables is in L1), every warp both.
 template <typename T, int ROPE>
-__global__ void __launch_bounds__(kRowThreads)
-k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v) {
-  __shared__ __half2 part[kRowThreads / 64][16][8];   // K warps: minima and maxima of eight dimensions
+__global__ void __launch_bounds__(kAppThreads, kAppPerSm)
+k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v, const int tasks, const int run) {
+  __shared__ float2 divisors[2][128];
+  __shared__ __half2 part[kAppThreads / 32][8][17];   // of every warp: minima and maxima of a block's eight pairs of dimensions
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane & 7, sub = lane >> 3;
+  fill_divisors(divisors[0], a.p.k_scale);
+  fill_divisors(divisors[1], a.p.v_scale);
   pdl_launch_dependents();
   pdl_wait();
-  const PageSpan s = page_span(a);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane & 15, pair = lane >> 4;
-  if (s.bad && tid == 0 && a.status) *a.status = MIXKV_ERR_INVALID_ARG;
-  if (s.id < 0) return;
-  const bool keys = (warp & 1) == 0;
-  const int half_warps = blockDim.x >> 6;
-  const T* src = keys ? k : v;
-  const long long row_stride = keys ? a.k_row : a.v_row;
-  const long long base = a.per_head ? 0 : s.h * (keys ? a.k_head : a.v_head);
-  const float third = keys ? a.p.k_scale : a.p.v_scale;
-  const float inv6 = (float)(1.0 / (6.0 * (double)third));
-  __half2 lo[4], hi[4];
+  const bool single = blockDim.x == 64;
+  const int step = single ? 4 : 4 * (blockDim.x >> 5);
+  const bool does_k = !single || warp == 0, does_v = !single || warp == 1;
+  __syncthreads();
+  const float k6 = (float)(1.0 / (6.0 * (double)a.p.k_scale)), v6 = (float)(1.0 / (6.0 * (double)a.p.v_scale));
+  bool bad = false;
+  const int end = min((int)(blockIdx.x + 1) * run, tasks);
+  for (int task = blockIdx.x * run; task < end; ++task) {
+    const PageSpan s = page_span(a, task);
+    const T* kr = k + (a.per_head ? 0 : s.h * a.k_head) + s.token * a.k_row + 16 * g;     // row r of the page at r * stride
+    const T* vr = v + (a.per_head ? 0 : s.h * a.v_head) + s.token * a.v_row + 16 * g;
+    const int* positions = a.positions + s.token;
+    const bool placed = s.id >= 0 && s.id < a.p.num_pages;
+    bad |= s.bad || (s.lo < s.hi && !placed);
+    __half2 lo[8], hi[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) lo[i] = __float2half2_rn(INFINITY), hi[i] = __float2half2_rn(-INFINITY);
-  const T* rows = src + base + (s.token - s.lo) * row_stride + 8 * c;    // row r of the page at r * row_stride
-  const int* positions = a.positions + (s.token - s.lo);
-  const PageRows in = rows_in(a, s);
-  for (int r0 = s.lo + 2 * (warp >> 1) + pair; r0 - pair < s.hi; r0 += 4 * half_warps) {
-    // two pairs of rows on their way at a time
-    uint4 raw[2];
-    int pos[2];
-    bool on[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = r0 + 2 * half_warps * j;
-      on[j] = r >= in.lo && r < in.hi;
-      pos[j] = ROPE && on[j] ? __ldg(positions + r) : 0;
-      raw[j] = on[j] ? __ldg(reinterpret_cast<const uint4*>(rows + r * row_stride)) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int r = r0 + 2 * half_warps * j;
-      if (r - pair >= s.hi) break;     // (the whole warp)
-      if (ROPE && (pos[j] < 0 || pos[j] >= a.table_len)) on[j] = false;   // (of V too: a token is written whole or not at all)
-      if (r < s.hi && !on[j] && c == 0 && a.status) *a.status = MIXKV_ERR_INVALID_ARG;
-      float x[8];
-      widen8<T>(raw[j], x);
-      if (ROPE && keys) {
-        const long long at = (long long)pos[j] * (a.rot >> 1);
-        rotate8<T, ROPE>(raw[j], x, c, a.rot, on[j] ? a.cosv + at : nullptr, a.sinv + at);
+    for (int i = 0; i < 8; ++i) lo[i] = __float2half2_rn(INFINITY), hi[i] = __float2half2_rn(-INFINITY);
+
+    int r = s.lo + (single ? 0 : 4 * warp) + sub;
+    bool on = r >= s.first && r < s.last;
+    Raw16 kk = load16(kr + r * a.k_row, on && does_k), vv = load16(vr + r * a.v_row, on && does_v);
+    int pos = ROPE && on ? __ldg(positions + r) : 0;
+    for (; r - sub < s.hi; r += step) {
+      const Raw16 kx = kk, vx = vv;
+      const int at = pos;
+      const bool have = on;
+      if (r - sub + step < s.hi) {      // the next rows on their way
+        const int next = r + step;
+        on = next >= s.first && next < s.last;
+        kk = load16(kr + next * a.k_row, on && does_k), vv = load16(vr + next * a.v_row, on && does_v);
+        pos = ROPE && on ? __ldg(positions + next) : 0;
       }
-      uint32_t scale;
-      const uint32_t w = quantise8(x, inv6, third, &scale);
-      if (!on[j]) continue;
-      unsigned char* tile = tile_ptr(a.p, s.id, r / kPageTile);
+      const bool turned = at >= 0 && at < a.table_len;
+      const bool write = have && placed && (!ROPE || turned);      // (a token is written whole or not at all)
+      bad |= r < s.hi && !write;
+      unsigned char* tile = tile_ptr(a.p, placed ? s.id : 0, r / kPageTile);
       const int rt = r % kPageTile;
-      *reinterpret_cast<uint32_t*>(tile + (keys ? k_code_at(rt, c) : v_code_at(rt, c))) = w;
-      if ((c & 1) == 0) tile[keys ? k_scale_at(rt, c >> 1) : v_scale_at(rt, c >> 1)] = (unsigned char)scale;
-      if (keys && a.p.bounds) {
-        uint32_t f[4];
-        codes_to_f16(w, f);
-        const uint32_t ss = scales_to_f16(scale | scale << 8);
+      Turn<ROPE> turn;      // (on its way while V is rounded)
+      if (ROPE && does_k) turn = load_turn<ROPE>(a, turned ? at : 0, g);
+      if (does_v) {
+        f32x2 x[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t y = mul_f16x2(f[i], ss);
-          lo[i] = __hmin2_nan(lo[i], *reinterpret_cast<const __half2*>(&y));
-          hi[i] = __hmax2_nan(hi[i], *reinterpret_cast<const __half2*>(&y));
+        for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(vx, i));
+        uint32_t scale;
+        const uint2 w = quantise16(x, v6, divisors[1], &scale);
+        if (write) {
+          *reinterpret_cast<uint2*>(tile + v_codes_at(rt, g)) = w;
+          tile[v_scale_at(rt, g)] = (unsigned char)scale;
+        }
+      }
+      if (does_k) {
+        f32x2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(kx, i));
+        if constexpr (ROPE != 0) {
+          rotate16<T, ROPE>(kx, x, g, a.rot, turn);
+        }
+        uint32_t scale;
+        const uint2 w = quantise16(x, k6, divisors[0], &scale);
+        if (write) {
+          *reinterpret_cast<uint2*>(tile + k_codes_at(rt, g)) = w;
+          tile[k_scale_at(rt, g)] = (unsigned char)scale;
+          if (a.p.bounds) {
+            uint32_t f[8];
+            codes_to_f16(w.x, *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
+            codes_to_f16(w.y, *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
+            const uint32_t ss = scales_to_f16(scale | scale << 8);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const uint32_t y = mul_f16x2(f[i], ss);
+              lo[i] = __hmin2_nan(lo[i], *reinterpret_cast<const __half2*>(&y));
+              hi[i] = __hmax2_nan(hi[i], *reinterpret_cast<const __half2*>(&y));
+            }
+          }
         }
       }
     }
-  }
-  if (!a.p.bounds) return;
-  if (keys) {
+    if (!a.p.bounds || !placed || s.lo >= s.hi) continue;
+    if (does_k) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo[i] = __hmin2_nan(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], 16));
-      hi[i] = __hmax2_nan(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], 16));
-      if (pair == 0) part[warp >> 1][c][i] = lo[i], part[warp >> 1][c][4 + i] = hi[i];
+      for (int i = 0; i < 8; ++i) {
+#pragma unroll
+        for (int o = 8; o < 32; o <<= 1) {
+          lo[i] = __hmin2_nan(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
+          hi[i] = __hmax2_nan(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
+        }
+        if (sub == 0) part[warp][g][i] = lo[i], part[warp][g][8 + i] = hi[i];
+      }
     }
-  }
-  __syncthreads();
-  if (tid < 128) {   // a thread takes one pair of dimensions of one bound (64 threads: two)
+    __syncthreads();
+    const int warps = single ? 1 : min((int)(blockDim.x >> 5), (s.hi - s.lo + 3) / 4);    // those that had rows
     for (int e = tid; e < 128; e += blockDim.x) {
-      const int cc = e >> 3, i = e & 7;   // (i < 4: minimum)
-      __half2 x = part[0][cc][i];
-      for (int w = 1; w < half_warps; ++w) x = i < 4 ? __hmin2_nan(x, part[w][cc][i]) : __hmax2_nan(x, part[w][cc][i]);
-      __half2* out = reinterpret_cast<__half2*>(a.p.bounds + ((long long)s.id * 2 + (i >> 2)) * kHeadDim) + 4 * cc + (i & 3);
-      if (s.lo > 0) x = i < 4 ? __hmin2_nan(x, *out) : __hmax2_nan(x, *out);
+      const bool most = e & 64;
+      const int block = (e & 63) >> 3, i = (most ? 8 : 0) + (e & 7);
+      __half2 x = part[0][block][i];
+      for (int w = 1; w < warps; ++w) x = most ? __hmax2_nan(x, part[w][block][i]) : __hmin2_nan(x, part[w][block][i]);
+      __half2* out = reinterpret_cast<__half2*>(a.p.bounds + ((long long)s.id * 2 + most) * kHeadDim) + (e & 63);
+      if (s.lo > 0) x = most ? __hmax2_nan(x, *out) : __hmin2_nan(x, *out);
       *out = x;
     }
+    if (task + 1 < end) __syncthreads();    // `part` is written again
   }
+  if (bad && a.status) *a.status = MIXKV_ERR_INVALID_ARG;
 }
 
-// A lane has eight dimensions of a row, as above.
+// A lane has a block of a row, as above.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) k_paged_read(const RowArgs a, T* __restrict__ k, T* __restrict__ v) {
   pdl_launch_dependents();
   pdl_wait();
-  const PageSpan s = page_span(a);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane & 15, pair = lane >> 4;
-  if (s.id < 0) return;
+  const PageSpan s = page_span(a, blockIdx.x);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane & 7, sub = lane >> 3;
+  if (s.id < 0 || s.id >= a.p.num_pages) return;
   const bool keys = (warp & 1) == 0;
-  T* dst = keys ? k : v;
   const float third = keys ? a.p.k_scale : a.p.v_scale;
-  const PageRows in = rows_in(a, s);
-  const long long out_stride = a.per_head ? kHeadDim : (long long)a.p.H * kHeadDim;
-  T* rows = dst + (s.token - s.lo) * out_stride + (a.per_head ? 0 : s.h * kHeadDim) + 8 * c;   // row r of the page at r * out_stride
-  const int step = blockDim.x >> 5;
-  for (int r0 = s.lo + 2 * (warp >> 1) + pair; r0 < in.hi; r0 += 4 * step) {
-    uint32_t w[4], scale[4];
+  const long long stride = a.per_head ? kHeadDim : (long long)a.p.H * kHeadDim;
+  T* rows = (keys ? k : v) + (a.per_head ? 0 : s.h * kHeadDim) + s.token * stride + 16 * g;   // row r of the page at r * stride
+  const int step = 4 * (blockDim.x >> 6);
+  for (int r0 = s.first + 4 * (warp >> 1) + sub; r0 < s.last; r0 += 2 * step) {
+    uint2 w[2];
+    uint32_t scale[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = min(r0 + j * step, s.hi - 1), rt = r % kPageTile;
+    for (int j = 0; j < 2; ++j) {
+      const int r = min(r0 + j * step, s.last - 1), rt = r % kPageTile;
       const unsigned char* tile = tile_ptr(a.p, s.id, r / kPageTile);
-      w[j] = *reinterpret_cast<const uint32_t*>(tile + (keys ? k_code_at(rt, c) : v_code_at(rt, c)));
-      scale[j] = tile[keys ? k_scale_at(rt, c >> 1) : v_scale_at(rt, c >> 1)];
+      w[j] = *reinterpret_cast<const uint2*>(tile + (keys ? k_codes_at(rt, g) : v_codes_at(rt, g)));
+      scale[j] = tile[keys ? k_scale_at(rt, g) : v_scale_at(rt, g)];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const int r = r0 + j * step;
-      if (r < in.lo || r >= in.hi) continue;
-      uint32_t f[4], out[4];
-      codes_to_f16(w[j], f);
+      if (r >= s.last) break;
+      uint32_t f[8], out[8];
+      codes_to_f16(w[j].x, *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
+      codes_to_f16(w[j].y, *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
       const uint32_t ss = scales_to_f16(scale[j] | scale[j] << 8);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 8; ++i) {
         const float2 y = widen2<__half>(mul_f16x2(f[i], ss));
         out[i] = narrow2<T>(__fmul_rn(y.x, third), __fmul_rn(y.y, third));
       }
-      *reinterpret_cast<uint4*>(rows + r * out_stride) = make_uint4(out[0], out[1], out[2], out[3]);
+      uint4* to = reinterpret_cast<uint4*>(rows + r * stride);
+      to[0] = make_uint4(out[0], out[1], out[2], out[3]), to[1] = make_uint4(out[4], out[5], out[6], out[7]);
     }
   }
 }
@@ -319,21 +394,28 @@ int check_rows(const mixkv_pages* c, int32_t type, int64_t num_tokens, const int
   if ((long long)c->batch * c->kv_heads * a->slots > 0x7fffffffll) return MIXKV_ERR_UNSUPPORTED;
   return MIXKV_OK;
 }
-template <typename F, typename... Args>
-int launch_rows(F kernel, const mixkv_pages* c, const RowArgs& a, void* stream, Args... args) {
-  const int rc = device_check(nullptr);
-  if (rc != MIXKV_OK) return rc;
-  const dim3 grid((unsigned)(c->batch * c->kv_heads * a.slots)), block(a.max_new > 1 ? kRowThreads : 64);
-  return launch_pdl(kernel, grid, block, 0, (cudaStream_t)stream, 1, a, args...) == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
-}
+int tasks_of(const mixkv_pages* c, const RowArgs& a) { return c->batch * c->kv_heads * a.slots; }
 template <typename T>
 int append_as(const mixkv_pages* c, const RowArgs& a, const void* k, const void* v, const int rope, void* stream) {
-  const T *kk = static_cast<const T*>(k), *vv = static_cast<const T*>(v);
-  switch (rope) {
-    case 0: return launch_rows(k_paged_append<T, 0>, c, a, stream, kk, vv);
-    case 1: return launch_rows(k_paged_append<T, 1>, c, a, stream, kk, vv);
-    default: return launch_rows(k_paged_append<T, 2>, c, a, stream, kk, vv);
-  }
+  const int rc = device_check(nullptr);
+  if (rc != MIXKV_OK) return rc;
+  void (*kernel)(RowArgs, const T*, const T*, int, int) =
+      rope == 0 ? k_paged_append<T, 0> : rope == 1 ? k_paged_append<T, 1> : k_paged_append<T, 2>;
+  const int tasks = tasks_of(c, a), slots = kAppPerSm * device_sm_count();
+  const int run = a.max_new > 1 ? (tasks + slots - 1) / slots : 1;
+  return launch_pdl(kernel, dim3((unsigned)((tasks + run - 1) / run)), dim3(a.max_new > 1 ? kAppThreads : 64), 0,
+                    (cudaStream_t)stream, 1, a, static_cast<const T*>(k), static_cast<const T*>(v), tasks, run) == cudaSuccess
+             ? MIXKV_OK
+             : MIXKV_ERR_CUDA;
+}
+template <typename T>
+int read_as(const mixkv_pages* c, const RowArgs& a, void* k, void* v, void* stream) {
+  const int rc = device_check(nullptr);
+  if (rc != MIXKV_OK) return rc;
+  return launch_pdl(k_paged_read<T>, dim3((unsigned)tasks_of(c, a)), dim3(a.max_new > 1 ? kRowThreads : 64), 0,
+                    (cudaStream_t)stream, 1, a, static_cast<T*>(k), static_cast<T*>(v)) == cudaSuccess
+             ? MIXKV_OK
+             : MIXKV_ERR_CUDA;
 }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -367,7 +449,7 @@ extern "C" int mixkv_paged_append(const mixkv_pages* c, const void* k, const voi
     if (!positions_opt || table_len < 1 || !aligned16(cos_opt) || !aligned16(sin_opt) || rot_dim < 1 || rot_dim > kHeadDim ||
         (reinterpret_cast<uintptr_t>(positions_opt) & 3u))
       return MIXKV_ERR_INVALID_ARG;
-    if (rot_dim % 16) return MIXKV_ERR_UNSUPPORTED;
+    if (rot_dim % (interleaved ? 16 : 32)) return MIXKV_ERR_UNSUPPORTED;
   }
   a.k_row = k_row_stride, a.k_head = k_head_stride, a.v_row = v_row_stride, a.v_head = v_head_stride;
   a.cosv = cos_opt, a.sinv = sin_opt, a.positions = positions_opt, a.table_len = table_len, a.rot = rot_dim;
@@ -383,8 +465,6 @@ extern "C" int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, 
   const int rc = check_rows(c, type, num_tokens, offsets_opt, offsets_per_head, max_new, &a);
   if (rc != MIXKV_OK) return rc;
   if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return MIXKV_ERR_INVALID_ARG;
-  if (type == MIXKV_TYPE_BF16)
-    return launch_rows(k_paged_read<__nv_bfloat16>, c, a, stream, static_cast<__nv_bfloat16*>(k_out),
-                       static_cast<__nv_bfloat16*>(v_out));
-  return launch_rows(k_paged_read<__half>, c, a, stream, static_cast<__half*>(k_out), static_cast<__half*>(v_out));
+  return type == MIXKV_TYPE_BF16 ? read_as<__nv_bfloat16>(c, a, k_out, v_out, stream)
+                                 : read_as<__half>(c, a, k_out, v_out, stream);
 }
