@@ -106,4 +106,10 @@ __device__ __forceinline__ uint32_t mul_f16x2(const uint32_t a, const uint32_t b
   return r;
 }
 
+__device__ __forceinline__ f32x2 mul2(const f32x2 a, const f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 }  // namespace mixkv

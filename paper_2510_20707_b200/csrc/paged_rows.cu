@@ -68,12 +68,6 @@ __device__ __forceinline__ float max3_nan(const float x, const float y, const fl
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
 }
-__device__ __forceinline__ f32x2 mul2(const f32x2 a, const f32x2 b) {
-  f32x2 d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 // Of every scale byte: scale * third and its rounded reciprocal.
 __device__ __forceinline__ void fill_divisors(float2* table, const float third) {
   for (int i = threadIdx.x; i < 128; i += blockDim.x) {

@@ -18,7 +18,9 @@ namespace {
 
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32;
 constexpr int kSelBins = 2 * kSelThreads;
-constexpr int kSelPages = 4, kSelRows = 8;   // pages of a warp at a time; query rows at a time
+// Query rows at a time, and pages of a warp at a time: 32 sums.
+__host__ __device__ constexpr int rows_at_once(const int R) { return R <= 4 ? 4 : 8; }
+__host__ __device__ constexpr int padded_rows(const int R) { return (R + rows_at_once(R) - 1) / rows_at_once(R) * rows_at_once(R); }
 constexpr uint32_t kKeyForced = 0xffffffffu, kKeyNan = 0xfffffffeu;   // (no number has either)
 
 struct SelArgs {
@@ -51,11 +53,6 @@ __device__ __forceinline__ float sum_each(float (&v)[32], const int lane) {
   return v[0];
 }
 
-// Bounds of four pages, as they lie in memory: dimensions 4 lane .. + 3.
-struct PageBounds {
-  uint2 lo[kSelPages], hi[kSelPages];
-};
-
 // Sum of x over the CTA's threads before this one (exclusive); *total: of all.  sums: a word per warp.
 __device__ __forceinline__ uint32_t block_before(const uint32_t x, uint32_t* sums, uint32_t* total, const int lane, const int warp) {
   uint32_t upto = x;
@@ -77,43 +74,80 @@ __device__ __forceinline__ uint32_t block_before(const uint32_t x, uint32_t* sum
   return before + upto - x;
 }
 
+// Words of pages begin .. end - 1 of a unit that has `pages`, by one warp; the next pages' bounds are on their way meanwhile.
+template <int RP>
+__device__ __forceinline__ void score_run(const SelArgs& a, const int* table, const int pages, const int begin, const int end,
+                                          const float4* qs, uint32_t* keys) {
+  constexpr int kPages = 32 / RP;
+  const int lane = threadIdx.x & 31;
+  // Bounds as they lie in memory, dimensions 4 lane .. + 3.  Of four pages at a time there is room for the next ones; eight are
+  // asked for again where they were.
+  constexpr int kSets = RP == 8 ? 2 : 1;
+  uint2 lo[kSets][kPages], hi[kSets][kPages];
+  int ids = begin + lane < end ? __ldg(table + begin + lane) : -1;     // of 32 pages from the last multiple of 32
+  auto fetch = [&](const int p0, uint2 (&to_lo)[kPages], uint2 (&to_hi)[kPages]) {
+#pragma unroll
+    for (int i = 0; i < kPages; ++i) {
+      const int id = __shfl_sync(0xffffffffu, ids, (p0 - begin + i) & 31);
+      to_lo[i] = to_hi[i] = make_uint2(0, 0);    // (a page outside the pool scores zero)
+      if (p0 + i < end && id >= 0 && id < a.p.num_pages) {
+        const __half* src = a.p.bounds + (long long)id * 2 * kHeadDim + 4 * lane;
+        to_lo[i] = __ldg(reinterpret_cast<const uint2*>(src)), to_hi[i] = __ldg(reinterpret_cast<const uint2*>(src + kHeadDim));
+      }
+    }
+  };
+  fetch(begin, lo[kSets - 1], hi[kSets - 1]);
+  for (int p0 = begin; p0 < end; p0 += kPages) {
+    uint32_t best = 0;
+    const bool more = p0 + kPages < end;
+    if (more && (p0 + kPages - begin) % 32 == 0) ids = p0 + kPages + lane < end ? __ldg(table + p0 + kPages + lane) : -1;
+    if constexpr (kSets == 2) {
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) lo[0][i] = lo[1][i], hi[0][i] = hi[1][i];
+      if (more) fetch(p0 + kPages, lo[1], hi[1]);
+    }
+#pragma unroll 1
+    for (int r0 = 0; r0 < padded_rows(a.R); r0 += RP) {
+      float v[32];
+#pragma unroll
+      for (int i = 0; i < kPages; ++i) {
+        const float2 l0 = widen2<__half>(lo[0][i].x), l1 = widen2<__half>(lo[0][i].y);
+        const float2 h0 = widen2<__half>(hi[0][i].x), h1 = widen2<__half>(hi[0][i].y);
+#pragma unroll
+        for (int r = 0; r < RP; ++r) {
+          const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
+          const float x0 = fmaf(up.x, h0.x, __fmul_rn(dn.x, l0.x)), x1 = fmaf(up.y, h0.y, __fmul_rn(dn.y, l0.y));
+          const float x2 = fmaf(up.z, h1.x, __fmul_rn(dn.z, l1.x)), x3 = fmaf(up.w, h1.y, __fmul_rn(dn.w, l1.y));
+          v[RP * i + r] = __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
+        }
+      }
+      if (kSets == 1 && more) fetch(p0 + kPages, lo[0], hi[0]);      // (RP == 4: there is one round of query rows)
+      uint32_t k = key_of(sum_each(v, lane));
+      // the first lane bits (the first halvings) are the page's, the others the query row's
+#pragma unroll
+      for (int o = kPages; o < 32; o <<= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+      best = max(best, k);
+    }
+    const int p = p0 + (int)(__brev(lane) >> (RP == 8 ? 30 : 29));
+    if (lane < kPages && p < end) keys[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a) {
   extern __shared__ __align__(16) unsigned char sm[];
   cg::cluster_group cluster = cg::this_cluster();
   const int S = (int)cluster.num_blocks(), crank = (int)cluster.block_rank(), u = blockIdx.x / S;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int b = u / a.p.H, h = u % a.p.H, rows_pad = (a.R + kSelRows - 1) / kSelRows * kSelRows;
+  const int b = u / a.p.H, h = u % a.p.H;
   float4* qs = reinterpret_cast<float4*>(sm);                    // [R padded][2][32]: max(q, 0), min(q, 0)
-  uint32_t* keys = reinterpret_cast<uint32_t*>(qs + rows_pad * 64);   // [pages], the first CTA's
+  uint32_t* keys = reinterpret_cast<uint32_t*>(qs + padded_rows(a.R) * 64);   // [pages], the first CTA's
   __shared__ uint32_t hist[kSelBins];
   __shared__ uint32_t sums[2][kSelWarps];
   __shared__ uint32_t found[2];
   pdl_launch_dependents();
   pdl_wait();
-  int n = min(a.p.rows[u], a.max_rows);
-  n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
-  const int pages = n <= 0 ? 0 : min((n + a.p.page_rows - 1) / a.p.page_rows, a.pages);
-  // a warp takes a run of pages, four at a time; the next four's bounds are on their way meanwhile
-  const int share = (pages + S * kSelWarps - 1) / (S * kSelWarps), run = (share + kSelPages - 1) / kSelPages * kSelPages;
-  const int begin = (crank * kSelWarps + warp) * run, end = min(begin + run, pages);
-  const int* table = a.p.table + (long long)u * a.p.max_pages;
-  int ids = begin + lane < end ? __ldg(table + begin + lane) : -1;     // of 32 pages from the last multiple of 32
-  auto fetch = [&](const int p0) {
-    PageBounds r;
-#pragma unroll
-    for (int i = 0; i < kSelPages; ++i) {
-      const int id = __shfl_sync(0xffffffffu, ids, (p0 - begin + i) & 31);
-      r.lo[i] = r.hi[i] = make_uint2(0, 0);    // (a page outside the pool scores zero)
-      if (p0 + i < end && id >= 0 && id < a.p.num_pages) {
-        const __half* src = a.p.bounds + (long long)id * 2 * kHeadDim + 4 * lane;
-        r.lo[i] = __ldg(reinterpret_cast<const uint2*>(src)), r.hi[i] = __ldg(reinterpret_cast<const uint2*>(src + kHeadDim));
-      }
-    }
-    return r;
-  };
-  PageBounds next = fetch(begin);
-  for (int e = tid; e < rows_pad * 32; e += kSelThreads) {
+  for (int e = tid; e < padded_rows(a.R) * 32; e += kSelThreads) {
     const int r = min(e >> 5, a.R - 1);      // (the rows of the padding repeat the last: a maximum does not mind)
     const T* src = static_cast<const T*>(a.q) + b * a.q_batch + (r / a.G) * a.q_token +
                    (long long)(h * a.G + r % a.G) * kHeadDim + 4 * (e & 31);
@@ -125,39 +159,18 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
     qs[(e >> 5) * 64 + (e & 31)] = make_float4(up(x.x), up(x.y), up(y.x), up(y.y));
     qs[(e >> 5) * 64 + 32 + (e & 31)] = make_float4(down(x.x), down(x.y), down(y.x), down(y.y));
   }
+  int n = min(a.p.rows[u], a.max_rows);
+  n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
+  const int pages = n <= 0 ? 0 : min((n + a.p.page_rows - 1) / a.p.page_rows, a.pages);
+  const int* table = a.p.table + (long long)u * a.p.max_pages;
+  const int at_once = 32 / rows_at_once(a.R), share = (pages + S * kSelWarps - 1) / (S * kSelWarps);
+  const int run = (share + at_once - 1) / at_once * at_once, begin = (crank * kSelWarps + warp) * run;
   uint32_t* keys0 = cluster.map_shared_rank(keys, 0);
   if (S > 1) cluster.sync();     // the first CTA runs
   else __syncthreads();
-  for (int p0 = begin; p0 < end; p0 += kSelPages) {
-    const PageBounds now = next;
-    if (p0 + kSelPages < end) {
-      if ((p0 + kSelPages - begin) % 32 == 0) ids = p0 + kSelPages + lane < end ? __ldg(table + p0 + kSelPages + lane) : -1;
-      next = fetch(p0 + kSelPages);
-    }
-    uint32_t best = 0;
-#pragma unroll 1
-    for (int r0 = 0; r0 < rows_pad; r0 += kSelRows) {
-      float v[32];
-#pragma unroll
-      for (int i = 0; i < kSelPages; ++i) {
-        const float2 l0 = widen2<__half>(now.lo[i].x), l1 = widen2<__half>(now.lo[i].y);
-        const float2 h0 = widen2<__half>(now.hi[i].x), h1 = widen2<__half>(now.hi[i].y);
-#pragma unroll
-        for (int r = 0; r < kSelRows; ++r) {
-          const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
-          const float x0 = fmaf(up.x, h0.x, __fmul_rn(dn.x, l0.x)), x1 = fmaf(up.y, h0.y, __fmul_rn(dn.y, l0.y));
-          const float x2 = fmaf(up.z, h1.x, __fmul_rn(dn.z, l1.x)), x3 = fmaf(up.w, h1.y, __fmul_rn(dn.w, l1.y));
-          v[kSelRows * i + r] = __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
-        }
-      }
-      uint32_t k = key_of(sum_each(v, lane));
-      // lane bits 0, 1 (the first halvings) are the page's, 2 .. 4 the query row's
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
-      best = max(best, k);
-    }
-    const int p = p0 + (__brev(lane) >> 30);
-    if (lane < 4 && p < end) keys0[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
+  if (begin < pages) {
+    if (a.R <= 4) score_run<4>(a, table, pages, begin, min(begin + run, pages), qs, keys0);
+    else score_run<8>(a, table, pages, begin, min(begin + run, pages), qs, keys0);
   }
   if (S > 1) cluster.sync();
   else __syncthreads();
@@ -224,7 +237,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
 }
 
 size_t select_smem(const int R, const int pages) {
-  return (size_t)((R + kSelRows - 1) / kSelRows * kSelRows) * 1024 + (size_t)pages * 4;
+  return (size_t)padded_rows(R) * 1024 + (size_t)pages * 4;
 }
 
 }  // namespace
@@ -260,7 +273,7 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   if (ensure_smem(kernel, most, done[bf16]) != cudaSuccess) return MIXKV_ERR_CUDA;
   // as many CTAs as keep four pages for every warp, while they fit the GPU
   int S = (int)(device_sm_count() / units < kMaxCluster ? device_sm_count() / units : kMaxCluster);
-  const long long rounds = (pages + kSelWarps * kSelPages - 1) / (kSelWarps * kSelPages);
+  const long long rounds = (pages + kSelWarps * 4 - 1) / (kSelWarps * 4);
   if (S > rounds) S = (int)rounds;
   if (S < 1) S = 1;
   const cudaError_t e = launch_pdl(kernel, dim3((unsigned)(units * S)), dim3(kSelThreads), smem, (cudaStream_t)stream, S, a);
