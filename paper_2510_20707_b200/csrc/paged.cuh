@@ -13,6 +13,22 @@ constexpr int kTileBytes = MIXKV_PAGE_TILE_BYTES;
 constexpr int kTileV = 1024, kTileKs = 2048, kTileVs = 2176;  // V codes, K scales, V scales inside a tile
 static_assert(kTileBytes == kTileVs + 128, "a tile");
 
+// n / d for 0 <= n < 2^31 as a product: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, n m exceeds n 2^(31 + l) / d by
+// less than 2^(31 + l) / d (n < 2^31, and m d - 2^(31 + l) <= 2^l).  A division of the hardware's kind is a chain of some twenty
+// instructions; a kernel of a few microseconds begins and ends with a handful of them.
+struct Divider {
+  uint32_t d, mul;
+  int shift;
+  Divider() = default;
+  explicit Divider(const uint32_t by) : d(by), mul(0), shift(0) {
+    int l = 0;
+    while ((1ull << l) < by) ++l;
+    if (l) mul = (uint32_t)((1ull << (31 + l)) / by + 1), shift = l - 1;
+  }
+  __device__ __forceinline__ int div(const int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
+  __device__ __forceinline__ int mod(const int n) const { return n - div(n) * (int)d; }
+};
+
 // What kernels take of a mixkv_pages.
 struct PagePool {
   unsigned char* pool;
@@ -23,6 +39,7 @@ struct PagePool {
   int max_pages, page_rows, tiles;   // tiles of a page
   int H;
   float k_scale, v_scale;
+  Divider by_heads, by_rows, by_tiles;   // of kv_heads, page_rows, tiles
 };
 
 inline int check_pages(const mixkv_pages* c, PagePool* p) {
@@ -40,7 +57,8 @@ inline int check_pages(const mixkv_pages* c, PagePool* p) {
       c->num_pages > 0x7fffffffll / (c->page_rows / kPageTile))
     return MIXKV_ERR_UNSUPPORTED;
   *p = PagePool{static_cast<unsigned char*>(c->pool), static_cast<__half*>(c->bounds_opt), c->table, c->rows,
-                c->num_pages, c->max_pages, c->page_rows, c->page_rows / kPageTile, c->kv_heads, c->k_scale, c->v_scale};
+                c->num_pages, c->max_pages, c->page_rows, c->page_rows / kPageTile, c->kv_heads, c->k_scale, c->v_scale, Divider(c->kv_heads),
+                Divider(c->page_rows), Divider(c->page_rows / kPageTile)};
   return MIXKV_OK;
 }
 
@@ -84,6 +102,13 @@ template <>
 __device__ __forceinline__ uint32_t narrow2<__half>(float x, float y) {
   const __half2 v = __floats2half2_rn(x, y);
   return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// This CTA's cluster in the grid (a CTA outside of one: its own number).
+__device__ __forceinline__ int cluster_id() {
+  uint32_t r;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(r));
+  return (int)r;
 }
 
 // The four bytes of a word, two codes each, as four fp16 pairs (low code in the low half).

@@ -46,11 +46,13 @@ struct AttArgs {
   const void* q;
   long long q_batch, q_token;
   int T, G, R;               // tokens, heads of a group, T * G
+  Divider by_group;          // of G
   int max_rows;
   const int *list, *counts;  // nullptr: all pages
   int top;
   int units;
   int ctas;                  // that share all steps evenly; 0: a cluster has a unit
+  int per;                   // outputs of a CTA of such a cluster
   float scale_log2e;         // k_scale included
   int* starts;               // [units + 1]: first step of every unit, units one after the other
   float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
@@ -64,11 +66,11 @@ struct UnitTiles {
 };
 __device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
   UnitTiles r;
-  int n = a.p.rows[u];
+  int n = __ldg(a.p.rows + u);
   n = min(n, a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
   r.n = max(n, 0);
-  r.tiles = a.list ? max(0, min(a.counts[u], a.top)) * a.p.tiles : (r.n + kPageTile - 1) / kPageTile;
+  r.tiles = a.list ? max(0, min(__ldg(a.counts + u), a.top)) * a.p.tiles : (r.n + kPageTile - 1) >> 4;
   r.steps = (r.tiles + 1) >> 1;
   return r;
 }
@@ -102,25 +104,29 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, const uint
                : "memory");
 }
 
-// Place in the pool and first row of tile `t` of a unit (-1, kNoRow: none).
+// Place in the pool and first row of tile `t` of a unit (-1, kNoRow: none).  The table is asked before the unit's rows are looked at:
+// both may be on their way.
 struct TileAt {
   int tile, row;
 };
 __device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const UnitTiles& ut, const int t) {
-  TileAt r = {-1, kNoRow};
-  if (t >= ut.tiles) return r;
-  const int slot = t / a.p.tiles, in = t - slot * a.p.tiles;
-  const int page = a.list ? a.list[(long long)u * a.top + slot] : slot;
-  if (page < 0 || page >= a.p.max_pages) return r;
+  const int slot = a.p.by_tiles.div(t), in = t - slot * a.p.tiles;
+  int page = slot;
+  if (a.list) page = slot < a.top ? __ldg(a.list + (long long)u * a.top + slot) : -1;
+  const int id = page >= 0 && page < a.p.max_pages ? __ldg(a.p.table + (long long)u * a.p.max_pages + page) : -1;
   const int row = page * a.p.page_rows + in * kPageTile;
-  if (row >= ut.n) return r;
-  const int id = a.p.table[(long long)u * a.p.max_pages + page];
-  if (id >= 0 && id < a.p.num_pages) r.tile = id * a.p.tiles + in, r.row = row;
-  return r;
+  if (id < 0 || id >= a.p.num_pages || t >= ut.tiles || row >= ut.n) return TileAt{-1, kNoRow};
+  return TileAt{id * a.p.tiles + in, row};
 }
 
 // Steps of a CTA when `ctas` of them share `total`: CTA c has those from c * share on, the last ones may have none.
 __device__ __forceinline__ int share_of(const int total, const int ctas) { return (total + ctas - 1) / ctas; }
+
+// Row of the output that query row r of a unit has.
+__device__ __forceinline__ long long out_row(const AttArgs& a, const int u, const int r) {
+  const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
+  return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
+}
 
 // The first `keep` of the four scales of a word, zeros for the others.
 __device__ __forceinline__ uint32_t keep_scales(const uint32_t w, const int keep) {
@@ -146,7 +152,7 @@ __device__ __forceinline__ void values(const uint4 (&v)[2], const uint32_t vs, c
   }
 }
 // Token of query row r of a unit (rows of the padding: the last).
-__device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return min(r, a.R - 1) / a.G; }
+__device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return a.by_group.div(min(r, a.R - 1)); }
 
 template <typename T, int NT>
 struct AttState {
@@ -158,14 +164,15 @@ struct AttState {
   // Query rows first .. first + 8 NT - 1 of a unit.  bf16 rows are divided by a power of two that brings their largest
   // magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it; the power goes into f.
   __device__ __forceinline__ void start(const AttArgs& a, const int u, const int first, const int g, const int t) {
-    const int b = u / a.p.H, h = u % a.p.H;
+    const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = first + 8 * nt + g;
       uint4 raw[4];
       const bool on = r < a.R;
-      const T* src = static_cast<const T*>(a.q) + b * a.q_batch + (on ? r / a.G : 0) * a.q_token +
-                     (long long)(h * a.G + (on ? r % a.G : 0)) * kHeadDim + 32 * t;
+      const int token = on ? a.by_group.div(r) : 0;
+      const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
+                     (long long)(h * a.G + (on ? r - token * a.G : 0)) * kHeadDim + 32 * t;
 #pragma unroll
       for (int i = 0; i < 4; ++i) raw[i] = on ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
       float most = 0.f;
@@ -385,7 +392,7 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
   pdl_wait();
 
   // steps lo .. hi - 1: of a cluster's unit, or of all units one after the other
-  int u = shares ? 0 : blockIdx.x / S, lo = crank * kAttWarps, hi;
+  int u = shares ? 0 : cluster_id(), lo = crank * kAttWarps, hi;
   if (shares) {
     // first steps of all units: a thread takes consecutive ones
     constexpr int kEach = kAttUnits / kAttThreads;
@@ -434,12 +441,11 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
   unsigned char* ring = smem + warp * kAttDepth * kStepBytes;
   int2* ring_rows = rows + warp * kAttDepth;
 
-  TileAt ahead[2];      // lane l knows the tiles of step 32 n + l of the warp, 32 n the last multiple at or before `sent`
+  TileAt ahead[2] = {};      // lane l knows the tiles of step 32 n + l of the warp, 32 n the last multiple at or before `sent`
   auto locate = [&](const int i) {
-    ahead[0] = ahead[1] = TileAt{-1, kNoRow};
-    if (i >= count) return;
     int f = begin + i * stride, v = u;
     if (shares) {
+      if (i >= count) return;
       int y = a.units;
       while (y - v > 1) {
         const int m = (v + y) >> 1;
@@ -518,10 +524,7 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
         const int r = 8 * nt + 2 * t + c;
         if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
       }
-    const int b = u / a.p.H, h = u % a.p.H;
-    auto out_at = [&](const int row) {
-      return ((long long)b * a.T + row / a.G) * ((long long)a.p.H * a.G) + (long long)h * a.G + row % a.G;
-    };
+    auto out_at = [&](const int row) { return out_row(a, u, row); };
     const bool whole = shares && lo <= starts[u] && end == starts[u + 1];
     const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
 #pragma unroll
@@ -572,13 +575,13 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
 
     // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
     cluster.sync();
-    for (int e = tid; e < S * live; e += kAttThreads) {
-      const int k = e / live, r = e % live;
-      allm[k * Q + r] = *cluster.map_shared_rank(&xm[r], k);
-      allz[k * Q + r] = *cluster.map_shared_rank(&xz[r], k);
+    for (int e = tid; e < S * Q; e += kAttThreads) {
+      const int k = e / Q, r = e % Q;
+      allm[e] = *cluster.map_shared_rank(&xm[r], k);
+      allz[e] = *cluster.map_shared_rank(&xz[r], k);
     }
     __syncthreads();
-    const int per = (live * kHeadDim + S - 1) / S;
+    const int per = a.per;
     for (int e = crank * per + tid; e < min((crank + 1) * per, live * kHeadDim); e += kAttThreads) {
       const int r = e / kHeadDim, dim = e % kHeadDim;
       float M = kNoRef;
@@ -644,8 +647,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a,
   }
   if (part == 0 && on) {
     const float by = den == 0.f ? 0.f : a.p.v_scale / den;
-    const int b = u / a.p.H, h = u % a.p.H;
-    const long long at = ((long long)b * a.T + row / a.G) * ((long long)a.p.H * a.G) + (long long)h * a.G + row % a.G;
+    const long long at = out_row(a, u, row);
     uint2 o;
     o.x = narrow2<T>(num.x * by, num.y * by), o.y = narrow2<T>(num.z * by, num.w * by);
     *(reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * kHeadDim) + lane) = o;
@@ -745,7 +747,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
     return fits[variant].ask(kernel, kAttThreads, smem, size, dev);
   });
   a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride;
-  a.T = q_tokens, a.G = gqa_ratio, a.R = R, a.max_rows = max_rows;
+  a.T = q_tokens, a.G = gqa_ratio, a.R = R, a.by_group = Divider(gqa_ratio), a.max_rows = max_rows;
   a.list = page_list_opt, a.counts = counts_opt, a.top = top;
   a.units = (int)units, a.ctas = shape.ctas;
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e * c->k_scale;
@@ -753,6 +755,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   a.part_mz = reinterpret_cast<float2*>(a.part + (size_t)shape.ctas * 2 * R * kHeadDim);
   a.starts = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + part_bytes(shape.ctas, R));
   a.out = out;
+  a.per = ((R < 8 * NT ? R : 8 * NT) * kHeadDim + shape.S - 1) / shape.S;
   const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
   cudaError_t e = launch_pdl(kernel, dim3(grid, groups), dim3(kAttThreads), smem, (cudaStream_t)stream, shape.S, a);
   if (e == cudaSuccess && shape.ctas) {

@@ -17,6 +17,7 @@ struct RowArgs {
   PagePool p;
   const int* offsets;     // nullptr: token b
   int per_head, max_new, slots;
+  Divider by_slots;
   long long num_tokens;
   long long k_row, k_head, v_row, v_head;   // strides, elements
   const float *cosv, *sinv;
@@ -28,7 +29,7 @@ struct RowArgs {
 // The new rows of a unit (head h of sequence b) that lie on the CTA's page.
 struct PageSpan {
   int u, h, page;          // unit, its head, column of the page table
-  int lo, hi;              // rows of the page
+  int lo, hi;              // new rows of the page
   int first, last;         // those of them whose token is in the input
   long long token;         // token (or row of the input) of row 0 of the page; there may be none
   int id;                  // what the table says, -1 beyond it
@@ -36,24 +37,25 @@ struct PageSpan {
 };
 __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) {
   PageSpan s;
-  s.u = task / a.slots;
-  const int slot = task % a.slots, b = s.u / a.p.H;
-  s.h = s.u % a.p.H;
+  s.u = a.by_slots.div(task);
+  const int slot = task - s.u * a.slots, b = a.p.by_heads.div(s.u);
+  s.h = s.u - b * a.p.H;
   const int rows = __ldg(a.p.rows + s.u);
-  long long first = b, n = 1;
+  int n = 1;
+  long long first = b;
   if (a.offsets) {
     const int i = a.per_head ? s.u : b;
-    first = __ldg(a.offsets + i), n = __ldg(a.offsets + i + 1) - first;
+    const int from = __ldg(a.offsets + i), to = __ldg(a.offsets + i + 1);
+    n = to > from ? (int)min((unsigned)to - (unsigned)from, (unsigned)a.max_new) : 0;
+    first = (long long)to - n;
   }
-  if (n > a.max_new) first += n - a.max_new, n = a.max_new;
-  long long r0 = (long long)rows - n;      // row of the first new token
-  s.bad = false;
-  if (r0 < 0) first -= r0, n += r0, r0 = 0, s.bad = true;
-  s.page = (int)(r0 / a.p.page_rows) + slot;
-  const long long begin = (long long)s.page * a.p.page_rows;
-  const long long lo = r0 > begin ? r0 : begin, end = begin + a.p.page_rows;
-  const long long hi = (long long)rows < end ? rows : end;
-  s.lo = (int)(lo - begin), s.hi = n > 0 && hi > lo ? (int)(hi - begin) : s.lo;
+  s.bad = rows < n;
+  if (s.bad) first += n - max(rows, 0), n = max(rows, 0);      // (only the last rows have a place)
+  const int r0 = rows - n;      // row of the first new token
+  s.page = n > 0 ? a.p.by_rows.div(r0) + slot : 0;
+  const long long begin = (long long)s.page * a.p.page_rows, end = begin + a.p.page_rows;
+  const long long lo = r0 > begin ? r0 : begin, hi = rows < end ? rows : end;
+  s.lo = n > 0 ? (int)(lo - begin) : 0, s.hi = n > 0 && hi > lo ? (int)(hi - begin) : s.lo;
   s.token = first + (begin - r0);
   // (rows r of the page with 0 <= token + r < num_tokens)
   const long long from = -s.token, to = a.num_tokens - s.token;
@@ -386,6 +388,7 @@ int check_rows(const mixkv_pages* c, int32_t type, int64_t num_tokens, const int
   a->slots = (a->max_new - 1 + c->page_rows - 1) / c->page_rows + 1;
   if (a->slots > c->max_pages + 1) a->slots = c->max_pages + 1;   // (one past the table: rows there are reported)
   if ((long long)c->batch * c->kv_heads * a->slots > 0x7fffffffll) return MIXKV_ERR_UNSUPPORTED;
+  a->by_slots = Divider(a->slots);
   return MIXKV_OK;
 }
 int tasks_of(const mixkv_pages* c, const RowArgs& a) { return c->batch * c->kv_heads * a.slots; }

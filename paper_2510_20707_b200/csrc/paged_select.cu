@@ -28,6 +28,7 @@ struct SelArgs {
   const void* q;
   long long q_batch, q_token;
   int T, G, R;
+  Divider by_group;
   int max_rows, pages;     // most pages of a head: room for its keys
   int top, first, last;
   int *list, *counts;
@@ -137,9 +138,9 @@ template <typename T>
 __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a) {
   extern __shared__ __align__(16) unsigned char sm[];
   cg::cluster_group cluster = cg::this_cluster();
-  const int S = (int)cluster.num_blocks(), crank = (int)cluster.block_rank(), u = blockIdx.x / S;
+  const int S = (int)cluster.num_blocks(), crank = (int)cluster.block_rank(), u = cluster_id();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int b = u / a.p.H, h = u % a.p.H;
+  const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
   float4* qs = reinterpret_cast<float4*>(sm);                    // [R padded][2][32]: max(q, 0), min(q, 0)
   uint32_t* keys = reinterpret_cast<uint32_t*>(qs + padded_rows(a.R) * 64);   // [pages], the first CTA's
   __shared__ uint32_t hist[kSelBins];
@@ -149,8 +150,9 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   pdl_wait();
   for (int e = tid; e < padded_rows(a.R) * 32; e += kSelThreads) {
     const int r = min(e >> 5, a.R - 1);      // (the rows of the padding repeat the last: a maximum does not mind)
-    const T* src = static_cast<const T*>(a.q) + b * a.q_batch + (r / a.G) * a.q_token +
-                   (long long)(h * a.G + r % a.G) * kHeadDim + 4 * (e & 31);
+    const int token = a.by_group.div(r);
+    const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
+                   (long long)(h * a.G + r - token * a.G) * kHeadDim + 4 * (e & 31);
     const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
     const float2 x = widen2<T>(w.x), y = widen2<T>(w.y);
     // (a NaN stays one in both parts)
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   }
   int n = min(a.p.rows[u], a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
-  const int pages = n <= 0 ? 0 : min((n + a.p.page_rows - 1) / a.p.page_rows, a.pages);
+  const int pages = n <= 0 ? 0 : min(a.p.by_rows.div(n + a.p.page_rows - 1), a.pages);
   const int* table = a.p.table + (long long)u * a.p.max_pages;
   const int at_once = 32 / rows_at_once(a.R), share = (pages + S * kSelWarps - 1) / (S * kSelWarps);
   const int run = (share + at_once - 1) / at_once * at_once, begin = (crank * kSelWarps + warp) * run;
@@ -265,6 +267,7 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   if (smem > most) return MIXKV_ERR_UNSUPPORTED;
   if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
   a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride, a.T = q_tokens, a.G = gqa_ratio, a.R = (int)R;
+  a.by_group = Divider(gqa_ratio);
   a.max_rows = max_rows, a.pages = (int)pages, a.top = top, a.first = keep_first, a.last = keep_last;
   a.list = page_list, a.counts = counts;
   const bool bf16 = type == MIXKV_TYPE_BF16;
