@@ -21,7 +21,8 @@ namespace cg = cooperative_groups;
 namespace mixkv {
 namespace {
 
-constexpr int kAttWarps = 4, kAttThreads = kAttWarps * 32;
+constexpr int kAttWarps = 4;                   // of a CTA of which an SM holds several
+constexpr int kAttWide = 16;                   // of one that has an SM for itself (one group of query rows)
 constexpr int kAttDepth = 2;                   // steps of a warp on their way or in work
 constexpr int kAttPair = 1;                    // up to so many groups of eight query rows a softmax step is two tiles, else one
 constexpr int kStepBytes = 2 * kTileBytes;
@@ -29,17 +30,17 @@ constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is no
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
 constexpr int kAttUnits = 1024;                // most units whose steps are dealt out evenly
-constexpr int kAttSteps = 5;                   // steps of a warp above which a join pays
+constexpr int kAttFew = 2, kAttFewRows = 8, kAttWideSteps = 8, kAttManySteps = 20;   // steps of a warp that settle how the work is split
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
 constexpr float kNoRef = -1e30f;               // reference before the first row: below any, and finite
 
 // rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
 // the cluster; barriers and rows of the rings
-__host__ __device__ constexpr size_t att_smem(int NT) {
-  return kAttWarps * (kAttDepth * kStepBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
-         kAttWarps * kAttDepth * 16 + 16;
+__host__ __device__ constexpr size_t att_smem(int NT, int W) {
+  return W * (kAttDepth * kStepBytes + 8 * NT * kAttPitch * 4) + (2 * W + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
+         W * kAttDepth * 16 + 16;
 }
-__host__ __device__ constexpr int att_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+__host__ __device__ constexpr int att_per_sm(int NT, int W) { return W > kAttWarps ? 1 : NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 
 struct AttArgs {
   PagePool p;
@@ -52,9 +53,9 @@ struct AttArgs {
   int top;
   int units;
   int ctas;                  // that share all steps evenly; 0: a cluster has a unit
-  int per;                   // outputs of a CTA of such a cluster
+  int per;                   // fours of outputs of a CTA of such a cluster
   float scale_log2e;         // k_scale included
-  int* starts;               // [units + 1]: first step of every unit, units one after the other
+  int2* spans;               // [units]: first CTA with a share of a unit, times two, plus one if its run begins before the unit; last CTA
   float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
   float2* part_mz;           // [2 ctas][R]: (reference, sum)
   void* out;
@@ -126,6 +127,14 @@ __device__ __forceinline__ int share_of(const int total, const int ctas) { retur
 __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, const int r) {
   const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
   return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
+}
+
+__device__ __forceinline__ void add_scaled(float4& sum, const float4& x, const float by) {
+  sum.x = fmaf(x.x, by, sum.x), sum.y = fmaf(x.y, by, sum.y), sum.z = fmaf(x.z, by, sum.z), sum.w = fmaf(x.w, by, sum.w);
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T* to, const float4& x, const float by) {   // four values times `by`
+  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(x.x * by, x.y * by), narrow2<T>(x.z * by, x.w * by));
 }
 
 // The first `keep` of the four scales of a word, zeros for the others.
@@ -212,7 +221,8 @@ struct AttState {
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        f[nt][c] = __shfl_sync(0xffffffffu, up, 4 * (2 * t + c)) * a.scale_log2e;
+        const float by = __shfl_sync(0xffffffffu, up, 4 * (2 * t + c)) * a.scale_log2e;
+        f[nt][c] = by < 1.2e-38f ? 1.2e-38f : by;    // (a NaN stays; never zero: times minus infinity it is the logit of a masked row)
         ref[nt][c] = kNoRef, z[nt][c] = 0.f;
       }
 #pragma unroll
@@ -245,11 +255,12 @@ struct AttState {
     }
   }
 
-  // HN tiles (one softmax step), whose first rows are row[], of a unit of n rows; `first`: the CTA's first query row.  EDGE: rows may lie
-  // beyond what a query row sees.
-  template <bool EDGE, int HN>
-  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tiles, const int (&row)[HN], const int n,
-                                       const int first, const int lane) {
+  // HN tiles (one softmax step), whose first rows are row[], of a unit of n rows; `first`: the CTA's first query row.  edge: rows may lie
+  // beyond what a query row sees.  (A flag and not a second copy of the code: a step that was alone in its kind waited for its
+  // instructions for longer than it took.)
+  template <int HN>
+  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tiles, const int (&row)[HN], const bool edge,
+                                       const int n, const int first, const int lane) {
     const int g = lane >> 2, t = lane & 3;
     float s[HN][NT][4];
 #pragma unroll
@@ -260,9 +271,7 @@ struct AttState {
         for (int i = 0; i < 4; ++i) s[h][nt][i] = 0.f;
       logits(tiles + h * kTileBytes, lane, s[h]);
     }
-    bool above = false;
-    uint32_t out = 0;     // EDGE: logits of rows that their query row does not see
-    if (EDGE) {
+    if (edge) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -272,10 +281,10 @@ struct AttState {
           for (int h = 0; h < HN; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2)
-              if (row[h] + 2 * (i >> 1) >= sees) out |= 1u << ((h * NT + nt) * 4 + i);
+              if (row[h] + 2 * (i >> 1) >= sees) s[h][nt][i] = -INFINITY;
         }
     }
-    auto gone = [&](const int h, const int nt, const int i) { return EDGE && (out >> ((h * NT + nt) * 4 + i) & 1u); };
+    bool above = false;
     float y[HN][NT][4];
 #pragma unroll
     for (int h = 0; h < HN; ++h)
@@ -283,7 +292,7 @@ struct AttState {
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[h][nt][i] = gone(h, nt, i) ? -INFINITY : fmaf(s[h][nt][i], f[nt][i & 1], -ref[nt][i & 1]);
+          y[h][nt][i] = fmaf(s[h][nt][i], f[nt][i & 1], -ref[nt][i & 1]);
           above |= y[h][nt][i] > kLag + kLift;
         }
     if (__any_sync(0xffffffffu, above)) {
@@ -296,7 +305,7 @@ struct AttState {
           for (int h = 0; h < HN; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2) {
-              y[h][nt][i] = gone(h, nt, i) ? -INFINITY : s[h][nt][i] * f[nt][c];
+              y[h][nt][i] = s[h][nt][i] * f[nt][c];
               mx = fmaxf(mx, y[h][nt][i]);
             }
           const float to = fmaxf(ref[nt][c], column_max(mx) - kLift);
@@ -329,7 +338,7 @@ struct AttState {
       // Rows that were never written can hold anything, a scale of NaN as well: their scales become zero.  A NaN in a row
       // that some of the query rows see must not reach the others through a weight of zero: such a tile is taken once per
       // token, with the rows that this token sees, and added to its own query rows alone.
-      if (EDGE) {
+      if (edge) {
         vs = keep_scales(vs, n - row[h] - 4 * t);
         const bool nan = ((((vs & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u)) != 0;   // a byte of 0x7f
         if (a.T > 1 && __any_sync(0xffffffffu, nan)) {
@@ -357,25 +366,25 @@ struct AttState {
   }
 };
 
-// grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
-template <typename T, int NT>
-__global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention(const AttArgs a) {
+// W warps.  grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
+template <typename T, int NT, int W>
+__global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(const AttArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
-  constexpr int Q = 8 * NT, kSums = Q * kAttPitch;
+  constexpr int Q = 8 * NT, kSums = Q * kAttPitch, kThreads = 32 * W;
   float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its sums where its rings were
-  static_assert(Q * kHeadDim * 4 <= kAttWarps * kAttDepth * kStepBytes, "sums of a CTA fit the rings");
-  float* sums = reinterpret_cast<float*>(smem + kAttWarps * kAttDepth * kStepBytes);   // [warps][Q][pitch]
-  float* wm = sums + kAttWarps * kSums;      // [warps][Q]
-  float* wz = wm + kAttWarps * Q;            // [warps][Q]
-  float* xm = wz + kAttWarps * Q;            // [Q]
+  static_assert(Q * kHeadDim * 4 <= W * kAttDepth * kStepBytes, "sums of a CTA fit the rings");
+  float* sums = reinterpret_cast<float*>(smem + W * kAttDepth * kStepBytes);   // [warps][Q][pitch]
+  float* wm = sums + W * kSums;      // [warps][Q]
+  float* wz = wm + W * Q;            // [warps][Q]
+  float* xm = wz + W * Q;            // [Q]
   float* xz = xm + Q;                        // [Q]
   float* allm = xz + Q;                      // [8][Q]
   float* allz = allm + kMaxCluster * Q;      // [8][Q]
   uint64_t* bars = reinterpret_cast<uint64_t*>(allz + kMaxCluster * Q);   // [warps][depth]
-  int2* rows = reinterpret_cast<int2*>(bars + kAttWarps * kAttDepth);   // [warps][depth]: first rows of a step's tiles
-  int* abort = reinterpret_cast<int*>(rows + kAttWarps * kAttDepth);
+  int2* rows = reinterpret_cast<int2*>(bars + W * kAttDepth);   // [warps][depth]: first rows of a step's tiles
+  int* abort = reinterpret_cast<int*>(rows + W * kAttDepth);
   __shared__ int starts[kAttUnits + 1];      // first step of every unit
-  __shared__ int warp_total[kAttWarps];
+  __shared__ int warp_total[W];
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const bool shares = a.ctas > 0;
@@ -392,10 +401,10 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
   pdl_wait();
 
   // steps lo .. hi - 1: of a cluster's unit, or of all units one after the other
-  int u = shares ? 0 : cluster_id(), lo = crank * kAttWarps, hi;
+  int u = shares ? 0 : cluster_id(), lo = crank * W, hi;
   if (shares) {
     // first steps of all units: a thread takes consecutive ones
-    constexpr int kEach = kAttUnits / kAttThreads;
+    constexpr int kEach = kAttUnits / kThreads;
     int mine[kEach], sum = 0;
     const int u0 = tid * kEach;
 #pragma unroll
@@ -411,7 +420,7 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
     if (lane == 31) warp_total[warp] = upto;
     __syncthreads();
     int at = upto - sum, total = 0;
-    for (int w = 0; w < kAttWarps; ++w) {
+    for (int w = 0; w < W; ++w) {
       if (w < warp) at += warp_total[w];
       total += warp_total[w];
     }
@@ -422,8 +431,13 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
     }
     if (tid == 0) starts[a.units] = total;
     __syncthreads();
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-      for (int i = tid; i <= a.units; i += kAttThreads) a.starts[i] = starts[i];
+    if (blockIdx.x + 1 == gridDim.x && blockIdx.y == 0) {      // (the CTA whose run is the shortest)
+      const int share = max(1, share_of(total, a.ctas));
+      for (int i = tid; i < a.units; i += kThreads) {
+        const int from = starts[i], to = starts[i + 1], c0 = from / share;
+        a.spans[i] = from < to ? make_int2(2 * c0 + (c0 * share < from), (to - 1) / share) : make_int2(0, -1);
+      }
+    }
     const int share = share_of(total, a.ctas);
     lo = blockIdx.x * share, hi = min(lo + share, total);
     if (lo >= hi) return;
@@ -436,7 +450,7 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
   } else {
     hi = unit_tiles(a, u).steps;
   }
-  const int stride = S * kAttWarps, begin = lo + warp;
+  const int stride = S * W, begin = lo + warp;
   const int count = begin < hi ? (hi - begin + stride - 1) / stride : 0;   // steps of this warp
   unsigned char* ring = smem + warp * kAttDepth * kStepBytes;
   int2* ring_rows = rows + warp * kAttDepth;
@@ -497,14 +511,12 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
       const bool inside = max(at.x, at.y) + kPageTile <= clear;
       if constexpr (NT <= kAttPair) {
         const int row[2] = {at.x, at.y};
-        if (inside) st.template step<false, 2>(a, tiles, row, n, first, lane);
-        else st.template step<true, 2>(a, tiles, row, n, first, lane);
+        st.template step<2>(a, tiles, row, !inside, n, first, lane);
       } else {
 #pragma unroll 1
         for (int h = 0; h < 2; ++h) {
           const int row[1] = {h ? at.y : at.x};
-          if (inside) st.template step<false, 1>(a, tiles + h * kTileBytes, row, n, first, lane);
-          else st.template step<true, 1>(a, tiles + h * kTileBytes, row, n, first, lane);
+          st.template step<1>(a, tiles + h * kTileBytes, row, !inside, n, first, lane);
         }
       }
       __syncwarp();     // every lane has read the slot
@@ -525,7 +537,7 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
         if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
       }
     auto out_at = [&](const int row) { return out_row(a, u, row); };
-    const bool whole = shares && lo <= starts[u] && end == starts[u + 1];
+    const bool whole = shares ? lo <= starts[u] && end == starts[u + 1] : S == 1;
     const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -539,29 +551,27 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
             *reinterpret_cast<float2*>(own + (8 * nt + 2 * t + c) * kAttPitch + 8 * g + 2 * m) =
                 make_float2(st.acc[nt][4 * half + m][c], st.acc[nt][4 * half + m][2 + c]);
       __syncthreads();
-      for (int e = tid; e < live * (kHeadDim / 4); e += kAttThreads) {
-        const int r = e / (kHeadDim / 4), x = 2 * (e % (kHeadDim / 4)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
+      for (int e = tid; e < live * (kHeadDim / 8); e += kThreads) {
+        const int r = e / (kHeadDim / 8), x = 4 * (e % (kHeadDim / 8)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
         float M = kNoRef;
 #pragma unroll
-        for (int w = 0; w < kAttWarps; ++w) M = fmaxf(M, wm[w * Q + r]);
-        float2 num = make_float2(0.f, 0.f);
+        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]);
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
         float den = 0.f;
 #pragma unroll
-        for (int w = 0; w < kAttWarps; ++w) {
+        for (int w = 0; w < W; ++w) {
           const float sc = ex2(wm[w * Q + r] - M);
-          const float2 v = *reinterpret_cast<const float2*>(sums + w * kSums + r * kAttPitch + x);
-          num.x = fmaf(v.x, sc, num.x), num.y = fmaf(v.y, sc, num.y);
+          add_scaled(num, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc);
           den = fmaf(wz[w * Q + r], sc, den);
         }
         if (whole) {
-          const float by = den == 0.f ? 0.f : a.p.v_scale / den;
-          *reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + out_at(first + r) * kHeadDim + dim) = narrow2<T>(num.x * by, num.y * by);
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den == 0.f ? 0.f : a.p.v_scale / den);
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
-          *reinterpret_cast<float2*>(a.part + at * kHeadDim + dim) = num;
+          *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
           if (dim == 0) a.part_mz[at] = make_float2(M, den);
         } else {
-          *reinterpret_cast<float2*>(xo + r * kHeadDim + dim) = num;
+          *reinterpret_cast<float4*>(xo + r * kHeadDim + dim) = num;
           if (dim == 0) xm[r] = M, xz[r] = den;
         }
       }
@@ -572,28 +582,29 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
       ++u;
       continue;
     }
+    if (whole) return;
 
     // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
     cluster.sync();
-    for (int e = tid; e < S * Q; e += kAttThreads) {
+    for (int e = tid; e < S * Q; e += kThreads) {
       const int k = e / Q, r = e % Q;
       allm[e] = *cluster.map_shared_rank(&xm[r], k);
       allz[e] = *cluster.map_shared_rank(&xz[r], k);
     }
     __syncthreads();
-    const int per = a.per;
-    for (int e = crank * per + tid; e < min((crank + 1) * per, live * kHeadDim); e += kAttThreads) {
-      const int r = e / kHeadDim, dim = e % kHeadDim;
+    for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
+      const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
       float M = kNoRef;
       for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
-      float num = 0.f, den = 0.f;
+      float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+      float den = 0.f;
+#pragma unroll 4
       for (int k = 0; k < S; ++k) {
         const float sc = ex2(allm[k * Q + r] - M);
-        num = fmaf(*cluster.map_shared_rank(&xo[e], k), sc, num);
+        add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc);
         den = fmaf(allz[k * Q + r], sc, den);
       }
-      const float by = den == 0.f ? 0.f : a.p.v_scale / den;
-      static_cast<T*>(a.out)[out_at(first + r) * kHeadDim + dim] = from_f32<T>(num * by);
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den == 0.f ? 0.f : a.p.v_scale / den);
     }
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
     return;
@@ -601,85 +612,111 @@ __global__ void __launch_bounds__(kAttThreads, att_per_sm(NT)) k_paged_attention
 }
 
 // Joins the shares of units that several CTAs had a part of, and writes zeros for units without rows.  per_row warps (a power
-// of two) take the shares of a query row in turn.
-constexpr int kJoinWarps = 8;
+// of two) take the shares of a query row in turn, a few at once with a running reference: what a share holds comes in one
+// round trip.
+constexpr int kJoinWarps = 16;
 template <typename T>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a, const int per_row) {
+__global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a, const Divider per_row, const Divider blocks) {
   __shared__ float4 sums[kJoinWarps][32];
-  __shared__ float stat[kJoinWarps];
+  __shared__ float2 stat[kJoinWarps];
   pdl_launch_dependents();
-  pdl_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int at_once = kJoinWarps / per_row, blocks = (a.R + at_once - 1) / at_once;   // rows of a CTA, CTAs of a unit
-  const int u = blockIdx.x / blocks, row = (blockIdx.x % blocks) * at_once + warp / per_row, part = warp % per_row;
-  const int from = a.starts[u], to = a.starts[u + 1], total = a.starts[a.units];
-  int c0 = 0, c1 = -1;
-  const int share = max(1, share_of(total, a.ctas));
-  if (from < to) {
-    c0 = from / share, c1 = (to - 1) / share;
-    if (c0 == c1) return;     // written by that CTA
-  }
+  const int u = blocks.div(blockIdx.x), slot = per_row.div(warp), part = warp - slot * per_row.d;
+  const int row = (blockIdx.x - u * blocks.d) * per_row.div(kJoinWarps) + slot;      // (blocks: CTAs of a unit)
+  pdl_wait();
+  const int2 span = __ldcg(a.spans + u);
+  const int c0 = span.x >> 1, c1 = span.y;
+  if (c0 == c1) return;     // written by that CTA
   const bool on = row < a.R;
-  auto part_of = [&](const int c) { return (2LL * c + (c * share < from)) * a.R + (on ? row : 0); };
-  float M = kNoRef;
-  for (int c = c0 + lane; c <= c1; c += 32) M = fmaxf(M, a.part_mz[part_of(c)].x);
-  M = warp_max(M);
+  constexpr int kAtOnce = 5;
+  float M = kNoRef, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  float den = 0.f;
-#pragma unroll 4
-  for (int c = c0 + part; c <= c1; c += per_row) {
-    const long long at = part_of(c);
-    const float2 mz = a.part_mz[at];
-    const float4 x = *(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
-    const float sc = ex2(mz.x - M);
-    num.x = fmaf(x.x, sc, num.x), num.y = fmaf(x.y, sc, num.y), num.z = fmaf(x.z, sc, num.z), num.w = fmaf(x.w, sc, num.w);
-    den = fmaf(mz.y, sc, den);
-  }
-  if (per_row > 1) {
-    sums[warp][lane] = num;
-    if (lane == 0) stat[warp] = den;
-    __syncthreads();
-    for (int w = warp + 1; part == 0 && w < warp + per_row; ++w) {
-      const float4 x = sums[w][lane];
-      num.x += x.x, num.y += x.y, num.z += x.z, num.w += x.w;
-      den += stat[w];
+#pragma unroll 1
+  for (int c = c0 + part; on && c <= c1; c += per_row.d * kAtOnce) {
+    float4 x[kAtOnce];
+    float2 mz[kAtOnce];
+    float to = M;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = min(c + i * (int)per_row.d, c1);
+      const long long at = (2LL * k + (k == c0 ? span.x & 1 : 0)) * a.R + row;
+      mz[i] = __ldcg(a.part_mz + at);
+      x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x);
+    const float shrink = ex2(M - to);
+    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
+    M = to;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float sc = c + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
+      add_scaled(num, x[i], sc);
+      den = fmaf(mz[i].y, sc, den);
     }
   }
-  if (part == 0 && on) {
-    const float by = den == 0.f ? 0.f : a.p.v_scale / den;
-    const long long at = out_row(a, u, row);
-    uint2 o;
-    o.x = narrow2<T>(num.x * by, num.y * by), o.y = narrow2<T>(num.z * by, num.w * by);
-    *(reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * kHeadDim) + lane) = o;
+  if (per_row.d > 1) {
+    sums[warp][lane] = num;
+    if (lane == 0) stat[warp] = make_float2(M, den);
+    __syncthreads();
+    if (part) return;
+    float to = M;
+    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, stat[warp + w].x);
+    const float shrink = ex2(M - to);
+    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
+    for (int w = 1; w < (int)per_row.d; ++w) {
+      const float2 mz = stat[warp + w];
+      const float sc = ex2(mz.x - to);
+      add_scaled(num, sums[warp + w][lane], sc);
+      den = fmaf(mz.y, sc, den);
+    }
   }
+  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den == 0.f ? 0.f : a.p.v_scale / den);
 }
 
 using AttKernel = void (*)(AttArgs);
 template <typename T>
-AttKernel att_kernel(const int NT) {
+AttKernel att_kernel(const int NT, const bool wide) {
   switch (NT) {
-    case 1: return k_paged_attention<T, 1>;
-    case 2: return k_paged_attention<T, 2>;
-    case 3: return k_paged_attention<T, 3>;
-    default: return k_paged_attention<T, 4>;
+    case 1: return wide ? k_paged_attention<T, 1, kAttWide> : k_paged_attention<T, 1, kAttWarps>;
+    case 2: return k_paged_attention<T, 2, kAttWarps>;
+    case 3: return k_paged_attention<T, 3, kAttWarps>;
+    default: return k_paged_attention<T, 4, kAttWarps>;
   }
 }
 
-// How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit.
+// How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit.  narrow(n), wide(n): clusters
+// of n CTAs of either kind that are resident at once.
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all steps
+  bool wide;
 };
-int att_slots(const int NT, const int sms) { return att_per_sm(NT) * sms; }
-template <typename Fit>
-AttShape att_shape(const long long units, const int groups, const long long steps, const int NT, const int sms, const Fit& fit) {
+int att_slots(const int NT, const int sms) { return att_per_sm(NT, kAttWarps) * sms; }
+template <typename Narrow, typename Wide>
+AttShape att_shape(const long long units, const int groups, const long long steps, const int NT, const int sms,
+                   const Narrow& narrow, const Wide& wide) {
   const long long slots = att_slots(NT, sms), all = units * groups;
-  int S = (int)(slots / all < kMaxCluster ? slots / all : kMaxCluster);
-  if (S > steps / kAttWarps) S = (int)(steps / kAttWarps);
-  if (S < 1) S = 1;
-  while (S > 1 && all > fit(S)) --S;
-  if (units <= kAttUnits && steps > (long long)S * kAttWarps * kAttSteps && groups < slots)
-    return {1, (int)(slots / groups)};
-  return {S, 0};
+  auto clusters = [&](const long long room, const int warps, const auto& fit) {
+    long long S = room / all < kMaxCluster ? room / all : kMaxCluster;
+    if (S > steps / warps) S = steps / warps;
+    if (S < 1) S = 1;
+    while (S > 1 && all > fit((int)S)) --S;
+    return (int)S;
+  };
+  int S = clusters(slots, kAttWarps, narrow);
+  const long long alone = (steps + S * kAttWarps - 1) / (S * kAttWarps);     // steps of a warp
+  if (alone <= (NT == 1 ? kAttFew : kAttFewRows)) return {S, 0, false};
+  if (NT == 1 && all <= sms) {
+    const int B = clusters(sms, kAttWide, wide);
+    if (steps <= (long long)B * kAttWide * kAttWideSteps) return {B, 0, true};
+  } else if (NT == 1 && alone <= kAttManySteps) {
+    return {S, 0, false};
+  }
+  if (units <= kAttUnits && groups < slots) {
+    const long long want = (units * steps + kAttWarps * 2 - 1) / (kAttWarps * 2);     // (two steps to a warp)
+    return {1, (int)(want < slots / groups ? want : slots / groups), false};
+  }
+  return {S, 0, false};
 }
 
 int queries_of(const mixkv_pages* c, const int32_t q_tokens, const int32_t gqa, int* groups, int* NT) {
@@ -692,10 +729,10 @@ int queries_of(const mixkv_pages* c, const int32_t q_tokens, const int32_t gqa, 
   if ((long long)c->batch * c->kv_heads * *groups > 1 << 24) return MIXKV_ERR_UNSUPPORTED;
   return MIXKV_OK;
 }
-// Workspace: part, part_mz, starts.
+// Workspace: part, part_mz, spans.
 size_t part_bytes(const int ctas, const long long R) { return (size_t)ctas * 2 * R * (kHeadDim + 2) * 4; }
 size_t att_workspace(const int NT, const int sms, const long long R) {
-  return part_bytes(att_slots(NT, sms), R) + (kAttUnits + 1) * sizeof(int);
+  return part_bytes(att_slots(NT, sms), R) + kAttUnits * sizeof(int2);
 }
 
 }  // namespace
@@ -737,15 +774,23 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   if (page_list_opt && tiles > (long long)top * a.p.tiles) tiles = (long long)top * a.p.tiles;
 
   const bool bf16 = type == MIXKV_TYPE_BF16;
-  static std::atomic<bool> done[2 * (kAttGroups + 1)][kMaxDevices];
-  static ClusterFit fits[2 * (kAttGroups + 1)];   // (by variant, as `done`)
-  const int variant = 2 * NT + bf16, dev = device_slot();
-  const AttKernel kernel = bf16 ? att_kernel<__nv_bfloat16>(NT) : att_kernel<__half>(NT);
-  const size_t smem = att_smem(NT);
-  if (ensure_smem(kernel, smem, done[variant], dev) != cudaSuccess) return MIXKV_ERR_CUDA;
-  const AttShape shape = att_shape(units, groups, (tiles + 1) / 2, NT, sms, [&](const int size) {
-    return fits[variant].ask(kernel, kAttThreads, smem, size, dev);
-  });
+  static std::atomic<bool> done[4 * (kAttGroups + 1)][kMaxDevices];
+  static ClusterFit fits[4 * (kAttGroups + 1)];   // (by variant, as `done`)
+  const int dev = device_slot();
+  auto variant = [&](const bool wide) { return 4 * NT + 2 * wide + bf16; };
+  auto warps = [&](const bool wide) { return wide ? kAttWide : kAttWarps; };
+  auto kernel_of = [&](const bool wide) { return bf16 ? att_kernel<__nv_bfloat16>(NT, wide) : att_kernel<__half>(NT, wide); };
+  auto resident = [&](const bool wide) {
+    return [&, wide](const int size) {
+      const size_t smem = att_smem(NT, warps(wide));
+      if (!answered(ensure_smem(kernel_of(wide), smem, done[variant(wide)], dev))) return 0;
+      return fits[variant(wide)].ask(kernel_of(wide), 32 * warps(wide), smem, size, dev);
+    };
+  };
+  const AttShape shape = att_shape(units, groups, (tiles + 1) / 2, NT, sms, resident(false), resident(true));
+  const AttKernel kernel = kernel_of(shape.wide);
+  const size_t smem = att_smem(NT, warps(shape.wide));
+  if (ensure_smem(kernel, smem, done[variant(shape.wide)], dev) != cudaSuccess) return MIXKV_ERR_CUDA;
   a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride;
   a.T = q_tokens, a.G = gqa_ratio, a.R = R, a.by_group = Divider(gqa_ratio), a.max_rows = max_rows;
   a.list = page_list_opt, a.counts = counts_opt, a.top = top;
@@ -753,18 +798,17 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e * c->k_scale;
   a.part = static_cast<float*>(workspace);
   a.part_mz = reinterpret_cast<float2*>(a.part + (size_t)shape.ctas * 2 * R * kHeadDim);
-  a.starts = reinterpret_cast<int*>(static_cast<unsigned char*>(workspace) + part_bytes(shape.ctas, R));
+  a.spans = reinterpret_cast<int2*>(static_cast<unsigned char*>(workspace) + part_bytes(shape.ctas, R));
   a.out = out;
-  a.per = ((R < 8 * NT ? R : 8 * NT) * kHeadDim + shape.S - 1) / shape.S;
+  a.per = ((R < 8 * NT ? R : 8 * NT) * (kHeadDim / 4) + shape.S - 1) / shape.S;
   const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
-  cudaError_t e = launch_pdl(kernel, dim3(grid, groups), dim3(kAttThreads), smem, (cudaStream_t)stream, shape.S, a);
+  cudaError_t e = launch_pdl(kernel, dim3(grid, groups), dim3(32 * warps(shape.wide)), smem, (cudaStream_t)stream, shape.S, a);
   if (e == cudaSuccess && shape.ctas) {
     int per_row = 1;      // warps that go through the shares of one query row
-    while (per_row < kJoinWarps && per_row * 4 * units < shape.ctas) per_row *= 2;
-    const int at_once = kJoinWarps / per_row;
-    e = launch_pdl(bf16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>,
-                   dim3((unsigned)(units * ((R + at_once - 1) / at_once))), dim3(kJoinWarps * 32), 0, (cudaStream_t)stream, 1,
-                   a, per_row);
+    while (per_row < kJoinWarps && per_row * 2 * units < shape.ctas) per_row *= 2;
+    const int at_once = kJoinWarps / per_row, blocks = (R + at_once - 1) / at_once;
+    e = launch_pdl(bf16 ? k_paged_join<__nv_bfloat16> : k_paged_join<__half>, dim3((unsigned)(units * blocks)),
+                   dim3(kJoinWarps * 32), 0, (cudaStream_t)stream, 1, a, Divider(per_row), Divider(blocks));
   }
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }
