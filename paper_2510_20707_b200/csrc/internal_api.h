@@ -37,6 +37,12 @@ int mixkv_internal_adapt_threads(int64_t sequences, int32_t heads, int32_t candi
 int mixkv_internal_gram_run(int32_t heads, int32_t cells, int32_t parts, int32_t whole_sectors, int64_t l2_bytes);
 int mixkv_internal_budget_clusters(int32_t pairs, int64_t keys_per_pair, const int32_t* alone);
 
+// How a paged attention is split (paged_attention.cu): (sequence, head) units, groups of query rows, steps (32 rows) of the longest
+// unit, groups of eight query rows of a CTA; narrow[n], wide[n]: clusters of n small and of n large CTAs held at once.  CTAs of a
+// unit's cluster and whether they are large, or the CTAs that share all steps (0: none do).
+void mixkv_internal_paged_shape(int64_t units, int32_t groups, int64_t steps, int32_t eights, int32_t sms, const int32_t* narrow,
+                                const int32_t* wide, int32_t* ctas, int32_t* large, int32_t* shared);
+
 // Rounds of a threshold search among keys lo .. hi that ends at `key` without listing any: keys [base, base + span] counted
 // in bins of 2^shift.  Returns their number (three at most).
 int mixkv_internal_search_rounds(uint32_t lo, uint32_t hi, uint32_t key, uint32_t* base, uint32_t* span, int32_t* shift);

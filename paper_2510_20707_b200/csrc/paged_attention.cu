@@ -740,6 +740,14 @@ size_t att_workspace(const int NT, const int sms, const long long R) {
 
 using namespace mixkv;
 
+extern "C" void mixkv_internal_paged_shape(int64_t units, int32_t groups, int64_t steps, int32_t eights, int32_t sms,
+                                           const int32_t* narrow, const int32_t* wide, int32_t* ctas, int32_t* large,
+                                           int32_t* shared) {
+  const AttShape s = att_shape(units, groups, steps, eights, sms, [&](const int n) { return narrow[n]; },
+                               [&](const int n) { return wide[n]; });
+  *ctas = s.S, *large = s.wide, *shared = s.ctas;
+}
+
 extern "C" int mixkv_paged_workspace_size(const mixkv_pages* c, int32_t q_tokens, int32_t gqa_ratio, size_t* bytes) {
   PagePool p;
   int rc = check_pages(c, &p), groups, NT;

@@ -477,3 +477,16 @@ def test_refusals():
         binding.paged_append(c.pages, torch.cat([k, k]), torch.cat([k, k]))     # two tokens, one sequence, no offsets
     with pytest.raises(TypeError):
         binding.paged_read(c.pages, 1, torch.float32)
+
+
+def test_the_example_runs():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    errors, outs = example.main(3)
+    # two 4-bit codes to a byte, blocks of 16: the rounding of normal values is about a tenth of them
+    assert len(errors) == 2 and max(errors) < 0.3
+    assert len(outs) == 4 and all(o.shape == (1, 1, 28, 128) and torch.isfinite(o.float()).all() for o in outs)

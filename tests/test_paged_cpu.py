@@ -156,3 +156,59 @@ def test_workspace_does_not_depend_on_rows_and_grows_with_queries(lib):
         assert lib.mixkv_paged_workspace_size(pages(**kw), T, G, C.byref(s)) == 0
         return s.value
     assert 0 < size(1, 4) < size(1, 8) and size(1, 4) == size(1, 4, max_pages=1000)
+
+
+NARROW = {1: 592, 2: 296, 3: 180, 4: 148, 5: 110, 6: 95, 7: 80, 8: 68}
+WIDE = {1: 148, 2: 74, 3: 45, 4: 33, 5: 26, 6: 22, 7: 15, 8: 15}
+
+
+@pytest.mark.parametrize("units,groups,steps,eights,shape", [
+    (4, 1, 16, 1, (4, 0, 0)),            # a short cache: a step for every warp of four small CTAs
+    (8, 1, 64, 1, (8, 0, 0)), (8, 1, 65, 1, (4, 1, 0)),       # two steps a warp, and one more: large CTAs
+    (32, 1, 512, 1, (4, 1, 0)), (32, 1, 513, 1, (1, 0, 592)),    # eight steps a warp of a large CTA, and one more: shares
+    (16, 1, 300, 1, (6, 1, 0)),          # of clusters of seven and eight large CTAs fifteen are held at once
+    (896, 1, 80, 1, (1, 0, 0)), (896, 1, 81, 1, (1, 0, 592)),    # more heads than SMs: twenty steps a warp
+    (1025, 1, 4096, 1, (1, 0, 0)),       # more heads than the shares' table holds
+    (8, 1, 4096, 1, (1, 0, 592)), (1, 1, 1025, 1, (1, 0, 129)),    # few long heads; no more shares than steps are worth
+    (32, 2, 230, 3, (1, 0, 148)), (32, 2, 128, 3, (4, 0, 0)), (1, 4, 1, 4, (1, 0, 0))])
+def test_how_an_attention_is_split(lib, units, groups, steps, eights, shape):
+    table = lambda t: (C.c_int32 * 9)(0, *[t[n] for n in range(1, 9)])
+    ctas, large, shared = (C.c_int32() for _ in range(3))
+    lib.mixkv_internal_paged_shape(C.c_int64(units), groups, C.c_int64(steps), eights, 148, table(NARROW), table(WIDE),
+                                   C.byref(ctas), C.byref(large), C.byref(shared))
+    assert (ctas.value, large.value, shared.value) == shape
+
+
+def test_what_the_paged_calls_enqueue(fake_cuda):
+    fake_cuda.reset(device=9, resident={n: 148 // n for n in range(1, 9)})
+    lib, names = fake_cuda.lib, lambda: [(x.kernel, x.grid, x.threads, x.cluster) for x in fake_cuda.launches()]
+    assert append(lib, pages(), off=None, most=1, n=2) == 0 and append(lib, pages(), n=5000, most=4000) == 0
+    assert names() == [("k_paged_append", 8, 64, 1), ("k_paged_append", 8 * 11, 128, 1)]
+    fake_cuda.reset(device=9, resident={n: 148 // n for n in range(1, 9)})
+    assert attend(lib, pages(), rows=512) == 0 and attend(lib, pages(max_pages=4096), rows=1 << 18) == 0
+    assert attend(lib, pages(max_pages=4096), rows=1 << 18, list=ONE, counts=ONE, top=8) == 0
+    assert names() == [("k_paged_attention", 32, 128, 4), ("k_paged_attention", 592, 128, 1),
+                       ("k_paged_join", 32, 512, 1), ("k_paged_attention", 32, 128, 4)]
+    fake_cuda.reset(device=9, resident={n: 148 // n for n in range(1, 9)})
+    assert select(lib, pages(), rows=640) == 0 and select(lib, pages(max_pages=4096), rows=1 << 18) == 0
+    assert names() == [("k_paged_select", 8, 512, 1), ("k_paged_select", 64, 512, 8)]
+
+
+def test_a_device_without_clusters_gets_none_for_the_attention(fake_cuda):
+    fake_cuda.reset(device=10, resident={n: 0 for n in range(2, 9)})
+    for rows in (100, 512, 4000):
+        assert attend(fake_cuda.lib, pages(max_pages=100), rows=rows) == 0
+    assert all(x.cluster == 1 for x in fake_cuda.launches())
+
+
+def test_division_by_multiplication():
+    # the reciprocal that the kernels index with, at the ends of every divisor's range
+    for d in [1, 2, 3, 5, 6, 7, 9, 15, 16, 17, 100, 127, 128, 129, 592, 1000, 65535, 65536, 65537, (1 << 24) - 1, 1 << 24,
+              (1 << 30) + 1, (1 << 31) - 1]:
+        l = (d - 1).bit_length()
+        m = (1 << (31 + l)) // d + 1
+        assert l == 0 or m < 1 << 32
+        for q in {0, 1, 2, (2 ** 31 - 1) // d, (2 ** 31 - 1) // d // 2}:
+            for n in (q * d - 1, q * d, q * d + d - 1):
+                if 0 <= n < 1 << 31:
+                    assert (n if l == 0 else (n * m >> 32) >> (l - 1)) == n // d, (n, d)
