@@ -421,7 +421,6 @@ PyObject* compress_outputs(PyObject* given, PyObject* aux, const int64_t lead, c
 struct Ref {   // an owned reference
   PyObject* o;
   explicit Ref(PyObject* x) : o(x) {}
-  Ref(Ref&& x) noexcept : o(x.release()) {}
   ~Ref() { Py_XDECREF(o); }
   PyObject* release() {
     PyObject* r = o;
@@ -604,45 +603,57 @@ PyObject* py_decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 void want(const bool ok, const char* what) {
   if (!ok) fail(PyExc_AssertionError, what);
 }
-// A mixkv_pages from a binding.Pages; `pool` and the other tensors stay alive through the attributes they are held by.
+// A mixkv_pages from a binding.Pages, which holds on to the tensors for the call.
 struct PagesArg {
   mixkv_pages c;
-  std::vector<Ref> held;
-  at::Tensor pool;
-  const at::Tensor& attr(PyObject* o, PyObject* name, const bool optional = false) {
-    PyObject* v = PyObject_GetAttr(o, name);
-    if (!v) throw Raised();
-    held.emplace_back(v);
-    static const at::Tensor none;
-    return optional && v == Py_None ? none : tensor(v);
+  PyObject* held[4] = {};
+  ~PagesArg() {
+    for (PyObject* o : held) Py_XDECREF(o);
   }
+  const at::Tensor* attr(const int i, PyObject* o, PyObject* name) {     // (nullptr: None)
+    held[i] = PyObject_GetAttr(o, name);
+    if (!held[i]) throw Raised();
+    return held[i] == Py_None ? nullptr : &tensor(held[i]);
+  }
+  const at::Tensor& pool() const { return THPVariable_Unpack(held[0]); }
   explicit PagesArg(PyObject* o) {
     if (!api.paged_append || !api.paged_read || !api.paged_select || !api.paged_ws_size || !api.paged_attention)
       fail(PyExc_OSError, "the library has no paged cache");
-    held.reserve(4);
-    pool = attr(o, nm.pool);
-    const at::Tensor table = attr(o, nm.table), rows = attr(o, nm.rows), bounds = attr(o, nm.bounds, true);
-    want(pool.is_cuda() && pool.dim() == 2 && pool.is_contiguous() && pool.element_size() == 1,
+    try {
+      take(o);
+    } catch (...) {     // (no destructor runs for what was not built)
+      for (PyObject* x : held) Py_XDECREF(x);
+      throw;
+    }
+  }
+  PagesArg(const PagesArg&) = delete;
+
+ private:
+  void take(PyObject* o) {
+    const at::Tensor *pool = attr(0, o, nm.pool), *table = attr(1, o, nm.table), *rows = attr(2, o, nm.rows),
+                     *bounds = attr(3, o, nm.bounds);
+    if (!pool || !table || !rows) fail(PyExc_TypeError, "a tensor is expected");
+    want(pool->is_cuda() && pool->dim() == 2 && pool->is_contiguous() && pool->element_size() == 1,
          "pool must be a contiguous CUDA tensor of bytes [pages, bytes of a page]");
-    want(table.scalar_type() == at::kInt && table.dim() == 3 && table.is_contiguous() && table.device() == pool.device(),
+    const auto device = pool->device();
+    want(table->scalar_type() == at::kInt && table->dim() == 3 && table->is_contiguous() && table->device() == device,
          "table must be a contiguous int32 tensor [batch, kv_heads, pages] on the pool's device");
-    want(rows.scalar_type() == at::kInt && rows.dim() == 2 && rows.is_contiguous() && rows.size(0) == table.size(0) &&
-             rows.size(1) == table.size(1) && rows.device() == pool.device(),
+    want(rows->scalar_type() == at::kInt && rows->dim() == 2 && rows->is_contiguous() && rows->size(0) == table->size(0) &&
+             rows->size(1) == table->size(1) && rows->device() == device,
          "rows must be a contiguous int32 tensor [batch, kv_heads] on the pool's device");
     c.page_rows = attr_int(o, nm.page_rows);
-    want(c.page_rows > 0 && pool.size(1) * 16 == (int64_t)c.page_rows * MIXKV_PAGE_TILE_BYTES,
+    want(c.page_rows > 0 && pool->size(1) * 16 == (int64_t)c.page_rows * MIXKV_PAGE_TILE_BYTES,
          "a page of the pool must have page_rows / 16 tiles");
-    if (bounds.defined())
-      want(bounds.scalar_type() == at::kHalf && bounds.is_contiguous() && bounds.dim() == 3 &&
-               bounds.size(0) == pool.size(0) && bounds.size(1) == 2 && bounds.size(2) == 128 &&
-               bounds.device() == pool.device(),
+    if (bounds)
+      want(bounds->scalar_type() == at::kHalf && bounds->is_contiguous() && bounds->dim() == 3 &&
+               bounds->size(0) == pool->size(0) && bounds->size(1) == 2 && bounds->size(2) == 128 && bounds->device() == device,
            "bounds must be a contiguous fp16 tensor [pages, 2, 128] on the pool's device");
-    c.pool = pool.data_ptr();
-    c.bounds_opt = bounds.defined() ? bounds.data_ptr() : nullptr;
-    c.table = ip(table), c.rows = ip(rows);
-    c.num_pages = pool.size(0);
-    c.max_pages = int32(table.size(2), "mixkv_pages"), c.batch = int32(table.size(0), "mixkv_pages");
-    c.kv_heads = int32(table.size(1), "mixkv_pages"), c.head_dim = 128;
+    c.pool = pool->data_ptr();
+    c.bounds_opt = bounds ? bounds->data_ptr() : nullptr;
+    c.table = ip(*table), c.rows = ip(*rows);
+    c.num_pages = pool->size(0);
+    c.max_pages = int32(table->size(2), "mixkv_pages"), c.batch = int32(table->size(0), "mixkv_pages");
+    c.kv_heads = int32(table->size(1), "mixkv_pages"), c.head_dim = 128;
     c.k_scale = attr_float(o, nm.k_scale), c.v_scale = attr_float(o, nm.v_scale);
   }
 };
@@ -654,7 +665,7 @@ int32_t paged_type(const at::ScalarType t) {
 const int32_t* row_offsets(PyObject* o, const int64_t n, const PagesArg& pages) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o);
-  want(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n + 1 && t.device() == pages.pool.device(),
+  want(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n + 1 && t.device() == pages.pool().device(),
        "offsets must be a contiguous int32 tensor [batch + 1] (compact rows: [batch * kv_heads + 1]) on the pool's device");
   return ip(t);
 }
@@ -668,7 +679,7 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]);
     const bool compact = k.dim() == 2;
     want((compact || (k.dim() == 3 && k.size(1) == c.kv_heads)) && k.sizes() == v.sizes() && k.size(-1) == 128 &&
-             k.stride(-1) == 1 && v.stride(-1) == 1 && k.device() == pages.pool.device() && v.device() == k.device() &&
+             k.stride(-1) == 1 && v.stride(-1) == 1 && k.device() == pages.pool().device() && v.device() == k.device() &&
              k.scalar_type() == v.scalar_type(),
          "k and v must be of one type and shape, [tokens, kv_heads, 128] or compact rows [rows, 128], on the pool's device");
     const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), pages);
@@ -722,15 +733,15 @@ PyObject* py_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), pages);
     want(tokens >= 0 && (!compact || offsets), "compact rows need offsets");
     const int32_t max_new = int32(a[4], what);
-    const CallStream stream(a[6], pages.pool);
+    const CallStream stream(a[6], pages.pool());
     at::Tensor k, v;
     int rc = MIXKV_OK;
     {
       const Unlocked u;
       const at::ScalarType type = half ? at::kHalf : at::kBFloat16;
-      std::vector<int64_t> size = {tokens, c.kv_heads, 128};
-      if (compact) size.erase(size.begin() + 1);
-      k = empty(size, type, pages.pool), v = empty(size, type, pages.pool);
+      const int64_t sizes[3] = {tokens, c.kv_heads, 128}, flat[2] = {tokens, 128};
+      const at::IntArrayRef size = compact ? at::IntArrayRef(flat, 2) : at::IntArrayRef(sizes, 3);
+      k = empty(size, type, pages.pool()), v = empty(size, type, pages.pool());
       if (tokens > 0)
         rc = api.paged_read(&c, k.data_ptr(), v.data_ptr(), half ? MIXKV_TYPE_FP16 : MIXKV_TYPE_BF16, tokens, offsets,
                             compact, max_new, stream.handle);
@@ -748,7 +759,7 @@ struct PagedQuery {
   int32_t type, tokens, gqa;
   PagedQuery(PyObject* o, const PagesArg& pages) : q(tensor(o)) {
     want(q.dim() == 4 && q.size(0) == pages.c.batch && q.size(2) % pages.c.kv_heads == 0 && q.size(3) == 128 &&
-             (q.size(2) <= 1 || q.stride(2) == 128) && q.stride(3) == 1 && q.device() == pages.pool.device(),
+             (q.size(2) <= 1 || q.stride(2) == 128) && q.stride(3) == 1 && q.device() == pages.pool().device(),
          "q must be [batch, tokens, kv_heads * gqa_ratio, 128], a token's heads packed, on the pool's device");
     type = paged_type(q.scalar_type());
     tokens = int32(q.size(1), "q"), gqa = int32(q.size(2) / pages.c.kv_heads, "q");
@@ -773,7 +784,7 @@ struct PagedSpace {   // the caller's workspace or one of the call's own
   PagedSpace(PyObject* o, const PagesArg& pages, const PagedQuery& q) {
     if (o != Py_None) {
       const at::Tensor& t = tensor(o);
-      want(t.is_cuda() && t.is_contiguous() && t.device() == pages.pool.device(),
+      want(t.is_cuda() && t.is_contiguous() && t.device() == pages.pool().device(),
            "workspace must be a contiguous tensor on the pool's device");
       data = t.data_ptr(), bytes = t.nbytes();
     } else {
@@ -781,7 +792,7 @@ struct PagedSpace {   // the caller's workspace or one of the call's own
     }
   }
   void fill(const PagesArg& pages) {   // (without the interpreter lock)
-    if (!data) own = empty({(int64_t)bytes}, at::kByte, pages.pool), data = own.data_ptr();
+    if (!data) own = empty({(int64_t)bytes}, at::kByte, pages.pool()), data = own.data_ptr();
   }
 };
 
@@ -793,13 +804,13 @@ PyObject* py_paged_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const PagedQuery q(a[1], pages);
     const int32_t top = int32(a[2], what), rows = int32(a[3], what), first = int32(a[4], what), last = int32(a[5], what);
     if (top < 1) check_status(MIXKV_ERR_INVALID_ARG, what);
-    const CallStream stream(a[6], pages.pool);
+    const CallStream stream(a[6], pages.pool());
     at::Tensor list, counts;
     int rc;
     {
       const Unlocked u;
-      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool);
-      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool);
+      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool());
+      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool());
       rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
                             last, ip(list), ip(counts), stream.handle);
     }
@@ -823,14 +834,14 @@ PyObject* py_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const at::Tensor &l = tensor(a[3]), &c = tensor(a[4]);
       want(l.scalar_type() == at::kInt && l.dim() == 3 && l.is_contiguous() && l.size(0) == pages.c.batch &&
                l.size(1) == pages.c.kv_heads && c.scalar_type() == at::kInt && c.is_contiguous() &&
-               c.numel() == (int64_t)pages.c.batch * pages.c.kv_heads && l.device() == pages.pool.device() &&
-               c.device() == pages.pool.device(),
+               c.numel() == (int64_t)pages.c.batch * pages.c.kv_heads && l.device() == pages.pool().device() &&
+               c.device() == pages.pool().device(),
            "page lists and counts must be contiguous int32 tensors [batch, kv_heads, top] and [batch, kv_heads]");
       list = ip(l), counts = ip(c), top = int32(l.size(2), what);
     }
     const double scale = PyFloat_AsDouble(a[5]);
     if (PyErr_Occurred()) throw Raised();
-    const CallStream stream(a[7], pages.pool);
+    const CallStream stream(a[7], pages.pool());
     PagedSpace ws(a[6], pages, q);
     at::Tensor out;
     int rc;
@@ -857,15 +868,15 @@ PyObject* py_paged_sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     if (top < 1) check_status(MIXKV_ERR_INVALID_ARG, what);
     const double scale = PyFloat_AsDouble(a[6]);
     if (PyErr_Occurred()) throw Raised();
-    const CallStream stream(a[8], pages.pool);
+    const CallStream stream(a[8], pages.pool());
     PagedSpace ws(a[7], pages, q);
     at::Tensor list, counts, out;
     int rc;
     {
       const Unlocked u;
       ws.fill(pages);
-      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool);
-      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool);
+      list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool());
+      counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool());
       out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
       rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
                             last, ip(list), ip(counts), stream.handle);
