@@ -354,7 +354,7 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  * offsets[b] .. offsets[b + 1] - 1 of k and v (n = rows after the call minus rows before it: the caller counts them into
  * c->rows first).  K is rotated by the tokens' positions on the way.
  *   k, v            device, type `type`: head h of token i at i * row_stride + h * head_stride elements (both multiples of
- *                   8; 16-byte aligned), num_tokens tokens
+ *                   16; 32-byte aligned), num_tokens tokens
  *   offsets_opt     device int32 [batch + 1], ascending; NULL: one token per sequence.  offsets_per_head != 0:
  *                   [batch * kv_heads + 1], every head its own range of rows, head_stride is not used: K_out, V_out and
  *                   out_row_offsets of a compressed layer as they are
@@ -380,7 +380,7 @@ int mixkv_paged_append(const mixkv_pages* c, const void* k, const void* v, int32
 
 /* The last n rows of every head back as dense rows: what mixkv_paged_append was given, rounded (and rotated).  offsets_opt,
  * offsets_per_head and max_new as there (n = the number of rows reads the whole head).
- *   k_out, v_out    device, type `type`, 16-byte aligned: [num_tokens, kv_heads, 128], or [num_tokens, 128] with
+ *   k_out, v_out    device, type `type`, 32-byte aligned: [num_tokens, kv_heads, 128], or [num_tokens, 128] with
  *                   offsets_per_head; rows that do not exist are not written */
 int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
                      const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, void* stream);

@@ -153,7 +153,10 @@ __device__ __forceinline__ uint32_t word16(const Raw16& r, const int i) {
 template <typename T>
 __device__ __forceinline__ Raw16 load16(const T* src, const bool on) {
   Raw16 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-  if (on) r.a = __ldg(reinterpret_cast<const uint4*>(src)), r.b = __ldg(reinterpret_cast<const uint4*>(src) + 1);
+  if (on)
+    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+        : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w), "=r"(r.b.x), "=r"(r.b.y), "=r"(r.b.z), "=r"(r.b.w)
+        : "l"(src));
   return r;
 }
 template <typename T>
@@ -360,17 +363,20 @@ __global__ void __launch_bounds__(kRowThreads) k_paged_read(const RowArgs a, T* 
     for (int j = 0; j < 2; ++j) {
       const int r = r0 + j * step;
       if (r >= s.last) break;
-      uint32_t f[8], out[8];
+      uint32_t f[8], out[8];      // (32 bytes a lane, one store)
       codes_to_f16(w[j].x, *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
       codes_to_f16(w[j].y, *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
       const uint32_t ss = scales_to_f16(scale[j] | scale[j] << 8);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float2 y = widen2<__half>(mul_f16x2(f[i], ss));
-        out[i] = narrow2<T>(__fmul_rn(y.x, third), __fmul_rn(y.y, third));
+        float a, b;
+        unpack2(mul2(pack2(y.x, y.y), pack2(third, third)), a, b);
+        out[i] = narrow2<T>(a, b);
       }
-      uint4* to = reinterpret_cast<uint4*>(rows + r * stride);
-      to[0] = make_uint4(out[0], out[1], out[2], out[3]), to[1] = make_uint4(out[4], out[5], out[6], out[7]);
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(rows + r * stride), "r"(out[0]), "r"(out[1]),
+                   "r"(out[2]), "r"(out[3]), "r"(out[4]), "r"(out[5]), "r"(out[6]), "r"(out[7])
+                   : "memory");
     }
   }
 }
@@ -414,7 +420,7 @@ int read_as(const mixkv_pages* c, const RowArgs& a, void* k, void* v, void* stre
              ? MIXKV_OK
              : MIXKV_ERR_CUDA;
 }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned(const void* p, const unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace
 }  // namespace mixkv
@@ -437,13 +443,13 @@ extern "C" int mixkv_paged_append(const mixkv_pages* c, const void* k, const voi
   RowArgs a = {};
   const int rc = check_rows(c, type, num_tokens, offsets_opt, offsets_per_head, max_new, &a);
   if (rc != MIXKV_OK) return rc;
-  if (!k || !v || !aligned16(k) || !aligned16(v)) return MIXKV_ERR_INVALID_ARG;
+  if (!k || !v || !aligned(k, 32) || !aligned(v, 32)) return MIXKV_ERR_INVALID_ARG;
   for (const int64_t stride : {k_row_stride, k_head_stride, v_row_stride, v_head_stride})
-    if (stride < 0 || stride % 8) return MIXKV_ERR_INVALID_ARG;
+    if (stride < 0 || stride % 16) return MIXKV_ERR_INVALID_ARG;
   const bool rope = cos_opt != nullptr;
   if (rope != (sin_opt != nullptr)) return MIXKV_ERR_INVALID_ARG;
   if (rope) {
-    if (!positions_opt || table_len < 1 || !aligned16(cos_opt) || !aligned16(sin_opt) || rot_dim < 1 || rot_dim > kHeadDim ||
+    if (!positions_opt || table_len < 1 || !aligned(cos_opt, 16) || !aligned(sin_opt, 16) || rot_dim < 1 || rot_dim > kHeadDim ||
         (reinterpret_cast<uintptr_t>(positions_opt) & 3u))
       return MIXKV_ERR_INVALID_ARG;
     if (rot_dim % (interleaved ? 16 : 32)) return MIXKV_ERR_UNSUPPORTED;
@@ -461,7 +467,7 @@ extern "C" int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, 
   RowArgs a = {};
   const int rc = check_rows(c, type, num_tokens, offsets_opt, offsets_per_head, max_new, &a);
   if (rc != MIXKV_OK) return rc;
-  if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out)) return MIXKV_ERR_INVALID_ARG;
+  if (!k_out || !v_out || !aligned(k_out, 32) || !aligned(v_out, 32)) return MIXKV_ERR_INVALID_ARG;
   return type == MIXKV_TYPE_BF16 ? read_as<__nv_bfloat16>(c, a, k_out, v_out, stream)
                                  : read_as<__half>(c, a, k_out, v_out, stream);
 }
