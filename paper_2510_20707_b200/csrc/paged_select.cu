@@ -98,6 +98,11 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
     }
   };
   fetch(begin, lo[kSets - 1], hi[kSets - 1]);
+  float4 up4[4], dn4[4];
+  if constexpr (RP == 4) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) up4[r] = qs[r * 64 + lane], dn4[r] = qs[r * 64 + 32 + lane];
+  }
   for (int p0 = begin; p0 < end; p0 += kPages) {
     uint32_t best = 0;
     const bool more = p0 + kPages < end;
@@ -110,16 +115,32 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
 #pragma unroll 1
     for (int r0 = 0; r0 < padded_rows(a.R); r0 += RP) {
       float v[32];
+      auto term = [&](const float4& up, const float4& dn, const float (&l)[4], const float (&g)[4]) {
+        const float x0 = fmaf(up.x, g[0], __fmul_rn(dn.x, l[0])), x1 = fmaf(up.y, g[1], __fmul_rn(dn.y, l[1]));
+        const float x2 = fmaf(up.z, g[2], __fmul_rn(dn.z, l[2])), x3 = fmaf(up.w, g[3], __fmul_rn(dn.w, l[3]));
+        return __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
+      };
+      auto widen = [&](const uint2& w, float (&x)[4]) {
+        const float2 p = widen2<__half>(w.x), q = widen2<__half>(w.y);
+        x[0] = p.x, x[1] = p.y, x[2] = q.x, x[3] = q.y;
+      };
+      if constexpr (RP == 4) {     // the query rows stay in registers, a page is widened at a time
 #pragma unroll
-      for (int i = 0; i < kPages; ++i) {
-        const float2 l0 = widen2<__half>(lo[0][i].x), l1 = widen2<__half>(lo[0][i].y);
-        const float2 h0 = widen2<__half>(hi[0][i].x), h1 = widen2<__half>(hi[0][i].y);
+        for (int i = 0; i < kPages; ++i) {
+          float l[4], g[4];
+          widen(lo[0][i], l), widen(hi[0][i], g);
+#pragma unroll
+          for (int r = 0; r < RP; ++r) v[RP * i + r] = term(up4[r], dn4[r], l, g);
+        }
+      } else {     // four pages stay widened, a query row is read at a time (read again for every page they were 256 of 450 clocks)
+        float l[kPages][4], g[kPages][4];
+#pragma unroll
+        for (int i = 0; i < kPages; ++i) widen(lo[0][i], l[i]), widen(hi[0][i], g[i]);
 #pragma unroll
         for (int r = 0; r < RP; ++r) {
           const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
-          const float x0 = fmaf(up.x, h0.x, __fmul_rn(dn.x, l0.x)), x1 = fmaf(up.y, h0.y, __fmul_rn(dn.y, l0.y));
-          const float x2 = fmaf(up.z, h1.x, __fmul_rn(dn.z, l1.x)), x3 = fmaf(up.w, h1.y, __fmul_rn(dn.w, l1.y));
-          v[RP * i + r] = __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
+#pragma unroll
+          for (int i = 0; i < kPages; ++i) v[RP * i + r] = term(up, dn, l[i], g[i]);
         }
       }
       if (kSets == 1 && more) fetch(p0 + kPages, lo[0], hi[0]);      // (RP == 4: there is one round of query rows)
