@@ -104,6 +104,11 @@ __device__ __forceinline__ uint32_t narrow2<__half>(float x, float y) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// What an earlier kernel of the stream may have written while this one was already resident (it waits in pdl_wait) is read by ordinary
+// loads: the read-only path is for data that does not change in a kernel's lifetime, and an SM's copy of it may be from before.
+template <typename T>
+__device__ __forceinline__ T fresh(const T* p) { return *p; }
+
 // This CTA's cluster in the grid (a CTA outside of one: its own number).
 __device__ __forceinline__ int cluster_id() {
   uint32_t r;

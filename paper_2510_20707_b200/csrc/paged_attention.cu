@@ -67,11 +67,11 @@ struct UnitTiles {
 };
 __device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
   UnitTiles r;
-  int n = __ldg(a.p.rows + u);
+  int n = fresh(a.p.rows + u);
   n = min(n, a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
   r.n = max(n, 0);
-  r.tiles = a.list ? max(0, min(__ldg(a.counts + u), a.top)) * a.p.tiles : (r.n + kPageTile - 1) >> 4;
+  r.tiles = a.list ? max(0, min(fresh(a.counts + u), a.top)) * a.p.tiles : (r.n + kPageTile - 1) >> 4;
   r.steps = (r.tiles + 1) >> 1;
   return r;
 }
@@ -113,8 +113,8 @@ struct TileAt {
 __device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const UnitTiles& ut, const int t) {
   const int slot = a.p.by_tiles.div(t), in = t - slot * a.p.tiles;
   int page = slot;
-  if (a.list) page = slot < a.top ? __ldg(a.list + (long long)u * a.top + slot) : -1;
-  const int id = page >= 0 && page < a.p.max_pages ? __ldg(a.p.table + (long long)u * a.p.max_pages + page) : -1;
+  if (a.list) page = slot < a.top ? fresh(a.list + (long long)u * a.top + slot) : -1;
+  const int id = page >= 0 && page < a.p.max_pages ? fresh(a.p.table + (long long)u * a.p.max_pages + page) : -1;
   const int row = page * a.p.page_rows + in * kPageTile;
   if (id < 0 || id >= a.p.num_pages || t >= ut.tiles || row >= ut.n) return TileAt{-1, kNoRow};
   return TileAt{id * a.p.tiles + in, row};
@@ -183,7 +183,7 @@ struct AttState {
       const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
                      (long long)(h * a.G + (on ? r - token * a.G : 0)) * kHeadDim + 32 * t;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) raw[i] = on ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
+      for (int i = 0; i < 4; ++i) raw[i] = on ? fresh(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
       float most = 0.f;
       bool odd = false;    // a NaN or an infinity
 #pragma unroll

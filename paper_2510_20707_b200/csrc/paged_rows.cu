@@ -40,12 +40,12 @@ __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) 
   s.u = a.by_slots.div(task);
   const int slot = task - s.u * a.slots, b = a.p.by_heads.div(s.u);
   s.h = s.u - b * a.p.H;
-  const int rows = __ldg(a.p.rows + s.u);
+  const int rows = fresh(a.p.rows + s.u);
   int n = 1;
   long long first = b;
   if (a.offsets) {
     const int i = a.per_head ? s.u : b;
-    const int from = __ldg(a.offsets + i), to = __ldg(a.offsets + i + 1);
+    const int from = fresh(a.offsets + i), to = fresh(a.offsets + i + 1);
     n = to > from ? (int)min((unsigned)to - (unsigned)from, (unsigned)a.max_new) : 0;
     first = (long long)to - n;
   }
@@ -61,7 +61,7 @@ __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) 
   const long long from = -s.token, to = a.num_tokens - s.token;
   s.first = from > s.lo ? (int)(from < s.hi ? from : s.hi) : s.lo;
   s.last = to < s.hi ? (int)(to > s.lo ? to : s.lo) : s.hi;
-  s.id = s.lo < s.hi && s.page < a.p.max_pages ? __ldg(a.p.table + (long long)s.u * a.p.max_pages + s.page) : -1;
+  s.id = s.lo < s.hi && s.page < a.p.max_pages ? fresh(a.p.table + (long long)s.u * a.p.max_pages + s.page) : -1;
   return s;
 }
 
@@ -154,9 +154,10 @@ template <typename T>
 __device__ __forceinline__ Raw16 load16(const T* src, const bool on) {
   Raw16 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
   if (on)
-    asm("ld.global.nc.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
         : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w), "=r"(r.b.x), "=r"(r.b.y), "=r"(r.b.z), "=r"(r.b.w)
-        : "l"(src));
+        : "l"(src)
+        : "memory");
   return r;
 }
 template <typename T>
@@ -181,7 +182,7 @@ __device__ __forceinline__ Turn<ROPE> load_turn(const RowArgs& a, const int pos,
   const long long from = (long long)pos * half + (16 * g < a.rot ? at : 0);
 #pragma unroll
   for (int i = 0; i < (ROPE == 1 ? 4 : 2); ++i)
-    t.cs[i] = __ldg(reinterpret_cast<const float4*>(a.cosv + from) + i), t.sn[i] = __ldg(reinterpret_cast<const float4*>(a.sinv + from) + i);
+    t.cs[i] = fresh(reinterpret_cast<const float4*>(a.cosv + from) + i), t.sn[i] = fresh(reinterpret_cast<const float4*>(a.sinv + from) + i);
   return t;
 }
 
@@ -223,7 +224,7 @@ __device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const 
 // page needs of the tables is in L1), every warp both.
 template <typename T, int ROPE>
 __global__ void __launch_bounds__(kAppThreads, kAppPerSm)
-k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v, const int tasks, const int run) {
+k_paged_append(const RowArgs a, const T* k, const T* v, const int tasks, const int run) {
   __shared__ float2 divisors[2][128];
   __shared__ __half2 part[kAppThreads / 32][8][17];   // of every warp: minima and maxima of a block's eight pairs of dimensions
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane & 7, sub = lane >> 3;
@@ -252,7 +253,7 @@ k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v
     int r = s.lo + (single ? 0 : 4 * warp) + sub;
     bool on = r >= s.first && r < s.last;
     Raw16 kk = load16(kr + r * a.k_row, on && does_k), vv = load16(vr + r * a.v_row, on && does_v);
-    int pos = ROPE && on ? __ldg(positions + r) : 0;
+    int pos = ROPE && on ? fresh(positions + r) : 0;
     for (; r - sub < s.hi; r += step) {
       const Raw16 kx = kk, vx = vv;
       const int at = pos;
@@ -261,7 +262,7 @@ k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v
         const int next = r + step;
         on = next >= s.first && next < s.last;
         kk = load16(kr + next * a.k_row, on && does_k), vv = load16(vr + next * a.v_row, on && does_v);
-        pos = ROPE && on ? __ldg(positions + next) : 0;
+        pos = ROPE && on ? fresh(positions + next) : 0;
       }
       const bool turned = at >= 0 && at < a.table_len;
       const bool write = have && placed && (!ROPE || turned);      // (a token is written whole or not at all)
@@ -338,7 +339,7 @@ k_paged_append(const RowArgs a, const T* __restrict__ k, const T* __restrict__ v
 
 // A lane has a block of a row, as above.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) k_paged_read(const RowArgs a, T* __restrict__ k, T* __restrict__ v) {
+__global__ void __launch_bounds__(kRowThreads) k_paged_read(const RowArgs a, T* k, T* v) {
   pdl_launch_dependents();
   pdl_wait();
   const PageSpan s = page_span(a, blockIdx.x);

@@ -85,7 +85,7 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
   // asked for again where they were.
   constexpr int kSets = RP == 8 ? 2 : 1;
   uint2 lo[kSets][kPages], hi[kSets][kPages];
-  int ids = begin + lane < end ? __ldg(table + begin + lane) : -1;     // of 32 pages from the last multiple of 32
+  int ids = begin + lane < end ? fresh(table + begin + lane) : -1;     // of 32 pages from the last multiple of 32
   auto fetch = [&](const int p0, uint2 (&to_lo)[kPages], uint2 (&to_hi)[kPages]) {
 #pragma unroll
     for (int i = 0; i < kPages; ++i) {
@@ -93,7 +93,7 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
       to_lo[i] = to_hi[i] = make_uint2(0, 0);    // (a page outside the pool scores zero)
       if (p0 + i < end && id >= 0 && id < a.p.num_pages) {
         const __half* src = a.p.bounds + (long long)id * 2 * kHeadDim + 4 * lane;
-        to_lo[i] = __ldg(reinterpret_cast<const uint2*>(src)), to_hi[i] = __ldg(reinterpret_cast<const uint2*>(src + kHeadDim));
+        to_lo[i] = fresh(reinterpret_cast<const uint2*>(src)), to_hi[i] = fresh(reinterpret_cast<const uint2*>(src + kHeadDim));
       }
     }
   };
@@ -106,7 +106,7 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
   for (int p0 = begin; p0 < end; p0 += kPages) {
     uint32_t best = 0;
     const bool more = p0 + kPages < end;
-    if (more && (p0 + kPages - begin) % 32 == 0) ids = p0 + kPages + lane < end ? __ldg(table + p0 + kPages + lane) : -1;
+    if (more && (p0 + kPages - begin) % 32 == 0) ids = p0 + kPages + lane < end ? fresh(table + p0 + kPages + lane) : -1;
     if constexpr (kSets == 2) {
 #pragma unroll
       for (int i = 0; i < kPages; ++i) lo[0][i] = lo[1][i], hi[0][i] = hi[1][i];
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
     const int token = a.by_group.div(r);
     const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
                    (long long)(h * a.G + r - token * a.G) * kHeadDim + 4 * (e & 31);
-    const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
+    const uint2 w = fresh(reinterpret_cast<const uint2*>(src));
     const float2 x = widen2<T>(w.x), y = widen2<T>(w.y);
     // (a NaN stays one in both parts)
     auto up = [](float z) { return z < 0.f ? 0.f : z; };

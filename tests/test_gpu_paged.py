@@ -490,3 +490,30 @@ def test_the_example_runs():
     # two 4-bit codes to a byte, blocks of 16: the rounding of normal values is about a tenth of them
     assert len(errors) == 2 and max(errors) < 0.3
     assert len(outs) == 4 and all(o.shape == (1, 1, 28, 128) and torch.isfinite(o.float()).all() for o in outs)
+
+
+def test_what_changes_from_step_to_step_is_read_anew():
+    # rows, table, lists and rows of the pool are written by one kernel and read by the next, which is resident by then: in one
+    # loop without a pause, with outputs in the memory of earlier ones, every step gives what it gives when nothing overlaps
+    B, H, G, page, n = 3, 2, 4, 16, 60
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((n, B, H, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((n, B, 1, H * G, 128), generator=gen, device="cuda").bfloat16()
+    caches = [Cache(np.zeros((B, H), int), page, bounds=True, seed=i, room=n) for i in range(2)]
+
+    def steps(c, wait):
+        outs = []
+        for i in range(n):
+            c.pages.rows += 1
+            binding.paged_append(c.pages, k[i], v[i])
+            out, lists, counts = binding.paged_sparse_attention(c.pages, q[i], 2)
+            full = binding.paged_attention(c.pages, q[i])
+            if wait:
+                torch.cuda.synchronize()
+            outs.append((out, full))
+            del lists, counts
+        torch.cuda.synchronize()
+        return outs
+
+    for (a, b), (x, y) in zip(steps(caches[0], True), steps(caches[1], False)):
+        assert torch.equal(a, x) and torch.equal(b, y)
