@@ -24,7 +24,6 @@ namespace {
 constexpr int kAttWarps = 4;                   // of a CTA of which an SM holds several
 constexpr int kAttWide = 16;                   // of one that has an SM for itself (one group of query rows)
 constexpr int kAttDepth = 2;                   // steps of a warp on their way or in work
-constexpr int kAttPair = 1;                    // up to so many groups of eight query rows a softmax step is two tiles, else one
 constexpr int kStepBytes = 2 * kTileBytes;
 constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is not there: beyond all
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
@@ -255,16 +254,15 @@ struct AttState {
     }
   }
 
-  // HN tiles (one softmax step), whose first rows are row[], of a unit of n rows; `first`: the CTA's first query row.  edge: rows may lie
+  // Two tiles, whose first rows are row[], of a unit of n rows; `first`: the CTA's first query row.  edge: rows may lie
   // beyond what a query row sees.  (A flag and not a second copy of the code: a step that was alone in its kind waited for its
   // instructions for longer than it took.)
-  template <int HN>
-  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tiles, const int (&row)[HN], const bool edge,
+  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tiles, const int (&row)[2], const bool edge,
                                        const int n, const int first, const int lane) {
     const int g = lane >> 2, t = lane & 3;
-    float s[HN][NT][4];
+    float s[2][NT][4];
 #pragma unroll
-    for (int h = 0; h < HN; ++h) {
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -278,16 +276,16 @@ struct AttState {
         for (int c = 0; c < 2; ++c) {
           const int sees = n - a.T + 1 + token_of(a, first + 8 * nt + 2 * t + c) - 4 * (g >> 1) - (g & 1);
 #pragma unroll
-          for (int h = 0; h < HN; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2)
               if (row[h] + 2 * (i >> 1) >= sees) s[h][nt][i] = -INFINITY;
         }
     }
     bool above = false;
-    float y[HN][NT][4];
+    float y[2][NT][4];
 #pragma unroll
-    for (int h = 0; h < HN; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -302,7 +300,7 @@ struct AttState {
         for (int c = 0; c < 2; ++c) {
           float mx = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < HN; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2) {
               y[h][nt][i] = s[h][nt][i] * f[nt][c];
@@ -312,16 +310,16 @@ struct AttState {
           const float shrink = ex2(ref[nt][c] - to);
           ref[nt][c] = to, z[nt][c] *= shrink;
 #pragma unroll
-          for (int h = 0; h < HN; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2) y[h][nt][i] -= to;
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }
     }
-    uint32_t p[HN][NT][2];   // B fragments: query row g, tile rows 4 t, 4 t + 1 and 4 t + 2, 4 t + 3
+    uint32_t p[2][NT][2];   // B fragments: query row g, tile rows 4 t, 4 t + 1 and 4 t + 2, 4 t + 3
 #pragma unroll
-    for (int h = 0; h < HN; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -330,7 +328,7 @@ struct AttState {
         p[h][nt][1] = transpose8x8(narrow2<__half>(y[h][nt][2], y[h][nt][3]));
       }
 #pragma unroll
-    for (int h = 0; h < HN; ++h) {
+    for (int h = 0; h < 2; ++h) {
       const unsigned char* tile = tiles + h * kTileBytes;
       const uint4 v[2] = {*reinterpret_cast<const uint4*>(tile + kTileV + 16 * lane),
                           *reinterpret_cast<const uint4*>(tile + kTileV + 512 + 16 * lane)};
@@ -509,16 +507,8 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
       const int2 at = ring_rows[slot];
       const unsigned char* tiles = ring + slot * kStepBytes;
       const bool inside = max(at.x, at.y) + kPageTile <= clear;
-      if constexpr (NT <= kAttPair) {
-        const int row[2] = {at.x, at.y};
-        st.template step<2>(a, tiles, row, !inside, n, first, lane);
-      } else {
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const int row[1] = {h ? at.y : at.x};
-          st.template step<1>(a, tiles + h * kTileBytes, row, !inside, n, first, lane);
-        }
-      }
+      const int row[2] = {at.x, at.y};
+      st.step(a, tiles, row, !inside, n, first, lane);
       __syncwarp();     // every lane has read the slot
       if (sent < count) send();
       ++slot;
