@@ -393,10 +393,11 @@ int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, int32_t typ
  *   q               device, type `type`: [batch, q_tokens, kv_heads * gqa_ratio, 128], strides in elements of the first
  *                   two dimensions (multiples of 8), 16-byte aligned
  *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call
- *   top             pages to list
+ *   top             pages to list, at most 2^20
  *   page_list       out, int32 [batch, kv_heads, top]: ascending columns of the page table, -1 behind the last
  *   counts          out, int32 [batch, kv_heads]: min(top, pages of the head)
- * Needs c->bounds_opt; at most MIXKV_PAGES_MAX pages per head (of max_rows), else MIXKV_ERR_UNSUPPORTED. */
+ * Needs c->bounds_opt; at most MIXKV_PAGES_MAX pages per head (of max_rows), and 4 bytes for every page and 1 KB for every query
+ * row (a multiple of eight) within 219 KB, else MIXKV_ERR_UNSUPPORTED. */
 int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t type, int64_t q_batch_stride,
                        int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows, int32_t top,
                        int32_t keep_first, int32_t keep_last, int32_t* page_list, int32_t* counts, void* stream);

@@ -12,6 +12,7 @@ constexpr int kPageTile = 16;                                // rows of a tile
 constexpr int kTileBytes = MIXKV_PAGE_TILE_BYTES;
 constexpr int kTileV = 1024, kTileKs = 2048, kTileVs = 2176;  // V codes, K scales, V scales inside a tile
 static_assert(kTileBytes == kTileVs + 128, "a tile");
+constexpr int kMostListed = 1 << 20;                         // longest page list
 
 // n / d for 0 <= n < 2^31 as a product: with l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, n m exceeds n 2^(31 + l) / d by
 // less than 2^(31 + l) / d (n < 2^31, and m d - 2^(31 + l) <= 2^l).  A division of the hardware's kind is a chain of some twenty

@@ -10,8 +10,16 @@
 // Codes of two rows are interleaved (V) by one select per eight values before they are widened, so that a pair is two rows.
 //
 // Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a
-// tile instead of a reduction); weights are fp16 times 2^kLift, so that what is 2^-20 of the largest is still a normal
+// step instead of a reduction); weights are fp16 times 2^kLift, so that what is 2^-20 of the largest is still a normal
 // number; sums are fp32.
+//
+// What bounds it.  A row pair is 144 bytes; a tile of 16 costs a warp about 260 instructions: 64 conversions (two clocks each, as the
+// fp16 products), 64 products with scales, 16 matrix instructions (eight clocks), 16 selects.  256 heads of 1021 to 16384 rows (329 MB)
+// take 72 us in this kernel: 4.5 TB/s, an instruction issued in 60 % of the clocks, the arithmetic pipe busy in 54, the tensor
+// pipe in 26; the same copies without the arithmetic take 57 us.  Two tiles a softmax step instead of one: 293 for 347 instructions a tile,
+// and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as fast as sixteen with 128;
+// asking for values ahead of the vote, one copy for two tiles that follow one another, rings of three: no gain.  With query rows on
+// the sixteen side, one tile a step and a chunk per CTA the same call took 129 us, and now 76.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -29,7 +37,7 @@ constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is no
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
 constexpr int kAttUnits = 1024;                // most units whose steps are dealt out evenly
-constexpr int kAttFew = 2, kAttFewRows = 8, kAttWideSteps = 8, kAttManySteps = 20;   // steps of a warp that settle how the work is split
+constexpr int kAttFew = 2, kAttFewRows = 8, kAttWideSteps = 8, kAttManySteps = 20;   // steps of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
 constexpr float kNoRef = -1e30f;               // reference before the first row: below any, and finite
 
@@ -603,7 +611,8 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
 
 // Joins the shares of units that several CTAs had a part of, and writes zeros for units without rows.  per_row warps (a power
 // of two) take the shares of a query row in turn, a few at once with a running reference: what a share holds comes in one
-// round trip.
+// round trip.  It costs a call 4 to 6 us (8 heads of 131072 rows: 36.4 with a join that does nothing, 40.3).  Joined by the last
+// CTA of a unit instead, behind a fence and a count that a kernel before had to clear, 8 to 10.
 constexpr int kJoinWarps = 16;
 template <typename T>
 __global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a, const Divider per_row, const Divider blocks) {
@@ -677,6 +686,22 @@ AttKernel att_kernel(const int NT, const bool wide) {
 
 // How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit.  narrow(n), wide(n): clusters
 // of n CTAs of either kind that are resident at once.
+//
+// A cluster of small CTAs per unit, one of large CTAs that have an SM each, or all steps dealt out evenly and joined by a second
+// kernel; us a call, one token of four query heads, heads of one length (and of lengths from one row to that):
+//     heads x rows     small          large         shares
+//     8 x 2048         7.5            8.2           10.3        two steps for every warp of eight small CTAs
+//     8 x 4096         9.3            8.2           10.8
+//     8 x 16384       19.8 (21.5)    14.3 (14.4)    15.4 (16.6)
+//     8 x 65536       60.8 (67.7)    35.8 (36.7)    27.7 (23.4)
+//     64 x 4096       14.9 (13.4)    14.7 (14.5)    20.0 (17.3)
+//     64 x 8192       22.6 (19.8)    22.1 (22.4)    26.4 (21.0)   eight steps for every warp of two large CTAs
+//     64 x 16384      39.5 (31.7)    38.3 (37.2)    41.8 (29.5)
+//     256 x 2048      23.5 (20.2)    26.5 (21.7)    28.7 (36.2)   eight steps for every warp of two small CTAs
+//     256 x 4096      40.5 (32.3)    43.7 (33.4)    43.0 (43.1)
+//     256 x 16384    128.9 (102.5)  125.9 (98.1)   121.2 (88.2)
+// and 896 heads of 70 to 1639 rows 39.7 by small CTAs, 43.2 by shares.  More query rows make a step longer and the join a smaller
+// part (35 rows in two groups, small / shares: 8 heads of 2048 rows 13.3 / 16.8, of 8192 26.8 / 25.5, 32 of 8192 45.0 / 48.1).
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all steps
   bool wide;
@@ -702,7 +727,7 @@ AttShape att_shape(const long long units, const int groups, const long long step
   } else if (NT == 1 && alone <= kAttManySteps) {
     return {S, 0, false};
   }
-  if (units <= kAttUnits && groups < slots) {
+  if (units <= kAttUnits && groups < slots && units * steps <= 0x7fffffffll) {
     const long long want = (units * steps + kAttWarps * 2 - 1) / (kAttWarps * 2);     // (two steps to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups), false};
   }
@@ -760,6 +785,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
       !(softmax_scale >= 0.f) || q_batch_stride < 0 || q_token_stride < 0 || q_batch_stride % 8 || q_token_stride % 8 ||
       (page_list_opt == nullptr) != (counts_opt == nullptr) || (page_list_opt && top < 1))
     return MIXKV_ERR_INVALID_ARG;
+  if (page_list_opt && top > kMostListed) return MIXKV_ERR_UNSUPPORTED;
   if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15u)
     return MIXKV_ERR_INVALID_ARG;
   if ((rc = queries_of(c, q_tokens, gqa_ratio, &groups, &NT)) != MIXKV_OK) return rc;

@@ -1,12 +1,19 @@
 // Which pages of the paged cache a query attends to (score and order: include/mixkv.h).
 //
-// A cluster has one (sequence, KV head): its warps score runs of pages, four at a time, the scores go as order-preserving
-// words into the first CTA's shared memory, and that CTA lists the `top` largest.
-//
 // Score.  Lane l holds dimensions 4 l .. 4 l + 3 of the pages' bounds; of q max(q, 0) and min(q, 0) lie in shared memory, so a
 // term is fma(max(q, 0), hi, min(q, 0) * lo): one of the two products is zero, the other exact (11 + 6 bits).  The sum over
 // neighbouring pairs is two additions inside the lane and five across lanes; these are done for 32 (page, query row)
 // pairs at a time, every exchange halving the number of sums a lane still holds (31 exchanges for 32 sums, not 160).
+//
+// A cluster has one (sequence, KV head): its warps score runs of pages, four at a time, the scores go as order-preserving
+// words into the first CTA's shared memory, and that CTA lists the `top` largest.
+//
+// What bounds it: instructions.  A (page, query row) pair costs a warp about 20: 8 multiply-adds, 3 additions, 4 of the exchanges, the
+// rest for the bounds' way in.  32 heads of 16001 to 65536 rows in pages of 32 (40 800 pages, seven query heads) 22 us, of
+// which listing 5; 8 heads of 131072 rows in pages of 64, four query heads, 11.  Clusters of long heads work while those of
+// short ones have ended; equal runs of pages of all heads in a kernel of their own, through memory, took 22.7 and 9.9, and 1 us
+// more where there are few pages.  Two dimensions to an instruction, query rows in registers, bounds asked for further
+// ahead: level or slower.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -283,7 +290,7 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   const long long seen = max_rows < (long long)c->max_pages * c->page_rows ? max_rows : (long long)c->max_pages * c->page_rows;
   const long long pages = (seen + c->page_rows - 1) / c->page_rows;
   const long long units = (long long)c->batch * c->kv_heads;
-  if (R > MIXKV_PAGED_MAX_QUERIES || pages > MIXKV_PAGES_MAX) return MIXKV_ERR_UNSUPPORTED;
+  if (R > MIXKV_PAGED_MAX_QUERIES || pages > MIXKV_PAGES_MAX || top > kMostListed) return MIXKV_ERR_UNSUPPORTED;
   const size_t smem = select_smem((int)R, (int)pages), most = 227 * 1024 - 8192;
   if (smem > most) return MIXKV_ERR_UNSUPPORTED;
   if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
