@@ -191,6 +191,12 @@ __device__ __forceinline__ Turn<ROPE> load_turn(const RowArgs& a, const int pos,
   return t;
 }
 
+// a + b in halves: of a packed sum and the packed products before it, .rn or not, the compiler makes multiply-adds.
+__device__ __forceinline__ f32x2 add_rounded(const f32x2 a, const f32x2 b) {
+  float ax, ay, bx, by;
+  unpack2(a, ax, ay), unpack2(b, bx, by);
+  return pack2(__fadd_rn(ax, bx), __fadd_rn(ay, by));
+}
 // The rotation; products and sums are rounded one by one.  All lanes of the warp take part.
 template <typename T, int ROPE>
 __device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const int g, const int rot, const Turn<ROPE>& turn) {
@@ -207,8 +213,8 @@ __device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float4 cs = turn.cs[i], sn = turn.sn[i];
-      x[2 * i] = add2(mul2(x[2 * i], pack2(cs.x, cs.y)), mul2(wide2<T>(y[2 * i]), pack2(sn.x, sn.y)));
-      x[2 * i + 1] = add2(mul2(x[2 * i + 1], pack2(cs.z, cs.w)), mul2(wide2<T>(y[2 * i + 1]), pack2(sn.z, sn.w)));
+      x[2 * i] = add_rounded(mul2(x[2 * i], pack2(cs.x, cs.y)), mul2(wide2<T>(y[2 * i]), pack2(sn.x, sn.y)));
+      x[2 * i + 1] = add_rounded(mul2(x[2 * i + 1], pack2(cs.z, cs.w)), mul2(wide2<T>(y[2 * i + 1]), pack2(sn.z, sn.w)));
     }
   } else if (ROPE == 2 && inside) {
 #pragma unroll
@@ -219,7 +225,7 @@ __device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const 
       for (int e = 0; e < 4; ++e) {
         float p, q;
         unpack2(x[4 * i + e], p, q);
-        x[4 * i + e] = add2(mul2(x[4 * i + e], pack2(cc[e], cc[e])), mul2(pack2(-q, p), pack2(ss[e], ss[e])));
+        x[4 * i + e] = add_rounded(mul2(x[4 * i + e], pack2(cc[e], cc[e])), mul2(pack2(-q, p), pack2(ss[e], ss[e])));
       }
     }
   }

@@ -121,6 +121,38 @@ def test_append_and_read_back(dtype, page, rot, inter, H):
     assert torch.equal(kr.cpu(), back(kv, 0.5)) and torch.equal(vr.cpu(), back(vv, 2.0))
 
 
+@pytest.mark.parametrize("dtype,inter", [("bf16", False), ("fp16", True), ("bf16", True)])
+def test_products_of_the_rotation_are_rounded_before_their_sum(dtype, inter):
+    # 100 cos - 100 sin is 8, a quarter of the block's scale and so a code of zero, if both products are rounded first; with one
+    # of them unrounded it is more, and the code is the next.  One pair of eight sets the scale (192 / 6 = 32).
+    rng = np.random.default_rng(0)
+    n, pairs = 24, 64
+    s = rng.uniform(0.5, 0.9, 400000).astype(np.float32)
+    c = ((np.float32(100) * s).astype(np.float64) + 8.0) / 100.0
+    c = c.astype(np.float32)
+    cp, sp = np.float32(100) * c, np.float32(100) * s
+    exact_c, exact_s = 100.0 * c.astype(np.float64), 100.0 * s.astype(np.float64)
+    near = (cp - sp == 8) & ((exact_c - sp).astype(np.float32) > 8) & ((cp - exact_s).astype(np.float32) > 8)
+    assert near.sum() > n * pairs
+    cos, sin = (t[near][:n * pairs].reshape(n, pairs).copy() for t in (c, s))
+    cos[:, ::8], sin[:, ::8] = 1.0, 0.0
+    x = np.full((n, pairs), 100, np.float32)
+    y = x.copy()
+    x[:, ::8], y[:, ::8] = 192.0, 0.0
+    rows = np.stack([x, y], -1).reshape(n, 128) if inter else np.concatenate([x, y], 1)
+    cache = Cache([[n]], 32)
+    k = torch.from_numpy(rows).to(TYPES[dtype]).cuda()
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    binding.paged_append(cache.pages, k, torch.zeros_like(k), offsets=off, max_new=n, cos=torch.from_numpy(cos).cuda(),
+                         sin=torch.from_numpy(sin).cuda(), positions=torch.arange(n, dtype=torch.int32, device="cuda"),
+                         interleaved=inter)
+    kx = plain.rotate(rows, cos, sin, inter)
+    want = plain.values(*plain.quantise(kx))
+    firsts = want[:, ::2] if inter else want[:, :64]
+    assert (firsts[:, np.arange(pairs) % 8 != 0] == 0).all()
+    assert np.array_equal(cache.rows_of(0, 0)[0], want)
+
+
 def test_tokens_one_by_one_leave_what_one_call_leaves():
     B, H, page, n = 3, 2, 16, 37
     gen = torch.Generator(device="cuda").manual_seed(3)
