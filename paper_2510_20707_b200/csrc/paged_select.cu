@@ -1,19 +1,21 @@
 // Which pages of the paged cache a query attends to (score and order: include/mixkv.h).
 //
-// Score.  Lane l holds dimensions 4 l .. 4 l + 3 of the pages' bounds; of q max(q, 0) and min(q, 0) lie in shared memory, so a
-// term is fma(max(q, 0), hi, min(q, 0) * lo): one of the two products is zero, the other exact (11 + 6 bits).  The sum over
-// neighbouring pairs is two additions inside the lane and five across lanes; these are done for 32 (page, query row)
+// Score.  Lane l holds dimensions 4 l .. 4 l + 3 of the pages' bounds; of q max(q, 0) and min(q, 0) lie in shared memory.  Of a term's
+// two products with them one is zero, the other exact (11 + 6 bits), so that two neighbouring terms and their sum are one product and
+// three multiply-adds, rounded once; dimensions 0, 1 and 2, 3 of a lane go in the halves of one instruction.  The next sum is
+// inside the lane, five are across lanes; these are done for 32 (page, query row)
 // pairs at a time, every exchange halving the number of sums a lane still holds (31 exchanges for 32 sums, not 160).
 //
 // A cluster has one (sequence, KV head): its warps score runs of pages, four at a time, the scores go as order-preserving
 // words into the first CTA's shared memory, and that CTA lists the `top` largest.
 //
-// What bounds it: instructions.  A (page, query row) pair costs a warp about 20: 8 multiply-adds, 3 additions, 4 of the exchanges, the
-// rest for the bounds' way in.  32 heads of 16001 to 65536 rows in pages of 32 (40 800 pages, seven query heads) 22 us, of
-// which listing 5; 8 heads of 131072 rows in pages of 64, four query heads, 11.  Clusters of long heads work while those of
-// short ones have ended; equal runs of pages of all heads in a kernel of their own, through memory, took 22.7 and 9.9, and 1 us
-// more where there are few pages.  Two dimensions to an instruction, query rows in registers, bounds asked for further
-// ahead: level or slower.
+// What bounds it: the longest head.  32 heads of 16001 to 65536 rows in pages of 32 (40 800 pages, seven query heads) take 21 us: 5 to
+// start, 14 to score the longest with four CTAs (512 pages a head 3.7 us, 3600 clocks a step of sixteen warps, instructions issued in
+// 70 % of them), 2 to find the threshold; the multiprocessors work for half of that time.  8 heads of 131072 rows in pages
+// of 64, four query heads: 11.  Equal runs of pages of all heads in a kernel of their own, through memory, took as long, and 1 us
+// more where there are few pages; clusters of eight CTAs with 256 threads 24, of 128 threads 33.  Lanes that choose between their
+// sums instead of taking the rows in their own order, and one dimension to an instruction: 22.5.  Query rows in registers, bounds asked
+// for further ahead, q without its parts (fewer reads of shared memory, more instructions): level or slower.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -47,19 +49,29 @@ __device__ __forceinline__ uint32_t key_of(float x) {   // larger scores have la
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
-// Sums of v[i] over all lanes, neighbouring lanes first; afterwards v[0] is that of i = lane's number with its bits reversed.
+// Sums of v[i] over all lanes, neighbouring lanes first; v[kPages * r + i] holds a term of page i and query row r ^ row_of(lane).
+// Every halving of the query rows keeps the lower half: what a lane gives there is its neighbour's.  Afterwards v[0] is that of
+// row_of(lane) and of the page whose bits are the lane's upper ones, reversed.
+template <int RP>
 __device__ __forceinline__ float sum_each(float (&v)[32], const int lane) {
 #pragma unroll
   for (int o = 1, n = 16; o < 32; o <<= 1, n >>= 1) {
-    const bool odd = lane & o;
+    if (o < RP) {
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      const float give = odd ? v[i] : v[i + n], keep = odd ? v[i + n] : v[i];
-      v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      for (int i = 0; i < n; ++i) v[i] = v[i] + __shfl_xor_sync(0xffffffffu, v[i + n], o);
+    } else {
+      const bool odd = lane & o;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float give = odd ? v[i] : v[i + n], keep = odd ? v[i + n] : v[i];
+        v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+      }
     }
   }
   return v[0];
 }
+template <int RP>
+__device__ __forceinline__ int row_of(const int lane) { return (int)(__brev(lane) >> 27) / (32 / RP); }
 
 // Sum of x over the CTA's threads before this one (exclusive); *total: of all.  sums: a word per warp.
 __device__ __forceinline__ uint32_t block_before(const uint32_t x, uint32_t* sums, uint32_t* total, const int lane, const int warp) {
@@ -87,7 +99,7 @@ template <int RP>
 __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, const int pages, const int begin, const int end,
                                           const float4* qs, uint32_t* keys) {
   constexpr int kPages = 32 / RP;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, mine = row_of<RP>(lane);
   // Bounds as they lie in memory, dimensions 4 lane .. + 3.  Of four pages at a time there is room for the next ones; eight are
   // asked for again where they were.
   constexpr int kSets = RP == 8 ? 2 : 1;
@@ -108,7 +120,7 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
   float4 up4[4], dn4[4];
   if constexpr (RP == 4) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) up4[r] = qs[r * 64 + lane], dn4[r] = qs[r * 64 + 32 + lane];
+    for (int r = 0; r < 4; ++r) up4[r] = qs[(r ^ mine) * 64 + lane], dn4[r] = qs[(r ^ mine) * 64 + 32 + lane];
   }
   for (int p0 = begin; p0 < end; p0 += kPages) {
     uint32_t best = 0;
@@ -122,43 +134,45 @@ __device__ __forceinline__ void score_run(const SelArgs& a, const int* table, co
 #pragma unroll 1
     for (int r0 = 0; r0 < padded_rows(a.R); r0 += RP) {
       float v[32];
-      auto term = [&](const float4& up, const float4& dn, const float (&l)[4], const float (&g)[4]) {
-        const float x0 = fmaf(up.x, g[0], __fmul_rn(dn.x, l[0])), x1 = fmaf(up.y, g[1], __fmul_rn(dn.y, l[1]));
-        const float x2 = fmaf(up.z, g[2], __fmul_rn(dn.z, l[2])), x3 = fmaf(up.w, g[3], __fmul_rn(dn.w, l[3]));
-        return __fadd_rn(__fadd_rn(x0, x1), __fadd_rn(x2, x3));
+      // neighbouring terms of dimensions 0 and 2, then 1 and 3
+      auto term = [&](const float4& up, const float4& dn, const f32x2 (&l)[2], const f32x2 (&g)[2]) {
+        f32x2 x = fma2(pack2(up.x, up.y), g[0], mul2(pack2(dn.x, dn.y), l[0]));
+        x = fma2(pack2(up.z, up.w), g[1], fma2(pack2(dn.z, dn.w), l[1], x));
+        float a, b;
+        unpack2(x, a, b);
+        return __fadd_rn(a, b);
       };
-      auto widen = [&](const uint2& w, float (&x)[4]) {
+      auto widen = [&](const uint2& w, f32x2 (&x)[2]) {
         const float2 p = widen2<__half>(w.x), q = widen2<__half>(w.y);
-        x[0] = p.x, x[1] = p.y, x[2] = q.x, x[3] = q.y;
+        x[0] = pack2(p.x, q.x), x[1] = pack2(p.y, q.y);
       };
       if constexpr (RP == 4) {     // the query rows stay in registers, a page is widened at a time
 #pragma unroll
         for (int i = 0; i < kPages; ++i) {
-          float l[4], g[4];
+          f32x2 l[2], g[2];
           widen(lo[0][i], l), widen(hi[0][i], g);
 #pragma unroll
-          for (int r = 0; r < RP; ++r) v[RP * i + r] = term(up4[r], dn4[r], l, g);
+          for (int r = 0; r < RP; ++r) v[kPages * r + i] = term(up4[r], dn4[r], l, g);
         }
       } else {     // four pages stay widened, a query row is read at a time (read again for every page they were 256 of 450 clocks)
-        float l[kPages][4], g[kPages][4];
+        f32x2 l[kPages][2], g[kPages][2];
 #pragma unroll
         for (int i = 0; i < kPages; ++i) widen(lo[0][i], l[i]), widen(hi[0][i], g[i]);
 #pragma unroll
         for (int r = 0; r < RP; ++r) {
-          const float4 up = qs[(r0 + r) * 64 + lane], dn = qs[(r0 + r) * 64 + 32 + lane];
+          const float4 up = qs[(r0 + (r ^ mine)) * 64 + lane], dn = qs[(r0 + (r ^ mine)) * 64 + 32 + lane];
 #pragma unroll
-          for (int i = 0; i < kPages; ++i) v[RP * i + r] = term(up, dn, l[i], g[i]);
+          for (int i = 0; i < kPages; ++i) v[kPages * r + i] = term(up, dn, l[i], g[i]);
         }
       }
       if (kSets == 1 && more) fetch(p0 + kPages, lo[0], hi[0]);      // (RP == 4: there is one round of query rows)
-      uint32_t k = key_of(sum_each(v, lane));
-      // the first lane bits (the first halvings) are the page's, the others the query row's
+      uint32_t k = key_of(sum_each<RP>(v, lane));
 #pragma unroll
-      for (int o = kPages; o < 32; o <<= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
+      for (int o = 1; o < RP; o <<= 1) k = max(k, __shfl_xor_sync(0xffffffffu, k, o));
       best = max(best, k);
     }
-    const int p = p0 + (int)(__brev(lane) >> (RP == 8 ? 30 : 29));
-    if (lane < kPages && p < end) keys[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
+    const int p = p0 + (int)(__brev(lane) >> 27) % kPages;
+    if (lane % RP == 0 && p < end) keys[p] = p < a.first || p >= pages - a.last ? kKeyForced : best;
   }
 }
 
@@ -169,7 +183,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   const int S = (int)cluster.num_blocks(), crank = (int)cluster.block_rank(), u = cluster_id();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
-  float4* qs = reinterpret_cast<float4*>(sm);                    // [R padded][2][32]: max(q, 0), min(q, 0)
+  float4* qs = reinterpret_cast<float4*>(sm);                    // [R padded][2][32]: max(q, 0), min(q, 0), dimensions 0, 2, 1, 3 of a lane
   uint32_t* keys = reinterpret_cast<uint32_t*>(qs + padded_rows(a.R) * 64);   // [pages], the first CTA's
   __shared__ uint32_t hist[kSelBins];
   __shared__ uint32_t sums[2][kSelWarps];
@@ -186,8 +200,8 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
     // (a NaN stays one in both parts)
     auto up = [](float z) { return z < 0.f ? 0.f : z; };
     auto down = [](float z) { return z > 0.f ? 0.f : z; };
-    qs[(e >> 5) * 64 + (e & 31)] = make_float4(up(x.x), up(x.y), up(y.x), up(y.y));
-    qs[(e >> 5) * 64 + 32 + (e & 31)] = make_float4(down(x.x), down(x.y), down(y.x), down(y.y));
+    qs[(e >> 5) * 64 + (e & 31)] = make_float4(up(x.x), up(y.x), up(x.y), up(y.y));
+    qs[(e >> 5) * 64 + 32 + (e & 31)] = make_float4(down(x.x), down(y.x), down(x.y), down(y.y));
   }
   int n = min(a.p.rows[u], a.max_rows);
   n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
