@@ -403,7 +403,6 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
     if (warp == 0) *abort = 0;
   }
   __syncthreads();
-  pdl_launch_dependents();
   pdl_wait();
 
   // steps lo .. hi - 1: of a cluster's unit, or of all units one after the other
@@ -524,6 +523,7 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
     }
     if (lost && lane == 0) drain_ring(bar, kAttDepth, sent);
 
+    pdl_launch_dependents();      // (the next kernel's CTAs, where this one's have ended)
     // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others
     float* own = sums + warp * kSums;
 #pragma unroll

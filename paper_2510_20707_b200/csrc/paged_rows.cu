@@ -1,15 +1,19 @@
 // Rows into the paged 4-bit cache and back (format and rounding: include/mixkv.h).
 //
-// One CTA has one page of one head, so a page's bounds have one owner and need no atomics.  A warp takes four rows at a
-// time, eight lanes each, a lane one block of 16 dimensions: the largest magnitude, the scale and the codes of a block are
-// one lane's (32 bytes in, 8 out).  The rotation's partner dimensions lie rot_dim / 2 on, in another lane's registers.
-// (Two rows at a time, half a block per lane and K and V in warps of their own took 262 instructions a row instead of
-// 150, and half of the warps waited for the others.)
+// A page of one head is one CTA's, or one warp's, so that its bounds have one owner and need no atomics.  A warp takes four rows at
+// a time, eight lanes each, a lane 16 dimensions of V and of K: the largest magnitude, the scale and the codes of a block are one
+// lane's.  Of K that is turned in pairs (i, i + rot_dim / 2) a lane has eight dimensions of either side instead, and the largest magnitudes
+// are exchanged between the two lanes of two blocks; with a block per lane and the partner's dimensions fetched from it, every lane
+// loaded the angles of sixteen pairs, and a call took 13 us longer than one without a rotation, where it takes 5.
+// (Two rows at a time, half a block per lane and K and V in warps of their own took 262 instructions a row instead of 115, and half
+// of the warps waited for the others.)
 //
-// What bounds it.  Append: latencies and instructions together; 4 x 32768 rows (67 MB in, 19 out) take 39 us, 2.2 TB/s, an
-// instruction in 49 % of the clocks with sixteen warps an SM, and as long with twelve.  The cosines and sines are on their way while V is
-// rounded.  Divisors and reciprocals of the 127 scales come from a table that a CTA fills once.  Reading back: 16 us (19 MB in, 67
-// out), 5.4 TB/s; with 16-byte stores 20.
+// What bounds it.  Append: latencies.  4 x 32768 rows in pages of 64 (67 MB in, 17 of angles, 19 out) take 27 us, 3.8 TB/s.  A step of
+// a warp that has its SM for itself takes 0.8 us, a chain of about 1400 clocks (load, largest magnitude, scale, divisor, quotient, codes,
+// 115 instructions a row); sixteen warps an SM, as registers allow, are in each other's way half of the time.  The angles come by
+// asynchronous copies a step ahead, the positions two (31 us with loads while V is rounded).  All of a row by such copies, three
+// steps ahead: 30; twenty warps with 96 registers: 32.  Divisors and reciprocals of the 127 scales come from a table that a CTA fills
+// once.  Reading back: 16 us (19 MB in, 67 out), 5.4 TB/s; with 16-byte stores 20.
 #include "paged.cuh"
 
 namespace mixkv {
@@ -17,6 +21,7 @@ namespace {
 
 constexpr int kRowThreads = 256;   // of a CTA that reads many rows of a page; one row per head: 64
 constexpr int kAppThreads = 128, kAppPerSm = 4;   // of a CTA that may get many rows, and such CTAs per SM
+constexpr int kAppAlone = 8;       // pages per SM above which a warp has a page alone (append_as)
 
 struct RowArgs {
   PagePool p;
@@ -42,9 +47,10 @@ struct PageSpan {
 };
 __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) {
   PageSpan s;
-  s.u = a.by_slots.div(task);
-  const int slot = task - s.u * a.slots, b = a.p.by_heads.div(s.u);
-  s.h = s.u - b * a.p.H;
+  // heads of a token next to one another: they are in memory, and they are turned by the same angles
+  const int at = a.p.by_heads.div(task), b = a.by_slots.div(at), slot = at - b * a.slots;
+  s.h = task - at * a.p.H;
+  s.u = b * a.p.H + s.h;
   const int rows = fresh(a.p.rows + s.u);
   int n = 1;
   long long first = b;
@@ -84,57 +90,59 @@ __device__ __forceinline__ void fill_divisors(float2* table, const float third) 
   }
 }
 
-// A block of 16 values -> its codes, and *scale.
-//
-// x / d is rounded to nearest by Markstein's correction of x times the rounded reciprocal: the remainder of that first quotient is
-// exact, and one step with it rounds correctly while nothing over- or underflows.  Blocks of infinities and of extreme scales
-// are divided.  (A code of zero has either sign.)
-__device__ __forceinline__ uint2 quantise16(const f32x2 (&x)[8], const float inv6, const float2* divisors, uint32_t* scale) {
+// Largest magnitude of eight values.
+__device__ __forceinline__ float largest8(const f32x2* x) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
     float a, b;
     unpack2(x[i], a, b);
     m = max3_nan(m, fabsf(a), fabsf(b));
   }
+  return m;
+}
+// Scale byte of a block whose largest magnitude is m; inv6: 1 / (6 k_scale).
+__device__ __forceinline__ uint32_t scale_of(const float m, const float inv6) {
   unsigned short s;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(0.f), "f"(__fmul_rn(m, inv6)));
-  *scale = s & 0x7fu;
-  const float2 div = divisors[s & 0x7fu];
+  return s & 0x7fu;
+}
+// Codes of eight values of a block.  div: its divisor and the rounded reciprocal; divide: by division.
+//
+// x / d is rounded to nearest by Markstein's correction of x times the rounded reciprocal: the remainder of that first quotient is
+// exact, and one step with it rounds correctly while nothing over- or underflows.  Blocks of infinities and of extreme scales
+// (unsafe) are divided.  (A code of zero has either sign.)
+__device__ __forceinline__ bool unsafe(const float m, const float2 div) { return !(m < 1e30f && div.x > 1e-30f); }   // (NaN, and d == 0, too)
+template <bool DIVIDE>
+__device__ __forceinline__ uint32_t codes8(const f32x2* x, const float2 div) {
   const f32x2 by = pack2(div.y, div.y), d = pack2(-div.x, -div.x);
-  f32x2 q[8];
+  f32x2 q[4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const f32x2 first = mul2(x[i], by);
-    q[i] = fma2(fma2(first, d, x[i]), by, first);
-  }
-  if (!(m < 1e30f && div.x > 1e-30f)) {     // (NaN, and d == 0, too)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DIVIDE) {
       float a, b;
       unpack2(x[i], a, b);
       q[i] = div.x == 0.f ? 0ull : pack2(__fdiv_rn(a, div.x), __fdiv_rn(b, div.x));
+    } else {
+      const f32x2 first = mul2(x[i], by);
+      q[i] = fma2(fma2(first, d, x[i]), by, first);
     }
   }
-  uint32_t w[2];
+  // (joined by byte moves: with the four bytes packed by one move, the two upper ones came out wrong where the codes are widened
+  // again for the bounds)
+  uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) unpack2(q[4 * i + e], v[2 * e], v[2 * e + 1]);
-    // (packed by shifts: with the four bytes packed by one move, the two upper ones came out wrong where the codes are widened
-    // again for the bounds)
-    w[i] = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t c;
-      asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}"
-          : "=r"(c)
-          : "f"(v[2 * e + 1]), "f"(v[2 * e]));
-      w[i] |= c << (8 * e);
-    }
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack2(q[i], a, b);
+    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u32.u8 %0, t;\n\t}" : "=r"(c[i]) : "f"(b), "f"(a));
   }
-  return make_uint2(w[0], w[1]);
+  return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
+}
+// Codes of sixteen values, eight of a block with largest magnitude ma and divisor da, eight of one with mb and db.
+__device__ __forceinline__ uint2 codes16(const f32x2 (&x)[8], const float ma, const float2 da, const float mb, const float2 db) {
+  if (unsafe(ma, da) || unsafe(mb, db)) return make_uint2(codes8<true>(x, da), codes8<true>(x + 4, db));
+  return make_uint2(codes8<false>(x, da), codes8<false>(x + 4, db));
 }
 
 // Where the codes and the scale of block g of row r lie inside a tile.
@@ -148,6 +156,7 @@ __device__ __forceinline__ int k_scale_at(const int r, const int g) {
   return kTileKs + 16 * ((r >> 2) * 2 + (r & 1)) + 4 * (g >> 1) + 2 * ((r >> 1) & 1) + (g & 1);
 }
 __device__ __forceinline__ int v_scale_at(const int r, const int g) { return kTileVs + 16 * g + r; }
+constexpr int kKCodesFour = 128, kVCodesFour = 16, kKScalesFour = 32, kVScalesFour = 4;     // from row r to row r + 4
 
 struct Raw16 {   // 16 values of 16 bits
   uint4 a, b;
@@ -155,15 +164,21 @@ struct Raw16 {   // 16 values of 16 bits
 __device__ __forceinline__ uint32_t word16(const Raw16& r, const int i) {
   return i == 0 ? r.a.x : i == 1 ? r.a.y : i == 2 ? r.a.z : i == 3 ? r.a.w : i == 4 ? r.b.x : i == 5 ? r.b.y : i == 6 ? r.b.z : r.b.w;
 }
+// (Without a row the registers keep what they have: nothing of it is written.)
 template <typename T>
-__device__ __forceinline__ Raw16 load16(const T* src, const bool on) {
-  Raw16 r = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-  if (on)
-    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-        : "=r"(r.a.x), "=r"(r.a.y), "=r"(r.a.z), "=r"(r.a.w), "=r"(r.b.x), "=r"(r.b.y), "=r"(r.b.z), "=r"(r.b.w)
-        : "l"(src)
-        : "memory");
-  return r;
+__device__ __forceinline__ void load16(Raw16& r, const T* src, const bool on) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %9, 0;\n\t@p ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
+      : "+r"(r.a.x), "+r"(r.a.y), "+r"(r.a.z), "+r"(r.a.w), "+r"(r.b.x), "+r"(r.b.y), "+r"(r.b.z), "+r"(r.b.w)
+      : "l"(src), "r"((uint32_t)on)
+      : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void load8x2(Raw16& r, const T* a, const T* b, const bool on) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %10, 0;\n\t@p ld.global.v4.b32 {%0, %1, %2, %3}, [%8];\n\t"
+      "@p ld.global.v4.b32 {%4, %5, %6, %7}, [%9];\n\t}"
+      : "+r"(r.a.x), "+r"(r.a.y), "+r"(r.a.z), "+r"(r.a.w), "+r"(r.b.x), "+r"(r.b.y), "+r"(r.b.z), "+r"(r.b.w)
+      : "l"(a), "l"(b), "r"((uint32_t)on)
+      : "memory");
 }
 template <typename T>
 __device__ __forceinline__ f32x2 wide2(const uint32_t w) {
@@ -173,53 +188,60 @@ __device__ __forceinline__ f32x2 wide2(const uint32_t w) {
 template <>
 __device__ __forceinline__ f32x2 wide2<__nv_bfloat16>(const uint32_t w) { return bf16x2_wide(w); }
 
-// What a lane's block g is rotated by: cosines and sines of its pairs (ROPE 2: eight of each), from the token's row of the tables.
-// ROPE 1: pairs (i, i + rot / 2), 2: (2 i, 2 i + 1).
-template <int ROPE>
-struct Turn {
-  float4 cs[ROPE == 1 ? 4 : 2], sn[ROPE == 1 ? 4 : 2];
+// What lane g of a row has of K: eight dimensions from a on (x), eight from b on (y).  Pairs (i, i + rot / 2) lie in two blocks, and the
+// two lanes of these blocks have eight pairs each (so neither needs the other's dimensions, nor the same cosines); else a lane
+// has a block.
+struct Eights {
+  int a, b;
+  bool split;
 };
 template <int ROPE>
-__device__ __forceinline__ Turn<ROPE> load_turn(const RowArgs& a, const int pos, const int g) {
-  Turn<ROPE> t;
-  const int half = a.rot >> 1;
-  const int at = ROPE == 2 ? 8 * g : 16 * g < half ? 16 * g : 16 * g - half;
-  const long long from = (long long)pos * half + (16 * g < a.rot ? at : 0);
-#pragma unroll
-  for (int i = 0; i < (ROPE == 1 ? 4 : 2); ++i)
-    t.cs[i] = fresh(reinterpret_cast<const float4*>(a.cosv + from) + i), t.sn[i] = fresh(reinterpret_cast<const float4*>(a.sinv + from) + i);
-  return t;
+__device__ __forceinline__ Eights eights_of(const int g, const int rot) {
+  const int half = rot >> 1;
+  if (ROPE != 1 || 16 * g >= rot) return Eights{16 * g, 16 * g + 8, false};
+  return 16 * g < half ? Eights{16 * g, 16 * g + half, true} : Eights{16 * g + 8 - half, 16 * g + 8, true};
 }
+// Cosines and sines of a lane's eight pairs, ROPE 1: (i, i + rot / 2), 2: (2 i, 2 i + 1), from the token's row of the tables; a lane
+// copies 16-byte pieces for itself (piece i at i * blockDim.x), and waits for all but its last group of them.
+__device__ __forceinline__ void ask_turn(const RowArgs& a, uint4* to, const int pos, const int at, const bool on) {
+  if (on) {
+    const long long from = (long long)pos * (a.rot >> 1) + at;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to + i * blockDim.x)),
+                   "l"((i < 2 ? a.cosv : a.sinv) + from + 4 * (i & 1))
+                   : "memory");
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void wait_turn() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
-// a + b in halves: of a packed sum and the packed products before it, .rn or not, the compiler makes multiply-adds.
+// a + b and a - b in halves: of a packed sum and the packed products before it, .rn or not, the compiler makes multiply-adds.
 __device__ __forceinline__ f32x2 add_rounded(const f32x2 a, const f32x2 b) {
   float ax, ay, bx, by;
   unpack2(a, ax, ay), unpack2(b, bx, by);
   return pack2(__fadd_rn(ax, bx), __fadd_rn(ay, by));
 }
-// The rotation; products and sums are rounded one by one.  All lanes of the warp take part.
-template <typename T, int ROPE>
-__device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const int g, const int rot, const Turn<ROPE>& turn) {
-  const int half = rot >> 1, lane = threadIdx.x & 31;
-  const bool inside = 16 * g < rot;
-  if constexpr (ROPE == 1) {
-    const bool low = 16 * g < half;
-    const int from = !inside ? lane : low ? lane + (half >> 4) : lane - (half >> 4);
-    const uint32_t flip = low ? 0x80008000u : 0u;     // x cos - y sin is x cos + (-y) sin
-    uint32_t y[8];
+__device__ __forceinline__ f32x2 sub_rounded(const f32x2 a, const f32x2 b) {
+  float ax, ay, bx, by;
+  unpack2(a, ax, ay), unpack2(b, bx, by);
+  return pack2(__fsub_rn(ax, bx), __fsub_rn(ay, by));
+}
+// The rotation of a lane's eight pairs by the pieces at `turn`; products and sums are rounded one by one.
+template <int ROPE>
+__device__ __forceinline__ void rotate8(f32x2 (&x)[8], const float4* turn) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __shfl_sync(0xffffffffu, word16(raw, i), from) ^ flip;
-    if (!inside) return;
+  for (int i = 0; i < 2; ++i) {
+    const float4 cs = turn[i * blockDim.x], sn = turn[(2 + i) * blockDim.x];
+    if constexpr (ROPE == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 cs = turn.cs[i], sn = turn.sn[i];
-      x[2 * i] = add_rounded(mul2(x[2 * i], pack2(cs.x, cs.y)), mul2(wide2<T>(y[2 * i]), pack2(sn.x, sn.y)));
-      x[2 * i + 1] = add_rounded(mul2(x[2 * i + 1], pack2(cs.z, cs.w)), mul2(wide2<T>(y[2 * i + 1]), pack2(sn.z, sn.w)));
-    }
-  } else if (ROPE == 2 && inside) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float4 cs = turn.cs[i], sn = turn.sn[i];
+      for (int e = 0; e < 2; ++e) {
+        const f32x2 c = e ? pack2(cs.z, cs.w) : pack2(cs.x, cs.y), s = e ? pack2(sn.z, sn.w) : pack2(sn.x, sn.y);
+        const f32x2 u = x[2 * i + e], w = x[4 + 2 * i + e];
+        x[2 * i + e] = sub_rounded(mul2(u, c), mul2(w, s));
+        x[4 + 2 * i + e] = add_rounded(mul2(w, c), mul2(u, s));
+      }
+    } else {
       const float cc[4] = {cs.x, cs.y, cs.z, cs.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -231,121 +253,161 @@ __device__ __forceinline__ void rotate16(const Raw16& raw, f32x2 (&x)[8], const 
   }
 }
 
-// A CTA of two warps has one page, K and V of one row each; one of four warps has a run of pages (of a head mostly: what the next
-// page needs of the tables is in L1), every warp both.
+// A CTA of two warps has one page, K and V of one row each.  Of four warps each has a page (alone), or all have one; every warp both
+// K and V.
 template <typename T, int ROPE>
 __global__ void __launch_bounds__(kAppThreads, kAppPerSm)
-k_paged_append(const RowArgs a, const T* k, const T* v, const int tasks, const int run) {
+k_paged_append(const RowArgs a, const T* k, const T* v, const int tasks, const bool alone) {
+  extern __shared__ __align__(16) uint4 turns[];      // what K's next two rows (the one row) are turned by
   __shared__ float2 divisors[2][128];
   __shared__ __half2 part[kAppThreads / 32][8][17];   // of every warp: minima and maxima of a block's eight pairs of dimensions
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane & 7, sub = lane >> 3;
   fill_divisors(divisors[0], a.p.k_scale);
   fill_divisors(divisors[1], a.p.v_scale);
-  pdl_launch_dependents();
   pdl_wait();
   const bool single = blockDim.x == 64;
-  const int step = single ? 4 : 4 * (blockDim.x >> 5);
+  const int team = single || alone ? 1 : blockDim.x >> 5, step = 4 * team;     // warps that share the page's rows
   const bool does_k = !single || warp == 0, does_v = !single || warp == 1;
   __syncthreads();
+  const int task = alone ? blockIdx.x * (kAppThreads / 32) + warp : blockIdx.x;
+  if (task >= tasks) return;      // (a warp that is alone)
   const float k6 = (float)(1.0 / (6.0 * (double)a.p.k_scale)), v6 = (float)(1.0 / (6.0 * (double)a.p.v_scale));
-  bool bad = false;
-  const int end = min((int)(blockIdx.x + 1) * run, tasks);
-  for (int task = blockIdx.x * run; task < end; ++task) {
-    const PageSpan s = page_span(a, task);
-    const T* kr = k + (a.per_head ? 0 : s.h * a.k_head) + s.token * a.k_row + 16 * g;     // row r of the page at r * stride
-    const T* vr = v + (a.per_head ? 0 : s.h * a.v_head) + s.token * a.v_row + 16 * g;
-    const int* positions = a.positions + s.token;
-    const bool placed = s.id >= 0 && s.id < a.p.num_pages;
-    bad |= s.bad || (s.lo < s.hi && !placed);
-    __half2 lo[8], hi[8];
+  const Eights own = eights_of<ROPE>(g, a.rot);
+  const bool inside = ROPE && 16 * g < a.rot;
+  const int partner = !own.split ? lane : own.a == 16 * g ? lane + (a.rot >> 5) : lane - (a.rot >> 5);
+  const PageSpan s = page_span(a, task);
+  const bool placed = s.id >= 0 && s.id < a.p.num_pages;
+  bool bad = s.bad || (s.lo < s.hi && !placed);
+  __half2 lo[8], hi[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) lo[i] = __float2half2_rn(INFINITY), hi[i] = __float2half2_rn(-INFINITY);
+  for (int i = 0; i < 8; ++i) lo[i] = __float2half2_rn(INFINITY), hi[i] = __float2half2_rn(-INFINITY);
 
-    int r = s.lo + (single ? 0 : 4 * warp) + sub;
-    bool on = r >= s.first && r < s.last;
-    Raw16 kk = load16(kr + r * a.k_row, on && does_k), vv = load16(vr + r * a.v_row, on && does_v);
-    int pos = ROPE && on ? fresh(positions + r) : 0;
-    for (; r - sub < s.hi; r += step) {
-      const Raw16 kx = kk, vx = vv;
-      const int at = pos;
-      const bool have = on;
-      if (r - sub + step < s.hi) {      // the next rows on their way
-        const int next = r + step;
-        on = next >= s.first && next < s.last;
-        kk = load16(kr + next * a.k_row, on && does_k), vv = load16(vr + next * a.v_row, on && does_v);
-        pos = ROPE && on ? fresh(positions + next) : 0;
+  int r = s.lo + (team == 1 ? 0 : 4 * warp) + sub;
+  bool on = r >= s.first && r < s.last;
+  // (row r of the page is row s.token + r of the input)
+  const T* kr = k + (a.per_head ? 0 : s.h * a.k_head) + (s.token + r) * a.k_row + own.a;
+  const T* vr = v + (a.per_head ? 0 : s.h * a.v_head) + (s.token + r) * a.v_row + 16 * g;
+  const int* positions = a.positions + (s.token + r);
+  Raw16 kk = {}, vv = {};
+  auto load_k = [&](const bool on) {
+    if constexpr (ROPE == 1) load8x2(kk, kr, kr + (own.b - own.a), on);
+    else load16(kk, kr, on);
+  };
+  load_k(on && does_k), load16(vv, vr, on && does_v);
+  // a row's angles are on their way while the row before it is rounded, its position while the one before that is
+  bool turned = true;
+  int pos = 0, odd = 0;
+  if constexpr (ROPE != 0) {
+    const int now = on ? fresh(positions) : 0;
+    positions += step;
+    pos = r + step >= s.first && r + step < s.last ? fresh(positions) : 0;
+    turned = now >= 0 && now < a.table_len;
+    ask_turn(a, turns + tid, now, ROPE == 1 ? own.a : 8 * g, on && does_k && inside && turned);
+  }
+  // places of the lane's rows in a tile: those of row r % 4, and the same further on for every four rows
+  unsigned char* const page = tile_ptr(a.p, placed ? s.id : 0, 0);
+  const int k_at = k_codes_at(r & 3, ROPE == 1 ? 0 : g), v_at = v_codes_at(r & 3, g);
+  const int ks_at = k_scale_at(r & 3, g), vs_at = v_scale_at(r & 3, g);
+  for (; r - sub < s.hi; r += step) {
+    const int next = r + step;
+    const bool write = on && placed && turned;      // (a token is written whole or not at all)
+    on = next >= s.first && next < s.last;
+    kr += step * a.k_row, vr += step * a.v_row;
+    if constexpr (ROPE != 0) {
+      turned = pos >= 0 && pos < a.table_len;
+      ask_turn(a, turns + (odd ^ 1) * 4 * blockDim.x + tid, pos, ROPE == 1 ? own.a : 8 * g, on && does_k && inside && turned);
+      positions += step;
+      if (next + step >= s.first && next + step < s.last) pos = fresh(positions);
+    }
+    bad |= r < s.hi && !write;
+    unsigned char* tile = page + (r / kPageTile) * kTileBytes;
+    const int four = (r % kPageTile) >> 2;
+    if (does_v) {
+      f32x2 x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(vv, i));
+      load16(vv, vr, on);      // the next row on its way
+      const float m = max3_nan(largest8(x), largest8(x + 4), 0.f);
+      const uint32_t scale = scale_of(m, v6);
+      const float2 div = divisors[1][scale];
+      const uint2 w = codes16(x, m, div, m, div);
+      if (write) {
+        *reinterpret_cast<uint2*>(tile + v_at + kVCodesFour * four) = w;
+        tile[vs_at + kVScalesFour * four] = (unsigned char)scale;
       }
-      const bool turned = at >= 0 && at < a.table_len;
-      const bool write = have && placed && (!ROPE || turned);      // (a token is written whole or not at all)
-      bad |= r < s.hi && !write;
-      unsigned char* tile = tile_ptr(a.p, placed ? s.id : 0, r / kPageTile);
-      const int rt = r % kPageTile;
-      Turn<ROPE> turn;      // (on its way while V is rounded)
-      if (ROPE && does_k) turn = load_turn<ROPE>(a, turned ? at : 0, g);
-      if (does_v) {
-        f32x2 x[8];
+    }
+    if (does_k) {
+      f32x2 x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(vx, i));
-        uint32_t scale;
-        const uint2 w = quantise16(x, v6, divisors[1], &scale);
-        if (write) {
-          *reinterpret_cast<uint2*>(tile + v_codes_at(rt, g)) = w;
-          tile[v_scale_at(rt, g)] = (unsigned char)scale;
-        }
+      for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(kk, i));
+      load_k(on);
+      if constexpr (ROPE != 0) {
+        wait_turn();
+        if (inside) rotate8<ROPE>(x, reinterpret_cast<const float4*>(turns + odd * 4 * blockDim.x + tid));
+        odd ^= 1;
       }
-      if (does_k) {
-        f32x2 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = wide2<T>(word16(kx, i));
-        if constexpr (ROPE != 0) {
-          rotate16<T, ROPE>(kx, x, g, a.rot, turn);
+      // of the two blocks that the lane has a part of (one and the same, if they are not split)
+      float ma = largest8(x), mb = largest8(x + 4);
+      if constexpr (ROPE == 1) {
+        const float oa = __shfl_sync(0xffffffffu, ma, partner), ob = __shfl_sync(0xffffffffu, mb, partner);
+        ma = max3_nan(ma, own.split ? oa : ob, 0.f), mb = max3_nan(mb, own.split ? ob : oa, 0.f);
+      } else {
+        ma = mb = max3_nan(ma, mb, 0.f);
+      }
+      const uint32_t sa = scale_of(ma, k6), sb = ROPE == 1 ? scale_of(mb, k6) : sa;
+      const uint2 w = codes16(x, ma, divisors[0][sa], mb, divisors[0][sb]);
+      if (write) {
+        unsigned char* codes = tile + k_at + kKCodesFour * four;
+        if constexpr (ROPE == 1) {
+          *reinterpret_cast<uint32_t*>(codes + own.a / 2) = w.x, *reinterpret_cast<uint32_t*>(codes + own.b / 2) = w.y;
+        } else {
+          *reinterpret_cast<uint2*>(codes) = w;
         }
-        uint32_t scale;
-        const uint2 w = quantise16(x, k6, divisors[0], &scale);
-        if (write) {
-          *reinterpret_cast<uint2*>(tile + k_codes_at(rt, g)) = w;
-          tile[k_scale_at(rt, g)] = (unsigned char)scale;
-          if (a.p.bounds) {
-            uint32_t f[8];
-            codes_to_f16(w.x, *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
-            codes_to_f16(w.y, *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
-            const uint32_t ss = scales_to_f16(scale | scale << 8);
+        tile[ks_at + kKScalesFour * four] = (unsigned char)(own.a >> 4 == g ? sa : sb);
+        if (a.p.bounds) {
+          uint32_t f[8];
+          codes_to_f16(w.x, *reinterpret_cast<uint32_t(*)[4]>(&f[0]));
+          codes_to_f16(w.y, *reinterpret_cast<uint32_t(*)[4]>(&f[4]));
+          const uint32_t fa = scales_to_f16(sa | sa << 8), fb = ROPE == 1 ? scales_to_f16(sb | sb << 8) : fa;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t y = mul_f16x2(f[i], ss);
-              lo[i] = __hmin2_nan(lo[i], *reinterpret_cast<const __half2*>(&y));
-              hi[i] = __hmax2_nan(hi[i], *reinterpret_cast<const __half2*>(&y));
-            }
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t y = mul_f16x2(f[i], i < 4 ? fa : fb);
+            lo[i] = __hmin2_nan(lo[i], *reinterpret_cast<const __half2*>(&y));
+            hi[i] = __hmax2_nan(hi[i], *reinterpret_cast<const __half2*>(&y));
           }
         }
       }
     }
-    if (!a.p.bounds || !placed || s.lo >= s.hi) continue;
-    if (does_k) {
+  }
+  pdl_launch_dependents();      // (sooner, its CTAs would crowd the few multiprocessors that this one leaves free)
+  if (bad && a.status) *a.status = MIXKV_ERR_INVALID_ARG;
+  if (!a.p.bounds || !placed || s.lo >= s.hi) return;      // (all that share a page)
+  if (does_k) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int o = 8; o < 32; o <<= 1) {
-          lo[i] = __hmin2_nan(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
-          hi[i] = __hmax2_nan(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
-        }
-        if (sub == 0) part[warp][g][i] = lo[i], part[warp][g][8 + i] = hi[i];
+      for (int o = 8; o < 32; o <<= 1) {
+        lo[i] = __hmin2_nan(lo[i], __shfl_xor_sync(0xffffffffu, lo[i], o));
+        hi[i] = __hmax2_nan(hi[i], __shfl_xor_sync(0xffffffffu, hi[i], o));
+      }
+      if (sub == 0) {
+        const int d = (i < 4 ? own.a : own.b) + 2 * (i & 3);
+        part[warp][d >> 4][(d & 15) >> 1] = lo[i], part[warp][d >> 4][8 + ((d & 15) >> 1)] = hi[i];
       }
     }
-    __syncthreads();
-    const int warps = single ? 1 : min((int)(blockDim.x >> 5), (s.hi - s.lo + 3) / 4);    // those that had rows
-    for (int e = tid; e < 128; e += blockDim.x) {
-      const bool most = e & 64;
-      const int block = (e & 63) >> 3, i = (most ? 8 : 0) + (e & 7);
-      __half2 x = part[0][block][i];
-      for (int w = 1; w < warps; ++w) x = most ? __hmax2_nan(x, part[w][block][i]) : __hmin2_nan(x, part[w][block][i]);
-      __half2* out = reinterpret_cast<__half2*>(a.p.bounds + ((long long)s.id * 2 + most) * kHeadDim) + (e & 63);
-      if (s.lo > 0) x = most ? __hmax2_nan(x, *out) : __hmin2_nan(x, *out);
-      *out = x;
-    }
-    if (task + 1 < end) __syncthreads();    // `part` is written again
   }
-  if (bad && a.status) *a.status = MIXKV_ERR_INVALID_ARG;
+  if (alone) __syncwarp();
+  else __syncthreads();
+  const int first = alone ? warp : 0, warps = team == 1 ? 1 : min(team, (s.hi - s.lo + 3) / 4);    // those that had rows
+  for (int e = alone ? lane : tid; e < 128; e += alone ? 32 : blockDim.x) {
+    const bool most = e & 64;
+    const int block = (e & 63) >> 3, i = (most ? 8 : 0) + (e & 7);
+    __half2 x = part[first][block][i];
+    for (int w = 1; w < warps; ++w) x = most ? __hmax2_nan(x, part[w][block][i]) : __hmin2_nan(x, part[w][block][i]);
+    __half2* out = reinterpret_cast<__half2*>(a.p.bounds + ((long long)s.id * 2 + most) * kHeadDim) + (e & 63);
+    if (s.lo > 0) x = most ? __hmax2_nan(x, *out) : __hmin2_nan(x, *out);
+    *out = x;
+  }
 }
 
 // A lane has a block of a row, as above.
@@ -414,14 +476,17 @@ template <typename T>
 int append_as(const mixkv_pages* c, const RowArgs& a, const void* k, const void* v, const int rope, void* stream) {
   const int rc = device_check(nullptr);
   if (rc != MIXKV_OK) return rc;
-  void (*kernel)(RowArgs, const T*, const T*, int, int) =
+  void (*kernel)(RowArgs, const T*, const T*, int, bool) =
       rope == 0 ? k_paged_append<T, 0> : rope == 1 ? k_paged_append<T, 1> : k_paged_append<T, 2>;
-  // Two pages to a CTA: one leaves the tables it fills first to be filled more often, an equal share of a whole wave (four and
-  // eight pages here) lets it wait for the last.  4 x 32768 rows in pages of 64 55.6 / 55.2 / 54.7 us on one, two and four
-  // pages (append and read back), 8 ragged chunks in pages of 32 45.4 / 43.4 / 48.8.
-  const int tasks = tasks_of(c, a), run = tasks > kAppPerSm * device_sm_count() ? 2 : 1;
-  return launch_pdl(kernel, dim3((unsigned)((tasks + run - 1) / run)), dim3(a.max_new > 1 ? kAppThreads : 64), 0,
-                    (cudaStream_t)stream, 1, a, static_cast<const T*>(k), static_cast<const T*>(v), tasks, run) == cudaSuccess
+  // A page to a warp or to four: four end a page sooner, but a page begins with a chain of loads (rows, table, first rows), which four
+  // times as many CTAs go through.  Pages of 64 rows, us: 512 pages 18.3 alone / 9.9 by four, 1024 20.5 / 18.2, 2048 27.1 / 33.4; of 16
+  // rows: 512 7.3 / 5.6, 1024 8.1 / 9.8, 2048 10.1 / 17.6.  (CTAs of one or two such warps: level.)
+  const int tasks = tasks_of(c, a);
+  const bool many = a.max_new > 1, alone = many && tasks > kAppAlone * device_sm_count();
+  const int threads = many ? kAppThreads : 64;
+  return launch_pdl(kernel, dim3((unsigned)(alone ? (tasks + kAppThreads / 32 - 1) / (kAppThreads / 32) : tasks)),
+                    dim3(threads), rope == 0 ? 0 : (many ? 2 : 1) * 64 * threads, (cudaStream_t)stream, 1, a,
+                    static_cast<const T*>(k), static_cast<const T*>(v), tasks, alone) == cudaSuccess
              ? MIXKV_OK
              : MIXKV_ERR_CUDA;
 }

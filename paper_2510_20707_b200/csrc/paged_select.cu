@@ -188,7 +188,6 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   __shared__ uint32_t hist[kSelBins];
   __shared__ uint32_t sums[2][kSelWarps];
   __shared__ uint32_t found[2];
-  pdl_launch_dependents();
   pdl_wait();
   for (int e = tid; e < padded_rows(a.R) * 32; e += kSelThreads) {
     const int r = min(e >> 5, a.R - 1);      // (the rows of the padding repeat the last: a maximum does not mind)
@@ -218,6 +217,8 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   }
   if (S > 1) cluster.sync();
   else __syncthreads();
+  // (the next kernel's CTAs come now, spread over the GPU: at the start they would have crowded the multiprocessors without a cluster)
+  pdl_launch_dependents();
   if (crank) return;
 
   // The `top`-th largest word: keys between `low` and `high` are counted in bins, the bin that holds it is taken apart next, until
