@@ -413,10 +413,10 @@ k_paged_append(const RowArgs a, const T* k, const T* v, const int tasks, const b
 // A lane has a block of a row, as above.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) k_paged_read(const RowArgs a, T* k, T* v) {
-  pdl_launch_dependents();
   pdl_wait();
   const PageSpan s = page_span(a, blockIdx.x);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane & 7, sub = lane >> 3;
+  pdl_launch_dependents();      // (not sooner: as above)
   if (s.id < 0 || s.id >= a.p.num_pages) return;
   const bool keys = (warp & 1) == 0;
   const float third = keys ? a.p.k_scale : a.p.v_scale;
