@@ -153,6 +153,38 @@ def test_products_of_the_rotation_are_rounded_before_their_sum(dtype, inter):
     assert np.array_equal(cache.rows_of(0, 0)[0], want)
 
 
+@pytest.mark.parametrize("dtype,page,rot,inter", [
+    ("bf16", 16, 128, False), ("fp16", 16, 64, False), ("bf16", 16, 32, True), ("fp16", 32, 0, False), ("bf16", 32, 96, False)])
+def test_many_pages_in_one_call_leave_what_few_at_a_time_leave(dtype, page, rot, inter):
+    # more pages than a GPU has warps' groups for: a warp has a page alone; a piece of a hundred rows is shared by four
+    B, H, n, piece = 3, 4, 2105 * page // 16, 100
+    old = np.arange(B * H).reshape(B, H) * 7 % 40
+    gen = torch.Generator(device="cuda").manual_seed(page + rot)
+    k, v = (torch.randn((B, n, H, 128), generator=gen, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    k[1, 77], v[2, 5, 1, 16:32] = 0.0, 0.0          # blocks of zeros
+    k[0, 1000, 2, 40], v[0, 13, 3, 3] = float("inf"), float("nan")
+    pos = torch.randint(0, 3000, (B, n), generator=gen, device="cuda", dtype=torch.int32)
+    kw = {}
+    if rot:
+        pos[1, 1500] = 3000                          # outside the tables: not written, reported
+        kw = dict(zip(("cos", "sin"), (torch.from_numpy(t).cuda() for t in rope_tables(3000, rot))), interleaved=inter)
+    whole, parts = (Cache(old + n, page, ks=0.5, bounds=True, seed=7) for _ in range(2))
+    status = torch.zeros(2, dtype=torch.int32, device="cuda")
+    off = lambda m: torch.arange(0, B * m + 1, m, dtype=torch.int32, device="cuda")
+    flat = lambda t: t.reshape(-1, *t.shape[2:]).contiguous()
+    binding.paged_append(whole.pages, flat(k), flat(v), offsets=off(n), max_new=n, status=status[:1],
+                         **(dict(kw, positions=flat(pos)) if rot else {}))
+    parts.pages.rows.copy_(torch.from_numpy(old.astype(np.int32)))
+    for i in range(0, n, piece):
+        m = min(piece, n - i)
+        parts.pages.rows += m
+        binding.paged_append(parts.pages, flat(k[:, i:i + m]), flat(v[:, i:i + m]), offsets=off(m), max_new=m, status=status[1:],
+                             **(dict(kw, positions=flat(pos[:, i:i + m])) if rot else {}))
+    assert torch.equal(whole.pages.pool, parts.pages.pool)
+    assert torch.equal(whole.pages.bounds.view(torch.int16), parts.pages.bounds.view(torch.int16))
+    assert (status != 0).tolist() == [bool(rot)] * 2
+
+
 def test_tokens_one_by_one_leave_what_one_call_leaves():
     B, H, page, n = 3, 2, 16, 37
     gen = torch.Generator(device="cuda").manual_seed(3)
