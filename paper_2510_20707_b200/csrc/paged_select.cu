@@ -13,9 +13,10 @@
 // start, 14 to score the longest with four CTAs (512 pages a head 3.7 us, 3600 clocks a step of sixteen warps, instructions issued in
 // 70 % of them), 2 to find the threshold; the multiprocessors work for half of that time.  8 heads of 131072 rows in pages
 // of 64, four query heads: 11.  Equal runs of pages of all heads in a kernel of their own, through memory, took as long, and 1 us
-// more where there are few pages; clusters of eight CTAs with 256 threads 24, of 128 threads 33, of 512, more than fit at once, 27.  Lanes that choose between their
-// sums instead of taking the rows in their own order, and one dimension to an instruction: 22.5.  Query rows in registers, bounds asked
-// for further ahead, q without its parts (fewer reads of shared memory, more instructions): level or slower.
+// more where there are few pages; clusters of eight CTAs with 256 threads 24, of 128 threads 33, of 512, more than fit at once, 27.
+// Lanes that choose between their sums instead of taking the rows in their own order, and one dimension to an instruction: 22.5.
+// Query rows in registers, bounds asked for further ahead, q without its parts (fewer reads of shared memory, more instructions):
+// level or slower.
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
