@@ -233,6 +233,7 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
   __syncthreads();
   low = __reduce_min_sync(0xffffffffu, lane < kSelWarps ? sums[0][lane] : 0xffffffffu);
   high = __reduce_max_sync(0xffffffffu, lane < kSelWarps ? sums[1][lane] : 0u);
+  __syncthreads();     // sums is written again, at once where all words are one: a late warp would see other ends and search alone
   uint32_t want = take;     // of the words low .. high
   bool exact = take == pages;       // all words from `low` on are taken
   while (!exact && low < high) {

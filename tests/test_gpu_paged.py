@@ -581,3 +581,19 @@ def test_what_changes_from_step_to_step_is_read_anew():
 
     for (a, b), (x, y) in zip(steps(caches[0], True), steps(caches[1], False)):
         assert torch.equal(a, x) and torch.equal(b, y)
+
+
+@pytest.mark.parametrize("pages,top,G", [(40, 6, 2), (700, 3, 7), (1999, 500, 4)])
+def test_pages_of_one_score_in_every_head(pages, top, G):
+    # the search for the threshold has nothing to take apart: equal scores, a query of NaN, or every page kept; over and over, with
+    # every word of the lists as before the first call where none is due
+    B, H, page = 4, 8, 16
+    c = Cache(np.full((B, H), pages * page), page, bounds=True)
+    c.pages.bounds.fill_(1.0)
+    q = queries(B, 1, H * G, "bf16")
+    odd = q.clone()
+    odd[..., 5] = float("nan")
+    want = torch.arange(top, dtype=torch.int32, device="cuda").expand(B, H, top)
+    for query, first, last in ((q, 0, 0), (odd, 0, 0), (q, pages // 2, pages), (q, pages, 0)):
+        got = [binding.paged_select(c.pages, query, top, keep_first=first, keep_last=last) for _ in range(100)]
+        assert all(torch.equal(lists, want) and bool((counts == top).all()) for lists, counts in got)
