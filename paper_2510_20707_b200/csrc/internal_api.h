@@ -43,6 +43,10 @@ int mixkv_internal_budget_clusters(int32_t pairs, int64_t keys_per_pair, const i
 void mixkv_internal_paged_shape(int64_t units, int32_t groups, int64_t steps, int32_t eights, int32_t sms, const int32_t* narrow,
                                 const int32_t* wide, int32_t* ctas, int32_t* large, int32_t* shared);
 
+// What the 32 lanes of a warp are told by its common wait for an mbarrier: answers[0 .. 31] for a phase that is complete for the even
+// lanes only, where a wait of the CTA has run out before, answers[32 .. 63] for one that is complete (1: complete).
+int mixkv_internal_warp_waits(int32_t* answers_dev, void* stream);
+
 // Rounds of a threshold search among keys lo .. hi that ends at `key` without listing any: keys [base, base + span] counted
 // in bins of 2^shift.  Returns their number (three at most).
 int mixkv_internal_search_rounds(uint32_t lo, uint32_t hi, uint32_t key, uint32_t* base, uint32_t* span, int32_t* shift);

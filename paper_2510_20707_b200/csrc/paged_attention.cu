@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
     const int n = unit_tiles(a, u).n;
     const int clear = n - a.T + 1;   // rows below are seen by all
     for (; f < end && !lost; f += stride) {
-      if (!mbar_wait(&bar[slot], parity, abort)) {
+      if (!mbar_wait_warp(&bar[slot], parity, abort)) {
         lost = true;
         break;
       }
@@ -521,7 +521,10 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
       ++slot;
       if (slot == kAttDepth) slot = 0, parity ^= 1;
     }
-    if (lost && lane == 0) drain_ring(bar, kAttDepth, sent);
+    if (lost) {     // (once: the units that follow have no copies)
+      if (lane == 0) drain_ring(bar, kAttDepth, sent);
+      sent = 0;
+    }
 
     pdl_launch_dependents();      // (the next kernel's CTAs, where this one's have ended)
     // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others

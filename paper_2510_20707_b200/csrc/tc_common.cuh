@@ -69,6 +69,12 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   }
 }
 
+// The same for a whole warp, with one answer: lanes give up one by one (their clocks differ, and another warp may raise *abort
+// between two of them), and a warp that goes on with some of its lanes waits for the others at its next vote or shuffle.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort)) != 0;
+}
+
 // TMA tile loads (no multicast); coordinates innermost first.
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* tm, int x, int y, int z,
                                             uint64_t* bar) {

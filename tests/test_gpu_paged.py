@@ -1,4 +1,6 @@
 """GPU parity of the paged 4-bit cache (append, read back, page selection, attention) against its plain definition."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -597,3 +599,11 @@ def test_pages_of_one_score_in_every_head(pages, top, G):
     for query, first, last in ((q, 0, 0), (odd, 0, 0), (q, pages // 2, pages), (q, pages, 0)):
         got = [binding.paged_select(c.pages, query, top, keep_first=first, keep_last=last) for _ in range(100)]
         assert all(torch.equal(lists, want) and bool((counts == top).all()) for lists, counts in got)
+
+
+def test_a_wait_that_runs_out_does_so_for_the_whole_warp():
+    # (a wait inside the attention; here one that is over for half of a warp's lanes, after the time is up)
+    answers = torch.full((64,), 7, dtype=torch.int32, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert binding.load_library().mixkv_internal_warp_waits(C.c_void_p(answers.data_ptr()), C.c_void_p(stream)) == 0
+    assert answers.tolist() == [0] * 32 + [1] * 32
