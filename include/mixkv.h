@@ -358,7 +358,8 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  *   offsets_opt     device int32 [batch + 1], ascending; NULL: one token per sequence.  offsets_per_head != 0:
  *                   [batch * kv_heads + 1], every head its own range of rows, head_stride is not used: K_out, V_out and
  *                   out_row_offsets of a compressed layer as they are
- *   max_new         upper bound on n; of more, a head's last max_new are written
+ *   max_new         upper bound on n; of more, a head's last max_new are written, and the others reported as those without a
+ *                   place are
  *   cos_opt, sin_opt  device fp32 [table_len, rot_dim / 2], 16-byte aligned; both NULL: no rotation.  Dimension i of a
  *                   pair becomes x cos - y sin, its partner y cos + x sin, in fp32; pairs are (i, i + rot_dim / 2), or
  *                   with interleaved != 0 (2 i, 2 i + 1), below rot_dim (at most 128; a multiple of 32,
@@ -371,7 +372,8 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  * they are computed.
  * Bounds (if there are any) of a page that begins with a new row are set, those of a page that had rows are widened.
  * Pages are written by one call at a time.  A token whose page (table entry outside the pool, row beyond the table or
- * below zero), position or place in k lies outside gives MIXKV_ERR_INVALID_ARG in *status_dev and is not written. */
+ * below zero), position or place in k lies outside, and one beyond max_new, gives MIXKV_ERR_INVALID_ARG in *status_dev and is not
+ * written. */
 int mixkv_paged_append(const mixkv_pages* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
                        int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
                        const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, const float* cos_opt,
@@ -379,7 +381,7 @@ int mixkv_paged_append(const mixkv_pages* c, const void* k, const void* v, int32
                        const int32_t* positions_opt, int32_t* status_dev, void* stream);
 
 /* The last n rows of every head back as dense rows: what mixkv_paged_append was given, rounded (and rotated).  offsets_opt,
- * offsets_per_head and max_new as there (n = the number of rows reads the whole head).
+ * offsets_per_head and max_new as there (n = the number of rows reads the whole head; of more than max_new the last are read).
  *   k_out, v_out    device, type `type`, 32-byte aligned: [num_tokens, kv_heads, 128], or [num_tokens, 128] with
  *                   offsets_per_head; rows that do not exist are not written */
 int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,

@@ -370,26 +370,30 @@ def new_pages(batch: int, kv_heads: int, max_rows: int, page_rows: int = 64, bou
 
 
 def paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
-                 max_new: int = 1, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
+                 max_new: Optional[int] = None, cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None,
                  positions: Optional[torch.Tensor] = None, interleaved: bool = False,
                  status: Optional[torch.Tensor] = None, stream=None) -> None:
     """mixkv_paged_append: writes the last rows of every head (count them into ``pages.rows`` first), rounded to 4 bits.
     k, v [tokens, kv_heads, 128] bf16 or fp16 (tokens and heads may be strided): sequence b's are ``offsets[b] ..
-    offsets[b + 1] - 1`` (int32 device tensor), at most ``max_new`` of them; without offsets one per sequence.  Or compact
-    rows [rows, 128] with an offset per (sequence, head): ``K_out``, ``V_out`` and ``out_row_offsets`` of
-    :func:`compress_layer`.  With ``cos`` and ``sin`` [length, rot_dim / 2] fp32, K is rotated by the tables' rows
+    offsets[b + 1] - 1`` (int32 device tensor), at most ``max_new`` of them (default: the rows of k; a bound near the longest
+    range launches fewer CTAs); without offsets one per sequence.  Or compact rows [rows, 128] with an offset per
+    (sequence, head): ``K_out``, ``V_out`` and ``out_row_offsets`` of :func:`compress_layer`.  With ``cos`` and ``sin`` [length, rot_dim / 2] fp32, K is rotated by the tables' rows
     ``positions`` (int32, one per token).  ``status``: an int32 device word, zeroed by the caller, that receives
-    MIXKV_ERR_INVALID_ARG for rows without a place."""
+    MIXKV_ERR_INVALID_ARG for rows without a place or beyond ``max_new``."""
+    if max_new is None:
+        max_new = 1 if offsets is None else max(1, k.size(0))
     (_host_module or _host()).paged_append(pages, k, v, offsets, max_new, cos, sin, positions, interleaved, status, stream)
 
 
 def paged_read(pages: Pages, tokens: int, dtype: torch.dtype = torch.bfloat16,
-               offsets: Optional[torch.Tensor] = None, max_new: int = 1, compact: bool = False, stream=None):
+               offsets: Optional[torch.Tensor] = None, max_new: Optional[int] = None, compact: bool = False, stream=None):
     """mixkv_paged_read: the last rows of every head as dense K, V [tokens, kv_heads, 128] (``compact``: [tokens, 128],
     with an offset per (sequence, head)); offsets and max_new as in :func:`paged_append`.  Rows that do not exist are
     left as they come from the allocator."""
     if dtype not in (torch.bfloat16, torch.float16):
         raise TypeError("paged_read gives bf16 or fp16")
+    if max_new is None:
+        max_new = 1 if offsets is None else max(1, tokens)
     return (_host_module or _host()).paged_read(pages, tokens, dtype == torch.float16, offsets, max_new, compact, stream)
 
 

@@ -43,7 +43,7 @@ struct PageSpan {
   int first, last;         // those of them whose token is in the input
   long long token;         // token (or row of the input) of row 0 of the page; there may be none
   int id;                  // what the table says, -1 beyond it
-  bool bad;                // a new row below row zero
+  bool bad;                // a new row below row zero, or more of them than the call allows
 };
 __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) {
   PageSpan s;
@@ -53,15 +53,19 @@ __device__ __forceinline__ PageSpan page_span(const RowArgs& a, const int task) 
   s.u = b * a.p.H + s.h;
   const int rows = fresh(a.p.rows + s.u);
   int n = 1;
+  bool over = false;
   long long first = b;
   if (a.offsets) {
     const int i = a.per_head ? s.u : b;
     const int from = fresh(a.offsets + i), to = fresh(a.offsets + i + 1);
-    n = to > from ? (int)min((unsigned)to - (unsigned)from, (unsigned)a.max_new) : 0;
+    const unsigned all = to > from ? (unsigned)to - (unsigned)from : 0u;
+    over = all > (unsigned)a.max_new;
+    n = (int)min(all, (unsigned)a.max_new);
     first = (long long)to - n;
   }
   s.bad = rows < n;
   if (s.bad) first += n - max(rows, 0), n = max(rows, 0);      // (only the last rows have a place)
+  s.bad |= over;
   const int r0 = rows - n;      // row of the first new token
   s.page = n > 0 ? a.p.by_rows.div(r0) + slot : 0;
   const long long begin = (long long)s.page * a.p.page_rows, end = begin + a.p.page_rows;

@@ -607,3 +607,30 @@ def test_a_wait_that_runs_out_does_so_for_the_whole_warp():
     stream = torch.cuda.current_stream().cuda_stream
     assert binding.load_library().mixkv_internal_warp_waits(C.c_void_p(answers.data_ptr()), C.c_void_p(stream)) == 0
     assert answers.tolist() == [0] * 32 + [1] * 32
+
+
+@pytest.mark.parametrize("compact", [False, True])
+def test_more_new_rows_than_a_call_allows_are_reported(compact):
+    # 5, 1 and 40 new rows of two heads; without a bound, or with the longest, all of them are written; with a smaller one a head's
+    # last rows are, and the status says that it was too small
+    new, H, page = np.array([5, 1, 40]), 2, 16
+    per = np.repeat(new, H) if compact else new
+    N = int(per.sum())
+    off = torch.from_numpy(np.concatenate([[0], per.cumsum()]).astype(np.int32)).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((N, 128) if compact else (N, H, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    pools = {}
+    for most in (None, 40, 39, 8, 1):
+        c = Cache(new[:, None].repeat(H, 1), page, bounds=True, seed=4)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        binding.paged_append(c.pages, k, v, offsets=off, status=status, **({} if most is None else dict(max_new=most)))
+        assert status.item() == (0 if most in (None, 40) else -1), most
+        pools[most] = c.pages.pool
+    assert torch.equal(pools[None], pools[40])
+    rows, _ = plain.get_rows(pools[40].cpu().numpy(), c.table[2, 1], page, 40)
+    last, _ = plain.get_rows(pools[8].cpu().numpy(), c.table[2, 1], page, 40)
+    assert np.isfinite(rows).all() and np.isnan(last[:32]).all() and np.array_equal(last[32:], rows[32:])
+    c.pages.pool = pools[40]
+    kr, vr = binding.paged_read(c.pages, N, offsets=off, compact=compact)
+    kq, vq = (plain.values(*plain.quantise(f32(x))) for x in (k, v))
+    assert torch.equal(kr.cpu(), torch.from_numpy(kq).bfloat16()) and torch.equal(vr.cpu(), torch.from_numpy(vq).bfloat16())
