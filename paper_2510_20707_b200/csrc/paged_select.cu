@@ -318,12 +318,18 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   const bool bf16 = type == MIXKV_TYPE_BF16;
   void (*kernel)(SelArgs) = bf16 ? k_paged_select<__nv_bfloat16> : k_paged_select<__half>;
   static std::atomic<bool> done[2][kMaxDevices];
-  if (ensure_smem(kernel, most, done[bf16]) != cudaSuccess) return MIXKV_ERR_CUDA;
-  // as many CTAs as keep four pages for every warp, while they fit the GPU
+  const int dev = device_slot();
+  if (ensure_smem(kernel, most, done[bf16], dev) != cudaSuccess) return MIXKV_ERR_CUDA;
+  // As many CTAs as keep four pages for every warp, while the clusters are all resident at once, a CTA to an SM (asked with the most
+  // shared memory: what is remembered does not depend on the call).  65536 rows in pages of 32, seven query heads, us, with the largest
+  // number that fits / with one CTA to every SM, of which some clusters wait: 16 heads 17.4 / 22.5, 24 19.6 / 29.3, 37 25.8 / 36.2,
+  // 47 34.4 / 45.8.  Heads of lengths from a quarter to that make room for one another: 24 18.4 / 18.4, 37 25.3 / 28.6, 47 33.5 / 28.2.
   int S = (int)(device_sm_count() / units < kMaxCluster ? device_sm_count() / units : kMaxCluster);
   const long long rounds = (pages + kSelWarps * 4 - 1) / (kSelWarps * 4);
   if (S > rounds) S = (int)rounds;
   if (S < 1) S = 1;
+  static ClusterFit fits[2];
+  while (S > 1 && units > fits[bf16].ask(kernel, kSelThreads, most, S, dev)) --S;
   const cudaError_t e = launch_pdl(kernel, dim3((unsigned)(units * S)), dim3(kSelThreads), smem, (cudaStream_t)stream, S, a);
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }

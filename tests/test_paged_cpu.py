@@ -212,3 +212,22 @@ def test_division_by_multiplication():
             for n in (q * d - 1, q * d, q * d + d - 1):
                 if 0 <= n < 1 << 31:
                     assert (n if l == 0 else (n * m >> 32) >> (l - 1)) == n // d, (n, d)
+
+
+@pytest.mark.parametrize("units,size", [(1, 8), (14, 8), (15, 6), (16, 6), (21, 6), (22, 6), (23, 5), (26, 5), (27, 4), (34, 4), (37, 3),
+                                        (44, 3), (45, 2), (48, 2), (74, 2), (75, 1), (148, 1), (600, 1)])
+def test_clusters_of_the_selection_are_resident_at_once(fake_cuda, units, size):
+    # of clusters of seven and eight fourteen are held at once, as the SM groups of a chip leave it (the runtime without a device
+    # answers with twice what it is given for small CTAs)
+    fits = {1: 148, 2: 74, 3: 44, 4: 34, 5: 26, 6: 22, 7: 14, 8: 14}
+    fake_cuda.reset(device=11, resident={n: m // 2 for n, m in fits.items()})
+    assert select(fake_cuda.lib, pages(batch=units, kv_heads=1, max_pages=4096), rows=1 << 18) == 0
+    launch, = fake_cuda.launches()
+    assert (launch.kernel, launch.grid, launch.cluster) == ("k_paged_select", units * size, size)
+
+
+def test_a_device_without_clusters_gets_none_for_the_selection(fake_cuda):
+    fake_cuda.reset(device=12, resident={n: 0 for n in range(2, 9)})
+    assert select(fake_cuda.lib, pages(max_pages=4096), rows=1 << 18) == 0
+    launch, = fake_cuda.launches()
+    assert (launch.grid, launch.cluster) == (8, 1)
