@@ -411,7 +411,8 @@ int mixkv_paged_workspace_size(const mixkv_pages* c, int32_t q_tokens, int32_t g
  * Token t attends to rows 0 .. rows - q_tokens + t of its KV head; a token that has no row gets zeros.
  *   q               as in mixkv_paged_select; q_tokens * gqa_ratio <= MIXKV_PAGED_MAX_QUERIES
  *   page_list_opt   device int32 [batch, kv_heads, top], counts_opt [batch, kv_heads]: attend to the rows of these
- *                   pages only (ascending, as mixkv_paged_select lists them); NULL, NULL, 0: to all
+ *                   pages only (ascending, as mixkv_paged_select lists them; counts_opt entries, at most top, are looked at, and
+ *                   those that are no page of the head have no rows); NULL, NULL, 0: to all
  *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call.  It steers how the rows of a head are
  *                   split
  *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned

@@ -687,8 +687,9 @@ AttKernel att_kernel(const int NT, const bool wide) {
   }
 }
 
-// How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit.  narrow(n), wide(n): clusters
-// of n CTAs of either kind that are resident at once.
+// How the work is split.  units: (sequence, head) pairs; groups of query rows; steps of the longest unit, as its rows and `top` have it, and
+// `most` that one can have on the device (what a list counts is the caller's word): the shares' sum over all units has 31 bits.
+// narrow(n), wide(n): clusters of n CTAs of either kind that are resident at once.
 //
 // A cluster of small CTAs per unit, one of large CTAs that have an SM each, or all steps dealt out evenly and joined by a second
 // kernel; us a call, one token of four query heads, heads of one length (and of lengths from one row to that):
@@ -711,7 +712,7 @@ struct AttShape {
 };
 int att_slots(const int NT, const int sms) { return att_per_sm(NT, kAttWarps) * sms; }
 template <typename Narrow, typename Wide>
-AttShape att_shape(const long long units, const int groups, const long long steps, const int NT, const int sms,
+AttShape att_shape(const long long units, const int groups, const long long steps, const long long most, const int NT, const int sms,
                    const Narrow& narrow, const Wide& wide) {
   const long long slots = att_slots(NT, sms), all = units * groups;
   auto clusters = [&](const long long room, const int warps, const auto& fit) {
@@ -730,7 +731,7 @@ AttShape att_shape(const long long units, const int groups, const long long step
   } else if (NT == 1 && alone <= kAttManySteps) {
     return {S, 0, false};
   }
-  if (units <= kAttUnits && groups < slots && units * steps <= 0x7fffffffll) {
+  if (units <= kAttUnits && groups < slots && units * most <= 0x7fffffffll) {
     const long long want = (units * steps + kAttWarps * 2 - 1) / (kAttWarps * 2);     // (two steps to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups), false};
   }
@@ -761,7 +762,7 @@ using namespace mixkv;
 extern "C" void mixkv_internal_paged_shape(int64_t units, int32_t groups, int64_t steps, int32_t eights, int32_t sms,
                                            const int32_t* narrow, const int32_t* wide, int32_t* ctas, int32_t* large,
                                            int32_t* shared) {
-  const AttShape s = att_shape(units, groups, steps, eights, sms, [&](const int n) { return narrow[n]; },
+  const AttShape s = att_shape(units, groups, steps, steps, eights, sms, [&](const int n) { return narrow[n]; },
                                [&](const int n) { return wide[n]; });
   *ctas = s.S, *large = s.wide, *shared = s.ctas;
 }
@@ -798,7 +799,8 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
   if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
   const long long seen = max_rows < (long long)c->max_pages * c->page_rows ? max_rows : (long long)c->max_pages * c->page_rows;
   long long tiles = (seen + kPageTile - 1) / kPageTile;
-  if (page_list_opt && tiles > (long long)top * a.p.tiles) tiles = (long long)top * a.p.tiles;
+  const long long listed = (long long)top * a.p.tiles, most = page_list_opt ? listed : tiles;
+  if (page_list_opt && tiles > listed) tiles = listed;
 
   const bool bf16 = type == MIXKV_TYPE_BF16;
   static std::atomic<bool> done[4 * (kAttGroups + 1)][kMaxDevices];
@@ -814,7 +816,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
       return fits[variant(wide)].ask(kernel_of(wide), 32 * warps(wide), smem, size, dev);
     };
   };
-  const AttShape shape = att_shape(units, groups, (tiles + 1) / 2, NT, sms, resident(false), resident(true));
+  const AttShape shape = att_shape(units, groups, (tiles + 1) / 2, (most + 1) / 2, NT, sms, resident(false), resident(true));
   const AttKernel kernel = kernel_of(shape.wide);
   const size_t smem = att_smem(NT, warps(shape.wide));
   if (ensure_smem(kernel, smem, done[variant(shape.wide)], dev) != cudaSuccess) return MIXKV_ERR_CUDA;

@@ -231,3 +231,14 @@ def test_a_device_without_clusters_gets_none_for_the_selection(fake_cuda):
     assert select(fake_cuda.lib, pages(max_pages=4096), rows=1 << 18) == 0
     launch, = fake_cuda.launches()
     assert (launch.grid, launch.cluster) == (8, 1)
+
+
+def test_lists_longer_than_the_heads_do_not_run_over_the_shares_sum(fake_cuda):
+    # what `counts` says is taken for the number of entries: 1024 heads x 2^20 entries x 8 steps are 2^33, which no prefix of 31 bits
+    # holds, so a cluster has a head each; lists of 2^17 entries (2^30 steps) are shared out
+    fake_cuda.reset(device=13, resident={n: 148 // n for n in range(1, 9)})
+    c = pages(batch=128, kv_heads=8, max_pages=1024, page_rows=256)
+    for top in (1 << 20, (1 << 18) + 1, 1 << 17):
+        assert attend(fake_cuda.lib, c, rows=1 << 18, list=ONE, counts=ONE, top=top) == 0
+    assert [(x.kernel, x.grid) for x in fake_cuda.launches()] == [
+        ("k_paged_attention", 1024), ("k_paged_attention", 1024), ("k_paged_attention", 592), ("k_paged_join", 1024)]
