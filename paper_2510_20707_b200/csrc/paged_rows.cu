@@ -114,9 +114,10 @@ __device__ __forceinline__ uint32_t scale_of(const float m, const float inv6) {
 // Codes of eight values of a block.  div: its divisor and the rounded reciprocal; divide: by division.
 //
 // x / d is rounded to nearest by Markstein's correction of x times the rounded reciprocal: the remainder of that first quotient is
-// exact, and one step with it rounds correctly while nothing over- or underflows.  Blocks of infinities and of extreme scales
-// (unsafe) are divided.  (A code of zero has either sign.)
-__device__ __forceinline__ bool unsafe(const float m, const float2 div) { return !(m < 1e30f && div.x > 1e-30f); }   // (NaN, and d == 0, too)
+// exact, and one step with it rounds correctly while nothing over- or underflows: x / d stays below 1e36, and the remainder of
+// an x that is no code of zero (above d / 8, 2^-63) is a multiple of 2^-47 x.  Blocks of infinities, of extreme values or scales (unsafe) are
+// divided.  (A code of zero has either sign.)
+__device__ __forceinline__ bool unsafe(const float m, const float2 div) { return !(m < 1e18f && div.x > 1e-18f); }   // (NaN, and d == 0, too)
 template <bool DIVIDE>
 __device__ __forceinline__ uint32_t codes8(const f32x2* x, const float2 div) {
   const f32x2 by = pack2(div.y, div.y), d = pack2(-div.x, -div.x);

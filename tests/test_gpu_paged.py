@@ -634,3 +634,22 @@ def test_more_new_rows_than_a_call_allows_are_reported(compact):
     kr, vr = binding.paged_read(c.pages, N, offsets=off, compact=compact)
     kq, vq = (plain.values(*plain.quantise(f32(x))) for x in (k, v))
     assert torch.equal(kr.cpu(), torch.from_numpy(kq).bfloat16()) and torch.equal(vr.cpu(), torch.from_numpy(vq).bfloat16())
+
+
+@pytest.mark.parametrize("ks,vs,top", [(1e-13, 1.0, 9e29), (1.0, 3e-16, 1e25), (1e-20, 1e-25, 1.0), (1e-30, 1e-36, 60000.0),
+                                       (1e17, 1e25, 3e18), (1e30, 1e30, 2e38), (0.7, 1.3, 50.0), (3e-5, 700.0, 1e3)])
+def test_values_far_from_their_scale(ks, vs, top):
+    # quotients from far below a code to far beyond the largest, where a quotient may leave the range of fp32: each keeps its sign.  Scales of
+    # every kind of significand
+    rng = np.random.default_rng(3)
+    n = 64
+    x = rng.standard_normal((n, 128)) * top * 10.0 ** rng.uniform(-9, 0, (n, 8)).repeat(16, 1)
+    x[0], x[1, :64], x[1, 64:] = -top, top, -top
+    x = torch.from_numpy(x).bfloat16().cuda()
+    c = Cache([[n]], 16, ks=ks, vs=vs)
+    binding.paged_append(c.pages, x, x, offsets=torch.tensor([0, n], dtype=torch.int32, device="cuda"), max_new=n)
+    k, v = plain.get_rows(c.pool(), c.table[0, 0], 16, n)
+    for got, scale in ((k, ks), (v, vs)):
+        want = plain.values(*plain.quantise(f32(x), scale))
+        assert np.array_equal(got, want)
+        assert (want[0] <= 0).all() and (want[1, :64] >= 0).all()
