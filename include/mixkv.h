@@ -343,8 +343,8 @@ typedef struct mixkv_pages {
   int32_t page_rows;     /* a multiple of 16, at most 256 */
   int32_t batch, kv_heads;
   int32_t head_dim;      /* 128 */
-  float k_scale, v_scale; /* > 0: a third factor of all values, for caches whose blocks are far from the range of e4m3
-                            (largest magnitudes of 0.1 to 2000 need none) */
+  float k_scale, v_scale; /* 1.2e-38 (normal numbers) to 3e38: a third factor of all values, for caches whose blocks are far from
+                            the range of e4m3 (largest magnitudes of 0.1 to 2000 need none) */
 } mixkv_pages;
 
 /* Bytes of a page.  Host-only. */

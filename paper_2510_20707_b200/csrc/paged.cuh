@@ -1,6 +1,8 @@
 // The paged 4-bit cache (format: include/mixkv.h): where things lie, and the small conversions its kernels share.
 #pragma once
 
+#include <cfloat>
+
 #include <cuda_fp16.h>
 
 #include "internal_api.h"
@@ -45,8 +47,9 @@ struct PagePool {
 
 inline int check_pages(const mixkv_pages* c, PagePool* p) {
   if (!c || !c->pool || !c->table || !c->rows) return MIXKV_ERR_INVALID_ARG;
-  if (c->num_pages < 1 || c->max_pages < 1 || c->batch < 1 || c->kv_heads < 1 || !(c->k_scale > 0.f) ||
-      !(c->v_scale > 0.f) || c->k_scale > 3e38f || c->v_scale > 3e38f)
+  // (of a subnormal scale the reciprocal is infinite, and a block of zeros would be NaN)
+  const auto is_scale = [](const float x) { return x >= FLT_MIN && x <= 3e38f; };
+  if (c->num_pages < 1 || c->max_pages < 1 || c->batch < 1 || c->kv_heads < 1 || !is_scale(c->k_scale) || !is_scale(c->v_scale))
     return MIXKV_ERR_INVALID_ARG;
   if (c->page_rows < kPageTile || c->page_rows % kPageTile || c->page_rows > MIXKV_PAGE_MAX_ROWS)
     return MIXKV_ERR_INVALID_ARG;

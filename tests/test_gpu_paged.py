@@ -653,3 +653,13 @@ def test_values_far_from_their_scale(ks, vs, top):
         want = plain.values(*plain.quantise(f32(x), scale))
         assert np.array_equal(got, want)
         assert (want[0] <= 0).all() and (want[1, :64] >= 0).all()
+
+
+def test_blocks_of_zeros_at_the_least_scale():
+    c = Cache([[16]], 16, ks=float(np.finfo(np.float32).tiny), vs=float(np.finfo(np.float32).tiny))
+    x = torch.zeros((16, 128), device="cuda").bfloat16()
+    x[3], x[5, :16] = 1e-38, 2e-36
+    binding.paged_append(c.pages, x, x, offsets=torch.tensor([0, 16], dtype=torch.int32, device="cuda"))
+    want = plain.values(*plain.quantise(f32(x), c.pages.k_scale))
+    assert all(np.array_equal(got, want) for got in plain.get_rows(c.pool(), c.table[0, 0], 16, 16))
+    assert (want[[0, 1, 2, 4]] == 0).all() and (want[3] > 0).all() and (want[5, :16] > 0).all()

@@ -242,3 +242,16 @@ def test_lists_longer_than_the_heads_do_not_run_over_the_shares_sum(fake_cuda):
         assert attend(fake_cuda.lib, c, rows=1 << 18, list=ONE, counts=ONE, top=top) == 0
     assert [(x.kernel, x.grid) for x in fake_cuda.launches()] == [
         ("k_paged_attention", 1024), ("k_paged_attention", 1024), ("k_paged_attention", 592), ("k_paged_join", 1024)]
+
+
+@pytest.mark.parametrize("name", ["k_scale", "v_scale"])
+def test_scales_without_a_reciprocal_are_refused(lib, name):
+    # 1 / (6 x) of a subnormal number can be beyond fp32: a block of zeros would become one of NaN
+    least = float(np.finfo(np.float32).tiny)
+    most = float(np.finfo(np.float32).max)
+    assert 1 / (6 * least) < most < 1 / (6 * 1e-40)
+    for bad in (1e-40, float(np.nextafter(np.float32(least), np.float32(0))), 3.1e38, -1.0):
+        c = pages(**{name: bad})
+        assert append(lib, c) == attend(lib, c) == select(lib, c) == -1, bad
+    if not torch.cuda.is_available():
+        assert append(lib, pages(**{name: least})) == -4 and append(lib, pages(**{name: 3e38})) == -4
