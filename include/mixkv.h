@@ -366,7 +366,8 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  *                   interleaved of 16)
  *   positions_opt   device int32 [num_tokens], needed with cos_opt: row of the tables.  It is not the row in the cache: a
  *                   compressed cache has fewer rows than its sequence has tokens
- * Rounding: the scale of a block is e4m3(min(max |x| / (6 k_scale), 448)), nearest even; a code is the nearest to
+ * Rounding: the scale of a block is e4m3(min(max |x| c, 448)), nearest even, with c the fp32 number nearest to 1 / (6 k_scale) and the
+ * product in fp32 (not the quotient, which at ties can have another byte where k_scale is no power of two); a code is the nearest to
  * x / (scale k_scale), ties to the even code, largest magnitude 6 (the sign of a code of zero is not defined); a block of zeros, or one that is too small for e4m3,
  * is zero; one that holds a NaN is NaN.  Every operation is rounded by itself, so codes are the same wherever
  * they are computed.

@@ -663,3 +663,26 @@ def test_blocks_of_zeros_at_the_least_scale():
     want = plain.values(*plain.quantise(f32(x), c.pages.k_scale))
     assert all(np.array_equal(got, want) for got in plain.get_rows(c.pool(), c.table[0, 0], 16, 16))
     assert (want[[0, 1, 2, 4]] == 0).all() and (want[3] > 0).all() and (want[5, :16] > 0).all()
+
+
+@pytest.mark.parametrize("scale", [1.25, 0.7, 1.3])
+def test_the_scale_is_a_product_with_the_reciprocal(scale):
+    # every fp16 magnitude as a block's largest: the stored byte is that of the product with the rounded reciprocal, worked out here in
+    # 64 bits; the quotient max |x| / (6 scale) can have another (46 of them at 1.25, none at 0.7)
+    every = np.arange(1, 0x7C00, dtype=np.uint16).view(np.float16).astype(np.float64)
+    c = np.float64(np.float32(1.0 / (6.0 * np.float64(np.float32(scale)))))
+    byte = lambda y: torch.from_numpy(np.minimum(y, 448.0).astype(np.float32)).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    product = byte(np.float32(every * c).astype(np.float64))
+    quotient = byte(every / (6.0 * np.float64(np.float32(scale))))
+    assert (product != quotient).sum() == {1.25: 46, 0.7: 0, 1.3: 16}[scale]
+    at = np.arange(every.size)
+    n = -(-every.size // 8)
+    rows = np.zeros((n, 128))
+    rows.reshape(-1)[at * 16 + at % 16] = every * np.where(at % 3, 1, -1)
+    x = torch.from_numpy(rows).half().cuda()
+    cache = Cache([[n]], 16, ks=scale, vs=scale)
+    binding.paged_append(cache.pages, x, x, offsets=torch.tensor([0, n], dtype=torch.int32, device="cuda"), max_new=n)
+    tiles, r = cache.pool().reshape(-1, plain.TILE_BYTES), np.arange(n)
+    mine = tiles[cache.table[0, 0, r // 16]]
+    for place in (plain.KS_AT, plain.VS_AT):
+        assert np.array_equal(mine[r[:, None], place[r % 16]].reshape(-1)[:every.size], product)
