@@ -758,7 +758,7 @@ struct PagedQuery {
   const at::Tensor& q;
   int32_t type, tokens, gqa;
   PagedQuery(PyObject* o, const PagesArg& pages) : q(tensor(o)) {
-    want(q.dim() == 4 && q.size(0) == pages.c.batch && q.size(2) % pages.c.kv_heads == 0 && q.size(3) == 128 &&
+    want(q.dim() == 4 && q.size(0) == pages.c.batch && pages.c.kv_heads > 0 && q.size(2) % pages.c.kv_heads == 0 && q.size(3) == 128 &&
              (q.size(2) <= 1 || q.stride(2) == 128) && q.stride(3) == 1 && q.device() == pages.pool().device(),
          "q must be [batch, tokens, kv_heads * gqa_ratio, 128], a token's heads packed, on the pool's device");
     type = paged_type(q.scalar_type());

@@ -686,3 +686,19 @@ def test_the_scale_is_a_product_with_the_reciprocal(scale):
     mine = tiles[cache.table[0, 0, r // 16]]
     for place in (plain.KS_AT, plain.VS_AT):
         assert np.array_equal(mine[r[:, None], place[r % 16]].reshape(-1)[:every.size], product)
+
+
+def test_a_table_without_heads_is_refused():
+    # (the binding divided q's heads by the table's)
+    pages = binding.Pages(pool=torch.zeros((1, binding.page_bytes(16)), dtype=torch.uint8, device="cuda"),
+                          table=torch.zeros((1, 0, 1), dtype=torch.int32, device="cuda"),
+                          rows=torch.zeros((1, 0), dtype=torch.int32, device="cuda"), page_rows=16,
+                          bounds=torch.zeros((1, 2, 128), dtype=torch.float16, device="cuda"))
+    q = queries(1, 1, 4, "bf16")
+    for call in (lambda: binding.paged_attention(pages, q, 16), lambda: binding.paged_select(pages, q, 1, 16),
+                 lambda: binding.paged_sparse_attention(pages, q, 1, 16), lambda: binding.paged_workspace(pages, q),
+                 lambda: binding.paged_append(pages, torch.zeros((1, 0, 128), device="cuda").half(),
+                                              torch.zeros((1, 0, 128), device="cuda").half()),
+                 lambda: binding.paged_read(pages, 1)):
+        with pytest.raises((AssertionError, binding.MixKVError)):
+            call()
