@@ -661,6 +661,8 @@ int32_t paged_type(const at::ScalarType t) {
   want(t == at::kBFloat16 || t == at::kHalf, "bf16 or fp16 is expected");
   return t == at::kBFloat16 ? MIXKV_TYPE_BF16 : MIXKV_TYPE_FP16;
 }
+// Stride of a dimension; of one element none is walked, and a view may hold any.
+int64_t step(const at::Tensor& t, const int64_t dim) { return t.size(dim) == 1 ? 0 : t.stride(dim); }
 // Offsets of the new rows: None or an int32 tensor of n + 1 words.
 const int32_t* row_offsets(PyObject* o, const int64_t n, const PagesArg& pages) {
   if (o == Py_None) return nullptr;
@@ -713,8 +715,8 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int rc = MIXKV_OK;
     if (k.size(0) > 0) {
       const Unlocked u;
-      rc = api.paged_append(&c, k.data_ptr(), v.data_ptr(), type, k.size(0), k.stride(0), compact ? 0 : k.stride(1),
-                            v.stride(0), compact ? 0 : v.stride(1), offsets, compact, max_new, cosv, sinv, table_len, rot,
+      rc = api.paged_append(&c, k.data_ptr(), v.data_ptr(), type, k.size(0), step(k, 0), compact ? 0 : step(k, 1),
+                            step(v, 0), compact ? 0 : step(v, 1), offsets, compact, max_new, cosv, sinv, table_len, rot,
                             interleaved, positions, status, stream.handle);
     }
     check_status(rc, what);
@@ -811,7 +813,7 @@ PyObject* py_paged_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const Unlocked u;
       list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool());
       counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool());
-      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
+      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, step(q.q, 0), step(q.q, 1), q.tokens, q.gqa, rows, top, first,
                             last, ip(list), ip(counts), stream.handle);
     }
     check_status(rc, what);
@@ -849,7 +851,7 @@ PyObject* py_paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
       const Unlocked u;
       ws.fill(pages);
       out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
-      rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, (float)scale,
+      rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, step(q.q, 0), step(q.q, 1), q.tokens, q.gqa, (float)scale,
                                rows, list, counts, top, ws.data, ws.bytes, out.data_ptr(), stream.handle);
     }
     check_status(rc, what);
@@ -878,11 +880,11 @@ PyObject* py_paged_sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
       list = empty({pages.c.batch, pages.c.kv_heads, top}, at::kInt, pages.pool());
       counts = empty({pages.c.batch, pages.c.kv_heads}, at::kInt, pages.pool());
       out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
-      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa, rows, top, first,
+      rc = api.paged_select(&pages.c, q.q.data_ptr(), q.type, step(q.q, 0), step(q.q, 1), q.tokens, q.gqa, rows, top, first,
                             last, ip(list), ip(counts), stream.handle);
       if (rc == MIXKV_OK) {
         what = "mixkv_paged_attention";
-        rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, q.q.stride(0), q.q.stride(1), q.tokens, q.gqa,
+        rc = api.paged_attention(&pages.c, q.q.data_ptr(), q.type, step(q.q, 0), step(q.q, 1), q.tokens, q.gqa,
                                  (float)scale, rows, ip(list), ip(counts), top, ws.data, ws.bytes, out.data_ptr(),
                                  stream.handle);
       }

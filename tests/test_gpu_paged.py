@@ -702,3 +702,20 @@ def test_a_table_without_heads_is_refused():
                  lambda: binding.paged_read(pages, 1)):
         with pytest.raises((AssertionError, binding.MixKVError)):
             call()
+
+
+def test_the_stride_of_a_dimension_of_one_does_not_matter():
+    # one token of one sequence in the output of a projection whose width is no multiple of 16, one KV head
+    G, wide = 4, 6 * 128 + 3
+    proj = torch.randn((2, wide), generator=torch.Generator(device="cuda").manual_seed(0), device="cuda").bfloat16()
+    q = proj[:1].as_strided((1, 1, G, 128), (wide, 7, 128, 1))
+    k, v = (proj[:1].as_strided((1, 1, 128), (wide, 5, 1), 128 * i) for i in (4, 5))
+    packed = lambda t: torch.empty(t.shape, dtype=t.dtype, device="cuda").copy_(t)
+    caches = [Cache([[40]], 16, bounds=True, seed=1) for _ in range(2)]
+    outs = []
+    for c, (x, y, z) in zip(caches, ((q, k, v), tuple(map(packed, (q, k, v))))):
+        c.fill()
+        binding.paged_append(c.pages, y, z)
+        outs.append((c.pages.pool, binding.paged_attention(c.pages, x), *binding.paged_select(c.pages, x, 2),
+                     *binding.paged_sparse_attention(c.pages, x, 2)))
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
