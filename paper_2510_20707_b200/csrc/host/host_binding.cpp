@@ -707,7 +707,7 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int32_t* status = nullptr;
     if (a[9] != Py_None) {
       const at::Tensor& t = tensor(a[9]);
-      want(t.scalar_type() == at::kInt && t.is_cuda() && t.numel() >= 1, "status must be an int32 CUDA tensor");
+      want(t.scalar_type() == at::kInt && t.numel() >= 1 && t.device() == k.device(), "status must be an int32 tensor on the pool's device");
       status = ip(t);
     }
     const CallStream stream(a[10], k);

@@ -719,3 +719,29 @@ def test_the_stride_of_a_dimension_of_one_does_not_matter():
         outs.append((c.pages.pool, binding.paged_attention(c.pages, x), *binding.paged_select(c.pages, x, 2),
                      *binding.paged_sparse_attention(c.pages, x, 2)))
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+def on_device(t, index):
+    """t as a tensor that says it is on CUDA device `index` (there may be no such device: nothing of it may be touched)."""
+    class Managed(C.Structure):
+        _fields_ = [("data", C.c_void_p), ("device_type", C.c_int32), ("device", C.c_int32), ("ndim", C.c_int32),
+                    ("code", C.c_uint8), ("bits", C.c_uint8), ("lanes", C.c_uint16), ("shape", C.POINTER(C.c_int64)),
+                    ("strides", C.c_void_p), ("offset", C.c_uint64), ("context", C.c_void_p), ("deleter", C.c_void_p)]
+    assert t.dim() == 1 and t.dtype == torch.int32
+    size = (C.c_int64 * 1)(t.numel())
+    m = Managed(data=t.data_ptr(), device_type=2, device=index, ndim=1, code=0, bits=32, lanes=1, shape=size)
+    new = C.pythonapi.PyCapsule_New
+    new.restype, new.argtypes = C.py_object, [C.c_void_p, C.c_char_p, C.c_void_p]
+    out = torch.utils.dlpack.from_dlpack(new(C.addressof(m), b"dltensor", None))
+    out.held = m, size, t
+    return out
+
+
+def test_a_status_word_of_another_device_is_refused():
+    c = Cache([[3, 3]], 16)
+    k = torch.zeros((1, 2, 128), dtype=torch.bfloat16, device="cuda")
+    word = torch.zeros(1, dtype=torch.int32, device="cuda")
+    binding.paged_append(c.pages, k, k, status=on_device(word, 0))
+    for bad in (on_device(word, 1), word.cpu(), word[:0], word.float()):
+        with pytest.raises(AssertionError):
+            binding.paged_append(c.pages, k, k, status=bad)
