@@ -45,6 +45,8 @@ struct PagePool {
   Divider by_heads, by_rows, by_tiles;   // of kv_heads, page_rows, tiles
 };
 
+inline bool aligned(const void* p, const unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
 inline int check_pages(const mixkv_pages* c, PagePool* p) {
   if (!c || !c->pool || !c->table || !c->rows) return MIXKV_ERR_INVALID_ARG;
   // (of a subnormal scale the reciprocal is infinite, and a block of zeros would be NaN)
@@ -53,8 +55,7 @@ inline int check_pages(const mixkv_pages* c, PagePool* p) {
     return MIXKV_ERR_INVALID_ARG;
   if (c->page_rows < kPageTile || c->page_rows % kPageTile || c->page_rows > MIXKV_PAGE_MAX_ROWS)
     return MIXKV_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(c->pool) & 15u) || (reinterpret_cast<uintptr_t>(c->bounds_opt) & 15u) ||
-      (reinterpret_cast<uintptr_t>(c->table) & 3u) || (reinterpret_cast<uintptr_t>(c->rows) & 3u))
+  if (!aligned(c->pool, 16) || !aligned(c->bounds_opt, 16) || !aligned(c->table, 4) || !aligned(c->rows, 4))
     return MIXKV_ERR_INVALID_ARG;
   if (c->head_dim != kHeadDim) return MIXKV_ERR_UNSUPPORTED;
   if ((long long)c->batch * c->kv_heads > (1 << 24) || (long long)c->max_pages * c->page_rows > (1ll << 30) ||

@@ -790,7 +790,7 @@ extern "C" int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_
       (page_list_opt == nullptr) != (counts_opt == nullptr) || (page_list_opt && top < 1))
     return MIXKV_ERR_INVALID_ARG;
   if (page_list_opt && top > kMostListed) return MIXKV_ERR_UNSUPPORTED;
-  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(workspace)) & 15u)
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || !aligned(page_list_opt, 4) || !aligned(counts_opt, 4))
     return MIXKV_ERR_INVALID_ARG;
   if ((rc = queries_of(c, q_tokens, gqa_ratio, &groups, &NT)) != MIXKV_OK) return rc;
   const long long units = (long long)c->batch * c->kv_heads;

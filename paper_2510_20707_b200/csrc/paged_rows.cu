@@ -465,7 +465,7 @@ int check_rows(const mixkv_pages* c, int32_t type, int64_t num_tokens, const int
   const int rc = check_pages(c, &a->p);
   if (rc != MIXKV_OK) return rc;
   if ((type != MIXKV_TYPE_BF16 && type != MIXKV_TYPE_FP16) || num_tokens < 0 || max_new < 1 || (per_head && !offsets) ||
-      (reinterpret_cast<uintptr_t>(offsets) & 3u))
+      !aligned(offsets, 4))
     return MIXKV_ERR_INVALID_ARG;
   if (max_new > (1 << 30)) return MIXKV_ERR_UNSUPPORTED;
   a->offsets = offsets, a->per_head = per_head != 0, a->max_new = offsets ? max_new : 1, a->num_tokens = num_tokens;
@@ -504,7 +504,6 @@ int read_as(const mixkv_pages* c, const RowArgs& a, void* k, void* v, void* stre
              ? MIXKV_OK
              : MIXKV_ERR_CUDA;
 }
-bool aligned(const void* p, const unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 }  // namespace
 }  // namespace mixkv
@@ -527,14 +526,14 @@ extern "C" int mixkv_paged_append(const mixkv_pages* c, const void* k, const voi
   RowArgs a = {};
   const int rc = check_rows(c, type, num_tokens, offsets_opt, offsets_per_head, max_new, &a);
   if (rc != MIXKV_OK) return rc;
-  if (!k || !v || !aligned(k, 32) || !aligned(v, 32)) return MIXKV_ERR_INVALID_ARG;
+  if (!k || !v || !aligned(k, 32) || !aligned(v, 32) || !aligned(status_dev, 4)) return MIXKV_ERR_INVALID_ARG;
   for (const int64_t stride : {k_row_stride, k_head_stride, v_row_stride, v_head_stride})
     if (stride < 0 || stride % 16) return MIXKV_ERR_INVALID_ARG;
   const bool rope = cos_opt != nullptr;
   if (rope != (sin_opt != nullptr)) return MIXKV_ERR_INVALID_ARG;
   if (rope) {
     if (!positions_opt || table_len < 1 || !aligned(cos_opt, 16) || !aligned(sin_opt, 16) || rot_dim < 1 || rot_dim > kHeadDim ||
-        (reinterpret_cast<uintptr_t>(positions_opt) & 3u))
+        !aligned(positions_opt, 4))
       return MIXKV_ERR_INVALID_ARG;
     if (rot_dim % (interleaved ? 16 : 32)) return MIXKV_ERR_UNSUPPORTED;
   }

@@ -301,7 +301,7 @@ extern "C" int mixkv_paged_select(const mixkv_pages* c, const void* q, int32_t t
   if (rc != MIXKV_OK) return rc;
   if (!c->bounds_opt || !q || !page_list || !counts || (type != MIXKV_TYPE_BF16 && type != MIXKV_TYPE_FP16) ||
       q_tokens < 1 || gqa_ratio < 1 || max_rows < 1 || top < 1 || keep_first < 0 || keep_last < 0 || q_batch_stride < 0 ||
-      q_token_stride < 0 || q_batch_stride % 8 || q_token_stride % 8 || (reinterpret_cast<uintptr_t>(q) & 15u))
+      q_token_stride < 0 || q_batch_stride % 8 || q_token_stride % 8 || !aligned(q, 16) || !aligned(page_list, 4) || !aligned(counts, 4))
     return MIXKV_ERR_INVALID_ARG;
   const long long R = (long long)q_tokens * gqa_ratio;
   const long long seen = max_rows < (long long)c->max_pages * c->page_rows ? max_rows : (long long)c->max_pages * c->page_rows;

@@ -255,3 +255,13 @@ def test_scales_without_a_reciprocal_are_refused(lib, name):
         assert append(lib, c) == attend(lib, c) == select(lib, c) == -1, bad
     if not torch.cuda.is_available():
         assert append(lib, pages(**{name: least})) == -4 and append(lib, pages(**{name: 3e38})) == -4
+
+
+def test_words_between_words_are_refused(lib):
+    # (the kernels would fault on them)
+    c, odd = pages(), C.c_void_p(258)
+    assert select(lib, c, list=odd) == select(lib, c, counts=odd) == -1
+    assert attend(lib, c, list=odd, counts=ONE, top=4) == attend(lib, c, list=ONE, counts=odd, top=4) == -1
+    assert append(lib, c, off=odd) == append(lib, c, cos=ONE, sin=ONE, len=4, rot=64, pos=odd) == -1
+    assert lib.mixkv_paged_append(c, ONE, ONE, 0, 8, 512, 128, 512, 128, ONE, 0, 4, None, None, 0, 0, 0, None, odd, None) == -1
+    assert lib.mixkv_paged_read(c, ONE, ONE, 0, 8, odd, 0, 4, None) == -1
