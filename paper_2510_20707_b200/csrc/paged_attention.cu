@@ -20,6 +20,8 @@
 // and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as fast as sixteen with 128;
 // asking for values ahead of the vote, one copy for two tiles that follow one another, rings of three: no gain.  With query rows on
 // the sixteen side, one tile a step and a chunk per CTA the same call took 129 us, and now 76.
+#include <cfloat>
+
 #include <cooperative_groups.h>
 
 #include "paged.cuh"
@@ -39,7 +41,7 @@ constexpr int kAttGroups = 4;                  // most groups of eight query row
 constexpr int kAttUnits = 1024;                // most units whose steps are dealt out evenly
 constexpr int kAttFew = 2, kAttFewRows = 8, kAttWideSteps = 8, kAttManySteps = 20;   // steps of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
-constexpr float kNoRef = -1e30f;               // reference before the first row: below any, and finite
+constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
 
 // rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
 // the cluster; barriers and rows of the rings
@@ -290,6 +292,8 @@ struct AttState {
               if (row[h] + 2 * (i >> 1) >= sees) s[h][nt][i] = -INFINITY;
         }
     }
+    // (A logit is rounded before the reference, itself a logit, is taken from it: of a product that is not, equal logits beyond 2^24 would
+    // differ from it by their last bits, whole powers of two.)
     bool above = false;
     float y[2][NT][4];
 #pragma unroll
@@ -298,7 +302,7 @@ struct AttState {
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          y[h][nt][i] = fmaf(s[h][nt][i], f[nt][i & 1], -ref[nt][i & 1]);
+          y[h][nt][i] = __fsub_rn(__fmul_rn(s[h][nt][i], f[nt][i & 1]), ref[nt][i & 1]);
           above |= y[h][nt][i] > kLag + kLift;
         }
     if (__any_sync(0xffffffffu, above)) {
@@ -311,7 +315,7 @@ struct AttState {
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = c; i < 4; i += 2) {
-              y[h][nt][i] = s[h][nt][i] * f[nt][c];
+              y[h][nt][i] = __fmul_rn(s[h][nt][i], f[nt][c]);
               mx = fmaxf(mx, y[h][nt][i]);
             }
           const float to = fmaxf(ref[nt][c], column_max(mx) - kLift);
@@ -320,7 +324,7 @@ struct AttState {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int i = c; i < 4; i += 2) y[h][nt][i] -= to;
+            for (int i = c; i < 4; i += 2) y[h][nt][i] = __fsub_rn(y[h][nt][i], to);
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }

@@ -745,3 +745,27 @@ def test_a_status_word_of_another_device_is_refused():
     for bad in (on_device(word, 1), word.cpu(), word[:0], word.float()):
         with pytest.raises(AssertionError):
             binding.paged_append(c.pages, k, k, status=bad)
+
+
+@pytest.mark.parametrize("gain", [-1e35, -1e32, -1e29, 1e29, 1e35])
+@pytest.mark.parametrize("n,T", [(100, 1), (100, 3), (9000, 1)])
+def test_logits_of_any_size(gain, n, T):
+    # keys of one value, and one of half of it in the second head: with logits this far from zero the first head's output is the mean
+    # of its values, the second's the value of the odd key alone, or the mean of the others
+    c, odd = Cache([[n, n]], 32), n // 3
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    k, v = torch.ones((2, n, 128), device="cuda"), torch.randn((2, n, 128), generator=gen, device="cuda")
+    k[1, odd] = 0.5
+    off = torch.tensor([0, n, 2 * n], dtype=torch.int32, device="cuda")
+    binding.paged_append(c.pages, k.view(-1, 128).bfloat16(), v.view(-1, 128).bfloat16(), offsets=off, max_new=n)
+    q = torch.full((1, T, 4, 128), gain, device="cuda").bfloat16()
+    out = binding.paged_attention(c.pages, q)[0].double().cpu().numpy()
+    for h in range(2):
+        _, V = c.rows_of(0, h)
+        for t in range(T):
+            seen = np.arange(n - T + 1 + t)
+            if h:
+                seen = np.array([odd]) if gain < 0 else seen[seen != odd]
+            want, mass = V[seen].mean(0), np.abs(V[seen]).mean(0)
+            # the output's rounding; sums of n equal weights in fp32
+            assert (np.abs(out[t, 2 * h:2 * h + 2] - want) <= 2.0 ** -8 * np.abs(want) + n * 2.0 ** -23 * mass).all(), (h, t)
