@@ -126,6 +126,7 @@ def attention(q, K, V, T, scale):
 def scores(q, lo, hi):
     """q [rows, 128], lo, hi [pages, 128], all fp32 -> scores [pages], summed as the format defines it."""
     q, lo, hi = (np.asarray(x, np.float32) for x in (q, lo, hi))
+    q = np.where(np.isinf(q), np.float32(np.nan), q)
     with np.errstate(invalid="ignore"):
         x = np.maximum(q[:, None] * lo[None], q[:, None] * hi[None])
         for _ in range(7):

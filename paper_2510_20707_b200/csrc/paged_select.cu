@@ -196,8 +196,10 @@ __global__ void __launch_bounds__(kSelThreads, 1) k_paged_select(const SelArgs a
     const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
                    (long long)(h * a.G + r - token * a.G) * kHeadDim + 4 * (e & 31);
     const uint2 w = fresh(reinterpret_cast<const uint2*>(src));
-    const float2 x = widen2<T>(w.x), y = widen2<T>(w.y);
-    // (a NaN stays one in both parts)
+    float2 x = widen2<T>(w.x), y = widen2<T>(w.y);
+    // (a NaN stays one in both parts; an infinity becomes one, whatever the bounds that it would meet)
+    auto known = [](float z) { return fabsf(z) < INFINITY ? z : NAN; };
+    x.x = known(x.x), x.y = known(x.y), y.x = known(y.x), y.y = known(y.y);
     auto up = [](float z) { return z < 0.f ? 0.f : z; };
     auto down = [](float z) { return z > 0.f ? 0.f : z; };
     qs[(e >> 5) * 64 + (e & 31)] = make_float4(up(x.x), up(y.x), up(x.y), up(y.y));

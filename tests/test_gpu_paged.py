@@ -769,3 +769,21 @@ def test_logits_of_any_size(gain, n, T):
             want, mass = V[seen].mean(0), np.abs(V[seen]).mean(0)
             # the output's rounding; sums of n equal weights in fp32
             assert (np.abs(out[t, 2 * h:2 * h + 2] - want) <= 2.0 ** -8 * np.abs(want) + n * 2.0 ** -23 * mass).all(), (h, t)
+
+
+@pytest.mark.parametrize("G", [2, 7])
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_a_query_that_is_no_number_selects_like_nan(bad, G):
+    # keys of one sign and keys of zero: bounds that are zero on one side or on both
+    c = Cache([[16 * 50] * 4], 16, bounds=True)
+    k, v, off = c.fill()
+    k = k.view(4, -1, 128).clone()
+    k[0], k[1], k[2, ::3] = k[0].abs(), -k[1].abs(), 0.0
+    k[:2, 100:300, ::2] = 0.0
+    binding.paged_append(c.pages, k.view(-1, 128), v, offsets=off, max_new=800)
+    q = queries(1, 1, 4 * G, "bf16", 3)
+    q[0, 0, G - 1::G, 20] = bad
+    for first, last in ((0, 0), (1, 2)):
+        lists, _ = binding.paged_select(c.pages, q, 7, keep_first=first, keep_last=last)
+        assert np.array_equal(lists.cpu().numpy(), oracle_select(c, q, 1, G, 7, first, last))
+        assert lists[0, 0].tolist() == ([0, 1, 2, 3, 4, 5, 6] if not last else [0, 1, 2, 3, 4, 48, 49])
