@@ -335,7 +335,7 @@ enum { MIXKV_TYPE_BF16 = 0, MIXKV_TYPE_FP16 = 1 };
 typedef struct mixkv_pages {
   void* pool;            /* device, 16-byte aligned: page p at p * mixkv_paged_page_bytes */
   void* bounds_opt;      /* device fp16 [num_pages, 2, 128], 16-byte aligned, or NULL: elementwise minimum and maximum of
-                            the K values of a page, without k_scale (exact) */
+                            the K values that a page has had since it began, without k_scale (exact) */
   const int32_t* table;  /* device [batch, kv_heads, max_pages]: page of a head's rows p * page_rows .. */
   const int32_t* rows;   /* device [batch, kv_heads]: rows of every head, those that a call appends included */
   int64_t num_pages;     /* pages in the pool */
@@ -371,7 +371,10 @@ int mixkv_paged_page_bytes(int32_t page_rows, size_t* bytes);
  * x / (scale k_scale), ties to the even code, largest magnitude 6 (the sign of a code of zero is not defined); a block of zeros, or one that is too small for e4m3,
  * is zero; one that holds a NaN is NaN.  Every operation is rounded by itself, so codes are the same wherever
  * they are computed.
- * Bounds (if there are any) of a page that begins with a new row are set, those of a page that had rows are widened.
+ * Bounds (if there are any) of a page that begins with a new row are set, those of a page that had rows are widened.  Rows are taken back
+ * (a draft's rejected tokens) by counting them out of c->rows; the next append writes over them.  Bounds of a page that keeps rows are
+ * not narrowed: they hold for the rows there are, as wide as for those that were taken back too, until the page begins anew (with a NaN
+ * among these the page is selected first until then).
  * Pages are written by one call at a time.  A token whose page (table entry outside the pool, row beyond the table or
  * below zero), position or place in k lies outside, and one beyond max_new, gives MIXKV_ERR_INVALID_ARG in *status_dev and is not
  * written. */

@@ -787,3 +787,37 @@ def test_a_query_that_is_no_number_selects_like_nan(bad, G):
         lists, _ = binding.paged_select(c.pages, q, 7, keep_first=first, keep_last=last)
         assert np.array_equal(lists.cpu().numpy(), oracle_select(c, q, 1, G, 7, first, last))
         assert lists[0, 0].tolist() == ([0, 1, 2, 3, 4, 5, 6] if not last else [0, 1, 2, 3, 4, 48, 49])
+
+
+def test_rows_that_are_taken_back():
+    # a draft of six tokens behind 29 rows (pages of 16), of which two are kept; then four others.  Rows and attention are those of a
+    # cache that never saw the rejected ones; bounds of the page that kept rows cover them as well, those of the page that begins anew do not
+    H, G, page = 2, 4, 16
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((39, H, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    kept = list(range(31)) + list(range(35, 39))
+    for nan in (False, True):
+        if nan:
+            k[31, 1, 9] = float("nan")        # the first rejected token, row 31 of the second page
+        c, clean = (Cache([[35, 35]], page, bounds=True, seed=1) for _ in range(2))
+
+        def put(cache, rows, tokens):
+            cache.pages.rows.fill_(rows)
+            off = torch.tensor([0, len(tokens)], dtype=torch.int32, device="cuda")
+            binding.paged_append(cache.pages, k[tokens], v[tokens], offsets=off)
+
+        put(c, 29, list(range(29)))
+        put(c, 35, list(range(29, 35)))
+        put(c, 35, kept[31:])
+        put(clean, 35, kept)
+        q = queries(1, 4, H * G, "bf16")
+        assert torch.equal(binding.paged_attention(c.pages, q), binding.paged_attention(clean.pages, q))
+        values = plain.values(*plain.quantise(f32(k)))
+        for h in range(H):
+            ids = c.table[0, h]
+            got = c.pages.bounds.double().cpu().numpy()[ids]
+            had = [kept[:16], kept[16:31] + [31, 35], kept[32:]]     # (row 31: the rejected token, then the one that took its place)
+            for p, rows in enumerate(had):
+                assert np.array_equal(got[p], [values[rows, h].min(0), values[rows, h].max(0)], equal_nan=True)
+            lists, _ = binding.paged_select(c.pages, q[:, :1], 1, keep_first=0, keep_last=0)
+            assert not (nan and h) or lists[0, 1].tolist() == [1]
