@@ -29,7 +29,6 @@ struct Divider {
     if (l) mul = (uint32_t)((1ull << (31 + l)) / by + 1), shift = l - 1;
   }
   __device__ __forceinline__ int div(const int n) const { return mul ? (int)(__umulhi((uint32_t)n, mul) >> shift) : n; }
-  __device__ __forceinline__ int mod(const int n) const { return n - div(n) * (int)d; }
 };
 
 // What kernels take of a mixkv_pages.
@@ -71,19 +70,6 @@ inline int check_pages(const mixkv_pages* c, PagePool* p) {
 __device__ __forceinline__ unsigned char* tile_ptr(const PagePool& p, const int id, const int t) {
   return p.pool + (long long)(id * p.tiles + t) * kTileBytes;
 }
-
-template <typename T>
-__device__ __forceinline__ float to_f32(T x);
-template <>
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <>
-__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
-template <typename T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half from_f32(float x) { return __float2half_rn(x); }
 
 // Two adjacent 16-bit values of a word, widened.
 template <typename T>

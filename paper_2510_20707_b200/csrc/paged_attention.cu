@@ -541,7 +541,6 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
         const int r = 8 * nt + 2 * t + c;
         if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
       }
-    auto out_at = [&](const int row) { return out_row(a, u, row); };
     const bool whole = shares ? lo <= starts[u] && end == starts[u + 1] : S == 1;
     const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
 #pragma unroll
