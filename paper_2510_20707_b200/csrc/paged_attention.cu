@@ -141,9 +141,13 @@ __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, cons
 __device__ __forceinline__ void add_scaled(float4& sum, const float4& x, const float by) {
   sum.x = fmaf(x.x, by, sum.x), sum.y = fmaf(x.y, by, sum.y), sum.z = fmaf(x.z, by, sum.z), sum.w = fmaf(x.w, by, sum.w);
 }
+// Four outputs: sums of weighted values over the sum of weights (zeros where there were none), times v_scale.  (The quotient of the two
+// factors could be subnormal.)
 template <typename T>
-__device__ __forceinline__ void store_row(T* to, const float4& x, const float by) {   // four values times `by`
-  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(x.x * by, x.y * by), narrow2<T>(x.z * by, x.w * by));
+__device__ __forceinline__ void store_row(T* to, const float4& num, const float den, const float v_scale) {
+  const float by = den == 0.f ? 0.f : 1.f / den;
+  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(num.x * by * v_scale, num.y * by * v_scale),
+                                             narrow2<T>(num.z * by * v_scale, num.w * by * v_scale));
 }
 
 // The first `keep` of the four scales of a word, zeros for the others.
@@ -569,7 +573,7 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
           den = fmaf(wz[w * Q + r], sc, den);
         }
         if (whole) {
-          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den == 0.f ? 0.f : a.p.v_scale / den);
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, a.p.v_scale);
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
           *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
@@ -608,7 +612,7 @@ __global__ void __launch_bounds__(32 * W, att_per_sm(NT, W)) k_paged_attention(c
         add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc);
         den = fmaf(allz[k * Q + r], sc, den);
       }
-      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den == 0.f ? 0.f : a.p.v_scale / den);
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, a.p.v_scale);
     }
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
     return;
@@ -676,7 +680,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_paged_join(const AttArgs a,
       den = fmaf(mz.y, sc, den);
     }
   }
-  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den == 0.f ? 0.f : a.p.v_scale / den);
+  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den, a.p.v_scale);
 }
 
 using AttKernel = void (*)(AttArgs);

@@ -821,3 +821,39 @@ def test_rows_that_are_taken_back():
                 assert np.array_equal(got[p], [values[rows, h].min(0), values[rows, h].max(0)], equal_nan=True)
             lists, _ = binding.paged_select(c.pages, q[:, :1], 1, keep_first=0, keep_last=0)
             assert not (nan and h) or lists[0, 1].tolist() == [1]
+
+
+@pytest.mark.parametrize("ks,vs", [(1.0, 1e-37), (1e-37, 1e30), (1.3, 0.7), (1e3, 1e-30)])
+@pytest.mark.parametrize("lens", [[[700, 33]], [[9000, 5000]], [[300] * 4] * 40])
+def test_caches_of_any_scale(lens, ks, vs):
+    # rows whose K is of the size of k_scale, V of that of v_scale, attended to by queries that make logits of ordinary size, over
+    # clusters, shares and single CTAs: outputs of the size of v_scale, with the error of ordinary ones
+    lens = np.array(lens)
+    c = Cache(lens, 32, ks=ks, vs=vs, seed=2)
+    n, off = int(lens.sum()), torch.from_numpy(np.concatenate([[0], lens.reshape(-1).cumsum()]).astype(np.int32)).cuda()
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((n, 128), generator=gen, device="cuda") for _ in range(2))
+    binding.paged_append(c.pages, (k * ks).bfloat16(), (v * vs).bfloat16(), offsets=off, max_new=int(lens.max()))
+    B, H = lens.shape
+    q = (torch.randn((B, 1, 3 * H, 128), generator=gen, device="cuda") / ks).bfloat16()
+    out = binding.paged_attention(c.pages, q).double().cpu().numpy() / vs
+    qf = q.double().cpu().numpy() * ks
+    for b, h in {(0, 0), (B - 1, H - 1)}:
+        K, V = plain.get_rows(c.pool(), c.table[b, h], 32, int(lens[b, h]))
+        want, mass, size = plain.attention(qf[b, :, 3 * h:3 * h + 3], K, V, 1, 1 / np.sqrt(128))
+        off_by = 2.0 ** -23 * 128 * size[..., None] + 2.0 ** -20
+        tol = 2.0 ** -8 * np.abs(want) + mass * (2.0 ** -11 + 2 * off_by) + lens[b, h] * 2.0 ** -31 * np.abs(V).max()
+        assert (np.abs(out[b, :, 3 * h:3 * h + 3] - want) <= tol).all(), (b, h)
+
+
+@pytest.mark.parametrize("lens", [[[70000]], [[900, 7]], [[4000, 4000]]])
+def test_many_equal_weights_at_the_least_scale(lens):
+    # (the quotient of the least scale and a sum of weights is subnormal; the output is not)
+    lens, vs = np.array(lens), float(np.finfo(np.float32).tiny)
+    c = Cache(lens, 64, vs=vs, seed=2)
+    n, off = int(lens.sum()), torch.from_numpy(np.concatenate([[0], lens.reshape(-1).cumsum()]).astype(np.int32)).cuda()
+    k, v = torch.ones((n, 128), device="cuda").bfloat16(), torch.full((n, 128), 3 * vs, device="cuda").bfloat16()
+    binding.paged_append(c.pages, k, v, offsets=off, max_new=int(lens.max()))
+    out = binding.paged_attention(c.pages, torch.zeros((1, 1, 2 * lens.shape[1], 128), dtype=torch.bfloat16, device="cuda"))
+    V = c.rows_of(0, 0)[1]
+    assert (np.abs(out.double().cpu().numpy() - V[0, 0]) <= 2.0 ** -8 * V[0, 0]).all() and (V == V[0, 0]).all()
