@@ -394,8 +394,9 @@ int mixkv_paged_read(const mixkv_pages* c, void* k_out, void* v_out, int32_t typ
 /* Pages of every (sequence, KV head) that a query would miss most: a page's score is the largest, over the query rows
  * of the head, of sum_d max(q_d lo_d, q_d hi_d), with lo and hi its bounds: no key of the page has a larger product with q.
  * The 128 terms are summed as neighbouring pairs, seven times over, in fp32 (the products are exact, for queries up to 1e35): the
- * same scores wherever they are computed.  A query row that holds a NaN or an infinity has a score of NaN.  The first keep_first and the last keep_last pages go first, then NaN, then by score; ties go to the
- * lower page.
+ * same scores wherever they are computed.  A query row that holds a NaN or an infinity has a score of NaN; a page outside the pool
+ * counts as one whose bounds are zero.  The first keep_first and the last keep_last pages go first, then NaN, then by score; ties go
+ * to the lower page.
  *   q               device, type `type`: [batch, q_tokens, kv_heads * gqa_ratio, 128], strides in elements of the first
  *                   two dimensions (multiples of 8), 16-byte aligned
  *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call

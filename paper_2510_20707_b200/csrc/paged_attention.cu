@@ -11,13 +11,16 @@
 //
 // Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a
 // step instead of a reduction); weights are fp16 times 2^kLift, so that what is 2^-20 of the largest is still a normal
-// number; sums are fp32.
+// number; sums are fp32.  The weights enter the sum of values as ONE fp16 number, the sum of weights unrounded.  As two parts they
+// double the products of the values: 256 heads of 1021 to 16384 rows 82.7 us a call for 75.9, a draft of 35 query rows 36.7 for 31.1.  What
+// that would buy is seen in fp16 outputs alone, 2.1e-4 from 64 bits (their own rounding) in place of 2.8e-4 with the draft; bf16 outputs
+// are 1.7e-3 from them in both.
 //
-// What bounds it.  A row pair is 144 bytes; a tile of 16 costs a warp about 260 instructions: 64 conversions (two clocks each, as the
-// fp16 products), 64 products with scales, 16 matrix instructions (eight clocks), 16 selects.  256 heads of 1021 to 16384 rows (329 MB)
-// take 72 us in this kernel: 4.5 TB/s, an instruction issued in 60 % of the clocks, the arithmetic pipe busy in 54, the tensor
-// pipe in 26; the same copies without the arithmetic take 57 us.  Two tiles a softmax step instead of one: 293 for 347 instructions a tile,
-// and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as fast as sixteen with 128;
+// What bounds it.  A row pair is 144 bytes; a tile of 16 costs a warp 303 instructions (43.3 M for 142 848 tiles): 64 conversions (two
+// clocks each, as the fp16 products), 64 products with scales, 16 matrix instructions (eight clocks), 16 selects.  256 heads of 1021 to
+// 16384 rows (329 MB) take 74 us in this kernel under the profiler: 4.5 TB/s, an instruction issued in 60 % of the clocks, the arithmetic
+// pipe busy in 52, the tensor pipe in 25; the same copies without the arithmetic take 57 us.  Two tiles a softmax step instead of one: 54
+// instructions a tile fewer, and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as fast as sixteen with 128;
 // asking for values ahead of the vote, one copy for two tiles that follow one another, rings of three: no gain.  With query rows on
 // the sixteen side, one tile a step and a chunk per CTA the same call took 129 us, and now 76.
 #include <cfloat>
@@ -49,6 +52,11 @@ __host__ __device__ constexpr size_t att_smem(int NT, int W) {
   return W * (kAttDepth * kStepBytes + 8 * NT * kAttPitch * 4) + (2 * W + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
          W * kAttDepth * 16 + 16;
 }
+// CTAs of an SM, which sets the registers of a thread.  One group of query rows: comment above.  Two groups: three CTAs of 168 registers
+// spill 124 bytes, two spill nothing and are 2 to 10 % faster (16 query rows, us: 64 heads of 4096 rows 20.7 with three, 18.6 with two, 256
+// of 2048 35.5 and 32.9, of 8192 95.4 and 93.4): not taken so far.  Three groups: two CTAs of 249 registers, no spills; three spill 544
+// bytes (24 rows, 256 heads of 2048: 42.4 with two, 62.2 with three).  Four: 255 registers, the most there are, spill 348 bytes with two,
+// 1760 with three (32 rows: 59.1 and 155.7).
 __host__ __device__ constexpr int att_per_sm(int NT, int W) { return W > kAttWarps ? 1 : NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 
 struct AttArgs {
