@@ -378,9 +378,10 @@ def paged_append(pages: Pages, k: torch.Tensor, v: torch.Tensor, offsets: Option
     offsets[b + 1] - 1`` (int32 device tensor), at most ``max_new`` of them (default: the rows of k; a bound near the longest
     range launches fewer CTAs); without offsets one per sequence.  Or compact rows [rows, 128] with an offset per
     (sequence, head): ``K_out``, ``V_out`` and ``out_row_offsets`` of :func:`compress_layer`.  Rows are taken back (rejected
-    tokens of a draft) by counting them out of ``pages.rows``; bounds of a page that keeps rows stay as wide as they were.  With ``cos`` and ``sin``
-    [length, rot_dim / 2] fp32, K is rotated by the tables' rows ``positions`` (int32, one per token).  ``status``: an int32
-    device word, zeroed by the caller, that receives MIXKV_ERR_INVALID_ARG for rows without a place or beyond ``max_new``."""
+    tokens of a draft) by counting them out of ``pages.rows``; bounds of a page that keeps rows stay as wide as they were.
+    With ``cos`` and ``sin`` [length, rot_dim / 2] fp32, K is rotated by the tables' rows ``positions`` (int32, one per
+    token).  ``status``: an int32 device word, zeroed by the caller, that receives MIXKV_ERR_INVALID_ARG for rows without a
+    place or beyond ``max_new``."""
     if max_new is None:
         max_new = 1 if offsets is None else max(1, k.size(0))
     (_host_module or _host()).paged_append(pages, k, v, offsets, max_new, cos, sin, positions, interleaved, status, stream)

@@ -20,9 +20,9 @@
 // clocks each, as the fp16 products), 64 products with scales, 16 matrix instructions (eight clocks), 16 selects.  256 heads of 1021 to
 // 16384 rows (329 MB) take 74 us in this kernel under the profiler: 4.5 TB/s, an instruction issued in 60 % of the clocks, the arithmetic
 // pipe busy in 52, the tensor pipe in 25; the same copies without the arithmetic take 57 us.  Two tiles a softmax step instead of one: 54
-// instructions a tile fewer, and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as fast as sixteen with 128;
-// asking for values ahead of the vote, one copy for two tiles that follow one another, rings of three: no gain.  With query rows on
-// the sixteen side, one tile a step and a chunk per CTA the same call took 129 us, and now 76.
+// instructions a tile fewer, and 8 % of the time of such calls, 10 % with 32 query rows.  Twelve warps an SM with 159 registers are as
+// fast as sixteen with 128; asking for values ahead of the vote, one copy for two tiles that follow one another, rings of three: no gain.
+// With query rows on the sixteen side, one tile a step and a chunk per CTA the same call took 129 us, and now 76.
 #include <cfloat>
 
 #include <cooperative_groups.h>
