@@ -587,8 +587,7 @@ def test_what_changes_from_step_to_step_is_read_anew():
 
 @pytest.mark.parametrize("pages,top,G", [(40, 6, 2), (700, 3, 7), (1999, 500, 4)])
 def test_pages_of_one_score_in_every_head(pages, top, G):
-    # the search for the threshold has nothing to take apart: equal scores, a query of NaN, or every page kept; over and over, with
-    # every word of the lists as before the first call where none is due
+    # the search for the threshold has nothing to take apart: equal scores, a query of NaN, or every page kept
     B, H, page = 4, 8, 16
     c = Cache(np.full((B, H), pages * page), page, bounds=True)
     c.pages.bounds.fill_(1.0)
