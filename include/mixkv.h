@@ -429,6 +429,102 @@ int mixkv_paged_attention(const mixkv_pages* c, const void* q, int32_t type, int
                           int32_t max_rows, const int32_t* page_list_opt, const int32_t* counts_opt, int32_t top,
                           void* workspace, size_t workspace_bytes, void* out, void* stream);
 
+/* A paged KV cache held in 8 bits that keeps count of attention: closer to the 16-bit rows than the 4-bit pages above, and with an
+ * eviction that keeps what has been attended to most while the model answers (no counterpart in the paper, whose selection ends with
+ * prefill).  Pages, table and rows are as in mixkv_pages.
+ *
+ * Format.  A page is a run of tiles of 16 rows, MIXKV_CACHE8_TILE_BYTES each.  A tile is a block: a value is a code of 8 bits times
+ * the block's scale, one for its 16 rows of K and one for those of V.  Row r of a tile has the code of dimension d of K at
+ * 128 r + 16 ((d >> 4) ^ (r & 7)) + (d & 15) and of V 2048 bytes behind; the fp32 scale of K is at 4096, that of V at 4100, and eight
+ * bytes behind them have no meaning.  Codes are int8 (-127 .. 127: equal steps, finer where no few dimensions are far larger than the
+ * others) or e4m3 (a relative error of at most 2^-4 for each value above scale / 64).
+ * Rounding: scale = max |x| c with c the fp32 number nearest to 1 / 127 or 1 / 448, product in fp32, zero if below 2^-126; code = the
+ * nearest to the fp32 product of x and the rounded reciprocal of the scale, ties to even (int8) or to the even code (e4m3).  A block
+ * that gets a NaN or an infinity has a scale of NaN, and so all its values, until it begins anew.  Every operation is rounded by
+ * itself: codes are the same wherever they are computed. */
+enum { MIXKV_CODE_INT8 = 0, MIXKV_CODE_E4M3 = 1 };
+#define MIXKV_CACHE8_TILE_BYTES 4112
+#define MIXKV_CACHE8_MAX_QUERIES 128  /* q_tokens * gqa_ratio */
+
+typedef struct mixkv_cache8 {
+  void* pool;            /* device, 16-byte aligned: page p at p * mixkv_cache8_page_bytes */
+  float* mass_opt;       /* device [num_pages, page_rows] or NULL: accumulated attention weight of every row */
+  const int32_t* table;  /* device [batch, kv_heads, max_pages]: page of a head's rows p * page_rows .. */
+  int32_t* rows;         /* device [batch, kv_heads]: rows of every head, those that a call appends included */
+  int64_t num_pages;     /* pages in the pool */
+  int32_t max_pages;     /* columns of the table */
+  int32_t page_rows;     /* a multiple of 16, at most 256 */
+  int32_t batch, kv_heads;
+  int32_t head_dim;      /* 128 */
+  int32_t code;          /* MIXKV_CODE_* */
+} mixkv_cache8;
+
+/* Bytes of a page.  Host-only. */
+int mixkv_cache8_page_bytes(int32_t page_rows, size_t* bytes);
+
+/* Appends rows to the cache, as mixkv_paged_append does (the caller counts them into c->rows first; K comes as it is to be
+ * attended to): tokens offsets[b] .. offsets[b + 1] - 1 of k and v are the last rows of sequence b, or with offsets_per_head of one
+ * head.  Strides in elements, multiples of 16; k and v 32-byte aligned.
+ * Rows that join a block which has rows: its scale becomes the larger of its own and that of the new rows, and if it grows, the codes of
+ * its old rows are rounded again, from fp32(code * old scale).  A block that begins with a new row is set, whatever was there.  The mass
+ * of new rows (if there is any) is set to zero.
+ * Rows are taken back (a draft's rejected tokens) by counting them out of c->rows; the scale of a block that keeps rows stays.
+ * Of more than max_new new rows of a head the last are written.  These others, and tokens whose place (table entry outside the pool, row
+ * beyond the table or below zero, token not in k) does not exist, are not written and give MIXKV_ERR_INVALID_ARG in *status_dev.
+ * Pages are written by one call at a time. */
+int mixkv_cache8_append(const mixkv_cache8* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
+                        int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
+                        const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, int32_t* status_dev,
+                        void* stream);
+
+/* The last n rows of every head back as dense rows, fp32(code * scale) rounded to `type`; arguments as in mixkv_paged_read. */
+int mixkv_cache8_read(const mixkv_cache8* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
+                      const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, void* stream);
+
+/* Workspace of a mixkv_cache8_attention call with these arguments, or with a smaller max_rows.  With accumulate it holds the
+ * logits of all rows that a call sees: 4 bytes for each of the query rows (an even number) and every row of every head, as if all
+ * heads had the most that max_rows, or sinks and window, let them see.  Asks the device for its SMs. */
+int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows, int32_t window,
+                                int32_t sinks, int32_t accumulate, size_t* bytes);
+
+/* softmax(q K^T scale) V over the cache: q_tokens new tokens per sequence, the last of its rows (append theirs first).  Token t
+ * is row p = rows - q_tokens + t of its KV head and attends to rows j <= p; with window > 0 to those of them that have j < sinks or
+ * j > p - window: the last `window` rows, itself included, and the first `sinks` (rows are counted in the cache: what was evicted has
+ * no place).  A token that has no row gets zeros.
+ *   q               device, type `type`: [batch, q_tokens, kv_heads * gqa_ratio, 128], strides in elements of the first
+ *                   two dimensions (multiples of 8), 16-byte aligned; q_tokens * gqa_ratio <= MIXKV_CACHE8_MAX_QUERIES
+ *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call.  It steers how the rows of a head are
+ *                   split
+ *   accumulate      nonzero: adds to the mass of every row that a query row sees the weights it got, of all tokens and heads of
+ *                   the group (needs c->mass_opt; sums in one order, the same every time)
+ *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned
+ * Logits, softmax statistics and sums are fp32, the weights enter the value sum as fp16 and the mass as fp32.  softmax_scale 0 means
+ * 1 / sqrt(128).  A page outside the pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that
+ * sees a NaN, is NaN (as is the mass of the rows it sees), and so is what a wait inside the kernel ran out on (there is no status
+ * word). */
+int mixkv_cache8_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
+                           int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
+                           int32_t max_rows, int32_t window, int32_t sinks, int32_t accumulate, void* workspace,
+                           size_t workspace_bytes, void* out, void* stream);
+
+/* Eviction by accumulated attention weight: of every head the first keep_first rows, the last keep_last and, of the others, those of
+ * the largest mass are written to `into`, in their order: min(rows, budget) of them.  A NaN ranks above every number, ties go
+ * to the lower row.  c stays as it is (its pages may be shared with other sequences); the pages of `into` must not be among those that
+ * c's rows lie on.  Kept rows are read as fp32(code * scale) and written as an append to an empty cache writes them; their mass goes with
+ * them (if into->mass_opt is given), and into->rows is set.
+ *   into            batch, kv_heads, code as in c; its own table and rows; the pool and the page size may be c's
+ *   budget          rows to keep of a head, at least keep_first + keep_last and 1
+ *   budgets_opt     device int32 [batch, kv_heads] or NULL: budgets of the heads' own, used as
+ *                   min(max(value, keep_first + keep_last), budget)
+ *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call
+ *   idx             out, device int32 [batch, kv_heads, budget]: rows that were kept, ascending, -1 behind the last
+ *   status_dev      device int32, optional: MIXKV_ERR_INVALID_ARG where a kept row has no place in `into` (its table names no page
+ *                   of the pool, or is too short); that row is not written
+ * Needs c->mass_opt.  A row on a page outside c's pool has a mass below all others and is zeros if it is kept. */
+int mixkv_cache8_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
+                       int32_t keep_first, int32_t keep_last, int32_t max_rows, int32_t* idx, int32_t* status_dev,
+                       void* stream);
+
 /* Number of kernels one mixkv_compress_layer[s] call WITH events enqueues, and the name of the
  * i-th of them (NULL when i is out of range), for the measurement hook.  The route depends on the
  * shape: fixed budgets take three kernels (pass1, pass2, tail; max pooling adds poolsum) while

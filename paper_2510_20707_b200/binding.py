@@ -43,7 +43,9 @@ EXPORTS = ("mixkv_default_params", "mixkv_workspace_size", "mixkv_scores", "mixk
            "mixkv_similarity_workspace_size", "mixkv_similarity_map", "mixkv_decode_attention",
            "mixkv_selftest_bounded_wait", "mixkv_launches_for", "mixkv_stage_name_for",
            "mixkv_device_check", "mixkv_paged_page_bytes", "mixkv_paged_append", "mixkv_paged_read",
-           "mixkv_paged_select", "mixkv_paged_workspace_size", "mixkv_paged_attention")
+           "mixkv_paged_select", "mixkv_paged_workspace_size", "mixkv_paged_attention",
+           "mixkv_cache8_page_bytes", "mixkv_cache8_append", "mixkv_cache8_read", "mixkv_cache8_workspace_size",
+           "mixkv_cache8_attention", "mixkv_cache8_evict")
 
 
 class MixKVError(RuntimeError):
@@ -65,6 +67,12 @@ class _CPages(C.Structure):
                 ("num_pages", C.c_int64), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
                 ("batch", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
                 ("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+class _CCache8(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("mass_opt", C.c_void_p), ("table", C.c_void_p), ("rows", C.c_void_p),
+                ("num_pages", C.c_int64), ("max_pages", C.c_int32), ("page_rows", C.c_int32),
+                ("batch", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("code", C.c_int32)]
 
 
 @dataclass
@@ -104,6 +112,21 @@ class Pages:
     bounds: Optional[torch.Tensor] = None
     k_scale: float = 1.0
     v_scale: float = 1.0
+
+
+@dataclass
+class Cache8:
+    """A paged 8-bit KV cache (``mixkv_cache8`` in include/mixkv.h, which gives the format): pool [pages, bytes of a page] uint8,
+    table [batch, kv_heads, columns] int32, rows [batch, kv_heads] int32 (those that a call appends included), code ``"int8"`` or
+    ``"e4m3"``, mass [pages, page_rows] fp32 or None: the attention weight that every row has gathered (eviction needs it).  The
+    tensors are the caller's, which gives pages out and counts rows; :func:`new_cache8` makes them for a cache whose heads own their
+    pages from the start."""
+    pool: torch.Tensor
+    table: torch.Tensor
+    rows: torch.Tensor
+    page_rows: int
+    code: str = "int8"
+    mass: Optional[torch.Tensor] = None
 
 
 _lib: Optional[C.CDLL] = None
@@ -164,6 +187,13 @@ def load_library() -> C.CDLL:
         lib.mixkv_paged_workspace_size.argtypes = [C.POINTER(_CPages), i32, i32, C.POINTER(sz)]
         lib.mixkv_paged_attention.argtypes = [C.POINTER(_CPages), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float, i32,
                                               vp, vp, i32, vp, sz, vp, vp]
+        lib.mixkv_cache8_page_bytes.argtypes = [i32, C.POINTER(sz)]
+        lib.mixkv_cache8_append.argtypes = [C.POINTER(_CCache8), vp, vp, i32] + [C.c_int64] * 5 + [vp, i32, i32, vp, vp]
+        lib.mixkv_cache8_read.argtypes = [C.POINTER(_CCache8), vp, vp, i32, C.c_int64, vp, i32, i32, vp]
+        lib.mixkv_cache8_workspace_size.argtypes = [C.POINTER(_CCache8)] + [i32] * 6 + [C.POINTER(sz)]
+        lib.mixkv_cache8_attention.argtypes = [C.POINTER(_CCache8), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float] + [
+            i32] * 4 + [vp, sz, vp, vp]
+        lib.mixkv_cache8_evict.argtypes = [C.POINTER(_CCache8), C.POINTER(_CCache8), i32, vp, i32, i32, i32, vp, vp, vp]
         lib.mixkv_selftest_bounded_wait.argtypes = [vp, vp, vp]
         lib.mixkv_stage_name.restype = C.c_char_p
         lib.mixkv_stage_name.argtypes = [C.POINTER(_CParams), i32]
@@ -405,7 +435,7 @@ def paged_workspace(pages: Pages, q: torch.Tensor, max_rows: Optional[int] = Non
     return torch.empty((_host_module or _host()).paged_workspace_size(pages, q), dtype=torch.uint8, device=q.device)
 
 
-def _seen_rows(pages: Pages, max_rows: Optional[int]) -> int:
+def _seen_rows(pages, max_rows: Optional[int]) -> int:
     return pages.table.size(2) * pages.page_rows if max_rows is None else max_rows
 
 
@@ -432,6 +462,80 @@ def paged_sparse_attention(pages: Pages, q: torch.Tensor, top: int, max_rows: Op
     """:func:`paged_select`, then :func:`paged_attention` over what it lists, in one call -> (out, page_list, counts)."""
     return (_host_module or _host()).paged_sparse_attention(pages, q, top, _seen_rows(pages, max_rows), keep_first,
                                                             keep_last, softmax_scale, workspace, stream)
+
+
+def cache8_page_bytes(page_rows: int) -> int:
+    """mixkv_cache8_page_bytes: bytes of a page of so many rows (a multiple of 16) of one KV head."""
+    out = C.c_size_t(0)
+    rc = load_library().mixkv_cache8_page_bytes(page_rows, C.byref(out))
+    if rc != 0:
+        raise MixKVError(rc, "mixkv_cache8_page_bytes")
+    return int(out.value)
+
+
+def new_cache8(batch: int, kv_heads: int, max_rows: int, page_rows: int = 64, code: str = "int8", mass: bool = False,
+               device="cuda") -> Cache8:
+    """An empty cache with room for max_rows rows of every head.  The pages of a head follow one another in the pool; a program
+    that shares a pool between sequences fills its own table instead."""
+    n = -(-max_rows // page_rows)
+    total = batch * kv_heads * n
+    return Cache8(pool=torch.empty((total, cache8_page_bytes(page_rows)), dtype=torch.uint8, device=device),
+                  table=torch.arange(total, dtype=torch.int32, device=device).view(batch, kv_heads, n),
+                  rows=torch.zeros((batch, kv_heads), dtype=torch.int32, device=device), page_rows=page_rows, code=code,
+                  mass=torch.zeros((total, page_rows), device=device) if mass else None)
+
+
+def cache8_append(cache: Cache8, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
+                  max_new: Optional[int] = None, status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """mixkv_cache8_append: writes the last rows of every head (count them into ``cache.rows`` first), rounded to 8 bits, and sets
+    their mass to zero.  k, v, offsets, max_new and status as in :func:`paged_append`; K comes as it is to be attended to.  A
+    block of 16 rows has one scale: rows that join it may make the codes of its older rows coarser."""
+    if max_new is None:
+        max_new = 1 if offsets is None else max(1, k.size(0))
+    (_host_module or _host()).cache8_append(cache, k, v, offsets, max_new, status, stream)
+
+
+def cache8_read(cache: Cache8, tokens: int, dtype: torch.dtype = torch.bfloat16, offsets: Optional[torch.Tensor] = None,
+                max_new: Optional[int] = None, compact: bool = False, stream=None):
+    """mixkv_cache8_read: the last rows of every head as dense K, V [tokens, kv_heads, 128] (``compact``: [tokens, 128], with an
+    offset per (sequence, head)); offsets and max_new as in :func:`paged_append`.  Rows that do not exist are left as they come
+    from the allocator."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError("cache8_read gives bf16 or fp16")
+    if max_new is None:
+        max_new = 1 if offsets is None else max(1, tokens)
+    return (_host_module or _host()).cache8_read(cache, tokens, dtype == torch.float16, offsets, max_new, compact, stream)
+
+
+def cache8_workspace(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = None, window: int = 0, sinks: int = 0,
+                     accumulate: bool = False) -> torch.Tensor:
+    """A workspace for :func:`cache8_attention` calls with such arguments (or a smaller ``max_rows``); it belongs to one call at
+    a time.  With ``accumulate`` it holds the logits of every row that a call sees."""
+    return torch.empty((_host_module or _host()).cache8_workspace_size(cache, q, _seen_rows(cache, max_rows), window, sinks,
+                                                                       accumulate), dtype=torch.uint8, device=q.device)
+
+
+def cache8_attention(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = None, window: int = 0, sinks: int = 0,
+                     accumulate: bool = False, softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """mixkv_cache8_attention: q [batch, tokens, kv_heads * gqa_ratio, 128] bf16 or fp16, the newest tokens of every sequence
+    (append theirs first) -> the same shape and type.  ``max_rows``: upper bound on ``cache.rows`` (default: what the table has room
+    for).  ``window`` > 0: a token sees the last ``window`` rows up to its own, and the first ``sinks``.  ``accumulate``: what every
+    row got of the softmax's weight, over tokens and heads of the group, is added to ``cache.mass``."""
+    return (_host_module or _host()).cache8_attention(cache, q, _seen_rows(cache, max_rows), window, sinks, accumulate,
+                                                      softmax_scale, workspace, stream)
+
+
+def cache8_evict(cache: Cache8, into: Cache8, budget: int, budgets: Optional[torch.Tensor] = None, keep_first: int = 0,
+                 keep_last: int = 0, max_rows: Optional[int] = None, status: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+    """mixkv_cache8_evict: of every head the first ``keep_first`` rows, the last ``keep_last`` and the heaviest of the others, at
+    most ``budget`` in all (``budgets``, int32 [batch, kv_heads]: of every head its own, at most ``budget``), are written to ``into``, whose
+    rows are set -> idx [batch, kv_heads, budget] int32, the rows that were kept, ascending, -1 behind the last.  ``cache`` stays as it
+    is; ``into`` has pages, a table and rows of its own (its pool may be the same).  ``status``: an int32 device word, zeroed
+    by the caller, that receives MIXKV_ERR_INVALID_ARG for rows without a place in ``into``."""
+    return (_host_module or _host()).cache8_evict(cache, into, budget, budgets, keep_first, keep_last,
+                                                  _seen_rows(cache, max_rows), status, stream)
 
 
 def selftest_bounded_wait(stream=None):

@@ -1,0 +1,795 @@
+// Attention of the newest tokens over the paged 8-bit cache (format: include/mixkv.h), over all rows or over a sliding window and
+// the first rows, and the weight that every row got of it.
+//
+// A warp takes a tile of 16 cache rows per step, brought by a bulk copy into a ring of its own.  Codes become fp16 exactly; the scale
+// of a block is one number for the whole tile, so it multiplies logits and sums, not codes.  The products run as m16n8k16 with the
+// CACHE on the sixteen-row side and the query rows (tokens x heads of the group) on the eight-column side:
+//   S^T[row, query]  = K q^T      A: rows g and g + 8 of the tile, a lane their dimensions 32 t .. 32 t + 31 (k-step s: 4 s .. 4 s + 3)
+//   O^T[dim, query] += V^T P^T    A: dimensions 16 g + 2 m, + 1 of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9; P^T from S^T by a transposing move
+// Two rows of V are interleaved by byte moves before they are widened, so that a pair is two rows of one dimension.
+//
+// Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a step instead of
+// a reduction); weights are fp16 times 2^kLift, sums are fp32.  A tile's products of values start from zero and join the sums by
+// its scale: weights times scales would leave fp16's range.
+//
+// Weights of rows: what a row got is known when the sums are, so the logits go to the workspace as fp32 (R of them for a row of 257
+// bytes) and a second kernel takes the exponentials of one row's in a fixed order and adds their sum to the row's mass.
+#include <cfloat>
+
+#include <cooperative_groups.h>
+
+#include "attend.cuh"
+#include "cache8.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace mixkv {
+namespace {
+
+constexpr int kAttWarps = 4;
+constexpr int kAttDepth = 3;                   // tiles of a warp on their way or in work
+constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is not there: beyond all
+constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
+constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
+constexpr int kAttUnits = 1024;                // most units whose tiles are dealt out evenly
+constexpr int kMassTiles = 8;                  // of a CTA that adds weights up
+constexpr int kAttFew = 4, kAttFewRows = 16;   // tiles of a warp (att_shape)
+constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
+constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
+
+// rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
+// the cluster; barriers and rows of the rings
+__host__ __device__ constexpr size_t att_smem(int NT) {
+  return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
+         kAttWarps * kAttDepth * 16 + 16;
+}
+__host__ __device__ constexpr int att_per_sm(int NT) { return NT <= 2 ? 3 : 2; }
+
+struct AttArgs {
+  CachePool p;
+  const void* q;
+  long long q_batch, q_token;
+  int T, G, R;               // tokens, heads of a group, T * G
+  Divider by_group;          // of G
+  int max_rows;
+  int window, sinks;         // window 0: all rows
+  int units;
+  int ctas;                  // that share all tiles evenly; 0: a cluster has a unit
+  int per;                   // fours of outputs of a CTA of such a cluster
+  float scale_log2e;
+  int2* spans;               // [units]: first CTA with a share of a unit, times two, plus one if its run begins before the unit; last CTA
+  float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
+  float2* part_mz;           // [2 ctas][R]: (reference, sum)
+  float2* stats;             // [units][R]: (reference, 1 / sum) of a query row
+  float* logits;             // [units][cap][16][pitch], log2 units; nullptr: weights are not asked for
+  int cap, pitch;            // tiles of a unit that a call can see; query rows, made even
+  void* out;
+};
+
+// Tiles of a unit that the call sees, numbered 0 .. tiles - 1: tile i is number i, and from `sink` on i - gap.
+struct UnitTiles {
+  int n, tiles, sink, gap;
+};
+__device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
+  UnitTiles r;
+  int n = fresh(a.p.rows + u);
+  n = min(n, a.max_rows);
+  n = (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows);
+  r.n = n = max(n, 0);
+  r.tiles = (n + kBlockRows - 1) >> 4;
+  r.sink = r.tiles, r.gap = 0;
+  if (a.window > 0) {     // token 0 sees the lowest rows of the window, from n - T - window + 1 on
+    const int low = (int)max(0ll, (long long)n - a.T + 1 - a.window) >> 4, sink = (min(a.sinks, n) + kBlockRows - 1) >> 4;
+    if (low > sink) r.sink = sink, r.gap = low - sink, r.tiles -= r.gap;
+  }
+  return r;
+}
+// Rows that query row's token (of T) sees: up to `last`, and from `low` on or below the sinks.
+struct Seen {
+  int last, low;
+};
+__device__ __forceinline__ Seen seen_by(const AttArgs& a, const int n, const int token) {
+  const int p = n - a.T + token;
+  return Seen{p, a.window > 0 ? (int)max((long long)p - a.window + 1, -1ll) : -1};
+}
+
+// Place in the pool and first row of tile number `i` of a unit (-1, kNoRow: none).
+struct TileAt {
+  int tile, row;
+};
+__device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const UnitTiles& ut, const int i) {
+  if (i >= ut.tiles) return TileAt{-1, kNoRow};
+  const int t = i < ut.sink ? i : i + ut.gap, page = a.p.by_tiles.div(t), in = t - page * a.p.tiles;
+  const int id = fresh(a.p.table + (long long)u * a.p.max_pages + page);
+  if (id < 0 || id >= a.p.num_pages) return TileAt{-1, kNoRow};
+  return TileAt{id * a.p.tiles + in, t * kBlockRows};
+}
+
+// Row of the output that query row r of a unit has.
+__device__ __forceinline__ long long out_row(const AttArgs& a, const int u, const int r) {
+  const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
+  return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
+}
+// Four outputs: sums of weighted values over the sum of weights (zeros where there were none).
+template <typename T>
+__device__ __forceinline__ void store_row(T* to, const float4& num, const float den) {
+  const float by = den == 0.f ? 0.f : 1.f / den;
+  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(num.x * by, num.y * by), narrow2<T>(num.z * by, num.w * by));
+}
+__device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float den) {
+  if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, den == 0.f ? 0.f : 1.f / den);
+}
+// Token of query row r of a unit (rows of the padding: the last).
+__device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return a.by_group.div(min(r, a.R - 1)); }
+
+__device__ __forceinline__ uint32_t word_of(const uint4& v, const int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+template <typename T, int NT, bool E4M3>
+struct AttState {
+  uint32_t q[NT][8][2];     // B fragments: query row g, dimensions 32 t + 4 s .. + 3
+  float f[NT][2];           // products of codes to log2 units, without the block's scale: query rows 2 t, 2 t + 1
+  float acc[NT][8][4];      // dimensions 16 g + 2 m (0, 1), 16 g + 2 m + 1 (2, 3) of query rows 2 t, 2 t + 1
+  float ref[NT][2], z[NT][2];   // weights are 2^(logit - ref)
+  static constexpr bool IsBf16 = std::is_same<T, __nv_bfloat16>::value;
+
+  // Query rows first .. first + 8 NT - 1 of a unit.  bf16 rows are divided by a power of two that brings their largest
+  // magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it; the power goes into f.
+  __device__ __forceinline__ void start(const AttArgs& a, const int u, const int first, const int g, const int t) {
+    const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = first + 8 * nt + g;
+      uint4 raw[4];
+      const bool on = r < a.R;
+      const int token = on ? a.by_group.div(r) : 0;
+      const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
+                     (long long)(h * a.G + (on ? r - token * a.G : 0)) * kHeadDim + 32 * t;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raw[i] = on ? fresh(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
+      uint32_t bits = 0;       // magnitudes in the order of their bits, infinities and NaN above the others
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bits = __vmaxu2(bits, word_of(raw[i], e) & 0x7fff7fffu);
+      bits = max(bits & 0xffffu, bits >> 16);
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+      const float most = widen2<T>(bits).x;
+      const bool odd = !(most < INFINITY);
+      // 2^e <= most < 2^(e + 1) (subnormal: 2^-126); down = 2^-e
+      const uint32_t e = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+      const bool scaled = IsBf16 && most > 0.f && !odd;
+      const float down = scaled ? __uint_as_float((254u - e) << 23) : 1.f;
+      const float up = odd ? NAN : scaled ? __uint_as_float(e << 23) : 1.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t x = word_of(raw[i], w);
+          if constexpr (IsBf16) {
+            const float2 y = widen2<T>(x);
+            x = narrow2<__half>(y.x * down, y.y * down);
+          }
+          q[nt][2 * i + (w >> 1)][w & 1] = odd ? 0u : x;
+        }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        f[nt][c] = __shfl_sync(0xffffffffu, up, 4 * (2 * t + c)) * a.scale_log2e;
+        ref[nt][c] = kNoRef, z[nt][c] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[nt][i][c] = 0.f;
+    }
+  }
+
+  // s[2 j + c] = product of row g + 8 j of the tile and query row 8 nt + 2 t + c
+  __device__ __forceinline__ void products(const unsigned char* tile, const int g, const int t, float (&s)[NT][4]) const {
+    float odd[NT][4];      // (two chains of four instead of one of eight)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[nt][i] = odd[nt][i] = 0.f;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const unsigned char* at = tile + piece_at(g, 2 * t + half);
+      const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at + 8 * 128);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t a0, a2, a1, a3;
+        codes_to_half<E4M3>(word_of(a, w), a0, a2);
+        codes_to_half<E4M3>(word_of(b, w), a1, a3);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          mma_f16((w & 1) ? odd[nt] : s[nt], a0, a1, a2, a3, q[nt][4 * half + w][0], q[nt][4 * half + w][1]);
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[nt][i] += odd[nt][i];
+  }
+
+  // A tile whose first row is `row`, of a unit of n rows; `first`: the CTA's first query row.  edge: some query row does not see some row.
+  // logits: where they go (of row 0, the CTA's first query row), or nullptr.
+  __device__ __forceinline__ void step(const AttArgs& a, const unsigned char* tile, const int row, const bool edge, const int n,
+                                       const int first, const int lane, float* logits) {
+    const int g = lane >> 2, t = lane & 3;
+    float y[NT][4];
+    products(tile, g, t, y);
+    const float2 scale = *reinterpret_cast<const float2*>(tile + kBlockScales);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[nt][i] = __fmul_rn(y[nt][i], f[nt][i & 1] * scale.x);
+    if (edge) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int r = row + g + 8 * j;
+            if (r > see.last || (r < see.low && r >= a.sinks)) y[nt][2 * j + c] = -INFINITY;
+          }
+        }
+    }
+    if (logits) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+          if (first + 8 * nt + 2 * t < a.R)
+            *reinterpret_cast<float2*>(logits + (g + 8 * j) * a.pitch + 8 * nt + 2 * t) = make_float2(y[nt][2 * j], y[nt][2 * j + 1]);
+    }
+    // (A logit is rounded before the reference, itself a logit, is taken from it: of a product that is not, equal logits beyond 2^24 would
+    // differ from it by their last bits, whole powers of two.)
+    bool above = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) above |= __fsub_rn(y[nt][i], ref[nt][i & 1]) > kLag + kLift;
+    if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const float to = fmaxf(ref[nt][c], column_max(fmaxf(y[nt][c], y[nt][2 + c])) - kLift);
+          const float shrink = ex2(ref[nt][c] - to);
+          ref[nt][c] = to, z[nt][c] *= shrink;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
+        }
+    }
+    uint32_t p[NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[nt][i] = ex2(__fsub_rn(y[nt][i], ref[nt][i & 1])), z[nt][i & 1] += y[nt][i];
+      p[nt][0] = transpose8x8(narrow2<__half>(y[nt][0], y[nt][1]));
+      p[nt][1] = transpose8x8(narrow2<__half>(y[nt][2], y[nt][3]));
+    }
+    // A block whose values are NaN must not reach, through weights of zero, a query row that sees none of its rows.
+    bool into[NT][2];
+    const bool some = edge && scale.y != scale.y;
+    if (some) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
+          into[nt][c] = row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks);
+        }
+    }
+    uint4 v[2][2];       // 16 dimensions of rows 2 t + e + 8 h
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int o = 0; o < 2; ++o) {
+        const uint32_t sel = o ? 0x7362u : 0x5140u;
+        uint32_t a0, a1, a2, a3;
+        codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], w), word_of(v[0][1], w), sel), a0, a1);
+        codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], w), word_of(v[1][1], w), sel), a2, a3);
+        const int m = 2 * w + o;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+          mma_f16(d, a0, a1, a2, a3, p[nt][0], p[nt][1]);
+          if (some) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if (into[nt][c & 1]) acc[nt][m][c] = fmaf(d[c], scale.y, acc[nt][m][c]);
+          } else {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[nt][m][c] = fmaf(d[c], scale.y, acc[nt][m][c]);
+          }
+        }
+      }
+  }
+};
+
+// grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
+template <typename T, int NT, bool E4M3>
+__global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_attention(const AttArgs a) {
+  extern __shared__ __align__(128) unsigned char smem[];
+  constexpr int W = kAttWarps, Q = 8 * NT, kSums = Q * kAttPitch, kThreads = 32 * W, kRing = kAttDepth * kBlockBytes;
+  float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its sums where its rings were
+  static_assert(Q * kHeadDim * 4 <= W * kRing, "sums of a CTA fit the rings");
+  static_assert(kBlockBytes % 16 == 0, "tiles in the ring are 16-byte aligned");
+  float* sums = reinterpret_cast<float*>(smem + W * kRing);   // [warps][Q][pitch]
+  float* wm = sums + W * kSums;      // [warps][Q]
+  float* wz = wm + W * Q;            // [warps][Q]
+  float* xm = wz + W * Q;            // [Q]
+  float* xz = xm + Q;                        // [Q]
+  float* allm = xz + Q;                      // [8][Q]
+  float* allz = allm + kMaxCluster * Q;      // [8][Q]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(allz + kMaxCluster * Q);   // [warps][depth]
+  int* rows = reinterpret_cast<int*>(bars + W * kAttDepth);   // [warps][depth]: first rows of the tiles
+  int* abort = rows + W * kAttDepth;
+  __shared__ int starts[kAttUnits + 1];      // first tile of every unit
+  __shared__ int warp_total[W];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const bool shares = a.ctas > 0;
+  const int S = shares ? 1 : (int)cluster.num_blocks(), crank = shares ? 0 : (int)cluster.block_rank();
+  const int first = blockIdx.y * Q, live = min(Q, a.R - first);
+  uint64_t* bar = bars + warp * kAttDepth;
+  if (lane == 0) {
+    for (int d = 0; d < kAttDepth; ++d) mbar_init(&bar[d], 1);
+    mbar_init_fence();
+    if (warp == 0) *abort = 0;
+  }
+  __syncthreads();
+  pdl_wait();
+
+  // tiles lo .. hi - 1: of a cluster's unit, or of all units one after the other
+  int u = shares ? 0 : cluster_id(), lo = crank * W, hi;
+  if (shares) {
+    // first tiles of all units: a thread takes consecutive ones
+    constexpr int kEach = kAttUnits / kThreads;
+    int mine[kEach], sum = 0;
+    const int u0 = tid * kEach;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) mine[i] = u0 + i < a.units ? unit_tiles(a, u0 + i).tiles : 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sum += mine[i];
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_total[warp] = upto;
+    __syncthreads();
+    int at = upto - sum, total = 0;
+    for (int w = 0; w < W; ++w) {
+      if (w < warp) at += warp_total[w];
+      total += warp_total[w];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (u0 + i < a.units) starts[u0 + i] = at;
+      at += mine[i];
+    }
+    if (tid == 0) starts[a.units] = total;
+    __syncthreads();
+    const int share = share_of(total, a.ctas);
+    if (blockIdx.x + 1 == gridDim.x && blockIdx.y == 0) {      // (the CTA whose run is the shortest)
+      for (int i = tid; i < a.units; i += kThreads) {
+        const int from = starts[i], to = starts[i + 1], c0 = from < to ? from / share : 0;
+        a.spans[i] = from < to ? make_int2(2 * c0 + (c0 * share < from), (to - 1) / share) : make_int2(0, -1);
+      }
+    }
+    lo = blockIdx.x * share, hi = min(lo + share, total);
+    if (lo >= hi) return;
+    int x = 0, y = a.units;     // the last unit that begins at or before lo
+    while (y - x > 1) {
+      const int m = (x + y) >> 1;
+      (starts[m] <= lo ? x : y) = m;
+    }
+    u = x;
+  } else {
+    hi = unit_tiles(a, u).tiles;
+  }
+  const int stride = S * W, begin = lo + warp;
+  const int count = begin < hi ? (hi - begin + stride - 1) / stride : 0;   // tiles of this warp
+  unsigned char* ring = smem + warp * kRing;
+  int* ring_rows = rows + warp * kAttDepth;
+
+  TileAt ahead = {};      // lane l knows tile 32 n + l of the warp, 32 n the last multiple at or before `sent`
+  auto locate = [&](const int i) {
+    int f = begin + i * stride, v = u;
+    if (i >= count) return;
+    if (shares) {
+      int y = a.units;
+      while (y - v > 1) {
+        const int m = (v + y) >> 1;
+        (starts[m] <= f ? v : y) = m;
+      }
+      f -= starts[v];
+    }
+    ahead = tile_at(a, v, unit_tiles(a, v), f);
+  };
+  locate(lane);
+  int sent = 0, slot_out = 0;
+  auto send = [&]() {   // the copy of the warp's tile `sent`
+    if ((sent & 31) == 0 && sent) locate(sent + lane);
+    if (lane == (sent & 31)) {
+      uint64_t* full = &bar[slot_out];
+      ring_rows[slot_out] = ahead.row;
+      if (ahead.tile >= 0) {
+        mbar_expect_tx(full, kBlockBytes);
+        bulk_load(ring + slot_out * kBlockBytes, a.p.pool + (long long)ahead.tile * kBlockBytes, kBlockBytes, full);
+      } else {
+        mbar_arrive(full);    // nothing to come
+      }
+    }
+    ++sent, slot_out = slot_out + 1 == kAttDepth ? 0 : slot_out + 1;
+  };
+  while (sent < min(count, kAttDepth)) send();
+  int slot = 0;
+  uint32_t parity = 0;
+  bool lost = false;
+
+  for (int f = begin;;) {     // one unit after the other
+    int end = hi, from = 0;
+    if (shares) {
+      while (starts[u + 1] <= max(lo, starts[u])) ++u;    // (units without tiles)
+      end = min(hi, starts[u + 1]), from = starts[u];
+    }
+    AttState<T, NT, E4M3> st;
+    st.start(a, u, first, g, t);
+    const int n = unit_tiles(a, u).n;
+    const int clear = n - a.T + 1;                               // rows below are seen by all,
+    const int low = a.window > 0 ? seen_by(a, n, a.T - 1).low : -1;   // from here on, or among the sinks
+    float* logits = a.logits ? a.logits + (long long)u * a.cap * kBlockRows * a.pitch + first : nullptr;
+    for (; f < end && !lost; f += stride) {
+      if (!mbar_wait_warp(&bar[slot], parity, abort)) {
+        lost = true;
+        break;
+      }
+      const int row = ring_rows[slot];
+      float* to = logits ? logits + (long long)(f - from) * (kBlockRows * a.pitch) : nullptr;
+      if (row != kNoRow) {
+        const bool inside = row + kBlockRows <= clear && (row >= low || row + kBlockRows <= a.sinks);
+        st.step(a, ring + slot * kBlockBytes, row, !inside, n, first, lane, to);
+      }
+      __syncwarp();     // every lane has read the slot
+      if (sent < count) send();
+      ++slot;
+      if (slot == kAttDepth) slot = 0, parity ^= 1;
+    }
+    if (lost) {     // (once: the units that follow have no copies)
+      if (lane == 0) drain_ring(bar, kAttDepth, sent);
+      sent = 0;
+    }
+
+    pdl_launch_dependents();      // (the next kernel's CTAs, where this one's have ended)
+    // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others
+    float* own = sums + warp * kSums;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float z = column_sum(st.z[nt][c]);
+        const int r = 8 * nt + 2 * t + c;
+        if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
+      }
+    const bool whole = shares ? lo <= starts[u] && end == starts[u + 1] : S == 1;
+    const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half) __syncthreads();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+            *reinterpret_cast<float2*>(own + (8 * nt + 2 * t + c) * kAttPitch + 8 * g + 2 * m) =
+                make_float2(st.acc[nt][4 * half + m][c], st.acc[nt][4 * half + m][2 + c]);
+      __syncthreads();
+      for (int e = tid; e < live * (kHeadDim / 8); e += kThreads) {
+        const int r = e / (kHeadDim / 8), x = 4 * (e % (kHeadDim / 8)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
+        float M = kNoRef;
+#pragma unroll
+        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]);
+        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+        float den = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+          const float sc = ex2(wm[w * Q + r] - M);
+          add_scaled(num, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc);
+          den = fmaf(wz[w * Q + r], sc, den);
+        }
+        if (whole) {
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den);
+          if (dim == 0) store_stat(a, u, first + r, M, den);
+        } else if (shares) {
+          const long long at = (long long)share * a.R + first + r;
+          *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
+          if (dim == 0) a.part_mz[at] = make_float2(M, den);
+        } else {
+          *reinterpret_cast<float4*>(xo + r * kHeadDim + dim) = num;
+          if (dim == 0) xm[r] = M, xz[r] = den;
+        }
+      }
+    }
+    if (shares) {
+      if (end == hi) return;
+      __syncthreads();
+      ++u;
+      continue;
+    }
+    if (whole) return;
+
+    // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
+    cluster.sync();
+    for (int e = tid; e < S * Q; e += kThreads) {
+      const int k = e / Q, r = e % Q;
+      allm[e] = *cluster.map_shared_rank(&xm[r], k);
+      allz[e] = *cluster.map_shared_rank(&xz[r], k);
+    }
+    __syncthreads();
+    for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
+      const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
+      float M = kNoRef;
+      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+      float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+      float den = 0.f;
+#pragma unroll 4
+      for (int k = 0; k < S; ++k) {
+        const float sc = ex2(allm[k * Q + r] - M);
+        add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc);
+        den = fmaf(allz[k * Q + r], sc, den);
+      }
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den);
+      if (dim == 0) store_stat(a, u, first + r, M, den);
+    }
+    cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
+    return;
+  }
+}
+
+// Joins the shares of units that several CTAs had a part of, and writes zeros for units without rows.  per_row warps (a power
+// of two) take the shares of a query row in turn, a few at once with a running reference: what a share holds comes in one
+// round trip.
+constexpr int kJoinWarps = 16;
+template <typename T>
+__global__ void __launch_bounds__(kJoinWarps * 32) k_cache8_join(const AttArgs a, const Divider per_row, const Divider blocks) {
+  __shared__ float4 sums[kJoinWarps][32];
+  __shared__ float2 stat[kJoinWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int u = blocks.div(blockIdx.x), slot = per_row.div(warp), part = warp - slot * per_row.d;
+  const int row = (blockIdx.x - u * blocks.d) * per_row.div(kJoinWarps) + slot;      // (blocks: CTAs of a unit)
+  pdl_wait();
+  pdl_launch_dependents();
+  const int2 span = __ldcg(a.spans + u);
+  const int c0 = span.x >> 1, c1 = span.y;
+  if (c0 == c1) return;     // written by that CTA
+  const bool on = row < a.R;
+  constexpr int kAtOnce = 5;
+  float M = kNoRef, den = 0.f;
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+  for (int c = c0 + part; on && c <= c1; c += per_row.d * kAtOnce) {
+    float4 x[kAtOnce];
+    float2 mz[kAtOnce];
+    float to = M;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int k = min(c + i * (int)per_row.d, c1);
+      const long long at = (2LL * k + (k == c0 ? span.x & 1 : 0)) * a.R + row;
+      mz[i] = __ldcg(a.part_mz + at);
+      x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x);
+    const float shrink = ex2(M - to);
+    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
+    M = to;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float sc = c + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
+      add_scaled(num, x[i], sc);
+      den = fmaf(mz[i].y, sc, den);
+    }
+  }
+  if (per_row.d > 1) {
+    sums[warp][lane] = num;
+    if (lane == 0) stat[warp] = make_float2(M, den);
+    __syncthreads();
+    if (part) return;
+    float to = M;
+    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, stat[warp + w].x);
+    const float shrink = ex2(M - to);
+    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
+    for (int w = 1; w < (int)per_row.d; ++w) {
+      const float2 mz = stat[warp + w];
+      const float sc = ex2(mz.x - to);
+      add_scaled(num, sums[warp + w][lane], sc);
+      den = fmaf(mz.y, sc, den);
+    }
+    M = to;
+  }
+  if (!on) return;
+  store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den);
+  if (lane == 0) store_stat(a, u, row, M, den);
+}
+
+// The weights that the rows of a unit got, added to their mass: a thread has a row.  grid.x: units, grid.y: kMassTiles tiles of them.
+__global__ void __launch_bounds__(kMassTiles * kBlockRows) k_cache8_mass(const AttArgs a) {
+  __shared__ float2 stats[MIXKV_CACHE8_MAX_QUERIES];
+  pdl_wait();
+  const int u = blockIdx.x, i = blockIdx.y * kMassTiles + threadIdx.x / kBlockRows, r = threadIdx.x % kBlockRows;
+  const UnitTiles ut = unit_tiles(a, u);
+  if (blockIdx.y * kMassTiles >= ut.tiles) return;
+  for (int e = threadIdx.x; e < a.R; e += blockDim.x) stats[e] = __ldcg(a.stats + (long long)u * a.R + e);
+  const TileAt at = tile_at(a, u, ut, i);
+  __syncthreads();
+  if (at.tile < 0 || at.row + r >= ut.n) return;
+  const float2* row = reinterpret_cast<const float2*>(a.logits + ((long long)u * a.cap + i) * (kBlockRows * a.pitch) + r * a.pitch);
+  float sum = 0.f;
+#pragma unroll 4
+  for (int e = 0; e < a.R; e += 2) {
+    const float2 y = __ldcg(row + (e >> 1));
+    // (what a query row does not see gets nothing of it, if it is NaN either)
+    if (y.x != -INFINITY) sum = fmaf(ex2(y.x - stats[e].x), stats[e].y, sum);
+    if (e + 1 < a.R && y.y != -INFINITY) sum = fmaf(ex2(y.y - stats[e + 1].x), stats[e + 1].y, sum);
+  }
+  float* mass = a.p.mass + (long long)at.tile * kBlockRows + r;     // (a page's tiles lie one after the other in both)
+  *mass += sum;
+}
+
+using AttKernel = void (*)(AttArgs);
+template <typename T, bool E4M3>
+AttKernel att_kernel_of(const int NT) {
+  switch (NT) {
+    case 1: return k_cache8_attention<T, 1, E4M3>;
+    case 2: return k_cache8_attention<T, 2, E4M3>;
+    case 3: return k_cache8_attention<T, 3, E4M3>;
+    default: return k_cache8_attention<T, 4, E4M3>;
+  }
+}
+AttKernel att_kernel(const bool bf16, const bool e4m3, const int NT) {
+  return bf16 ? e4m3 ? att_kernel_of<__nv_bfloat16, true>(NT) : att_kernel_of<__nv_bfloat16, false>(NT)
+              : e4m3 ? att_kernel_of<__half, true>(NT) : att_kernel_of<__half, false>(NT);
+}
+
+// How the work is split.  units: (sequence, head) pairs; groups of query rows; tiles of the longest unit.  resident(n): clusters of
+// n CTAs that are resident at once.  A cluster per unit, or all tiles dealt out evenly and joined by a second kernel.
+struct AttShape {
+  int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all tiles
+};
+int att_slots(const int NT, const int sms) { return att_per_sm(NT) * sms; }
+template <typename Resident>
+AttShape att_shape(const long long units, const int groups, const long long tiles, const int NT, const int sms, const Resident& resident) {
+  const long long slots = att_slots(NT, sms), all = units * groups;
+  long long most = slots / all < kMaxCluster ? slots / all : kMaxCluster;
+  if (most > tiles / kAttWarps) most = tiles / kAttWarps;
+  int S = most < 1 ? 1 : (int)most;
+  while (S > 1 && all > resident(S)) --S;
+  const long long alone = (tiles + S * kAttWarps - 1) / (S * kAttWarps);     // tiles of a warp
+  if (alone <= (NT == 1 ? kAttFew : kAttFewRows)) return {S, 0};
+  if (units <= kAttUnits && groups < slots && units * tiles <= 0x7fffffffll) {
+    const long long want = (units * tiles + kAttWarps * 4 - 1) / (kAttWarps * 4);     // (four tiles to a warp)
+    return {1, (int)(want < slots / groups ? want : slots / groups)};
+  }
+  return {S, 0};
+}
+
+// What a call with such arguments works with: its query rows, the rows it sees, its workspace.
+struct AttPlan {
+  int R, groups, NT, cap, pitch, sms;
+  long long tiles;                    // of the longest unit
+  size_t part, spans, stats, logits, bytes;   // offsets: sums at 0, (reference, sum) at `part`
+};
+int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, const int32_t max_rows, const int32_t window,
+             const int32_t sinks, const bool accumulate, AttPlan* p) {
+  if (q_tokens < 1 || gqa < 1 || max_rows < 1 || window < 0 || sinks < 0 || (accumulate && !c->mass_opt)) return MIXKV_ERR_INVALID_ARG;
+  const long long R = (long long)q_tokens * gqa, units = (long long)c->batch * c->kv_heads;
+  if (R > MIXKV_CACHE8_MAX_QUERIES) return MIXKV_ERR_UNSUPPORTED;
+  const int eights = (int)((R + 7) / 8);
+  p->R = (int)R, p->groups = (eights + kAttGroups - 1) / kAttGroups, p->NT = (eights + p->groups - 1) / p->groups;
+  if (units * p->groups > 1 << 24) return MIXKV_ERR_UNSUPPORTED;
+  const long long room = (long long)c->max_pages * c->page_rows, seen = max_rows < room ? max_rows : room;
+  p->tiles = (seen + kBlockRows - 1) / kBlockRows;
+  if (window > 0) {     // tiles of the sinks, of the window and of the tokens behind the first, each with a ragged end
+    const long long some = ((long long)sinks + kBlockRows - 1) / kBlockRows +
+                           ((long long)window + q_tokens - 1 + kBlockRows - 2) / kBlockRows + 1;
+    if (some < p->tiles) p->tiles = some;
+  }
+  if (accumulate && p->tiles > 65535ll * kMassTiles) return MIXKV_ERR_UNSUPPORTED;
+  p->cap = (int)p->tiles, p->pitch = ((int)R + 1) & ~1, p->sms = device_sm_count();
+  const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
+  p->part = up((size_t)att_slots(p->NT, p->sms) * 2 * R * kHeadDim * 4);
+  p->spans = up(p->part + (size_t)att_slots(p->NT, p->sms) * 2 * R * sizeof(float2));
+  p->stats = up(p->spans + kAttUnits * sizeof(int2));
+  p->logits = up(p->stats + (accumulate ? (size_t)units * R * sizeof(float2) : 0));
+  p->bytes = p->logits + (accumulate ? (size_t)units * p->cap * kBlockRows * p->pitch * 4 : 0);
+  return MIXKV_OK;
+}
+
+}  // namespace
+}  // namespace mixkv
+
+using namespace mixkv;
+
+extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t eights, int32_t sms,
+                                            const int32_t* resident, int32_t* ctas, int32_t* shared) {
+  const AttShape s = att_shape(units, groups, tiles, eights, sms, [&](const int n) { return resident[n]; });
+  *ctas = s.S, *shared = s.ctas;
+}
+
+extern "C" int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows,
+                                           int32_t window, int32_t sinks, int32_t accumulate, size_t* bytes) {
+  CachePool pool;
+  AttPlan p;
+  int rc = check_cache(c, &pool);
+  if (rc != MIXKV_OK) return rc;
+  if (!bytes) return MIXKV_ERR_INVALID_ARG;
+  if ((rc = att_plan(c, q_tokens, gqa_ratio, max_rows, window, sinks, accumulate != 0, &p)) != MIXKV_OK) return rc;
+  *bytes = p.bytes;
+  return MIXKV_OK;
+}
+
+extern "C" int mixkv_cache8_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
+                                      int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
+                                      int32_t max_rows, int32_t window, int32_t sinks, int32_t accumulate, void* workspace,
+                                      size_t workspace_bytes, void* out, void* stream) {
+  AttArgs a = {};
+  AttPlan p;
+  int rc = check_cache(c, &a.p);
+  if (rc != MIXKV_OK) return rc;
+  if (!q || !out || !workspace || (type != MIXKV_TYPE_BF16 && type != MIXKV_TYPE_FP16) || !(softmax_scale >= 0.f) ||
+      !(softmax_scale < INFINITY) || q_batch_stride < 0 || q_token_stride < 0 || q_batch_stride % 8 || q_token_stride % 8)
+    return MIXKV_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16)) return MIXKV_ERR_INVALID_ARG;
+  if ((rc = att_plan(c, q_tokens, gqa_ratio, max_rows, window, sinks, accumulate != 0, &p)) != MIXKV_OK) return rc;
+  if (workspace_bytes < p.bytes) return MIXKV_ERR_WORKSPACE_TOO_SMALL;
+  if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
+  const long long units = (long long)c->batch * c->kv_heads;
+  const bool bf16 = type == MIXKV_TYPE_BF16, e4m3 = c->code == MIXKV_CODE_E4M3;
+  static std::atomic<bool> done[4 * (kAttGroups + 1)][kMaxDevices];
+  static ClusterFit fits[4 * (kAttGroups + 1)];   // (by variant, as `done`)
+  const int dev = device_slot(), variant = 4 * p.NT + 2 * e4m3 + bf16;
+  const AttKernel kernel = att_kernel(bf16, e4m3, p.NT);
+  const size_t smem = att_smem(p.NT);
+  const AttShape shape = att_shape(units, p.groups, p.tiles, p.NT, p.sms, [&](const int size) {
+    if (!answered(ensure_smem(kernel, smem, done[variant], dev))) return 0;
+    return fits[variant].ask(kernel, 32 * kAttWarps, smem, size, dev);
+  });
+  if (ensure_smem(kernel, smem, done[variant], dev) != cudaSuccess) return MIXKV_ERR_CUDA;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.q = q, a.q_batch = q_batch_stride, a.q_token = q_token_stride;
+  a.T = q_tokens, a.G = gqa_ratio, a.R = p.R, a.by_group = Divider(gqa_ratio), a.max_rows = max_rows;
+  a.window = window, a.sinks = sinks;
+  a.units = (int)units, a.ctas = shape.ctas;
+  a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e;
+  a.part = reinterpret_cast<float*>(ws), a.part_mz = reinterpret_cast<float2*>(ws + p.part);
+  a.spans = reinterpret_cast<int2*>(ws + p.spans), a.stats = reinterpret_cast<float2*>(ws + p.stats);
+  a.logits = accumulate ? reinterpret_cast<float*>(ws + p.logits) : nullptr, a.cap = p.cap, a.pitch = p.pitch;
+  a.out = out;
+  a.per = ((p.R < 8 * p.NT ? p.R : 8 * p.NT) * (kHeadDim / 4) + shape.S - 1) / shape.S;
+  const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
+  const cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = launch_pdl(kernel, dim3(grid, p.groups), dim3(32 * kAttWarps), smem, st, shape.S, a);
+  if (e == cudaSuccess && shape.ctas) {
+    int per_row = 1;      // warps that go through the shares of one query row
+    while (per_row < kJoinWarps && per_row * 2 * units < shape.ctas) per_row *= 2;
+    const int at_once = kJoinWarps / per_row, blocks = (p.R + at_once - 1) / at_once;
+    e = launch_pdl(bf16 ? k_cache8_join<__nv_bfloat16> : k_cache8_join<__half>, dim3((unsigned)(units * blocks)),
+                   dim3(kJoinWarps * 32), 0, st, 1, a, Divider(per_row), Divider(blocks));
+  }
+  if (e == cudaSuccess && accumulate) {
+    const long long chunks = (p.tiles + kMassTiles - 1) / kMassTiles;
+    e = launch_pdl(k_cache8_mass, dim3((unsigned)units, (unsigned)chunks), dim3(kMassTiles * kBlockRows), 0, st, 1, a);
+  }
+  return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
+}

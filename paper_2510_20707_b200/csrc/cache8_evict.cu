@@ -1,0 +1,258 @@
+// Eviction by accumulated attention weight (include/mixkv.h): which rows of a head are kept, and their copy into other pages.
+//
+// k_cache8_pick: a cluster has a head.  A row's mass becomes a 32-bit key in the order of the numbers; the key of the last row that is kept
+// is found by its digits (11, 11 and 10 bits), each from one histogram of the keys that share the digits before it, summed over the
+// cluster through distributed shared memory.  Keys stay in shared memory between the passes where they fit.  Then every warp has
+// a run of rows: it counts what it keeps, learns where its run begins in the list, and writes it in order.  Equal keys are taken from the
+// lowest row on, so the list does not depend on how the rows were dealt out.
+//
+// k_cache8_move: a warp has K or V of one tile of the new cache, as an append has (cache8_rows.cu), and gathers its rows.
+#include <cooperative_groups.h>
+
+#include "cache8.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace mixkv {
+namespace {
+
+constexpr int kPickThreads = 1024, kPickWarps = kPickThreads / 32;
+constexpr int kBins = 2048;
+constexpr int kPickKeys = 40960;       // keys that a CTA keeps in shared memory
+constexpr int kPickRows = 2048;        // rows that a CTA of a cluster should have
+constexpr int kMoveWarps = 4;
+
+struct EvictArgs {
+  CachePool p, into;
+  int budget;
+  const int* budgets;
+  int first, last;
+  int max_rows;
+  int cached;              // keys that fit a CTA's shared memory
+  int* idx;                // [units][budget]
+  int* status;
+  int slots;               // tiles of a budget
+  Divider by_slots;
+};
+
+// The key of a row: the order of keys is that of masses, NaN above all and a row without a page below.
+__device__ __forceinline__ uint32_t key_of(const CachePool& p, const int u, const int row) {
+  const int page = p.by_rows.div(row);
+  const int id = fresh(p.table + (long long)u * p.max_pages + page);
+  if (id < 0 || id >= p.num_pages) return 0u;
+  const float m = fresh(p.mass + (long long)id * p.page_rows + (row - page * p.page_rows)) + 0.f;      // (-0 is 0)
+  const uint32_t b = __float_as_uint(m);
+  return m != m ? 0xffffffffu : b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
+__global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a) {
+  extern __shared__ uint32_t keys[];
+  __shared__ int hist[kBins];
+  __shared__ int warp_sum[kPickWarps];
+  __shared__ int2 warp_run[kPickWarps];      // of a warp's run: keys above the threshold, keys equal to it
+  __shared__ int2 cta_run;
+  __shared__ int found[3];                   // bin, what is left to take of it, keys in it
+  cg::cluster_group cluster = cg::this_cluster();
+  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank(), u = cluster_id();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  pdl_wait();
+  int n = min(fresh(a.p.rows + u), a.max_rows);
+  n = max(0, (int)min((long long)n, (long long)a.p.max_pages * a.p.page_rows));
+  const int budget = a.budgets ? min(max(fresh(a.budgets + u), a.first + a.last), a.budget) : a.budget;
+  const int kept = min(n, budget);
+  int* idx = a.idx + (long long)u * a.budget;
+  if (rank == 0) {
+    if (tid == 0) a.into.rows[u] = kept;
+    for (int i = kept + tid; i < a.budget; i += kPickThreads) idx[i] = -1;
+  }
+  if (n <= budget) {       // (the whole cluster)
+    for (int i = rank * kPickThreads + tid; i < n; i += S * kPickThreads) idx[i] = i;
+    return;
+  }
+  // rows m0 .. m0 + m - 1 compete for k places
+  const int m0 = a.first, m = n - a.first - a.last, k = budget - a.first - a.last;
+  if (rank == 0) {
+    for (int i = tid; i < a.first; i += kPickThreads) idx[i] = i;
+    for (int i = tid; i < a.last; i += kPickThreads) idx[a.first + k + i] = n - a.last + i;
+  }
+  if (k == 0) return;
+  const int each = (m + S - 1) / S, lo = min(rank * each, m), hi = min(lo + each, m), mine = hi - lo;
+  const bool cached = mine <= a.cached;
+  auto key = [&](const int i) { return cached ? keys[i] : key_of(a.p, u, m0 + lo + i); };
+  if (cached)
+    for (int i = tid; i < mine; i += kPickThreads) keys[i] = key_of(a.p, u, m0 + lo + i);
+
+  uint32_t prefix = 0;       // digits that are known, in place
+  int left = k;
+  bool exact = false;        // all that have them are taken
+  int shift = 32;
+#pragma unroll 1
+  for (int pass = 0; pass < 3 && !exact; ++pass) {
+    const int bits = pass == 2 ? 10 : 11;
+    const uint32_t above = pass == 0 ? 0u : 0xffffffffu << shift;
+    shift -= bits;
+    for (int i = tid; i < kBins; i += kPickThreads) hist[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < mine; i += kPickThreads) {
+      const uint32_t x = key(i);
+      if ((x & above) == prefix) atomicAdd(&hist[(x >> shift) & ((1u << bits) - 1u)], 1);
+    }
+    cluster.sync();
+    // thread t has bins 2047 - 2 t and the next lower one: the sum of what is above them
+    const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
+    int n1 = 0, n0 = 0;
+    for (int r = 0; r < S; ++r) {
+      const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(&hist[b0], r));
+      n0 += x.x, n1 += x.y;
+    }
+    int upto = n0 + n1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) warp_sum[warp] = upto;
+    __syncthreads();
+    int before = upto - n0 - n1;
+    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    if (before < left && before + n1 >= left) found[0] = b1, found[1] = left - before, found[2] = n1;
+    else if (before + n1 < left && before + n1 + n0 >= left) found[0] = b0, found[1] = left - before - n1, found[2] = n0;
+    cluster.sync();          // (no CTA clears its histogram before all have read it)
+    prefix |= (uint32_t)found[0] << shift;
+    left = found[1];
+    exact = found[1] == found[2];
+  }
+  // kept: keys above `top`, and the first `left` of those equal to it
+  const uint32_t top = exact ? prefix - 1u : prefix;     // (the lowest digits of a prefix are zero; key 0 alone is never all)
+  if (exact) left = 0;
+
+  const int run = (((mine + kPickWarps - 1) / kPickWarps) + 31) & ~31, from = min(warp * run, mine), to = min(from + run, mine);
+  int above = 0, equal = 0;
+  for (int i = from; i < to; i += 32) {
+    const uint32_t x = i + lane < to ? key(i + lane) : 0u;
+    const bool in = i + lane < to;
+    above += __popc(__ballot_sync(0xffffffffu, in && x > top));
+    equal += __popc(__ballot_sync(0xffffffffu, in && x == top));
+  }
+  if (lane == 0) warp_run[warp] = make_int2(above, equal);
+  __syncthreads();
+  if (warp == 0) {
+    int2 x = warp_run[lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
+    if (lane == 0) cta_run = x;
+  }
+  cluster.sync();
+  above = equal = 0;         // of all rows before the warp's run
+  for (int r = 0; r < rank; ++r) {
+    const int2 x = *cluster.map_shared_rank(&cta_run, r);
+    above += x.x, equal += x.y;
+  }
+  for (int w = 0; w < warp; ++w) above += warp_run[w].x, equal += warp_run[w].y;
+  for (int i = from; i < to; i += 32) {
+    const bool in = i + lane < to;
+    const uint32_t x = in ? key(i + lane) : 0u;
+    const unsigned more = __ballot_sync(0xffffffffu, in && x > top), same = __ballot_sync(0xffffffffu, in && x == top);
+    const unsigned below = (1u << lane) - 1u;
+    const int g = above + __popc(more & below), e = equal + __popc(same & below);
+    if (in && (x > top || (x == top && e < left))) idx[a.first + g + min(e, left)] = m0 + lo + i + lane;
+    above += __popc(more), equal += __popc(same);
+  }
+  cluster.sync();            // a CTA's shared memory stays alive until its peers have read it
+}
+
+template <bool E4M3>
+__global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs a, const int tasks) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane & 7, sub = lane >> 3;
+  const int job = blockIdx.x * kMoveWarps + warp;
+  pdl_wait();
+  if (job >= 2 * tasks) return;
+  const bool values = job & 1;
+  const int u = a.by_slots.div(job >> 1), t = (job >> 1) - u * a.slots;
+  const int kept = min(fresh(a.into.rows + u), a.budget), begin = t * kBlockRows;
+  if (begin >= kept) return;
+  const int page = a.into.by_tiles.div(t), in = t - page * a.into.tiles;
+  const int id = page < a.into.max_pages ? fresh(a.into.table + (long long)u * a.into.max_pages + page) : -1;
+  if (id < 0 || id >= a.into.num_pages) {
+    if (a.status && lane == 0) *a.status = MIXKV_ERR_INVALID_ARG;
+    return;
+  }
+  // row `lane` of the tile (lanes 0 .. 15): its place in the old cache, -1: none
+  int row = -1;
+  long long block = -1;
+  if (lane < kBlockRows && begin + lane < kept) {
+    row = fresh(a.idx + (long long)u * a.budget + begin + lane);
+    const int from = a.p.by_rows.div(row), old = fresh(a.p.table + (long long)u * a.p.max_pages + from);
+    row -= from * a.p.page_rows;
+    if (old >= 0 && old < a.p.num_pages) block = (long long)old * a.p.tiles + (row >> 4);
+  }
+  uint4 codes[4];
+  float scale[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const long long at = __shfl_sync(0xffffffffu, block, 4 * i + sub);
+    const int r = __shfl_sync(0xffffffffu, row, 4 * i + sub) & 15;
+    codes[i] = make_uint4(0, 0, 0, 0), scale[i] = 0.f;
+    if (at >= 0) {
+      const unsigned char* tile = a.p.pool + at * kBlockBytes;
+      codes[i] = *reinterpret_cast<const uint4*>(tile + (values ? kBlockV : 0) + piece_at(r, g));
+      scale[i] = *(reinterpret_cast<const float*>(tile + kBlockScales) + values);
+    }
+  }
+  float x[4][16];
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    values16<E4M3>(codes[i], scale[i], x[i]);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(x[i][e]) & 0x7fffffffu);
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  const float to = scale_of_largest<E4M3>(__uint_as_float(most)), by = by_scale(to);
+  unsigned char* tile = block_ptr(a.into, id, in);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<uint4*>(tile + (values ? kBlockV : 0) + piece_at(4 * i + sub, g)) = encode16<E4M3>(x[i], by);
+  if (lane == 0) *(reinterpret_cast<float*>(tile + kBlockScales) + values) = to;
+  if (values && a.into.mass && lane < kBlockRows && begin + lane < kept)
+    a.into.mass[(long long)id * a.into.page_rows + in * kBlockRows + lane] =
+        block >= 0 ? fresh(a.p.mass + block * kBlockRows + (row & 15)) : 0.f;
+}
+
+}  // namespace
+}  // namespace mixkv
+
+using namespace mixkv;
+
+extern "C" int mixkv_cache8_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
+                                  int32_t keep_first, int32_t keep_last, int32_t max_rows, int32_t* idx,
+                                  int32_t* status_dev, void* stream) {
+  EvictArgs a = {};
+  int rc = check_cache(c, &a.p);
+  if (rc != MIXKV_OK || (rc = check_cache(into, &a.into)) != MIXKV_OK) return rc;
+  if (!c->mass_opt || !idx || budget < 1 || keep_first < 0 || keep_last < 0 || (long long)keep_first + keep_last > budget ||
+      max_rows < 1 || into->batch != c->batch || into->kv_heads != c->kv_heads || into->code != c->code || into->rows == c->rows ||
+      !aligned(idx, 4) || !aligned(budgets_opt, 4) || !aligned(status_dev, 4))
+    return MIXKV_ERR_INVALID_ARG;
+  const long long units = (long long)c->batch * c->kv_heads, slots = ((long long)budget + kBlockRows - 1) / kBlockRows;
+  if (budget > (1 << 30) || units * slots > 0x3fffff00ll) return MIXKV_ERR_UNSUPPORTED;
+  if ((rc = device_check(nullptr)) != MIXKV_OK) return rc;
+  a.budget = budget, a.budgets = budgets_opt, a.first = keep_first, a.last = keep_last, a.max_rows = max_rows;
+  a.idx = idx, a.status = status_dev, a.slots = (int)slots, a.by_slots = Divider((uint32_t)slots);
+  const long long room = (long long)c->max_pages * c->page_rows, rows = max_rows < room ? max_rows : room;
+  // CTAs of a head: as many as its rows are worth, and no more than two to an SM
+  int S = 1;
+  while (S < kMaxCluster && S * (long long)kPickRows < rows && units * S * 2 <= 2LL * device_sm_count()) S *= 2;
+  const long long each = (rows + S - 1) / S;
+  a.cached = (int)(each < kPickKeys ? each : kPickKeys);
+  const size_t smem = (size_t)a.cached * 4;
+  static std::atomic<bool> done[kMaxDevices];
+  if (ensure_smem(k_cache8_pick, (size_t)kPickKeys * 4, done) != cudaSuccess) return MIXKV_ERR_CUDA;
+  const cudaStream_t st = (cudaStream_t)stream;
+  cudaError_t e = launch_pdl(k_cache8_pick, dim3((unsigned)(units * S)), dim3(kPickThreads), smem, st, S, a);
+  const int tasks = (int)(units * slots);
+  if (e == cudaSuccess)
+    e = launch_pdl(c->code == MIXKV_CODE_E4M3 ? k_cache8_move<true> : k_cache8_move<false>,
+                   dim3((unsigned)((2LL * tasks + kMoveWarps - 1) / kMoveWarps)), dim3(kMoveWarps * 32), 0, st, 1, a, tasks);
+  return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
+}

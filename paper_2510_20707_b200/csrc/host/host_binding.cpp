@@ -49,6 +49,11 @@ struct Api {
   decltype(&mixkv_paged_select) paged_select;
   decltype(&mixkv_paged_workspace_size) paged_ws_size;
   decltype(&mixkv_paged_attention) paged_attention;
+  decltype(&mixkv_cache8_append) cache8_append;
+  decltype(&mixkv_cache8_read) cache8_read;
+  decltype(&mixkv_cache8_workspace_size) cache8_ws_size;
+  decltype(&mixkv_cache8_attention) cache8_attention;
+  decltype(&mixkv_cache8_evict) cache8_evict;
 } api;
 PyObject* g_error = nullptr;   // binding.MixKVError
 
@@ -58,7 +63,7 @@ struct Names {
       *budget_mode, *budget, *ada_floor, *eps, *softmax_scale, *cuda_stream;
   PyObject *s_comp, *s_ex, *s_div, *rbar, *status, *idx, *counts, *idx_offsets, *K_out, *V_out,
       *out_row_offsets;
-  PyObject *pool, *table, *rows, *page_rows, *bounds, *k_scale, *v_scale;
+  PyObject *pool, *table, *rows, *page_rows, *bounds, *k_scale, *v_scale, *mass, *code, *int8, *e4m3;
 } nm;
 
 // A Python exception is set; unwinds to the entry point.
@@ -664,11 +669,20 @@ int32_t paged_type(const at::ScalarType t) {
 // Stride of a dimension; of one element none is walked, and a view may hold any.
 int64_t step(const at::Tensor& t, const int64_t dim) { return t.size(dim) == 1 ? 0 : t.stride(dim); }
 // Offsets of the new rows: None or an int32 tensor of n + 1 words.
-const int32_t* row_offsets(PyObject* o, const int64_t n, const PagesArg& pages) {
+template <typename Cache>
+const int32_t* row_offsets(PyObject* o, const int64_t n, const Cache& pages) {
   if (o == Py_None) return nullptr;
   const at::Tensor& t = tensor(o);
   want(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n + 1 && t.device() == pages.pool().device(),
        "offsets must be a contiguous int32 tensor [batch + 1] (compact rows: [batch * kv_heads + 1]) on the pool's device");
+  return ip(t);
+}
+
+// The word that a call reports in: None or an int32 tensor.
+int32_t* status_word(PyObject* o, const at::Tensor& like) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(o);
+  want(t.scalar_type() == at::kInt && t.numel() >= 1 && t.device() == like.device(), "status must be an int32 tensor on the pool's device");
   return ip(t);
 }
 
@@ -704,12 +718,7 @@ PyObject* py_paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       want(a[6] == Py_None, "sin without cos");
     }
     const bool interleaved = truth(a[8]);
-    int32_t* status = nullptr;
-    if (a[9] != Py_None) {
-      const at::Tensor& t = tensor(a[9]);
-      want(t.scalar_type() == at::kInt && t.numel() >= 1 && t.device() == k.device(), "status must be an int32 tensor on the pool's device");
-      status = ip(t);
-    }
+    int32_t* status = status_word(a[9], k);
     const CallStream stream(a[10], k);
     const int32_t type = paged_type(k.scalar_type());
     int rc = MIXKV_OK;
@@ -759,7 +768,8 @@ PyObject* py_paged_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
 struct PagedQuery {
   const at::Tensor& q;
   int32_t type, tokens, gqa;
-  PagedQuery(PyObject* o, const PagesArg& pages) : q(tensor(o)) {
+  template <typename Cache>
+  PagedQuery(PyObject* o, const Cache& pages) : q(tensor(o)) {
     want(q.dim() == 4 && q.size(0) == pages.c.batch && pages.c.kv_heads > 0 && q.size(2) % pages.c.kv_heads == 0 && q.size(3) == 128 &&
              (q.size(2) <= 1 || q.stride(2) == 128) && q.stride(3) == 1 && q.device() == pages.pool().device(),
          "q must be [batch, tokens, kv_heads * gqa_ratio, 128], a token's heads packed, on the pool's device");
@@ -896,6 +906,222 @@ PyObject* py_paged_sparse_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
   });
 }
 
+// ---- the paged 8-bit cache
+// A mixkv_cache8 from a binding.Cache8, which holds on to the tensors for the call.
+struct CacheArg {
+  mixkv_cache8 c;
+  PyObject* held[4] = {};
+  ~CacheArg() {
+    for (PyObject* o : held) Py_XDECREF(o);
+  }
+  const at::Tensor& pool() const { return THPVariable_Unpack(held[0]); }
+  explicit CacheArg(PyObject* o) {
+    if (!api.cache8_append || !api.cache8_read || !api.cache8_ws_size || !api.cache8_attention || !api.cache8_evict)
+      fail(PyExc_OSError, "the library has no 8-bit cache");
+    try {
+      take(o);
+    } catch (...) {     // (no destructor runs for what was not built)
+      for (PyObject* x : held) Py_XDECREF(x);
+      throw;
+    }
+  }
+  CacheArg(const CacheArg&) = delete;
+
+ private:
+  const at::Tensor* attr(const int i, PyObject* o, PyObject* name) {     // (nullptr: None)
+    held[i] = PyObject_GetAttr(o, name);
+    if (!held[i]) throw Raised();
+    return held[i] == Py_None ? nullptr : &tensor(held[i]);
+  }
+  static int32_t code_of(PyObject* o) {
+    const Ref v(PyObject_GetAttr(o, nm.code));
+    if (!v.o) throw Raised();
+    const int int8 = PyObject_RichCompareBool(v.o, nm.int8, Py_EQ), e4m3 = PyObject_RichCompareBool(v.o, nm.e4m3, Py_EQ);
+    if (int8 < 0 || e4m3 < 0) throw Raised();
+    want(int8 || e4m3, "code must be 'int8' or 'e4m3'");
+    return e4m3 ? MIXKV_CODE_E4M3 : MIXKV_CODE_INT8;
+  }
+  void take(PyObject* o) {
+    const at::Tensor *pool = attr(0, o, nm.pool), *table = attr(1, o, nm.table), *rows = attr(2, o, nm.rows),
+                     *mass = attr(3, o, nm.mass);
+    if (!pool || !table || !rows) fail(PyExc_TypeError, "a tensor is expected");
+    want(pool->is_cuda() && pool->dim() == 2 && pool->is_contiguous() && pool->element_size() == 1,
+         "pool must be a contiguous CUDA tensor of bytes [pages, bytes of a page]");
+    const auto device = pool->device();
+    want(table->scalar_type() == at::kInt && table->dim() == 3 && table->is_contiguous() && table->device() == device,
+         "table must be a contiguous int32 tensor [batch, kv_heads, pages] on the pool's device");
+    want(rows->scalar_type() == at::kInt && rows->dim() == 2 && rows->is_contiguous() && rows->size(0) == table->size(0) &&
+             rows->size(1) == table->size(1) && rows->device() == device,
+         "rows must be a contiguous int32 tensor [batch, kv_heads] on the pool's device");
+    c.page_rows = attr_int(o, nm.page_rows);
+    want(c.page_rows > 0 && pool->size(1) * 16 == (int64_t)c.page_rows * MIXKV_CACHE8_TILE_BYTES,
+         "a page of the pool must have page_rows / 16 tiles");
+    if (mass)
+      want(mass->scalar_type() == at::kFloat && mass->is_contiguous() && mass->dim() == 2 && mass->size(0) == pool->size(0) &&
+               mass->size(1) == c.page_rows && mass->device() == device,
+           "mass must be a contiguous fp32 tensor [pages, page_rows] on the pool's device");
+    c.pool = pool->data_ptr();
+    c.mass_opt = mass ? fp(*mass) : nullptr;
+    c.table = ip(*table), c.rows = ip(*rows);
+    c.num_pages = pool->size(0);
+    c.max_pages = int32(table->size(2), "mixkv_cache8"), c.batch = int32(table->size(0), "mixkv_cache8");
+    c.kv_heads = int32(table->size(1), "mixkv_cache8"), c.head_dim = 128;
+    c.code = code_of(o);
+  }
+};
+
+// cache8_append(cache, k, v, offsets, max_new, status, stream)
+PyObject* py_cache8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const char* what = "mixkv_cache8_append";
+    const CacheArg cache(a[0]);
+    const mixkv_cache8& c = cache.c;
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]);
+    const bool compact = k.dim() == 2;
+    want((compact || (k.dim() == 3 && k.size(1) == c.kv_heads)) && k.sizes() == v.sizes() && k.size(-1) == 128 &&
+             k.stride(-1) == 1 && v.stride(-1) == 1 && k.device() == cache.pool().device() && v.device() == k.device() &&
+             k.scalar_type() == v.scalar_type(),
+         "k and v must be of one type and shape, [tokens, kv_heads, 128] or compact rows [rows, 128], on the pool's device");
+    const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), cache);
+    want(!compact || offsets, "compact rows need offsets");
+    want(offsets || k.size(0) == c.batch, "without offsets there is one token per sequence");
+    const int32_t max_new = int32(a[4], what);
+    int32_t* status = status_word(a[5], k);
+    const c10::cuda::CUDAGuard device(k.device());
+    const CallStream stream(a[6], k);
+    const int32_t type = paged_type(k.scalar_type());
+    int rc = MIXKV_OK;
+    if (k.size(0) > 0) {
+      const Unlocked u;
+      rc = api.cache8_append(&c, k.data_ptr(), v.data_ptr(), type, k.size(0), step(k, 0), compact ? 0 : step(k, 1), step(v, 0),
+                             compact ? 0 : step(v, 1), offsets, compact, max_new, status, stream.handle);
+    }
+    check_status(rc, what);
+    Py_RETURN_NONE;
+  });
+}
+
+// cache8_read(cache, tokens, fp16, offsets, max_new, compact, stream) -> (k, v)
+PyObject* py_cache8_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 7, [&]() -> PyObject* {
+    const char* what = "mixkv_cache8_read";
+    const CacheArg cache(a[0]);
+    const mixkv_cache8& c = cache.c;
+    const int64_t tokens = int32(a[1], what);
+    const bool half = truth(a[2]), compact = truth(a[5]);
+    const int32_t* offsets = row_offsets(a[3], (int64_t)c.batch * (compact ? c.kv_heads : 1), cache);
+    want(tokens >= 0 && (!compact || offsets), "compact rows need offsets");
+    const int32_t max_new = int32(a[4], what);
+    const c10::cuda::CUDAGuard device(cache.pool().device());
+    const CallStream stream(a[6], cache.pool());
+    at::Tensor k, v;
+    int rc = MIXKV_OK;
+    {
+      const Unlocked u;
+      const at::ScalarType type = half ? at::kHalf : at::kBFloat16;
+      const int64_t sizes[3] = {tokens, c.kv_heads, 128}, flat[2] = {tokens, 128};
+      const at::IntArrayRef size = compact ? at::IntArrayRef(flat, 2) : at::IntArrayRef(sizes, 3);
+      k = empty(size, type, cache.pool()), v = empty(size, type, cache.pool());
+      if (tokens > 0)
+        rc = api.cache8_read(&c, k.data_ptr(), v.data_ptr(), half ? MIXKV_TYPE_FP16 : MIXKV_TYPE_BF16, tokens, offsets,
+                             compact, max_new, stream.handle);
+    }
+    check_status(rc, what);
+    Ref kr(THPVariable_Wrap(k)), vr(THPVariable_Wrap(v));
+    if (!kr.o || !vr.o) throw Raised();
+    return PyTuple_Pack(2, kr.o, vr.o);
+  });
+}
+
+// How a call of the attention looks at the cache.
+struct CacheView {
+  int32_t rows, window, sinks;
+  bool accumulate;
+  CacheView(PyObject* r, PyObject* w, PyObject* s, PyObject* acc, const char* what)
+      : rows(int32(r, what)), window(int32(w, what)), sinks(int32(s, what)), accumulate(truth(acc)) {}
+};
+size_t cache8_space(const CacheArg& cache, const PagedQuery& q, const CacheView& view) {
+  size_t need = 0;
+  check_status(api.cache8_ws_size(&cache.c, q.tokens, q.gqa, view.rows, view.window, view.sinks, view.accumulate, &need),
+               "mixkv_cache8_workspace_size");
+  return need;
+}
+// cache8_workspace_size(cache, q, max_rows, window, sinks, accumulate)
+PyObject* py_cache8_workspace_size(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> PyObject* {
+    const CacheArg cache(a[0]);
+    const c10::cuda::CUDAGuard device(cache.pool().device());
+    return PyLong_FromSize_t(cache8_space(cache, PagedQuery(a[1], cache), CacheView(a[2], a[3], a[4], a[5], "mixkv_cache8_workspace_size")));
+  });
+}
+
+// cache8_attention(cache, q, max_rows, window, sinks, accumulate, softmax_scale, workspace, stream)
+PyObject* py_cache8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const char* what = "mixkv_cache8_attention";
+    const CacheArg cache(a[0]);
+    const PagedQuery q(a[1], cache);
+    const CacheView view(a[2], a[3], a[4], a[5], what);
+    const double scale = PyFloat_AsDouble(a[6]);
+    if (PyErr_Occurred()) throw Raised();
+    const c10::cuda::CUDAGuard device(cache.pool().device());
+    const CallStream stream(a[8], cache.pool());
+    at::Tensor own, out;
+    void* ws = nullptr;
+    size_t bytes = 0;
+    if (a[7] != Py_None) {
+      const at::Tensor& t = tensor(a[7]);
+      want(t.is_cuda() && t.is_contiguous() && t.device() == cache.pool().device(),
+           "workspace must be a contiguous tensor on the pool's device");
+      ws = t.data_ptr(), bytes = t.nbytes();
+    } else {
+      bytes = cache8_space(cache, q, view);
+    }
+    int rc;
+    {
+      const Unlocked u;
+      if (!ws) own = empty({(int64_t)bytes}, at::kByte, cache.pool()), ws = own.data_ptr();
+      out = empty(q.q.sizes(), q.q.scalar_type(), q.q);
+      rc = api.cache8_attention(&cache.c, q.q.data_ptr(), q.type, step(q.q, 0), step(q.q, 1), q.tokens, q.gqa, (float)scale,
+                                view.rows, view.window, view.sinks, view.accumulate, ws, bytes, out.data_ptr(), stream.handle);
+    }
+    check_status(rc, what);
+    return THPVariable_Wrap(out);
+  });
+}
+
+// cache8_evict(cache, into, budget, budgets, keep_first, keep_last, max_rows, status, stream) -> idx
+PyObject* py_cache8_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const char* what = "mixkv_cache8_evict";
+    const CacheArg cache(a[0]), into(a[1]);
+    const at::Tensor& pool = cache.pool();
+    want(into.pool().device() == pool.device(), "both caches must be on one device");
+    const int32_t budget = int32(a[2], what), first = int32(a[4], what), last = int32(a[5], what), rows = int32(a[6], what);
+    const int32_t* budgets = nullptr;
+    if (a[3] != Py_None) {
+      const at::Tensor& t = tensor(a[3]);
+      want(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == (int64_t)cache.c.batch * cache.c.kv_heads &&
+               t.device() == pool.device(),
+           "budgets must be a contiguous int32 tensor [batch, kv_heads] on the pool's device");
+      budgets = ip(t);
+    }
+    int32_t* status = status_word(a[7], pool);
+    if (budget < 1) check_status(MIXKV_ERR_INVALID_ARG, what);
+    const c10::cuda::CUDAGuard device(pool.device());
+    const CallStream stream(a[8], pool);
+    at::Tensor idx;
+    int rc;
+    {
+      const Unlocked u;
+      idx = empty({cache.c.batch, cache.c.kv_heads, budget}, at::kInt, pool);
+      rc = api.cache8_evict(&cache.c, &into.c, budget, budgets, first, last, rows, ip(idx), status, stream.handle);
+    }
+    check_status(rc, what);
+    return THPVariable_Wrap(idx);
+  });
+}
+
 // setup(path of libmixkv.so, error class): resolves the library's entry points.
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 2, [&]() -> PyObject* {
@@ -924,6 +1150,11 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     find(api.paged_select, "mixkv_paged_select");
     find(api.paged_ws_size, "mixkv_paged_workspace_size");
     find(api.paged_attention, "mixkv_paged_attention");
+    find(api.cache8_append, "mixkv_cache8_append");
+    find(api.cache8_read, "mixkv_cache8_read");
+    find(api.cache8_ws_size, "mixkv_cache8_workspace_size");
+    find(api.cache8_attention, "mixkv_cache8_attention");
+    find(api.cache8_evict, "mixkv_cache8_evict");
     Py_XSETREF(g_error, Py_NewRef(a[1]));
     Py_RETURN_NONE;
   });
@@ -943,6 +1174,11 @@ PyMethodDef methods[] = {{"setup", FAST(py_setup)},
                          {"paged_select", FAST(py_paged_select)},
                          {"paged_attention", FAST(py_paged_attention)},
                          {"paged_sparse_attention", FAST(py_paged_sparse_attention)},
+                         {"cache8_append", FAST(py_cache8_append)},
+                         {"cache8_read", FAST(py_cache8_read)},
+                         {"cache8_workspace_size", FAST(py_cache8_workspace_size)},
+                         {"cache8_attention", FAST(py_cache8_attention)},
+                         {"cache8_evict", FAST(py_cache8_evict)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_mixkv_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -954,7 +1190,8 @@ PyMODINIT_FUNC PyInit__mixkv_host() {
       NAME(use_vnorm), NAME(mix_mode), NAME(budget_mode), NAME(budget), NAME(ada_floor), NAME(eps),
       NAME(softmax_scale), NAME(cuda_stream), NAME(s_comp), NAME(s_ex), NAME(s_div), NAME(rbar), NAME(status),
       NAME(idx), NAME(counts), NAME(idx_offsets), NAME(K_out), NAME(V_out), NAME(out_row_offsets),
-      NAME(pool), NAME(table), NAME(rows), NAME(page_rows), NAME(bounds), NAME(k_scale), NAME(v_scale);
+      NAME(pool), NAME(table), NAME(rows), NAME(page_rows), NAME(bounds), NAME(k_scale), NAME(v_scale),
+      NAME(mass), NAME(code), NAME(int8), NAME(e4m3);
 #undef NAME
   return PyModule_Create(&module);
 }

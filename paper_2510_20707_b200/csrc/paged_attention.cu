@@ -27,6 +27,7 @@
 
 #include <cooperative_groups.h>
 
+#include "attend.cuh"
 #include "paged.cuh"
 
 namespace cg = cooperative_groups;
@@ -93,35 +94,6 @@ __device__ __forceinline__ UnitTiles unit_tiles(const AttArgs& a, const int u) {
   return r;
 }
 
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2,
-                                        const uint32_t a3, const uint32_t b0, const uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-      "{%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t transpose8x8(const uint32_t x) {
-  uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-  return r;
-}
-__device__ __forceinline__ float column_max(float v) {   // over the eight lanes that hold a query row's logits
-  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
-  v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
-  return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
-}
-__device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor_sync(0xffffffffu, v, 4);
-  v += __shfl_xor_sync(0xffffffffu, v, 8);
-  return v + __shfl_xor_sync(0xffffffffu, v, 16);
-}
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, const uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
-               "l"(src), "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
-}
-
 // Place in the pool and first row of tile `t` of a unit (-1, kNoRow: none).  The table is asked before the unit's rows are looked at:
 // both may be on their way.
 struct TileAt {
@@ -137,18 +109,12 @@ __device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const U
   return TileAt{id * a.p.tiles + in, row};
 }
 
-// Steps of a CTA when `ctas` of them share `total`: CTA c has those from c * share on, the last ones may have none.
-__device__ __forceinline__ int share_of(const int total, const int ctas) { return (total + ctas - 1) / ctas; }
-
 // Row of the output that query row r of a unit has.
 __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, const int r) {
   const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
   return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
 }
 
-__device__ __forceinline__ void add_scaled(float4& sum, const float4& x, const float by) {
-  sum.x = fmaf(x.x, by, sum.x), sum.y = fmaf(x.y, by, sum.y), sum.z = fmaf(x.z, by, sum.z), sum.w = fmaf(x.w, by, sum.w);
-}
 // Four outputs: sums of weighted values over the sum of weights (zeros where there were none), times v_scale.  (The quotient of the two
 // factors could be subnormal.)
 template <typename T>
