@@ -447,7 +447,7 @@ enum { MIXKV_CODE_INT8 = 0, MIXKV_CODE_E4M3 = 1 };
 #define MIXKV_CACHE8_MAX_QUERIES 128  /* q_tokens * gqa_ratio */
 
 typedef struct mixkv_cache8 {
-  void* pool;            /* device, 16-byte aligned: page p at p * mixkv_cache8_page_bytes */
+  void* pool;            /* device, 16-byte aligned: page p at p * mixkv_cache_page_bytes */
   float* mass_opt;       /* device [num_pages, page_rows] or NULL: accumulated attention weight of every row */
   const int32_t* table;  /* device [batch, kv_heads, max_pages]: page of a head's rows p * page_rows .. */
   int32_t* rows;         /* device [batch, kv_heads]: rows of every head, those that a call appends included */
@@ -460,7 +460,7 @@ typedef struct mixkv_cache8 {
 } mixkv_cache8;
 
 /* Bytes of a page.  Host-only. */
-int mixkv_cache8_page_bytes(int32_t page_rows, size_t* bytes);
+int mixkv_cache_page_bytes(int32_t page_rows, size_t* bytes);
 
 /* Appends rows to the cache, as mixkv_paged_append does (the caller counts them into c->rows first; K comes as it is to be
  * attended to): tokens offsets[b] .. offsets[b + 1] - 1 of k and v are the last rows of sequence b, or with offsets_per_head of one
@@ -472,19 +472,19 @@ int mixkv_cache8_page_bytes(int32_t page_rows, size_t* bytes);
  * Of more than max_new new rows of a head the last are written.  These others, and tokens whose place (table entry outside the pool, row
  * beyond the table or below zero, token not in k) does not exist, are not written and give MIXKV_ERR_INVALID_ARG in *status_dev.
  * Pages are written by one call at a time. */
-int mixkv_cache8_append(const mixkv_cache8* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
+int mixkv_cache_append(const mixkv_cache8* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
                         int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
                         const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, int32_t* status_dev,
                         void* stream);
 
 /* The last n rows of every head back as dense rows, fp32(code * scale) rounded to `type`; arguments as in mixkv_paged_read. */
-int mixkv_cache8_read(const mixkv_cache8* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
+int mixkv_cache_read(const mixkv_cache8* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
                       const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, void* stream);
 
-/* Workspace of a mixkv_cache8_attention call with these arguments, or with a smaller max_rows.  With accumulate it holds the
+/* Workspace of a mixkv_cache_attention call with these arguments, or with a smaller max_rows.  With accumulate it holds the
  * logits of all rows that a call sees: 4 bytes for each of the query rows (an even number) and every row of every head, as if all
  * heads had the most that max_rows, or sinks and window, let them see.  Asks the device for its SMs. */
-int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows, int32_t window,
+int mixkv_cache_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows, int32_t window,
                                 int32_t sinks, int32_t accumulate, size_t* bytes);
 
 /* softmax(q K^T scale) V over the cache: q_tokens new tokens per sequence, the last of its rows (append theirs first).  Token t
@@ -502,7 +502,7 @@ int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t
  * 1 / sqrt(128).  A page outside the pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that
  * sees a NaN, is NaN (as is the mass of the rows it sees), and so is what a wait inside the kernel ran out on (there is no status
  * word). */
-int mixkv_cache8_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
+int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
                            int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
                            int32_t max_rows, int32_t window, int32_t sinks, int32_t accumulate, void* workspace,
                            size_t workspace_bytes, void* out, void* stream);
@@ -521,7 +521,7 @@ int mixkv_cache8_attention(const mixkv_cache8* c, const void* q, int32_t type, i
  *   status_dev      device int32, optional: MIXKV_ERR_INVALID_ARG where a kept row has no place in `into` (its table names no page
  *                   of the pool, or is too short); that row is not written
  * Needs c->mass_opt.  A row on a page outside c's pool has a mass below all others and is zeros if it is kept. */
-int mixkv_cache8_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
+int mixkv_cache_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
                        int32_t keep_first, int32_t keep_last, int32_t max_rows, int32_t* idx, int32_t* status_dev,
                        void* stream);
 

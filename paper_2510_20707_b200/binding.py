@@ -44,8 +44,8 @@ EXPORTS = ("mixkv_default_params", "mixkv_workspace_size", "mixkv_scores", "mixk
            "mixkv_selftest_bounded_wait", "mixkv_launches_for", "mixkv_stage_name_for",
            "mixkv_device_check", "mixkv_paged_page_bytes", "mixkv_paged_append", "mixkv_paged_read",
            "mixkv_paged_select", "mixkv_paged_workspace_size", "mixkv_paged_attention",
-           "mixkv_cache8_page_bytes", "mixkv_cache8_append", "mixkv_cache8_read", "mixkv_cache8_workspace_size",
-           "mixkv_cache8_attention", "mixkv_cache8_evict")
+           "mixkv_cache_page_bytes", "mixkv_cache_append", "mixkv_cache_read", "mixkv_cache_workspace_size",
+           "mixkv_cache_attention", "mixkv_cache_evict")
 
 
 class MixKVError(RuntimeError):
@@ -187,13 +187,13 @@ def load_library() -> C.CDLL:
         lib.mixkv_paged_workspace_size.argtypes = [C.POINTER(_CPages), i32, i32, C.POINTER(sz)]
         lib.mixkv_paged_attention.argtypes = [C.POINTER(_CPages), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float, i32,
                                               vp, vp, i32, vp, sz, vp, vp]
-        lib.mixkv_cache8_page_bytes.argtypes = [i32, C.POINTER(sz)]
-        lib.mixkv_cache8_append.argtypes = [C.POINTER(_CCache8), vp, vp, i32] + [C.c_int64] * 5 + [vp, i32, i32, vp, vp]
-        lib.mixkv_cache8_read.argtypes = [C.POINTER(_CCache8), vp, vp, i32, C.c_int64, vp, i32, i32, vp]
-        lib.mixkv_cache8_workspace_size.argtypes = [C.POINTER(_CCache8)] + [i32] * 6 + [C.POINTER(sz)]
-        lib.mixkv_cache8_attention.argtypes = [C.POINTER(_CCache8), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float] + [
+        lib.mixkv_cache_page_bytes.argtypes = [i32, C.POINTER(sz)]
+        lib.mixkv_cache_append.argtypes = [C.POINTER(_CCache8), vp, vp, i32] + [C.c_int64] * 5 + [vp, i32, i32, vp, vp]
+        lib.mixkv_cache_read.argtypes = [C.POINTER(_CCache8), vp, vp, i32, C.c_int64, vp, i32, i32, vp]
+        lib.mixkv_cache_workspace_size.argtypes = [C.POINTER(_CCache8)] + [i32] * 6 + [C.POINTER(sz)]
+        lib.mixkv_cache_attention.argtypes = [C.POINTER(_CCache8), vp, i32, C.c_int64, C.c_int64, i32, i32, C.c_float] + [
             i32] * 4 + [vp, sz, vp, vp]
-        lib.mixkv_cache8_evict.argtypes = [C.POINTER(_CCache8), C.POINTER(_CCache8), i32, vp, i32, i32, i32, vp, vp, vp]
+        lib.mixkv_cache_evict.argtypes = [C.POINTER(_CCache8), C.POINTER(_CCache8), i32, vp, i32, i32, i32, vp, vp, vp]
         lib.mixkv_selftest_bounded_wait.argtypes = [vp, vp, vp]
         lib.mixkv_stage_name.restype = C.c_char_p
         lib.mixkv_stage_name.argtypes = [C.POINTER(_CParams), i32]
@@ -465,11 +465,11 @@ def paged_sparse_attention(pages: Pages, q: torch.Tensor, top: int, max_rows: Op
 
 
 def cache8_page_bytes(page_rows: int) -> int:
-    """mixkv_cache8_page_bytes: bytes of a page of so many rows (a multiple of 16) of one KV head."""
+    """mixkv_cache_page_bytes: bytes of a page of so many rows (a multiple of 16) of one KV head."""
     out = C.c_size_t(0)
-    rc = load_library().mixkv_cache8_page_bytes(page_rows, C.byref(out))
+    rc = load_library().mixkv_cache_page_bytes(page_rows, C.byref(out))
     if rc != 0:
-        raise MixKVError(rc, "mixkv_cache8_page_bytes")
+        raise MixKVError(rc, "mixkv_cache_page_bytes")
     return int(out.value)
 
 
@@ -487,7 +487,7 @@ def new_cache8(batch: int, kv_heads: int, max_rows: int, page_rows: int = 64, co
 
 def cache8_append(cache: Cache8, k: torch.Tensor, v: torch.Tensor, offsets: Optional[torch.Tensor] = None,
                   max_new: Optional[int] = None, status: Optional[torch.Tensor] = None, stream=None) -> None:
-    """mixkv_cache8_append: writes the last rows of every head (count them into ``cache.rows`` first), rounded to 8 bits, and sets
+    """mixkv_cache_append: writes the last rows of every head (count them into ``cache.rows`` first), rounded to 8 bits, and sets
     their mass to zero.  k, v, offsets, max_new and status as in :func:`paged_append`; K comes as it is to be attended to.  A
     block of 16 rows has one scale: rows that join it may make the codes of its older rows coarser."""
     if max_new is None:
@@ -497,7 +497,7 @@ def cache8_append(cache: Cache8, k: torch.Tensor, v: torch.Tensor, offsets: Opti
 
 def cache8_read(cache: Cache8, tokens: int, dtype: torch.dtype = torch.bfloat16, offsets: Optional[torch.Tensor] = None,
                 max_new: Optional[int] = None, compact: bool = False, stream=None):
-    """mixkv_cache8_read: the last rows of every head as dense K, V [tokens, kv_heads, 128] (``compact``: [tokens, 128], with an
+    """mixkv_cache_read: the last rows of every head as dense K, V [tokens, kv_heads, 128] (``compact``: [tokens, 128], with an
     offset per (sequence, head)); offsets and max_new as in :func:`paged_append`.  Rows that do not exist are left as they come
     from the allocator."""
     if dtype not in (torch.bfloat16, torch.float16):
@@ -518,7 +518,7 @@ def cache8_workspace(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = N
 def cache8_attention(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = None, window: int = 0, sinks: int = 0,
                      accumulate: bool = False, softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None,
                      stream=None) -> torch.Tensor:
-    """mixkv_cache8_attention: q [batch, tokens, kv_heads * gqa_ratio, 128] bf16 or fp16, the newest tokens of every sequence
+    """mixkv_cache_attention: q [batch, tokens, kv_heads * gqa_ratio, 128] bf16 or fp16, the newest tokens of every sequence
     (append theirs first) -> the same shape and type.  ``max_rows``: upper bound on ``cache.rows`` (default: what the table has room
     for).  ``window`` > 0: a token sees the last ``window`` rows up to its own, and the first ``sinks``.  ``accumulate``: what every
     row got of the softmax's weight, over tokens and heads of the group, is added to ``cache.mass``."""
@@ -529,7 +529,7 @@ def cache8_attention(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = N
 def cache8_evict(cache: Cache8, into: Cache8, budget: int, budgets: Optional[torch.Tensor] = None, keep_first: int = 0,
                  keep_last: int = 0, max_rows: Optional[int] = None, status: Optional[torch.Tensor] = None,
                  stream=None) -> torch.Tensor:
-    """mixkv_cache8_evict: of every head the first ``keep_first`` rows, the last ``keep_last`` and the heaviest of the others, at
+    """mixkv_cache_evict: of every head the first ``keep_first`` rows, the last ``keep_last`` and the heaviest of the others, at
     most ``budget`` in all (``budgets``, int32 [batch, kv_heads]: of every head its own, at most ``budget``), are written to ``into``, whose
     rows are set -> idx [batch, kv_heads, budget] int32, the rows that were kept, ascending, -1 behind the last.  ``cache`` stays as it
     is; ``into`` has pages, a table and rows of its own (its pool may be the same).  ``status``: an int32 device word, zeroed

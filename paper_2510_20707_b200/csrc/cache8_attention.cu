@@ -727,7 +727,7 @@ extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64
   *ctas = s.S, *shared = s.ctas;
 }
 
-extern "C" int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows,
+extern "C" int mixkv_cache_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t gqa_ratio, int32_t max_rows,
                                            int32_t window, int32_t sinks, int32_t accumulate, size_t* bytes) {
   CachePool pool;
   AttPlan p;
@@ -739,7 +739,7 @@ extern "C" int mixkv_cache8_workspace_size(const mixkv_cache8* c, int32_t q_toke
   return MIXKV_OK;
 }
 
-extern "C" int mixkv_cache8_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
+extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
                                       int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
                                       int32_t max_rows, int32_t window, int32_t sinks, int32_t accumulate, void* workspace,
                                       size_t workspace_bytes, void* out, void* stream) {

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs
 
 using namespace mixkv;
 
-extern "C" int mixkv_cache8_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
+extern "C" int mixkv_cache_evict(const mixkv_cache8* c, const mixkv_cache8* into, int32_t budget, const int32_t* budgets_opt,
                                   int32_t keep_first, int32_t keep_last, int32_t max_rows, int32_t* idx,
                                   int32_t* status_dev, void* stream) {
   EvictArgs a = {};

@@ -195,14 +195,14 @@ int read_as(const mixkv_cache8* c, const RowArgs& a, void* k, void* v, void* str
 
 using namespace mixkv;
 
-extern "C" int mixkv_cache8_page_bytes(int32_t page_rows, size_t* bytes) {
+extern "C" int mixkv_cache_page_bytes(int32_t page_rows, size_t* bytes) {
   if (!bytes || page_rows < kBlockRows || page_rows % kBlockRows || page_rows > MIXKV_PAGE_MAX_ROWS)
     return MIXKV_ERR_INVALID_ARG;
   *bytes = (size_t)(page_rows / kBlockRows) * kBlockBytes;
   return MIXKV_OK;
 }
 
-extern "C" int mixkv_cache8_append(const mixkv_cache8* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
+extern "C" int mixkv_cache_append(const mixkv_cache8* c, const void* k, const void* v, int32_t type, int64_t num_tokens,
                                    int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
                                    int64_t v_head_stride, const int32_t* offsets_opt, int32_t offsets_per_head,
                                    int32_t max_new, int32_t* status_dev, void* stream) {
@@ -217,7 +217,7 @@ extern "C" int mixkv_cache8_append(const mixkv_cache8* c, const void* k, const v
   return type == MIXKV_TYPE_BF16 ? append_as<__nv_bfloat16>(c, a, k, v, stream) : append_as<__half>(c, a, k, v, stream);
 }
 
-extern "C" int mixkv_cache8_read(const mixkv_cache8* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
+extern "C" int mixkv_cache_read(const mixkv_cache8* c, void* k_out, void* v_out, int32_t type, int64_t num_tokens,
                                  const int32_t* offsets_opt, int32_t offsets_per_head, int32_t max_new, void* stream) {
   RowArgs a = {};
   const int rc = check_rows(c, type, num_tokens, offsets_opt, offsets_per_head, max_new, &a);

@@ -49,11 +49,11 @@ struct Api {
   decltype(&mixkv_paged_select) paged_select;
   decltype(&mixkv_paged_workspace_size) paged_ws_size;
   decltype(&mixkv_paged_attention) paged_attention;
-  decltype(&mixkv_cache8_append) cache8_append;
-  decltype(&mixkv_cache8_read) cache8_read;
-  decltype(&mixkv_cache8_workspace_size) cache8_ws_size;
-  decltype(&mixkv_cache8_attention) cache8_attention;
-  decltype(&mixkv_cache8_evict) cache8_evict;
+  decltype(&mixkv_cache_append) cache8_append;
+  decltype(&mixkv_cache_read) cache8_read;
+  decltype(&mixkv_cache_workspace_size) cache8_ws_size;
+  decltype(&mixkv_cache_attention) cache8_attention;
+  decltype(&mixkv_cache_evict) cache8_evict;
 } api;
 PyObject* g_error = nullptr;   // binding.MixKVError
 
@@ -973,7 +973,7 @@ struct CacheArg {
 // cache8_append(cache, k, v, offsets, max_new, status, stream)
 PyObject* py_cache8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject* {
-    const char* what = "mixkv_cache8_append";
+    const char* what = "mixkv_cache_append";
     const CacheArg cache(a[0]);
     const mixkv_cache8& c = cache.c;
     const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]);
@@ -1004,7 +1004,7 @@ PyObject* py_cache8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // cache8_read(cache, tokens, fp16, offsets, max_new, compact, stream) -> (k, v)
 PyObject* py_cache8_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 7, [&]() -> PyObject* {
-    const char* what = "mixkv_cache8_read";
+    const char* what = "mixkv_cache_read";
     const CacheArg cache(a[0]);
     const mixkv_cache8& c = cache.c;
     const int64_t tokens = int32(a[1], what);
@@ -1043,7 +1043,7 @@ struct CacheView {
 size_t cache8_space(const CacheArg& cache, const PagedQuery& q, const CacheView& view) {
   size_t need = 0;
   check_status(api.cache8_ws_size(&cache.c, q.tokens, q.gqa, view.rows, view.window, view.sinks, view.accumulate, &need),
-               "mixkv_cache8_workspace_size");
+               "mixkv_cache_workspace_size");
   return need;
 }
 // cache8_workspace_size(cache, q, max_rows, window, sinks, accumulate)
@@ -1051,14 +1051,14 @@ PyObject* py_cache8_workspace_size(PyObject*, PyObject* const* a, Py_ssize_t n) 
   return guarded(n, 6, [&]() -> PyObject* {
     const CacheArg cache(a[0]);
     const c10::cuda::CUDAGuard device(cache.pool().device());
-    return PyLong_FromSize_t(cache8_space(cache, PagedQuery(a[1], cache), CacheView(a[2], a[3], a[4], a[5], "mixkv_cache8_workspace_size")));
+    return PyLong_FromSize_t(cache8_space(cache, PagedQuery(a[1], cache), CacheView(a[2], a[3], a[4], a[5], "mixkv_cache_workspace_size")));
   });
 }
 
 // cache8_attention(cache, q, max_rows, window, sinks, accumulate, softmax_scale, workspace, stream)
 PyObject* py_cache8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject* {
-    const char* what = "mixkv_cache8_attention";
+    const char* what = "mixkv_cache_attention";
     const CacheArg cache(a[0]);
     const PagedQuery q(a[1], cache);
     const CacheView view(a[2], a[3], a[4], a[5], what);
@@ -1093,7 +1093,7 @@ PyObject* py_cache8_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // cache8_evict(cache, into, budget, budgets, keep_first, keep_last, max_rows, status, stream) -> idx
 PyObject* py_cache8_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> PyObject* {
-    const char* what = "mixkv_cache8_evict";
+    const char* what = "mixkv_cache_evict";
     const CacheArg cache(a[0]), into(a[1]);
     const at::Tensor& pool = cache.pool();
     want(into.pool().device() == pool.device(), "both caches must be on one device");
@@ -1150,11 +1150,11 @@ PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
     find(api.paged_select, "mixkv_paged_select");
     find(api.paged_ws_size, "mixkv_paged_workspace_size");
     find(api.paged_attention, "mixkv_paged_attention");
-    find(api.cache8_append, "mixkv_cache8_append");
-    find(api.cache8_read, "mixkv_cache8_read");
-    find(api.cache8_ws_size, "mixkv_cache8_workspace_size");
-    find(api.cache8_attention, "mixkv_cache8_attention");
-    find(api.cache8_evict, "mixkv_cache8_evict");
+    find(api.cache8_append, "mixkv_cache_append");
+    find(api.cache8_read, "mixkv_cache_read");
+    find(api.cache8_ws_size, "mixkv_cache_workspace_size");
+    find(api.cache8_attention, "mixkv_cache_attention");
+    find(api.cache8_evict, "mixkv_cache_evict");
     Py_XSETREF(g_error, Py_NewRef(a[1]));
     Py_RETURN_NONE;
   });

@@ -109,12 +109,12 @@ BAD_CACHES = [(dict(pool=0), -1), (dict(pool=ONE + 8), -1), (dict(table=0), -1),
 def test_every_entry_refuses_a_cache_that_is_none(lib, change, status):
     c, good = cache(**change), cache(rows=ONE + 64)
     size = C.c_size_t()
-    assert lib.mixkv_cache8_append(C.byref(c), ONE, ONE, 0, 2, 384, 128, 384, 128, None, 0, 1, None, None) == status
-    assert lib.mixkv_cache8_read(C.byref(c), ONE, ONE, 0, 2, None, 0, 1, None) == status
-    assert lib.mixkv_cache8_workspace_size(C.byref(c), 1, 4, 100, 0, 0, 0, C.byref(size)) == status
-    assert lib.mixkv_cache8_attention(C.byref(c), ONE, 0, 1536, 1536, 1, 4, 0.0, 100, 0, 0, 0, ONE, 1 << 40, ONE, None) == status
-    assert lib.mixkv_cache8_evict(C.byref(c), C.byref(good), 64, None, 1, 1, 100, ONE, None, None) == status
-    assert lib.mixkv_cache8_evict(C.byref(good), C.byref(c), 64, None, 1, 1, 100, ONE, None, None) == status
+    assert lib.mixkv_cache_append(C.byref(c), ONE, ONE, 0, 2, 384, 128, 384, 128, None, 0, 1, None, None) == status
+    assert lib.mixkv_cache_read(C.byref(c), ONE, ONE, 0, 2, None, 0, 1, None) == status
+    assert lib.mixkv_cache_workspace_size(C.byref(c), 1, 4, 100, 0, 0, 0, C.byref(size)) == status
+    assert lib.mixkv_cache_attention(C.byref(c), ONE, 0, 1536, 1536, 1, 4, 0.0, 100, 0, 0, 0, ONE, 1 << 40, ONE, None) == status
+    assert lib.mixkv_cache_evict(C.byref(c), C.byref(good), 64, None, 1, 1, 100, ONE, None, None) == status
+    assert lib.mixkv_cache_evict(C.byref(good), C.byref(c), 64, None, 1, 1, 100, ONE, None, None) == status
 
 
 @pytest.mark.parametrize("change,status", [
@@ -124,14 +124,14 @@ def test_append_and_read_refuse(lib, change, status):
     a = dict(k=ONE, v=ONE, type=0, tokens=2, ks=384, kh=128, vs=384, vh=128, offsets=None, per_head=0, max_new=1, status=None)
     a.update(change)
     c = cache()
-    got = lib.mixkv_cache8_append(C.byref(c), a["k"], a["v"], a["type"], a["tokens"], a["ks"], a["kh"], a["vs"], a["vh"], a["offsets"],
+    got = lib.mixkv_cache_append(C.byref(c), a["k"], a["v"], a["type"], a["tokens"], a["ks"], a["kh"], a["vs"], a["vh"], a["offsets"],
                                   a["per_head"], a["max_new"], a["status"], None)
     assert got == status
     if not {"ks", "vh", "status"} & set(change):
-        assert lib.mixkv_cache8_read(C.byref(c), a["k"], a["v"], a["type"], a["tokens"], a["offsets"], a["per_head"], a["max_new"],
+        assert lib.mixkv_cache_read(C.byref(c), a["k"], a["v"], a["type"], a["tokens"], a["offsets"], a["per_head"], a["max_new"],
                                      None) == status
     big = cache(batch=1 << 12, kv_heads=1 << 10, max_pages=1 << 12)
-    assert lib.mixkv_cache8_read(C.byref(big), ONE, ONE, 0, 2, ONE, 0, 1 << 20, None) == -2
+    assert lib.mixkv_cache_read(C.byref(big), ONE, ONE, 0, 2, ONE, 0, 1 << 20, None) == -2
 
 
 @pytest.mark.parametrize("change,status", [
@@ -144,7 +144,7 @@ def test_attention_refuses(lib, change, status):
              out=ONE, mass=ONE, pages=4, page_rows=64)
     a.update(change)
     c = cache(mass_opt=a["mass"], max_pages=a["pages"], page_rows=a["page_rows"])
-    assert lib.mixkv_cache8_attention(C.byref(c), a["q"], a["type"], a["qb"], a["qt"], a["T"], a["G"], a["scale"], a["max_rows"],
+    assert lib.mixkv_cache_attention(C.byref(c), a["q"], a["type"], a["qb"], a["qt"], a["T"], a["G"], a["scale"], a["max_rows"],
                                       a["window"], a["sinks"], a["accumulate"], a["ws"], a["nbytes"], a["out"], None) == status
 
 
@@ -156,7 +156,7 @@ def test_evict_refuses(lib, change, status):
     a = dict(budget=64, budgets=None, first=1, last=1, max_rows=100, idx=ONE, status=None, mass=ONE, batch=2, heads=3, code=0, rows=ONE + 64)
     a.update(change)
     c, into = cache(mass_opt=a["mass"]), cache(batch=a["batch"], kv_heads=a["heads"], code=a["code"], rows=a["rows"], mass_opt=0)
-    assert lib.mixkv_cache8_evict(C.byref(c), C.byref(into), a["budget"], a["budgets"], a["first"], a["last"], a["max_rows"], a["idx"],
+    assert lib.mixkv_cache_evict(C.byref(c), C.byref(into), a["budget"], a["budgets"], a["first"], a["last"], a["max_rows"], a["idx"],
                                   a["status"], None) == status
 
 
@@ -164,7 +164,7 @@ def test_a_workspace_for_more_rows_serves_fewer(lib):
     def need(max_rows, window=0, sinks=0, acc=1, T=2, G=3):
         size = C.c_size_t()
         c = cache(max_pages=1000)
-        assert lib.mixkv_cache8_workspace_size(C.byref(c), T, G, max_rows, window, sinks, acc, C.byref(size)) == 0
+        assert lib.mixkv_cache_workspace_size(C.byref(c), T, G, max_rows, window, sinks, acc, C.byref(size)) == 0
         return size.value
     sizes = [need(n) for n in (1, 16, 17, 1000, 64000, 1 << 29)]
     assert sizes == sorted(sizes) and sizes[-1] == sizes[-2]
