@@ -9,8 +9,7 @@
 // Two rows of V are interleaved by byte moves before they are widened, so that a pair is two rows of one dimension.
 //
 // Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a step instead of
-// a reduction); weights are fp16 times 2^kLift, sums are fp32.  A tile's products of values start from zero and join the sums by
-// its scale: weights times scales would leave fp16's range.
+// a reduction); weights are fp16 times 2^kLift, sums are fp32.
 //
 // Weights of rows: what a row got is known when the sums are, so the logits go to the workspace as fp32 (R of them for a row of 257
 // bytes) and a second kernel takes the exponentials of one row's in a fixed order and adds their sum to the row's mass.
@@ -32,16 +31,17 @@ constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is no
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
 constexpr int kAttUnits = 1024;                // most units whose tiles are dealt out evenly
-constexpr int kMassTiles = 8;                  // of a CTA that adds weights up
+constexpr int kMassTiles = 16;                 // of a CTA that adds weights up
 constexpr int kAttFew = 4, kAttFewRows = 16;   // tiles of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
+constexpr float kSmallest = 1.f / 4096;        // scale of values that goes into weights of fp16, in units of the largest
 constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
 
 // rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
 // the cluster; barriers and rows of the rings
 __host__ __device__ constexpr size_t att_smem(int NT) {
   return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
-         kAttWarps * kAttDepth * 16 + 16;
+         (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16;
 }
 __host__ __device__ constexpr int att_per_sm(int NT) { return NT <= 2 ? 3 : 2; }
 
@@ -59,7 +59,7 @@ struct AttArgs {
   float scale_log2e;
   int2* spans;               // [units]: first CTA with a share of a unit, times two, plus one if its run begins before the unit; last CTA
   float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
-  float2* part_mz;           // [2 ctas][R]: (reference, sum)
+  float4* part_mz;           // [2 ctas][R]: (reference, sum, unit of the sums of values, -)
   float2* stats;             // [units][R]: (reference, 1 / sum) of a query row
   float* logits;             // [units][cap][16][pitch], log2 units; nullptr: weights are not asked for
   int cap, pitch;            // tiles of a unit that a call can see; query rows, made even
@@ -110,11 +110,14 @@ __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, cons
   const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
   return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
 }
-// Four outputs: sums of weighted values over the sum of weights (zeros where there were none).
+// One over a power of two from 2^-126 to 2^126.
+__device__ __forceinline__ float inverse(const float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+// Four outputs: sums of weighted values over the sum of weights (zeros where there were none), times their unit.
 template <typename T>
-__device__ __forceinline__ void store_row(T* to, const float4& num, const float den) {
+__device__ __forceinline__ void store_row(T* to, const float4& num, const float den, const float unit) {
   const float by = den == 0.f ? 0.f : 1.f / den;
-  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(num.x * by, num.y * by), narrow2<T>(num.z * by, num.w * by));
+  *reinterpret_cast<uint2*>(to) =
+      make_uint2(narrow2<T>(num.x * by * unit, num.y * by * unit), narrow2<T>(num.z * by * unit, num.w * by * unit));
 }
 __device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float den) {
   if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, den == 0.f ? 0.f : 1.f / den);
@@ -130,12 +133,14 @@ struct AttState {
   float f[NT][2];           // products of codes to log2 units, without the block's scale: query rows 2 t, 2 t + 1
   float acc[NT][8][4];      // dimensions 16 g + 2 m (0, 1), 16 g + 2 m + 1 (2, 3) of query rows 2 t, 2 t + 1
   float ref[NT][2], z[NT][2];   // weights are 2^(logit - ref)
+  float vref;                   // acc is in units of it: a power of two above every scale of values so far
   static constexpr bool IsBf16 = std::is_same<T, __nv_bfloat16>::value;
 
   // Query rows first .. first + 8 NT - 1 of a unit.  bf16 rows are divided by a power of two that brings their largest
   // magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it; the power goes into f.
   __device__ __forceinline__ void start(const AttArgs& a, const int u, const int first, const int g, const int t) {
     const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
+    vref = FLT_MIN;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int r = first + 8 * nt + g;
@@ -186,11 +191,7 @@ struct AttState {
 
   // s[2 j + c] = product of row g + 8 j of the tile and query row 8 nt + 2 t + c
   __device__ __forceinline__ void products(const unsigned char* tile, const int g, const int t, float (&s)[NT][4]) const {
-    float odd[NT][4];      // (two chains of four instead of one of eight)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[nt][i] = odd[nt][i] = 0.f;
+    float odd[4];      // (of one group of query rows, two chains of four instead of one of eight)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const unsigned char* at = tile + piece_at(g, 2 * t + half);
@@ -200,15 +201,19 @@ struct AttState {
         uint32_t a0, a2, a1, a3;
         codes_to_half<E4M3>(word_of(a, w), a0, a2);
         codes_to_half<E4M3>(word_of(b, w), a1, a3);
+        const int k = 4 * half + w;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          mma_f16((w & 1) ? odd[nt] : s[nt], a0, a1, a2, a3, q[nt][4 * half + w][0], q[nt][4 * half + w][1]);
+        for (int nt = 0; nt < NT; ++nt) {
+          float(&d)[4] = NT == 1 && (k & 1) ? odd : s[nt];
+          if (k == 0 || (NT == 1 && k == 1)) mma_f16_first(d, a0, a1, a2, a3, q[nt][k][0], q[nt][k][1]);
+          else mma_f16(d, a0, a1, a2, a3, q[nt][k][0], q[nt][k][1]);
+        }
       }
     }
+    if constexpr (NT == 1) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[nt][i] += odd[nt][i];
+      for (int i = 0; i < 4; ++i) s[0][i] += odd[i];
+    }
   }
 
   // A tile whose first row is `row`, of a unit of n rows; `first`: the CTA's first query row.  edge: some query row does not see some row.
@@ -247,10 +252,14 @@ struct AttState {
     // (A logit is rounded before the reference, itself a logit, is taken from it: of a product that is not, equal logits beyond 2^24 would
     // differ from it by their last bits, whole powers of two.)
     bool above = false;
+    float x[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) above |= __fsub_rn(y[nt][i], ref[nt][i & 1]) > kLag + kLift;
+      for (int i = 0; i < 4; ++i) {
+        x[nt][i] = __fsub_rn(y[nt][i], ref[nt][i & 1]);
+        above |= x[nt][i] > kLag + kLift;
+      }
     if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -259,29 +268,35 @@ struct AttState {
           const float to = fmaxf(ref[nt][c], column_max(fmaxf(y[nt][c], y[nt][2 + c])) - kLift);
           const float shrink = ex2(ref[nt][c] - to);
           ref[nt][c] = to, z[nt][c] *= shrink;
+          x[nt][c] = __fsub_rn(y[nt][c], to), x[nt][2 + c] = __fsub_rn(y[nt][2 + c], to);
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }
     }
+    // The block's scale, in units of the largest so far, goes into the weights before they are rounded.  Where it is far smaller
+    // (weights would leave fp16's range), or NaN (it must not reach, through weights of zero, a query row that sees none of the
+    // block's rows), the tile's products begin at zero and join the sums by a multiply-add.
+    if (scale.y > vref) {
+      const float to = __uint_as_float(min((__float_as_uint(scale.y) & 0x7f800000u) + 0x00800000u, 253u << 23));
+      const float shrink = vref * inverse(to);
+      vref = to;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[nt][i][c] *= shrink;
+    }
+    const float ratio = scale.y * inverse(vref);
+    const bool aside = !(ratio >= kSmallest) && scale.y != 0.f;
+    const float by = aside ? 1.f : ratio;
     uint32_t p[NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[nt][i] = ex2(__fsub_rn(y[nt][i], ref[nt][i & 1])), z[nt][i & 1] += y[nt][i];
-      p[nt][0] = transpose8x8(narrow2<__half>(y[nt][0], y[nt][1]));
-      p[nt][1] = transpose8x8(narrow2<__half>(y[nt][2], y[nt][3]));
-    }
-    // A block whose values are NaN must not reach, through weights of zero, a query row that sees none of its rows.
-    bool into[NT][2];
-    const bool some = edge && scale.y != scale.y;
-    if (some) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
-          into[nt][c] = row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks);
-        }
+      for (int i = 0; i < 4; ++i) x[nt][i] = ex2(x[nt][i]), z[nt][i & 1] += x[nt][i];
+      p[nt][0] = transpose8x8(narrow2<__half>(x[nt][0] * by, x[nt][1] * by));
+      p[nt][1] = transpose8x8(narrow2<__half>(x[nt][2] * by, x[nt][3] * by));
     }
     uint4 v[2][2];       // 16 dimensions of rows 2 t + e + 8 h
 #pragma unroll
@@ -289,28 +304,27 @@ struct AttState {
 #pragma unroll
       for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
 #pragma unroll
-    for (int w = 0; w < 4; ++w)
+    for (int m = 0; m < 8; ++m) {
+      const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
+      uint32_t a0, a1, a2, a3;
+      codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
+      codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
+      if (!aside) {
 #pragma unroll
-      for (int o = 0; o < 2; ++o) {
-        const uint32_t sel = o ? 0x7362u : 0x5140u;
-        uint32_t a0, a1, a2, a3;
-        codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], w), word_of(v[0][1], w), sel), a0, a1);
-        codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], w), word_of(v[1][1], w), sel), a2, a3);
-        const int m = 2 * w + o;
+        for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt][m], a0, a1, a2, a3, p[nt][0], p[nt][1]);
+      } else {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float d[4] = {0.f, 0.f, 0.f, 0.f};
-          mma_f16(d, a0, a1, a2, a3, p[nt][0], p[nt][1]);
-          if (some) {
+          float d[4];
+          mma_f16_first(d, a0, a1, a2, a3, p[nt][0], p[nt][1]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if (into[nt][c & 1]) acc[nt][m][c] = fmaf(d[c], scale.y, acc[nt][m][c]);
-          } else {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) acc[nt][m][c] = fmaf(d[c], scale.y, acc[nt][m][c]);
+          for (int c = 0; c < 4; ++c) {
+            const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + (c & 1)));
+            if (row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks)) acc[nt][m][c] = fmaf(d[c], ratio, acc[nt][m][c]);
           }
         }
       }
+    }
   }
 };
 
@@ -329,7 +343,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
   float* xz = xm + Q;                        // [Q]
   float* allm = xz + Q;                      // [8][Q]
   float* allz = allm + kMaxCluster * Q;      // [8][Q]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(allz + kMaxCluster * Q);   // [warps][depth]
+  float* wv = allz + kMaxCluster * Q;        // [warps]: units of their sums of values
+  float* xv = wv + W;                        // of the CTA's; [3] fill up
+  float* allv = xv + 4;                      // [8]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(allv + kMaxCluster);   // [warps][depth]
   int* rows = reinterpret_cast<int*>(bars + W * kAttDepth);   // [warps][depth]: first rows of the tiles
   int* abort = rows + W * kAttDepth;
   __shared__ int starts[kAttUnits + 1];      // first tile of every unit
@@ -481,6 +498,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
         const int r = 8 * nt + 2 * t + c;
         if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
       }
+    if (lane == 0) wv[warp] = st.vref;
     const bool whole = shares ? lo <= starts[u] && end == starts[u + 1] : S == 1;
     const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
 #pragma unroll
@@ -497,27 +515,27 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       __syncthreads();
       for (int e = tid; e < live * (kHeadDim / 8); e += kThreads) {
         const int r = e / (kHeadDim / 8), x = 4 * (e % (kHeadDim / 8)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
-        float M = kNoRef;
+        float M = kNoRef, unit = FLT_MIN;
 #pragma unroll
-        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]);
+        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]), unit = fmaxf(unit, wv[w]);
         float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
         float den = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
           const float sc = ex2(wm[w * Q + r] - M);
-          add_scaled(num, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc);
+          add_scaled(num, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc * (wv[w] * inverse(unit)));
           den = fmaf(wz[w * Q + r], sc, den);
         }
         if (whole) {
-          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den);
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, unit);
           if (dim == 0) store_stat(a, u, first + r, M, den);
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
           *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
-          if (dim == 0) a.part_mz[at] = make_float2(M, den);
+          if (dim == 0) a.part_mz[at] = make_float4(M, den, unit, 0.f);
         } else {
           *reinterpret_cast<float4*>(xo + r * kHeadDim + dim) = num;
-          if (dim == 0) xm[r] = M, xz[r] = den;
+          if (dim == 0) xm[r] = M, xz[r] = den, *xv = unit;      // (the same for every r)
         }
       }
     }
@@ -535,21 +553,22 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       const int k = e / Q, r = e % Q;
       allm[e] = *cluster.map_shared_rank(&xm[r], k);
       allz[e] = *cluster.map_shared_rank(&xz[r], k);
+      if (r == 0) allv[k] = *cluster.map_shared_rank(xv, k);
     }
     __syncthreads();
     for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
       const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
-      float M = kNoRef;
-      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+      float M = kNoRef, unit = FLT_MIN;
+      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]), unit = fmaxf(unit, allv[k]);
       float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
       float den = 0.f;
 #pragma unroll 4
       for (int k = 0; k < S; ++k) {
         const float sc = ex2(allm[k * Q + r] - M);
-        add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc);
+        add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc * (allv[k] * inverse(unit)));
         den = fmaf(allz[k * Q + r], sc, den);
       }
-      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den);
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, unit);
       if (dim == 0) store_stat(a, u, first + r, M, den);
     }
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
@@ -564,7 +583,7 @@ constexpr int kJoinWarps = 16;
 template <typename T>
 __global__ void __launch_bounds__(kJoinWarps * 32) k_cache8_join(const AttArgs a, const Divider per_row, const Divider blocks) {
   __shared__ float4 sums[kJoinWarps][32];
-  __shared__ float2 stat[kJoinWarps];
+  __shared__ float4 stat[kJoinWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int u = blocks.div(blockIdx.x), slot = per_row.div(warp), part = warp - slot * per_row.d;
   const int row = (blockIdx.x - u * blocks.d) * per_row.div(kJoinWarps) + slot;      // (blocks: CTAs of a unit)
@@ -575,13 +594,17 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_cache8_join(const AttArgs a
   if (c0 == c1) return;     // written by that CTA
   const bool on = row < a.R;
   constexpr int kAtOnce = 5;
-  float M = kNoRef, den = 0.f;
+  float M = kNoRef, den = 0.f, unit = FLT_MIN;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto move = [&](const float to, const float wide) {      // to another reference and another unit
+    const float shrink = ex2(M - to), by = shrink * (unit * inverse(wide));
+    num.x *= by, num.y *= by, num.z *= by, num.w *= by, den *= shrink;
+    M = to, unit = wide;
+  };
 #pragma unroll 1
   for (int c = c0 + part; on && c <= c1; c += per_row.d * kAtOnce) {
-    float4 x[kAtOnce];
-    float2 mz[kAtOnce];
-    float to = M;
+    float4 x[kAtOnce], mz[kAtOnce];
+    float to = M, wide = unit;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const int k = min(c + i * (int)per_row.d, c1);
@@ -590,61 +613,69 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_cache8_join(const AttArgs a
       x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x);
-    const float shrink = ex2(M - to);
-    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
-    M = to;
+    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x), wide = fmaxf(wide, mz[i].z);
+    move(to, wide);
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const float sc = c + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
-      add_scaled(num, x[i], sc);
+      add_scaled(num, x[i], sc * (mz[i].z * inverse(unit)));
       den = fmaf(mz[i].y, sc, den);
     }
   }
   if (per_row.d > 1) {
     sums[warp][lane] = num;
-    if (lane == 0) stat[warp] = make_float2(M, den);
+    if (lane == 0) stat[warp] = make_float4(M, den, unit, 0.f);
     __syncthreads();
     if (part) return;
-    float to = M;
-    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, stat[warp + w].x);
-    const float shrink = ex2(M - to);
-    num.x *= shrink, num.y *= shrink, num.z *= shrink, num.w *= shrink, den *= shrink;
+    float to = M, wide = unit;
+    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, stat[warp + w].x), wide = fmaxf(wide, stat[warp + w].z);
+    move(to, wide);
     for (int w = 1; w < (int)per_row.d; ++w) {
-      const float2 mz = stat[warp + w];
-      const float sc = ex2(mz.x - to);
-      add_scaled(num, sums[warp + w][lane], sc);
+      const float4 mz = stat[warp + w];
+      const float sc = ex2(mz.x - M);
+      add_scaled(num, sums[warp + w][lane], sc * (mz.z * inverse(unit)));
       den = fmaf(mz.y, sc, den);
     }
-    M = to;
   }
   if (!on) return;
-  store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den);
+  store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den, unit);
   if (lane == 0) store_stat(a, u, row, M, den);
 }
 
-// The weights that the rows of a unit got, added to their mass: a thread has a row.  grid.x: units, grid.y: kMassTiles tiles of them.
-__global__ void __launch_bounds__(kMassTiles * kBlockRows) k_cache8_mass(const AttArgs a) {
+// The weights that the rows of a unit got, added to their mass.  grid.x: units, grid.y: `rounds` times kMassTiles tiles of them; a
+// thread has a row a round.  (Most of a ragged batch's CTAs may find no rows: four rounds make them a quarter.)
+__global__ void __launch_bounds__(kMassTiles * kBlockRows) k_cache8_mass(const AttArgs a, const int rounds) {
   __shared__ float2 stats[MIXKV_CACHE8_MAX_QUERIES];
   pdl_wait();
-  const int u = blockIdx.x, i = blockIdx.y * kMassTiles + threadIdx.x / kBlockRows, r = threadIdx.x % kBlockRows;
+  const int u = blockIdx.x, first = blockIdx.y * (rounds * kMassTiles), r = threadIdx.x % kBlockRows;
   const UnitTiles ut = unit_tiles(a, u);
-  if (blockIdx.y * kMassTiles >= ut.tiles) return;
+  if (first >= ut.tiles) return;
   for (int e = threadIdx.x; e < a.R; e += blockDim.x) stats[e] = __ldcg(a.stats + (long long)u * a.R + e);
-  const TileAt at = tile_at(a, u, ut, i);
   __syncthreads();
-  if (at.tile < 0 || at.row + r >= ut.n) return;
-  const float2* row = reinterpret_cast<const float2*>(a.logits + ((long long)u * a.cap + i) * (kBlockRows * a.pitch) + r * a.pitch);
-  float sum = 0.f;
+  const float* logits = a.logits + (long long)u * a.cap * (kBlockRows * a.pitch) + r * a.pitch;
+  // (what a query row does not see gets nothing of it, if it is NaN either)
+  const auto weight = [&](const float y, const int e) { return y != -INFINITY ? ex2(y - stats[e].x) * stats[e].y : 0.f; };
 #pragma unroll 4
-  for (int e = 0; e < a.R; e += 2) {
-    const float2 y = __ldcg(row + (e >> 1));
-    // (what a query row does not see gets nothing of it, if it is NaN either)
-    if (y.x != -INFINITY) sum = fmaf(ex2(y.x - stats[e].x), stats[e].y, sum);
-    if (e + 1 < a.R && y.y != -INFINITY) sum = fmaf(ex2(y.y - stats[e + 1].x), stats[e + 1].y, sum);
+  for (int k = 0; k < rounds; ++k) {
+    const int i = first + k * kMassTiles + threadIdx.x / kBlockRows;
+    const TileAt at = tile_at(a, u, ut, i);
+    if (at.tile < 0 || at.row + r >= ut.n) continue;
+    float* mass = a.p.mass + (long long)at.tile * kBlockRows + r;     // (a page's tiles lie one after the other in both)
+    const float* row = logits + (long long)i * (kBlockRows * a.pitch);
+    float sum = 0.f;
+    if (a.pitch == 4) {
+      const float4 y = __ldcg(reinterpret_cast<const float4*>(row));
+      sum = weight(y.x, 0) + weight(y.y, 1) + weight(y.z, 2) + (a.R > 3 ? weight(y.w, 3) : 0.f);
+    } else {
+#pragma unroll 4
+      for (int e = 0; e < a.R; e += 2) {
+        const float2 y = __ldcg(reinterpret_cast<const float2*>(row + e));
+        sum += weight(y.x, e);
+        if (e + 1 < a.R) sum += weight(y.y, e + 1);
+      }
+    }
+    *mass += sum;
   }
-  float* mass = a.p.mass + (long long)at.tile * kBlockRows + r;     // (a page's tiles lie one after the other in both)
-  *mass += sum;
 }
 
 using AttKernel = void (*)(AttArgs);
@@ -709,7 +740,7 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
   p->cap = (int)p->tiles, p->pitch = ((int)R + 1) & ~1, p->sms = device_sm_count();
   const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
   p->part = up((size_t)att_slots(p->NT, p->sms) * 2 * R * kHeadDim * 4);
-  p->spans = up(p->part + (size_t)att_slots(p->NT, p->sms) * 2 * R * sizeof(float2));
+  p->spans = up(p->part + (size_t)att_slots(p->NT, p->sms) * 2 * R * sizeof(float4));
   p->stats = up(p->spans + kAttUnits * sizeof(int2));
   p->logits = up(p->stats + (accumulate ? (size_t)units * R * sizeof(float2) : 0));
   p->bytes = p->logits + (accumulate ? (size_t)units * p->cap * kBlockRows * p->pitch * 4 : 0);
@@ -772,7 +803,7 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   a.window = window, a.sinks = sinks;
   a.units = (int)units, a.ctas = shape.ctas;
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e;
-  a.part = reinterpret_cast<float*>(ws), a.part_mz = reinterpret_cast<float2*>(ws + p.part);
+  a.part = reinterpret_cast<float*>(ws), a.part_mz = reinterpret_cast<float4*>(ws + p.part);
   a.spans = reinterpret_cast<int2*>(ws + p.spans), a.stats = reinterpret_cast<float2*>(ws + p.stats);
   a.logits = accumulate ? reinterpret_cast<float*>(ws + p.logits) : nullptr, a.cap = p.cap, a.pitch = p.pitch;
   a.out = out;
@@ -788,8 +819,10 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
                    dim3(kJoinWarps * 32), 0, st, 1, a, Divider(per_row), Divider(blocks));
   }
   if (e == cudaSuccess && accumulate) {
-    const long long chunks = (p.tiles + kMassTiles - 1) / kMassTiles;
-    e = launch_pdl(k_cache8_mass, dim3((unsigned)units, (unsigned)chunks), dim3(kMassTiles * kBlockRows), 0, st, 1, a);
+    const long long rounds = units * p.tiles > 16ll * kMassTiles * p.sms ? 4 : 1, each = rounds * kMassTiles;
+    const long long chunks = (p.tiles + each - 1) / each;
+    e = launch_pdl(k_cache8_mass, dim3((unsigned)units, (unsigned)chunks), dim3(kMassTiles * kBlockRows), 0, st, 1, a,
+                   (int)rounds);
   }
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }

@@ -79,8 +79,17 @@ __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a)
   const int each = (m + S - 1) / S, lo = min(rank * each, m), hi = min(lo + each, m), mine = hi - lo;
   const bool cached = mine <= a.cached;
   auto key = [&](const int i) { return cached ? keys[i] : key_of(a.p, u, m0 + lo + i); };
-  if (cached)
-    for (int i = tid; i < mine; i += kPickThreads) keys[i] = key_of(a.p, u, m0 + lo + i);
+  if (cached) {       // eight rows of a thread on their way: a page, then its mass, are two trips to memory
+    constexpr int kAtOnce = 8;
+    for (int i = tid; i < mine; i += kAtOnce * kPickThreads) {
+      uint32_t x[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) x[j] = key_of(a.p, u, m0 + lo + min(i + j * kPickThreads, mine - 1));
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+        if (i + j * kPickThreads < mine) keys[i + j * kPickThreads] = x[j];
+    }
+  }
 
   uint32_t prefix = 0;       // digits that are known, in place
   int left = k;
@@ -161,6 +170,25 @@ __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a)
   cluster.sync();            // a CTA's shared memory stays alive until its peers have read it
 }
 
+__device__ __forceinline__ float max_nan(const float x, const float y) {   // NaN if one is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+  return r;
+}
+// The largest magnitude of sixteen codes.
+template <bool E4M3>
+__device__ __forceinline__ float largest_code(const uint4& c) {
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  __half2 m = __float2half2_rn(0.f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t lo, hi;
+    codes_to_half<E4M3>(w[i], lo, hi);
+    m = __hmax2(m, __hmax2(__habs2(*reinterpret_cast<const __half2*>(&lo)), __habs2(*reinterpret_cast<const __half2*>(&hi))));
+  }
+  return fmaxf(__low2float(m), __high2float(m));
+}
+
 template <bool E4M3>
 __global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs a, const int tasks) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane & 7, sub = lane >> 3;
@@ -199,20 +227,19 @@ __global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs
       scale[i] = *(reinterpret_cast<const float*>(tile + kBlockScales) + values);
     }
   }
-  float x[4][16];
-  uint32_t most = 0;
+  // the largest magnitude: of a row's codes, times its scale (rounding keeps the order)
+  float most = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    values16<E4M3>(codes[i], scale[i], x[i]);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) most = max(most, __float_as_uint(x[i][e]) & 0x7fffffffu);
-  }
-  most = __reduce_max_sync(0xffffffffu, most);
-  const float to = scale_of_largest<E4M3>(__uint_as_float(most)), by = by_scale(to);
+  for (int i = 0; i < 4; ++i) most = max_nan(most, fabsf(__fmul_rn(largest_code<E4M3>(codes[i]), scale[i])));
+  const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);
+  const float to = scale_of_largest<E4M3>(__uint_as_float(bits)), by = by_scale(to);
   unsigned char* tile = block_ptr(a.into, id, in);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<uint4*>(tile + (values ? kBlockV : 0) + piece_at(4 * i + sub, g)) = encode16<E4M3>(x[i], by);
+  for (int i = 0; i < 4; ++i) {
+    float x[16];
+    values16<E4M3>(codes[i], scale[i], x);
+    *reinterpret_cast<uint4*>(tile + (values ? kBlockV : 0) + piece_at(4 * i + sub, g)) = encode16<E4M3>(x, by);
+  }
   if (lane == 0) *(reinterpret_cast<float*>(tile + kBlockScales) + values) = to;
   if (values && a.into.mass && lane < kBlockRows && begin + lane < kept)
     a.into.mass[(long long)id * a.into.page_rows + in * kBlockRows + lane] =
@@ -240,9 +267,9 @@ extern "C" int mixkv_cache_evict(const mixkv_cache8* c, const mixkv_cache8* into
   a.budget = budget, a.budgets = budgets_opt, a.first = keep_first, a.last = keep_last, a.max_rows = max_rows;
   a.idx = idx, a.status = status_dev, a.slots = (int)slots, a.by_slots = Divider((uint32_t)slots);
   const long long room = (long long)c->max_pages * c->page_rows, rows = max_rows < room ? max_rows : room;
-  // CTAs of a head: as many as its rows are worth, and no more than two to an SM
+  // CTAs of a head: as many as its rows are worth, and no more than one to an SM
   int S = 1;
-  while (S < kMaxCluster && S * (long long)kPickRows < rows && units * S * 2 <= 2LL * device_sm_count()) S *= 2;
+  while (S < kMaxCluster && S * (long long)kPickRows < rows && units * S * 2 <= device_sm_count()) S *= 2;
   const long long each = (rows + S - 1) / S;
   a.cached = (int)(each < kPickKeys ? each : kPickKeys);
   const size_t smem = (size_t)a.cached * 4;
