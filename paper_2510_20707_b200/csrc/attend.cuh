@@ -45,6 +45,13 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, const uint
                "l"(src), "r"(bytes), "r"(smem_u32(bar))
                : "memory");
 }
+// The same with an L2 eviction policy.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, const uint32_t bytes, uint64_t* bar, const uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
 
 // Steps of a CTA when `ctas` of them share `total`: CTA c has those from c * share on, the last ones may have none.
 __device__ __forceinline__ int share_of(const int total, const int ctas) { return (total + ctas - 1) / ctas; }

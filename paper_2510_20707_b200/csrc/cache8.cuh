@@ -85,13 +85,20 @@ __device__ __forceinline__ void codes_to_half(const uint32_t w, uint32_t& lo, ui
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(0x64806480u));
   }
 }
-// Four codes as fp32 numbers.
+// Four codes as fp32 numbers.  int8: a byte plus 128 in the low bits of 2^23.
 template <bool E4M3>
-__device__ __forceinline__ void codes_to_float(const uint32_t w, float (&x)[4]) {
-  uint32_t lo, hi;
-  codes_to_half<E4M3>(w, lo, hi);
-  const float2 a = widen2<__half>(lo), b = widen2<__half>(hi);
-  x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+__device__ __forceinline__ void codes_to_float(const uint32_t w, f32x2& a, f32x2& b) {
+  if constexpr (E4M3) {
+    uint32_t lo, hi;
+    codes_to_half<true>(w, lo, hi);
+    const float2 x = widen2<__half>(lo), y = widen2<__half>(hi);
+    a = pack2(x.x, x.y), b = pack2(y.x, y.y);
+  } else {
+    const uint32_t x = w ^ 0x80808080u;
+    const f32x2 off = pack2(-8388736.f, -8388736.f);
+    a = add2(pack2(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7441))), off);
+    b = add2(pack2(__uint_as_float(__byte_perm(x, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(x, 0x4b000000u, 0x7443))), off);
+  }
 }
 
 // Scale of a block whose largest magnitude is m (a NaN or an infinity: NaN).
@@ -104,10 +111,12 @@ __device__ __forceinline__ float larger_scale(const float a, const float b) { re
 // What values are multiplied by; zero (all codes are zero) for a scale of zero or NaN.
 __device__ __forceinline__ float by_scale(const float s) { return s > 0.f ? __frcp_rn(s) : 0.f; }
 // Codes of four values.  by > 0: they are finite, and no product is beyond the largest code by more than its own rounding.
-// int8: 1.5 * 2^23 + y has the nearest whole number to y, ties to even, in its low bits.
+// int8: 1.5 * 2^23 + y has the nearest whole number to y, ties to even, in its low bits.  (The sums are taken one by one: of packed
+// products and a packed sum the compiler makes multiply-adds.)
 template <bool E4M3>
-__device__ __forceinline__ uint32_t encode4(const float a, const float b, const float c, const float d, const float by) {
-  const float ya = __fmul_rn(a, by), yb = __fmul_rn(b, by), yc = __fmul_rn(c, by), yd = __fmul_rn(d, by);
+__device__ __forceinline__ uint32_t encode4(const f32x2 a, const f32x2 b, const float by) {
+  float ya, yb, yc, yd;
+  unpack2(mul2(a, pack2(by, by)), ya, yb), unpack2(mul2(b, pack2(by, by)), yc, yd);
   uint32_t r;
   if constexpr (E4M3) {
     asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f32 x, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 y, %4, %3;\n\t"
@@ -122,33 +131,36 @@ __device__ __forceinline__ uint32_t encode4(const float a, const float b, const 
   }
   return by > 0.f ? r : 0u;
 }
+template <typename T>
+__device__ __forceinline__ f32x2 widen_pair(const uint32_t w) {
+  const float2 v = widen2<T>(w);
+  return pack2(v.x, v.y);
+}
+template <>
+__device__ __forceinline__ f32x2 widen_pair<__nv_bfloat16>(const uint32_t w) { return bf16x2_wide(w); }
 template <typename T, bool E4M3>
 __device__ __forceinline__ uint4 encode16(const Sixteen& x, const float by) {
   uint32_t r[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 a = widen2<T>(x.w[2 * i]), b = widen2<T>(x.w[2 * i + 1]);
-    r[i] = encode4<E4M3>(a.x, a.y, b.x, b.y, by);
-  }
+  for (int i = 0; i < 4; ++i) r[i] = encode4<E4M3>(widen_pair<T>(x.w[2 * i]), widen_pair<T>(x.w[2 * i + 1]), by);
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 // Sixteen codes under scale `s` as fp32(code * s).
 template <bool E4M3>
-__device__ __forceinline__ void values16(const uint4& c, const float s, float (&x)[16]) {
+__device__ __forceinline__ void values16(const uint4& c, const float s, f32x2 (&x)[8]) {
   const uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float y[4];
-    codes_to_float<E4M3>(w[i], y);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[4 * i + e] = __fmul_rn(y[e], s);
+    f32x2 a, b;
+    codes_to_float<E4M3>(w[i], a, b);
+    x[2 * i] = mul2(a, pack2(s, s)), x[2 * i + 1] = mul2(b, pack2(s, s));
   }
 }
 template <bool E4M3>
-__device__ __forceinline__ uint4 encode16(const float (&x)[16], const float by) {
+__device__ __forceinline__ uint4 encode16(const f32x2 (&x)[8], const float by) {
   uint32_t r[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = encode4<E4M3>(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], by);
+  for (int i = 0; i < 4; ++i) r[i] = encode4<E4M3>(x[2 * i], x[2 * i + 1], by);
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
 

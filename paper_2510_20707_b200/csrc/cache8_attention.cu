@@ -31,17 +31,19 @@ constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is no
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
 constexpr int kAttUnits = 1024;                // most units whose tiles are dealt out evenly
-constexpr int kMassTiles = 16;                 // of a CTA that adds weights up
 constexpr int kAttFew = 4, kAttFewRows = 16;   // tiles of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
 constexpr float kSmallest = 1.f / 4096;        // scale of values that goes into weights of fp16, in units of the largest
 constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
 
+// Whether a warp has the queries in registers (with more of them there is no room).
+__host__ __device__ constexpr bool att_held(int NT) { return NT <= 2; }
 // rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
-// the cluster; barriers and rows of the rings
+// the cluster, and units; barriers and rows of the rings; what the queries were divided by, and they (or in
+// the place of the sums)
 __host__ __device__ constexpr size_t att_smem(int NT) {
   return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
-         (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16;
+         (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
 }
 __host__ __device__ constexpr int att_per_sm(int NT) { return NT <= 2 ? 3 : 2; }
 
@@ -98,10 +100,10 @@ struct TileAt {
   int tile, row;
 };
 __device__ __forceinline__ TileAt tile_at(const AttArgs& a, const int u, const UnitTiles& ut, const int i) {
-  if (i >= ut.tiles) return TileAt{-1, kNoRow};
-  const int t = i < ut.sink ? i : i + ut.gap, page = a.p.by_tiles.div(t), in = t - page * a.p.tiles;
-  const int id = fresh(a.p.table + (long long)u * a.p.max_pages + page);
-  if (id < 0 || id >= a.p.num_pages) return TileAt{-1, kNoRow};
+  // (without a window the table is asked before the unit's rows are looked at: both may be on their way)
+  const int t = a.window > 0 && i >= ut.sink ? i + ut.gap : i, page = a.p.by_tiles.div(t), in = t - page * a.p.tiles;
+  const int id = page < a.p.max_pages ? fresh(a.p.table + (long long)u * a.p.max_pages + page) : -1;
+  if (i >= ut.tiles || id < 0 || id >= a.p.num_pages) return TileAt{-1, kNoRow};
   return TileAt{id * a.p.tiles + in, t * kBlockRows};
 }
 
@@ -112,74 +114,94 @@ __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, cons
 }
 // One over a power of two from 2^-126 to 2^126.
 __device__ __forceinline__ float inverse(const float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
-// Four outputs: sums of weighted values over the sum of weights (zeros where there were none), times their unit.
+// Four outputs: sums of weighted values times one over the sum of weights (zero where there were none), times their unit.
 template <typename T>
-__device__ __forceinline__ void store_row(T* to, const float4& num, const float den, const float unit) {
-  const float by = den == 0.f ? 0.f : 1.f / den;
+__device__ __forceinline__ void store_row(T* to, const float4& num, const float by, const float unit) {
   *reinterpret_cast<uint2*>(to) =
       make_uint2(narrow2<T>(num.x * by * unit, num.y * by * unit), narrow2<T>(num.z * by * unit, num.w * by * unit));
 }
+__device__ __forceinline__ float one_over(const float den) { return den == 0.f ? 0.f : 1.f / den; }
 __device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float den) {
-  if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, den == 0.f ? 0.f : 1.f / den);
+  if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, one_over(den));
 }
 // Token of query row r of a unit (rows of the padding: the last).
 __device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return a.by_group.div(min(r, a.R - 1)); }
 
 __device__ __forceinline__ uint32_t word_of(const uint4& v, const int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// Query rows first .. first + 8 NT - 1 of a unit, as B fragments (k-step s of group nt and lane (g, t) at [nt][s][lane]: query row g,
+// dimensions 32 t + 4 s .. + 3) and what they are to be multiplied by, into shared memory.  bf16 rows are divided by a power of two that
+// brings their largest magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it.  A row with a NaN or an infinity is zeros times NaN.
+template <typename T, int NT>
+__device__ __forceinline__ void stage_queries(const AttArgs& a, const int u, const int first, const int warp, const int lane, uint2* q,
+                                              float* up) {
+  constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+  const int b = a.p.by_heads.div(u), h = u - b * a.p.H, g = lane >> 2, t = lane & 3;
+  for (int nt = warp; nt < NT; nt += kAttWarps) {
+    const int r = first + 8 * nt + g;
+    uint4 raw[4];
+    const bool on = r < a.R;
+    const int token = on ? a.by_group.div(r) : 0;
+    const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
+                   (long long)(h * a.G + (on ? r - token * a.G : 0)) * kHeadDim + 32 * t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = on ? fresh(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
+    uint32_t bits = 0;       // magnitudes in the order of their bits, infinities and NaN above the others
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bits = __vmaxu2(bits, word_of(raw[i], e) & 0x7fff7fffu);
+    bits = max(bits & 0xffffu, bits >> 16);
+    bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+    bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+    const float most = widen2<T>(bits).x;
+    const bool odd = !(most < INFINITY);
+    // 2^e <= most < 2^(e + 1) (subnormal: 2^-126); down = 2^-e
+    const uint32_t e = min(max(__float_as_uint(most) >> 23, 1u), 253u);
+    const bool scaled = kBf16 && most > 0.f && !odd;
+    const float down = scaled ? __uint_as_float((254u - e) << 23) : 1.f;
+    if (t == 0) up[8 * nt + g] = odd ? NAN : scaled ? __uint_as_float(e << 23) : 1.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        x[w] = word_of(raw[i], w);
+        if constexpr (kBf16) {
+          const float2 y = widen2<T>(x[w]);
+          x[w] = narrow2<__half>(y.x * down, y.y * down);
+        }
+        if (odd) x[w] = 0u;
+      }
+      q[(nt * 8 + 2 * i) * 32 + lane] = make_uint2(x[0], x[1]);
+      q[(nt * 8 + 2 * i + 1) * 32 + lane] = make_uint2(x[2], x[3]);
+    }
+  }
+}
+
 template <typename T, int NT, bool E4M3>
 struct AttState {
-  uint32_t q[NT][8][2];     // B fragments: query row g, dimensions 32 t + 4 s .. + 3
+  static constexpr bool kHeld = att_held(NT);
+  uint2 q[kHeld ? NT : 1][8];
+  const uint2* at;          // this lane's fragments in shared memory
   float f[NT][2];           // products of codes to log2 units, without the block's scale: query rows 2 t, 2 t + 1
   float acc[NT][8][4];      // dimensions 16 g + 2 m (0, 1), 16 g + 2 m + 1 (2, 3) of query rows 2 t, 2 t + 1
   float ref[NT][2], z[NT][2];   // weights are 2^(logit - ref)
   float vref;                   // acc is in units of it: a power of two above every scale of values so far
-  static constexpr bool IsBf16 = std::is_same<T, __nv_bfloat16>::value;
 
-  // Query rows first .. first + 8 NT - 1 of a unit.  bf16 rows are divided by a power of two that brings their largest
-  // magnitude to [1, 2): exact as fp16 but for what is 2^-24 of it; the power goes into f.
-  __device__ __forceinline__ void start(const AttArgs& a, const int u, const int first, const int g, const int t) {
-    const int b = a.p.by_heads.div(u), h = u - b * a.p.H;
+  __device__ __forceinline__ void start(const AttArgs& a, const uint2* staged, const float* up, const int lane) {
+    const int t = lane & 3;
+    at = staged + lane;
     vref = FLT_MIN;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int r = first + 8 * nt + g;
-      uint4 raw[4];
-      const bool on = r < a.R;
-      const int token = on ? a.by_group.div(r) : 0;
-      const T* src = static_cast<const T*>(a.q) + b * a.q_batch + token * a.q_token +
-                     (long long)(h * a.G + (on ? r - token * a.G : 0)) * kHeadDim + 32 * t;
+      if constexpr (kHeld) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) raw[i] = on ? fresh(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
-      uint32_t bits = 0;       // magnitudes in the order of their bits, infinities and NaN above the others
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) bits = __vmaxu2(bits, word_of(raw[i], e) & 0x7fff7fffu);
-      bits = max(bits & 0xffffu, bits >> 16);
-      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
-      bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
-      const float most = widen2<T>(bits).x;
-      const bool odd = !(most < INFINITY);
-      // 2^e <= most < 2^(e + 1) (subnormal: 2^-126); down = 2^-e
-      const uint32_t e = min(max(__float_as_uint(most) >> 23, 1u), 253u);
-      const bool scaled = IsBf16 && most > 0.f && !odd;
-      const float down = scaled ? __uint_as_float((254u - e) << 23) : 1.f;
-      const float up = odd ? NAN : scaled ? __uint_as_float(e << 23) : 1.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          uint32_t x = word_of(raw[i], w);
-          if constexpr (IsBf16) {
-            const float2 y = widen2<T>(x);
-            x = narrow2<__half>(y.x * down, y.y * down);
-          }
-          q[nt][2 * i + (w >> 1)][w & 1] = odd ? 0u : x;
-        }
+        for (int k = 0; k < 8; ++k) q[nt][k] = at[(nt * 8 + k) * 32];
+      }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        f[nt][c] = __shfl_sync(0xffffffffu, up, 4 * (2 * t + c)) * a.scale_log2e;
+        f[nt][c] = up[8 * nt + 2 * t + c] * a.scale_log2e;
         ref[nt][c] = kNoRef, z[nt][c] = 0.f;
       }
 #pragma unroll
@@ -194,19 +216,22 @@ struct AttState {
     float odd[4];      // (of one group of query rows, two chains of four instead of one of eight)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const unsigned char* at = tile + piece_at(g, 2 * t + half);
-      const uint4 a = *reinterpret_cast<const uint4*>(at), b = *reinterpret_cast<const uint4*>(at + 8 * 128);
+      const unsigned char* rows = tile + piece_at(g, 2 * t + half);
+      const uint4 lo = *reinterpret_cast<const uint4*>(rows), hi = *reinterpret_cast<const uint4*>(rows + 8 * 128);
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         uint32_t a0, a2, a1, a3;
-        codes_to_half<E4M3>(word_of(a, w), a0, a2);
-        codes_to_half<E4M3>(word_of(b, w), a1, a3);
+        codes_to_half<E4M3>(word_of(lo, w), a0, a2);
+        codes_to_half<E4M3>(word_of(hi, w), a1, a3);
         const int k = 4 * half + w;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float(&d)[4] = NT == 1 && (k & 1) ? odd : s[nt];
-          if (k == 0 || (NT == 1 && k == 1)) mma_f16_first(d, a0, a1, a2, a3, q[nt][k][0], q[nt][k][1]);
-          else mma_f16(d, a0, a1, a2, a3, q[nt][k][0], q[nt][k][1]);
+          uint2 b;
+          if constexpr (kHeld) b = q[nt][k];
+          else b = at[(nt * 8 + k) * 32];
+          if (k == 0 || (NT == 1 && k == 1)) mma_f16_first(d, a0, a1, a2, a3, b.x, b.y);
+          else mma_f16(d, a0, a1, a2, a3, b.x, b.y);
         }
       }
     }
@@ -303,27 +328,41 @@ struct AttState {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
+    // A fragments of dimensions 16 g + 2 m, + 1, handed to f one by one
+    const auto fragments = [&](const auto& f) {
 #pragma unroll
-    for (int m = 0; m < 8; ++m) {
-      const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
-      uint32_t a0, a1, a2, a3;
-      codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
-      codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
-      if (!aside) {
+      for (int m = 0; m < 8; ++m) {
+        const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
+        uint32_t a0, a1, a2, a3;
+        codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
+        codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
+        f(m, a0, a1, a2, a3);
+      }
+    };
+    if (__builtin_expect(!aside, 1)) {
+      fragments([&](const int m, const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt][m], a0, a1, a2, a3, p[nt][0], p[nt][1]);
-      } else {
+      });
+    } else {
+      bool into[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
+          into[nt][c] = row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks);
+        }
+      fragments([&](const int m, const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float d[4];
           mma_f16_first(d, a0, a1, a2, a3, p[nt][0], p[nt][1]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + (c & 1)));
-            if (row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks)) acc[nt][m][c] = fmaf(d[c], ratio, acc[nt][m][c]);
-          }
+          for (int c = 0; c < 4; ++c)
+            if (into[nt][c & 1]) acc[nt][m][c] = fmaf(d[c], ratio, acc[nt][m][c]);
         }
-      }
+      });
     }
   }
 };
@@ -348,7 +387,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
   float* allv = xv + 4;                      // [8]
   uint64_t* bars = reinterpret_cast<uint64_t*>(allv + kMaxCluster);   // [warps][depth]
   int* rows = reinterpret_cast<int*>(bars + W * kAttDepth);   // [warps][depth]: first rows of the tiles
-  int* abort = rows + W * kAttDepth;
+  int* abort = rows + W * kAttDepth;         // [4]
+  float* up = reinterpret_cast<float*>(abort + 4);      // [Q]
+  uint2* queries = reinterpret_cast<uint2*>(att_held(NT) ? sums : up + Q);   // [NT][8][32]
+  static_assert(NT * 2048 <= W * kSums * 4, "queries fit the place of the sums");
   __shared__ int starts[kAttUnits + 1];      // first tile of every unit
   __shared__ int warp_total[W];
   cg::cluster_group cluster = cg::this_cluster();
@@ -442,7 +484,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       ring_rows[slot_out] = ahead.row;
       if (ahead.tile >= 0) {
         mbar_expect_tx(full, kBlockBytes);
-        bulk_load(ring + slot_out * kBlockBytes, a.p.pool + (long long)ahead.tile * kBlockBytes, kBlockBytes, full);
+        bulk_load(ring + slot_out * kBlockBytes, a.p.pool + (long long)ahead.tile * kBlockBytes, kBlockBytes, full, l2_evict_first());
       } else {
         mbar_arrive(full);    // nothing to come
       }
@@ -461,7 +503,10 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       end = min(hi, starts[u + 1]), from = starts[u];
     }
     AttState<T, NT, E4M3> st;
-    st.start(a, u, first, g, t);
+    stage_queries<T, NT>(a, u, first, warp, lane, queries, up);
+    __syncthreads();
+    st.start(a, queries, up, lane);
+    if (att_held(NT)) __syncthreads();      // (before sums are written where they were)
     const int n = unit_tiles(a, u).n;
     const int clear = n - a.T + 1;                               // rows below are seen by all,
     const int low = a.window > 0 ? seen_by(a, n, a.T - 1).low : -1;   // from here on, or among the sinks
@@ -527,7 +572,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
           den = fmaf(wz[w * Q + r], sc, den);
         }
         if (whole) {
-          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, unit);
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
           if (dim == 0) store_stat(a, u, first + r, M, den);
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
@@ -568,7 +613,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
         add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc * (allv[k] * inverse(unit)));
         den = fmaf(allz[k * Q + r], sc, den);
       }
-      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, den, unit);
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
       if (dim == 0) store_stat(a, u, first + r, M, den);
     }
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
@@ -576,105 +621,124 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
   }
 }
 
-// Joins the shares of units that several CTAs had a part of, and writes zeros for units without rows.  per_row warps (a power
-// of two) take the shares of a query row in turn, a few at once with a running reference: what a share holds comes in one
-// round trip.
-constexpr int kJoinWarps = 16;
+// What is left when all tiles have been read.  grid.x: units, each_unit.d CTAs to one.
+//  - Shares: statistics of the query rows of units that several CTAs had a part of (every CTA of a unit for itself), the rows' outputs
+//    (each by one CTA, `per_row.d` warps, a power of two, taking the shares in turn) and zeros for units without rows.
+//  - Weights: every CTA adds what its run of the unit's rows got to their mass, a thread a row at a time.
+// In one kernel, since a launch and its first loads cost as much as either.
+constexpr int kEndWarps = 8, kEndThreads = kEndWarps * 32, kEndPerSm = 6;
 template <typename T>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_cache8_join(const AttArgs a, const Divider per_row, const Divider blocks) {
-  __shared__ float4 sums[kJoinWarps][32];
-  __shared__ float4 stat[kJoinWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int u = blocks.div(blockIdx.x), slot = per_row.div(warp), part = warp - slot * per_row.d;
-  const int row = (blockIdx.x - u * blocks.d) * per_row.div(kJoinWarps) + slot;      // (blocks: CTAs of a unit)
+__global__ void __launch_bounds__(kEndThreads) k_cache8_finish(const AttArgs a, const Divider each_unit, const Divider per_row) {
+  __shared__ float4 sums[kEndWarps][32];
+  __shared__ float4 stat[MIXKV_CACHE8_MAX_QUERIES];      // (reference, 1 / sum, unit, -)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int u = each_unit.div(blockIdx.x), C = (int)each_unit.d, c = blockIdx.x - u * C;
   pdl_wait();
-  pdl_launch_dependents();
-  const int2 span = __ldcg(a.spans + u);
+  const int2 span = a.ctas ? __ldcg(a.spans + u) : make_int2(0, 0);
   const int c0 = span.x >> 1, c1 = span.y;
-  if (c0 == c1) return;     // written by that CTA
-  const bool on = row < a.R;
-  constexpr int kAtOnce = 5;
-  float M = kNoRef, den = 0.f, unit = FLT_MIN;
-  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  auto move = [&](const float to, const float wide) {      // to another reference and another unit
-    const float shrink = ex2(M - to), by = shrink * (unit * inverse(wide));
-    num.x *= by, num.y *= by, num.z *= by, num.w *= by, den *= shrink;
-    M = to, unit = wide;
-  };
-#pragma unroll 1
-  for (int c = c0 + part; on && c <= c1; c += per_row.d * kAtOnce) {
-    float4 x[kAtOnce], mz[kAtOnce];
-    float to = M, wide = unit;
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int k = min(c + i * (int)per_row.d, c1);
-      const long long at = (2LL * k + (k == c0 ? span.x & 1 : 0)) * a.R + row;
-      mz[i] = __ldcg(a.part_mz + at);
-      x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
+  const bool joined = c0 != c1;
+  const auto part_row = [&](const int k, const int r) { return (2LL * k + (k == c0 ? span.x & 1 : 0)) * a.R + r; };
+  if (joined) {
+    int lanes = 1;       // that share a query row
+    while (lanes < 32 && lanes < c1 - c0 + 1) lanes *= 2;
+    const int at = lane & (lanes - 1), at_once = 32 / lanes;
+    for (int r = warp * at_once + lane / lanes; r - lane / lanes < a.R; r += kEndWarps * at_once) {
+      float M = kNoRef, den = 0.f, unit = FLT_MIN;
+      for (int k = c0 + at; k <= c1 && r < a.R; k += lanes) {
+        const float4 mz = __ldcg(a.part_mz + part_row(k, r));
+        const float to = fmaxf(M, mz.x);
+        den = fmaf(den, ex2(M - to), mz.y * ex2(mz.x - to));
+        M = to, unit = fmaxf(unit, mz.z);
+      }
+      float most = M;
+      for (int o = 1; o < lanes; o *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o)), unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
+      den *= ex2(M - most);
+      for (int o = 1; o < lanes; o *= 2) den += __shfl_xor_sync(0xffffffffu, den, o);
+      if (at == 0 && r < a.R) stat[r] = make_float4(most, one_over(den), unit, 0.f);
     }
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x), wide = fmaxf(wide, mz[i].z);
-    move(to, wide);
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const float sc = c + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
-      add_scaled(num, x[i], sc * (mz[i].z * inverse(unit)));
-      den = fmaf(mz[i].y, sc, den);
+  } else if (a.logits) {
+    for (int r = tid; r < a.R; r += kEndThreads) {
+      const float2 s = __ldcg(a.stats + (long long)u * a.R + r);
+      stat[r] = make_float4(s.x, s.y, 0.f, 0.f);
     }
   }
-  if (per_row.d > 1) {
-    sums[warp][lane] = num;
-    if (lane == 0) stat[warp] = make_float4(M, den, unit, 0.f);
-    __syncthreads();
-    if (part) return;
-    float to = M, wide = unit;
-    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, stat[warp + w].x), wide = fmaxf(wide, stat[warp + w].z);
-    move(to, wide);
-    for (int w = 1; w < (int)per_row.d; ++w) {
-      const float4 mz = stat[warp + w];
-      const float sc = ex2(mz.x - M);
-      add_scaled(num, sums[warp + w][lane], sc * (mz.z * inverse(unit)));
-      den = fmaf(mz.y, sc, den);
-    }
-  }
-  if (!on) return;
-  store_row(static_cast<T*>(a.out) + out_row(a, u, row) * kHeadDim + 4 * lane, num, den, unit);
-  if (lane == 0) store_stat(a, u, row, M, den);
-}
-
-// The weights that the rows of a unit got, added to their mass.  grid.x: units, grid.y: `rounds` times kMassTiles tiles of them; a
-// thread has a row a round.  (Most of a ragged batch's CTAs may find no rows: four rounds make them a quarter.)
-__global__ void __launch_bounds__(kMassTiles * kBlockRows) k_cache8_mass(const AttArgs a, const int rounds) {
-  __shared__ float2 stats[MIXKV_CACHE8_MAX_QUERIES];
-  pdl_wait();
-  const int u = blockIdx.x, first = blockIdx.y * (rounds * kMassTiles), r = threadIdx.x % kBlockRows;
-  const UnitTiles ut = unit_tiles(a, u);
-  if (first >= ut.tiles) return;
-  for (int e = threadIdx.x; e < a.R; e += blockDim.x) stats[e] = __ldcg(a.stats + (long long)u * a.R + e);
   __syncthreads();
-  const float* logits = a.logits + (long long)u * a.cap * (kBlockRows * a.pitch) + r * a.pitch;
+  if (joined) {
+    const int slot = per_row.div(warp), part = warp - slot * per_row.d, at_once = per_row.div(kEndWarps);
+    for (int base = c * at_once; base < a.R; base += C * at_once) {
+      const int r = base + slot;
+      const bool on = r < a.R;
+      const float4 s = stat[on ? r : 0];
+      float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+      constexpr int kAtOnce = 4;
+      for (int k = c0 + part; on && k <= c1; k += kAtOnce * per_row.d) {
+        float4 x[kAtOnce], mz[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const long long at = part_row(min(k + i * (int)per_row.d, c1), r);
+          mz[i] = __ldcg(a.part_mz + at);
+          x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          add_scaled(num, x[i], k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - s.x) * (mz[i].z * inverse(s.z)) : 0.f);
+      }
+      if (per_row.d > 1) {
+        __syncthreads();
+        sums[warp][lane] = num;
+        __syncthreads();
+        for (int w = 1; w < (int)per_row.d && !part; ++w) add_scaled(num, sums[warp + w][lane], 1.f);
+      }
+      if (on && !part) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, s.y, s.z);
+    }
+  }
+  if (!a.logits) return;
+  const UnitTiles ut = unit_tiles(a, u);
+  const int each = (ut.tiles + C - 1) / C, end = min((c + 1) * each, ut.tiles), in = tid % kBlockRows;
   // (what a query row does not see gets nothing of it, if it is NaN either)
-  const auto weight = [&](const float y, const int e) { return y != -INFINITY ? ex2(y - stats[e].x) * stats[e].y : 0.f; };
-#pragma unroll 4
-  for (int k = 0; k < rounds; ++k) {
-    const int i = first + k * kMassTiles + threadIdx.x / kBlockRows;
-    const TileAt at = tile_at(a, u, ut, i);
-    if (at.tile < 0 || at.row + r >= ut.n) continue;
-    float* mass = a.p.mass + (long long)at.tile * kBlockRows + r;     // (a page's tiles lie one after the other in both)
-    const float* row = logits + (long long)i * (kBlockRows * a.pitch);
-    float sum = 0.f;
+  const auto weight = [&](const float y, const int r) { return y != -INFINITY ? ex2(y - stat[r].x) * stat[r].y : 0.f; };
+  constexpr int kAtOnce = 4, kStep = kEndThreads / kBlockRows;       // (rows of a thread on their way)
+#pragma unroll 1
+  for (int i = c * each + tid / kBlockRows; i < end; i += kAtOnce * kStep) {
+    TileAt at[kAtOnce];
+    float was[kAtOnce], sum[kAtOnce];
+    const float* row = a.logits + (((long long)u * a.cap + i) * kBlockRows + in) * a.pitch;
+    const long long next = (long long)kStep * kBlockRows * a.pitch;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      at[k] = i + k * kStep < end ? tile_at(a, u, ut, i + k * kStep) : TileAt{-1, kNoRow};
+      if (at[k].row + in >= ut.n) at[k].tile = -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {     // (a page's tiles lie one after the other in the pool and in the masses)
+      sum[k] = 0.f;
+      was[k] = at[k].tile >= 0 ? fresh(a.p.mass + (long long)at[k].tile * kBlockRows + in) : 0.f;
+    }
     if (a.pitch == 4) {
-      const float4 y = __ldcg(reinterpret_cast<const float4*>(row));
-      sum = weight(y.x, 0) + weight(y.y, 1) + weight(y.z, 2) + (a.R > 3 ? weight(y.w, 3) : 0.f);
+      float4 y[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        y[k] = at[k].tile >= 0 ? __ldcg(reinterpret_cast<const float4*>(row + k * next)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+        sum[k] = weight(y[k].x, 0) + weight(y[k].y, 1) + weight(y[k].z, 2) + (a.R > 3 ? weight(y[k].w, 3) : 0.f);
     } else {
-#pragma unroll 4
-      for (int e = 0; e < a.R; e += 2) {
-        const float2 y = __ldcg(reinterpret_cast<const float2*>(row + e));
-        sum += weight(y.x, e);
-        if (e + 1 < a.R) sum += weight(y.y, e + 1);
+#pragma unroll 2
+      for (int r = 0; r < a.R; r += 2) {
+        float2 y[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          y[k] = at[k].tile >= 0 ? __ldcg(reinterpret_cast<const float2*>(row + k * next + r)) : make_float2(0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          sum[k] += weight(y[k].x, r);
+          if (r + 1 < a.R) sum[k] += weight(y[k].y, r + 1);
+        }
       }
     }
-    *mass += sum;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (at[k].tile >= 0) a.p.mass[(long long)at[k].tile * kBlockRows + in] = was[k] + sum[k];
   }
 }
 
@@ -736,7 +800,6 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
                            ((long long)window + q_tokens - 1 + kBlockRows - 2) / kBlockRows + 1;
     if (some < p->tiles) p->tiles = some;
   }
-  if (accumulate && p->tiles > 65535ll * kMassTiles) return MIXKV_ERR_UNSUPPORTED;
   p->cap = (int)p->tiles, p->pitch = ((int)R + 1) & ~1, p->sms = device_sm_count();
   const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
   p->part = up((size_t)att_slots(p->NT, p->sms) * 2 * R * kHeadDim * 4);
@@ -811,18 +874,18 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
   const cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = launch_pdl(kernel, dim3(grid, p.groups), dim3(32 * kAttWarps), smem, st, shape.S, a);
-  if (e == cudaSuccess && shape.ctas) {
+  if (e == cudaSuccess && (shape.ctas || accumulate)) {
     int per_row = 1;      // warps that go through the shares of one query row
-    while (per_row < kJoinWarps && per_row * 2 * units < shape.ctas) per_row *= 2;
-    const int at_once = kJoinWarps / per_row, blocks = (p.R + at_once - 1) / at_once;
-    e = launch_pdl(bf16 ? k_cache8_join<__nv_bfloat16> : k_cache8_join<__half>, dim3((unsigned)(units * blocks)),
-                   dim3(kJoinWarps * 32), 0, st, 1, a, Divider(per_row), Divider(blocks));
-  }
-  if (e == cudaSuccess && accumulate) {
-    const long long rounds = units * p.tiles > 16ll * kMassTiles * p.sms ? 4 : 1, each = rounds * kMassTiles;
-    const long long chunks = (p.tiles + each - 1) / each;
-    e = launch_pdl(k_cache8_mass, dim3((unsigned)units, (unsigned)chunks), dim3(kMassTiles * kBlockRows), 0, st, 1, a,
-                   (int)rounds);
+    while (per_row < kEndWarps && per_row * 2 * units < shape.ctas) per_row *= 2;
+    const int at_once = kEndWarps / per_row;
+    long long C = shape.ctas ? (p.R + at_once - 1) / at_once : 1;      // CTAs of a unit
+    if (accumulate) {     // as many as are resident at once, and no fewer than sixteen tiles to one
+      const long long room = kEndPerSm * p.sms / units, some = (p.tiles + 15) / 16;
+      C = room < some ? room : some;
+      if (C < 1) C = 1;
+    }
+    e = launch_pdl(bf16 ? k_cache8_finish<__nv_bfloat16> : k_cache8_finish<__half>, dim3((unsigned)(units * C)), dim3(kEndThreads), 0,
+                   st, 1, a, Divider((uint32_t)C), Divider(per_row));
   }
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }

@@ -6,7 +6,7 @@
 // a run of rows: it counts what it keeps, learns where its run begins in the list, and writes it in order.  Equal keys are taken from the
 // lowest row on, so the list does not depend on how the rows were dealt out.
 //
-// k_cache8_move: a warp has K or V of one tile of the new cache, as an append has (cache8_rows.cu), and gathers its rows.
+// k_cache8_move: a warp has a tile of the new cache, and gathers its rows: lanes as in an append (cache8_rows.cu).
 #include <cooperative_groups.h>
 
 #include "cache8.cuh"
@@ -194,56 +194,59 @@ __global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane & 7, sub = lane >> 3;
   const int job = blockIdx.x * kMoveWarps + warp;
   pdl_wait();
-  if (job >= 2 * tasks) return;
-  const bool values = job & 1;
-  const int u = a.by_slots.div(job >> 1), t = (job >> 1) - u * a.slots;
-  const int kept = min(fresh(a.into.rows + u), a.budget), begin = t * kBlockRows;
-  if (begin >= kept) return;
+  if (job >= tasks) return;
+  const int u = a.by_slots.div(job), t = job - u * a.slots, begin = t * kBlockRows;
+  // row `lane` of the tile (lanes 0 .. 15): its place in the old cache, -1: none.  (What is asked for does not wait for the number of rows.)
+  const int kept = min(fresh(a.into.rows + u), a.budget);
   const int page = a.into.by_tiles.div(t), in = t - page * a.into.tiles;
   const int id = page < a.into.max_pages ? fresh(a.into.table + (long long)u * a.into.max_pages + page) : -1;
+  int row = lane < kBlockRows && begin + lane < a.budget ? fresh(a.idx + (long long)u * a.budget + begin + lane) : -1;
+  if (begin >= kept) return;
   if (id < 0 || id >= a.into.num_pages) {
     if (a.status && lane == 0) *a.status = MIXKV_ERR_INVALID_ARG;
     return;
   }
-  // row `lane` of the tile (lanes 0 .. 15): its place in the old cache, -1: none
-  int row = -1;
-  long long block = -1;
-  if (lane < kBlockRows && begin + lane < kept) {
-    row = fresh(a.idx + (long long)u * a.budget + begin + lane);
+  int block = -1;
+  if (row >= 0) {
     const int from = a.p.by_rows.div(row), old = fresh(a.p.table + (long long)u * a.p.max_pages + from);
     row -= from * a.p.page_rows;
-    if (old >= 0 && old < a.p.num_pages) block = (long long)old * a.p.tiles + (row >> 4);
+    if (old >= 0 && old < a.p.num_pages) block = old * a.p.tiles + (row >> 4);
   }
-  uint4 codes[4];
-  float scale[4];
+  uint4 codes[2][4];
+  float2 scale[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const long long at = __shfl_sync(0xffffffffu, block, 4 * i + sub);
-    const int r = __shfl_sync(0xffffffffu, row, 4 * i + sub) & 15;
-    codes[i] = make_uint4(0, 0, 0, 0), scale[i] = 0.f;
+    const int at = __shfl_sync(0xffffffffu, block, 4 * i + sub), r = __shfl_sync(0xffffffffu, row, 4 * i + sub) & 15;
+    codes[0][i] = codes[1][i] = make_uint4(0, 0, 0, 0), scale[i] = make_float2(0.f, 0.f);
     if (at >= 0) {
-      const unsigned char* tile = a.p.pool + at * kBlockBytes;
-      codes[i] = *reinterpret_cast<const uint4*>(tile + (values ? kBlockV : 0) + piece_at(r, g));
-      scale[i] = *(reinterpret_cast<const float*>(tile + kBlockScales) + values);
+      const unsigned char* tile = a.p.pool + (long long)at * kBlockBytes;
+      codes[0][i] = *reinterpret_cast<const uint4*>(tile + piece_at(r, g));
+      codes[1][i] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(r, g));
+      scale[i] = *reinterpret_cast<const float2*>(tile + kBlockScales);
     }
   }
-  // the largest magnitude: of a row's codes, times its scale (rounding keeps the order)
-  float most = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) most = max_nan(most, fabsf(__fmul_rn(largest_code<E4M3>(codes[i]), scale[i])));
-  const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);
-  const float to = scale_of_largest<E4M3>(__uint_as_float(bits)), by = by_scale(to);
-  unsigned char* tile = block_ptr(a.into, id, in);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[16];
-    values16<E4M3>(codes[i], scale[i], x);
-    *reinterpret_cast<uint4*>(tile + (values ? kBlockV : 0) + piece_at(4 * i + sub, g)) = encode16<E4M3>(x, by);
-  }
-  if (lane == 0) *(reinterpret_cast<float*>(tile + kBlockScales) + values) = to;
-  if (values && a.into.mass && lane < kBlockRows && begin + lane < kept)
+  if (a.into.mass && lane < kBlockRows && begin + lane < kept)
     a.into.mass[(long long)id * a.into.page_rows + in * kBlockRows + lane] =
-        block >= 0 ? fresh(a.p.mass + block * kBlockRows + (row & 15)) : 0.f;
+        block >= 0 ? fresh(a.p.mass + (long long)block * kBlockRows + (row & 15)) : 0.f;
+  unsigned char* tile = block_ptr(a.into, id, in);
+  float to[2];
+#pragma unroll
+  for (int v = 0; v < 2; ++v) {
+    // the largest magnitude: of a row's codes, times its scale (rounding keeps the order)
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max_nan(most, fabsf(__fmul_rn(largest_code<E4M3>(codes[v][i]), v ? scale[i].y : scale[i].x)));
+    const uint32_t bits = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);
+    to[v] = scale_of_largest<E4M3>(__uint_as_float(bits));
+    const float by = by_scale(to[v]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x2 x[8];
+      values16<E4M3>(codes[v][i], v ? scale[i].y : scale[i].x, x);
+      *reinterpret_cast<uint4*>(tile + v * kBlockV + piece_at(4 * i + sub, g)) = encode16<E4M3>(x, by);
+    }
+  }
+  if (lane == 0) *reinterpret_cast<float2*>(tile + kBlockScales) = make_float2(to[0], to[1]);
 }
 
 }  // namespace
@@ -280,6 +283,6 @@ extern "C" int mixkv_cache_evict(const mixkv_cache8* c, const mixkv_cache8* into
   const int tasks = (int)(units * slots);
   if (e == cudaSuccess)
     e = launch_pdl(c->code == MIXKV_CODE_E4M3 ? k_cache8_move<true> : k_cache8_move<false>,
-                   dim3((unsigned)((2LL * tasks + kMoveWarps - 1) / kMoveWarps)), dim3(kMoveWarps * 32), 0, st, 1, a, tasks);
+                   dim3((unsigned)((tasks + kMoveWarps - 1) / kMoveWarps)), dim3(kMoveWarps * 32), 0, st, 1, a, tasks);
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }

@@ -76,23 +76,26 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_cache8_append(const RowArgs 
   if (job >= 2 * tasks) return;
   const bool values = job & 1;
   const TileSpan s = tile_span(a, job >> 1);
-  const bool placed = s.id >= 0 && s.id < a.p.num_pages;
-  const bool bad = s.bad || (s.lo < s.hi && (!placed || s.first > s.lo || s.last < s.hi));
-  if (bad && a.status && lane == 0) *a.status = MIXKV_ERR_INVALID_ARG;
-  if (s.lo >= s.hi || !placed) return;
-  unsigned char* tile = block_ptr(a.p, s.id, s.in);
-  unsigned char* codes = tile + (values ? kBlockV : 0);
-  float* scale_at = reinterpret_cast<float*>(tile + kBlockScales) + values;
+  if (s.lo >= s.hi) {
+    if (s.bad && a.status && lane == 0) *a.status = MIXKV_ERR_INVALID_ARG;
+    return;
+  }
   const long long row = values ? a.v_row : a.k_row, head = a.per_head ? 0 : s.h * (values ? a.v_head : a.k_head);
   const T* from = (values ? v : k) + head + 16 * g;
   Sixteen x[4] = {};
   uint4 old[4] = {};
   float was = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 4; ++i) {       // (on their way before it is known where they go)
     const int r = 4 * i + sub;
     if (r >= s.first && r < s.last) load_sixteen(x[i], from + (s.token + r) * row);
   }
+  const bool placed = s.id >= 0 && s.id < a.p.num_pages;
+  if ((s.bad || !placed || s.first > s.lo || s.last < s.hi) && a.status && lane == 0) *a.status = MIXKV_ERR_INVALID_ARG;
+  if (!placed) return;
+  unsigned char* tile = block_ptr(a.p, s.id, s.in);
+  unsigned char* codes = tile + (values ? kBlockV : 0);
+  float* scale_at = reinterpret_cast<float*>(tile + kBlockScales) + values;
   if (s.begun) {
     was = *scale_at;
 #pragma unroll
@@ -113,7 +116,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_cache8_append(const RowArgs 
     if (is_new) {
       old[i] = encode16<T, E4M3>(x[i], by);
     } else if (s.begun && grown) {
-      float y[16];
+      f32x2 y[8];
       values16<E4M3>(old[i], was, y);
       old[i] = encode16<E4M3>(y, by);
     }
@@ -144,11 +147,15 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_cache8_read(const RowArgs a,
   for (int i = 0; i < 4; ++i) {
     const int r = 4 * i + sub;
     if (r < s.first || r >= s.last) continue;
-    float y[16];
+    f32x2 y[8];
     values16<E4M3>(codes[i], scale, y);
     Sixteen out;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) out.w[j] = narrow2<T>(y[2 * j], y[2 * j + 1]);
+    for (int j = 0; j < 8; ++j) {
+      float lo, hi;
+      unpack2(y[j], lo, hi);
+      out.w[j] = narrow2<T>(lo, hi);
+    }
     store_sixteen(to + (s.token + r) * row, out);
   }
 }

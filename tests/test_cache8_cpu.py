@@ -138,7 +138,7 @@ def test_append_and_read_refuse(lib, change, status):
     (dict(q=0), -1), (dict(q=ONE + 8), -1), (dict(type=3), -1), (dict(qb=4), -1), (dict(qt=-8), -1), (dict(T=0), -1), (dict(G=0), -1),
     (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(max_rows=0), -1), (dict(window=-1), -1),
     (dict(sinks=-1), -1), (dict(ws=0), -1), (dict(ws=ONE + 8), -1), (dict(out=0), -1), (dict(out=ONE + 4), -1), (dict(T=43, G=3), -2),
-    (dict(nbytes=1000), -3), (dict(accumulate=1, mass=0), -1), (dict(accumulate=1, max_rows=1 << 30, pages=1 << 22, page_rows=256), -2)])
+    (dict(nbytes=1000), -3), (dict(accumulate=1, mass=0), -1)])
 def test_attention_refuses(lib, change, status):
     a = dict(q=ONE, type=0, qb=1536, qt=1536, T=1, G=4, scale=0.0, max_rows=100, window=0, sinks=0, accumulate=0, ws=ONE, nbytes=1 << 40,
              out=ONE, mass=ONE, pages=4, page_rows=64)
