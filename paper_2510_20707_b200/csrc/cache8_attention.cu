@@ -31,7 +31,7 @@ constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is no
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
 constexpr int kAttUnits = 1024;                // most units whose tiles are dealt out evenly
-constexpr int kAttFew = 4, kAttFewRows = 16;   // tiles of a warp (att_shape)
+constexpr int kAttFew = 6, kAttMany = 16, kAttEven = 24;   // tiles of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
 constexpr float kSmallest = 1.f / 4096;        // scale of values that goes into weights of fp16, in units of the largest
 constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
@@ -63,6 +63,7 @@ struct AttArgs {
   float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
   float4* part_mz;           // [2 ctas][R]: (reference, sum, unit of the sums of values, -)
   float2* stats;             // [units][R]: (reference, 1 / sum) of a query row
+  bool inside;               // the weights are added up by the clusters
   float* logits;             // [units][cap][16][pitch], log2 units; nullptr: weights are not asked for
   int cap, pitch;            // tiles of a unit that a call can see; query rows, made even
   void* out;
@@ -150,7 +151,7 @@ __device__ __forceinline__ void stage_queries(const AttArgs& a, const int u, con
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bits = __vmaxu2(bits, word_of(raw[i], e) & 0x7fff7fffu);
+      for (int e = 0; e < 4; ++e) bits = max_u16x2(bits, word_of(raw[i], e) & 0x7fff7fffu);
     bits = max(bits & 0xffffu, bits >> 16);
     bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
     bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
@@ -367,6 +368,77 @@ struct AttState {
   }
 };
 
+// Adds to the mass of a unit's rows what they got, a thread a row at a time: of the tiles number(0 .. n - 1).  stat: (reference, 1 / sum)
+// of the query rows, there once ready() has been called (by the whole CTA), which the first rows' logits do not wait for.
+template <int THREADS, typename Number, typename Ready>
+__device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const UnitTiles& ut, const float2* stat, const int n,
+                                            const Number& number, const Ready& ready) {
+  constexpr int kAtOnce = 4, kStep = THREADS / kBlockRows;       // rows of a thread on their way, eight query rows of each
+  const int in = threadIdx.x % kBlockRows;
+  const bool fours = (a.pitch & 3) == 0;
+  int at[kAtOnce];
+  float was[kAtOnce];
+  const float* row[kAtOnce];
+  float4 y[kAtOnce][2];
+  const auto load = [&](const int r0) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + 4 * h;
+        if (at[k] < 0 || r >= a.pitch) continue;
+        if (fours) {
+          y[k][h] = fresh(reinterpret_cast<const float4*>(row[k] + r));
+        } else {
+          const float2 lo = fresh(reinterpret_cast<const float2*>(row[k] + r));
+          const float2 hi = r + 2 < a.pitch ? fresh(reinterpret_cast<const float2*>(row[k] + r + 2)) : make_float2(0.f, 0.f);
+          y[k][h] = make_float4(lo.x, lo.y, hi.x, hi.y);
+        }
+      }
+  };
+  const auto begin = [&](const int i) {
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int tile = number(min(i + k * kStep, n - 1));
+      const TileAt t = tile_at(a, u, ut, tile);
+      at[k] = i + k * kStep < n && t.tile >= 0 && t.row + in < ut.n ? t.tile : -1;
+      row[k] = a.logits + (((long long)u * a.cap + tile) * kBlockRows + in) * a.pitch;
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)     // (a page's tiles lie one after the other in the pool and in the masses)
+      if (at[k] >= 0) was[k] = fresh(a.p.mass + (long long)at[k] * kBlockRows + in);
+    load(0);
+  };
+  // (what a query row does not see gets nothing of it, if it is NaN either)
+  const auto weight = [&](const float x, const int r) { return r < a.R && x != -INFINITY ? ex2(x - stat[r].x) * stat[r].y : 0.f; };
+  int i = threadIdx.x / kBlockRows;
+  if (i < n) begin(i);
+  ready();
+#pragma unroll 1
+  while (i < n) {
+    float sum[kAtOnce] = {};
+#pragma unroll 1
+    for (int r = 0;;) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (r + 4 * h < a.R) {
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k)
+            sum[k] += weight(y[k][h].x, r + 4 * h) + weight(y[k][h].y, r + 4 * h + 1) + weight(y[k][h].z, r + 4 * h + 2) +
+                      weight(y[k][h].w, r + 4 * h + 3);
+        }
+      r += 8;
+      if (r >= a.R) break;
+      load(r);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (at[k] >= 0) a.p.mass[(long long)at[k] * kBlockRows + in] = was[k] + sum[k];
+    i += kAtOnce * kStep;
+    if (i < n) begin(i);
+  }
+}
+
 // grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
 template <typename T, int NT, bool E4M3>
 __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_attention(const AttArgs a) {
@@ -393,6 +465,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
   static_assert(NT * 2048 <= W * kSums * 4, "queries fit the place of the sums");
   __shared__ int starts[kAttUnits + 1];      // first tile of every unit
   __shared__ int warp_total[W];
+  __shared__ float2 stat[Q];                 // (reference, 1 / sum) of a cluster's query rows
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const bool shares = a.ctas > 0;
@@ -574,6 +647,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
         if (whole) {
           store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
           if (dim == 0) store_stat(a, u, first + r, M, den);
+          if (dim == 0 && !shares) stat[r] = make_float2(M, one_over(den));
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
           *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
@@ -590,7 +664,18 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       ++u;
       continue;
     }
-    if (whole) return;
+    // (a cluster that has all query rows of its unit adds up the weights of the tiles that its CTAs read)
+    const auto weigh = [&]() {
+      if (!a.inside) return;
+      __syncthreads();
+      const int mine = unit_tiles(a, u).tiles - crank * W, round = S * W;     // tiles from the CTA's first on; to its next ones
+      const int tiles = mine <= 0 ? 0 : mine / round * W + min(mine % round, W);
+      add_weights<kThreads>(a, u, unit_tiles(a, u), stat, tiles, [&](const int i) { return crank * W + i / W * round + i % W; }, [] {});
+    };
+    if (whole) {
+      weigh();
+      return;
+    }
 
     // ---- the CTAs of the cluster merge through distributed shared memory, each a slice of the outputs
     cluster.sync();
@@ -601,6 +686,14 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       if (r == 0) allv[k] = *cluster.map_shared_rank(xv, k);
     }
     __syncthreads();
+    if (a.inside) {
+      for (int r = tid; r < live; r += kThreads) {
+        float M = kNoRef, den = 0.f;
+        for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+        for (int k = 0; k < S; ++k) den = fmaf(allz[k * Q + r], ex2(allm[k * Q + r] - M), den);
+        stat[r] = make_float2(M, one_over(den));
+      }
+    }
     for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
       const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
       float M = kNoRef, unit = FLT_MIN;
@@ -616,130 +709,91 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_atten
       store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
       if (dim == 0) store_stat(a, u, first + r, M, den);
     }
+    weigh();
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
     return;
   }
 }
 
-// What is left when all tiles have been read.  grid.x: units, each_unit.d CTAs to one.
-//  - Shares: statistics of the query rows of units that several CTAs had a part of (every CTA of a unit for itself), the rows' outputs
-//    (each by one CTA, `per_row.d` warps, a power of two, taking the shares in turn) and zeros for units without rows.
-//  - Weights: every CTA adds what its run of the unit's rows got to their mass, a thread a row at a time.
-// In one kernel, since a launch and its first loads cost as much as either.
-constexpr int kEndWarps = 8, kEndThreads = kEndWarps * 32, kEndPerSm = 6;
+// What is left when all tiles have been read.  grid.x: units, `join` + `add` CTAs to one.
+//  - join: outputs of the query rows of units that several CTAs had a part of, `per_row.d` warps, a power of two, taking the shares of a
+//    row in turn, and zeros for units without rows.
+//  - add: what a run of the unit's rows got of the weights goes to their mass.
+// Every CTA works out the statistics of the query rows for itself: the outputs and the masses do not wait for one another, nor either of them for
+// a launch and its first loads, which would cost as much as they do.
+constexpr int kEndWarps = 8, kEndThreads = kEndWarps * 32, kEndPerSm = 3;
 template <typename T>
-__global__ void __launch_bounds__(kEndThreads) k_cache8_finish(const AttArgs a, const Divider each_unit, const Divider per_row) {
+__global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const AttArgs a, const Divider by_unit, const int join, const int add,
+                                                                         const Divider per_row) {
   __shared__ float4 sums[kEndWarps][32];
-  __shared__ float4 stat[MIXKV_CACHE8_MAX_QUERIES];      // (reference, 1 / sum, unit, -)
+  __shared__ float2 stat[MIXKV_CACHE8_MAX_QUERIES];      // (reference, 1 / sum)
+  __shared__ float units[MIXKV_CACHE8_MAX_QUERIES];      // of sums of values
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int u = each_unit.div(blockIdx.x), C = (int)each_unit.d, c = blockIdx.x - u * C;
+  const int u = by_unit.div(blockIdx.x), c = blockIdx.x - u * (int)by_unit.d;
   pdl_wait();
   const int2 span = a.ctas ? __ldcg(a.spans + u) : make_int2(0, 0);
   const int c0 = span.x >> 1, c1 = span.y;
   const bool joined = c0 != c1;
   const auto part_row = [&](const int k, const int r) { return (2LL * k + (k == c0 ? span.x & 1 : 0)) * a.R + r; };
-  if (joined) {
-    int lanes = 1;       // that share a query row
-    while (lanes < 32 && lanes < c1 - c0 + 1) lanes *= 2;
-    const int at = lane & (lanes - 1), at_once = 32 / lanes;
-    for (int r = warp * at_once + lane / lanes; r - lane / lanes < a.R; r += kEndWarps * at_once) {
-      float M = kNoRef, den = 0.f, unit = FLT_MIN;
-      for (int k = c0 + at; k <= c1 && r < a.R; k += lanes) {
-        const float4 mz = __ldcg(a.part_mz + part_row(k, r));
-        const float to = fmaxf(M, mz.x);
-        den = fmaf(den, ex2(M - to), mz.y * ex2(mz.x - to));
-        M = to, unit = fmaxf(unit, mz.z);
-      }
-      float most = M;
-      for (int o = 1; o < lanes; o *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o)), unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
-      den *= ex2(M - most);
-      for (int o = 1; o < lanes; o *= 2) den += __shfl_xor_sync(0xffffffffu, den, o);
-      if (at == 0 && r < a.R) stat[r] = make_float4(most, one_over(den), unit, 0.f);
-    }
-  } else if (a.logits) {
-    for (int r = tid; r < a.R; r += kEndThreads) {
-      const float2 s = __ldcg(a.stats + (long long)u * a.R + r);
-      stat[r] = make_float4(s.x, s.y, 0.f, 0.f);
-    }
-  }
-  __syncthreads();
-  if (joined) {
-    const int slot = per_row.div(warp), part = warp - slot * per_row.d, at_once = per_row.div(kEndWarps);
-    for (int base = c * at_once; base < a.R; base += C * at_once) {
-      const int r = base + slot;
-      const bool on = r < a.R;
-      const float4 s = stat[on ? r : 0];
-      float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-      constexpr int kAtOnce = 4;
-      for (int k = c0 + part; on && k <= c1; k += kAtOnce * per_row.d) {
-        float4 x[kAtOnce], mz[kAtOnce];
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          const long long at = part_row(min(k + i * (int)per_row.d, c1), r);
-          mz[i] = __ldcg(a.part_mz + at);
-          x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
+  const auto statistics = [&]() {
+    if (joined) {
+      int lanes = 1;       // that share a query row
+      while (lanes < 32 && lanes < c1 - c0 + 1) lanes *= 2;
+      const int at = lane & (lanes - 1), at_once = 32 / lanes;
+      for (int r = warp * at_once + lane / lanes; r - lane / lanes < a.R; r += kEndWarps * at_once) {
+        float M = kNoRef, den = 0.f, unit = FLT_MIN;
+        for (int k = c0 + at; k <= c1 && r < a.R; k += lanes) {
+          const float4 mz = __ldcg(a.part_mz + part_row(k, r));
+          const float to = fmaxf(M, mz.x);
+          den = fmaf(den, ex2(M - to), mz.y * ex2(mz.x - to));
+          M = to, unit = fmaxf(unit, mz.z);
         }
-#pragma unroll
-        for (int i = 0; i < kAtOnce; ++i)
-          add_scaled(num, x[i], k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - s.x) * (mz[i].z * inverse(s.z)) : 0.f);
-      }
-      if (per_row.d > 1) {
-        __syncthreads();
-        sums[warp][lane] = num;
-        __syncthreads();
-        for (int w = 1; w < (int)per_row.d && !part; ++w) add_scaled(num, sums[warp + w][lane], 1.f);
-      }
-      if (on && !part) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, s.y, s.z);
-    }
-  }
-  if (!a.logits) return;
-  const UnitTiles ut = unit_tiles(a, u);
-  const int each = (ut.tiles + C - 1) / C, end = min((c + 1) * each, ut.tiles), in = tid % kBlockRows;
-  // (what a query row does not see gets nothing of it, if it is NaN either)
-  const auto weight = [&](const float y, const int r) { return y != -INFINITY ? ex2(y - stat[r].x) * stat[r].y : 0.f; };
-  constexpr int kAtOnce = 4, kStep = kEndThreads / kBlockRows;       // (rows of a thread on their way)
-#pragma unroll 1
-  for (int i = c * each + tid / kBlockRows; i < end; i += kAtOnce * kStep) {
-    TileAt at[kAtOnce];
-    float was[kAtOnce], sum[kAtOnce];
-    const float* row = a.logits + (((long long)u * a.cap + i) * kBlockRows + in) * a.pitch;
-    const long long next = (long long)kStep * kBlockRows * a.pitch;
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      at[k] = i + k * kStep < end ? tile_at(a, u, ut, i + k * kStep) : TileAt{-1, kNoRow};
-      if (at[k].row + in >= ut.n) at[k].tile = -1;
-    }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {     // (a page's tiles lie one after the other in the pool and in the masses)
-      sum[k] = 0.f;
-      was[k] = at[k].tile >= 0 ? fresh(a.p.mass + (long long)at[k].tile * kBlockRows + in) : 0.f;
-    }
-    if (a.pitch == 4) {
-      float4 y[kAtOnce];
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-        y[k] = at[k].tile >= 0 ? __ldcg(reinterpret_cast<const float4*>(row + k * next)) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-        sum[k] = weight(y[k].x, 0) + weight(y[k].y, 1) + weight(y[k].z, 2) + (a.R > 3 ? weight(y[k].w, 3) : 0.f);
-    } else {
-#pragma unroll 2
-      for (int r = 0; r < a.R; r += 2) {
-        float2 y[kAtOnce];
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
-          y[k] = at[k].tile >= 0 ? __ldcg(reinterpret_cast<const float2*>(row + k * next + r)) : make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k) {
-          sum[k] += weight(y[k].x, r);
-          if (r + 1 < a.R) sum[k] += weight(y[k].y, r + 1);
+        float most = M;
+        for (int o = 1; o < lanes; o *= 2) {
+          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
         }
+        den *= ex2(M - most);
+        for (int o = 1; o < lanes; o *= 2) den += __shfl_xor_sync(0xffffffffu, den, o);
+        if (at == 0 && r < a.R) stat[r] = make_float2(most, one_over(den)), units[r] = unit;
       }
+    } else if (c >= join) {
+      for (int r = tid; r < a.R; r += kEndThreads) stat[r] = __ldcg(a.stats + (long long)u * a.R + r);
+    }
+    __syncthreads();
+  };
+  if (c >= join) {
+    const UnitTiles ut = unit_tiles(a, u);
+    const int each = (ut.tiles + add - 1) / add, begin = min((c - join) * each, ut.tiles), n = min(each, ut.tiles - begin);
+    if (n > 0) add_weights<kEndThreads>(a, u, ut, stat, n, [&](const int i) { return begin + i; }, statistics);
+    return;
+  }
+  if (!joined) return;
+  statistics();
+  const int slot = per_row.div(warp), part = warp - slot * per_row.d, at_once = per_row.div(kEndWarps), r = c * at_once + slot;
+  const bool on = r < a.R;
+  const float2 s = stat[on ? r : 0];
+  const float unit = units[on ? r : 0];
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kAtOnce = 4;
+  for (int k = c0 + part; on && k <= c1; k += kAtOnce * per_row.d) {
+    float4 x[kAtOnce], mz[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const long long at = part_row(min(k + i * (int)per_row.d, c1), r);
+      mz[i] = __ldcg(a.part_mz + at);
+      x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
     }
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)
-      if (at[k].tile >= 0) a.p.mass[(long long)at[k].tile * kBlockRows + in] = was[k] + sum[k];
+    for (int i = 0; i < kAtOnce; ++i)
+      add_scaled(num, x[i], k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - s.x) * (mz[i].z * inverse(unit)) : 0.f);
   }
+  if (per_row.d > 1) {
+    sums[warp][lane] = num;
+    __syncthreads();
+    for (int w = 1; w < (int)per_row.d && !part; ++w) add_scaled(num, sums[warp + w][lane], 1.f);
+  }
+  if (on && !part) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, s.y, unit);
 }
 
 using AttKernel = void (*)(AttArgs);
@@ -757,21 +811,36 @@ AttKernel att_kernel(const bool bf16, const bool e4m3, const int NT) {
               : e4m3 ? att_kernel_of<__half, true>(NT) : att_kernel_of<__half, false>(NT);
 }
 
-// How the work is split.  units: (sequence, head) pairs; groups of query rows; tiles of the longest unit.  resident(n): clusters of
-// n CTAs that are resident at once.  A cluster per unit, or all tiles dealt out evenly and joined by a second kernel.
+// How the work is split.  units: (sequence, head) pairs; groups of query rows; tiles of the longest unit; even: a window cuts long units
+// to one length.  resident(n): clusters of n CTAs that are resident at once.
+//
+// A cluster per unit, or all tiles dealt out evenly and joined by a second kernel, which costs a call 4 us.  us a call, one token of
+// four query heads, heads of one length (and of lengths from one row to that), cluster / shares:
+//     heads x rows    no weights                        weights counted
+//     8 x 4096        11.5 / 10.8  (11.3 / 11.5)        13.5 / 12.2  (13.3 / 13.2)      eight tiles a warp on 64 CTAs
+//     32 x 4096       15.6 / 18.1  (13.4 / 15.5)        18.0 / 20.8  (15.8 / 18.5)      eight on 256
+//     64 x 4096       19.4 / 22.6  (17.0 / 18.5)        23.0 / 26.6  (20.4 / 22.2)      eleven on 384
+//     256 x 1024      19.8 / 22.9  (17.4 / 20.0)        23.9 / 26.8  (20.4 / 23.3)      sixteen on 256
+//     64 x 8192       30.6 / 32.1  (26.5 / 22.9)        36.3 / 37.3  (31.9 / 27.1)      21 on 384
+//     128 x 4096      30.3 / 32.1  (26.9 / 24.9)        36.2 / 38.3  (32.3 / 29.4)      21 on 384
+//     256 x 2048      32.4 / 32.3  (30.1 / 25.0)        42.1 / 38.2  (35.1 / 29.1)      32 on 256
+// So clusters up to sixteen tiles a warp (24 behind a window: 128 heads of a window of 4096 30.7 / 33.7), where they fill half of the GPU
+// at least, and up to six where they do not.  With more query rows a tile takes longer and the join counts for less (32 of them: 64 x
+// 8192 53.5 / 61.1 (50.9 / 46.8), 8 x 4096 17.7 / 16.9).
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all tiles
 };
 int att_slots(const int NT, const int sms) { return att_per_sm(NT) * sms; }
 template <typename Resident>
-AttShape att_shape(const long long units, const int groups, const long long tiles, const int NT, const int sms, const Resident& resident) {
+AttShape att_shape(const long long units, const int groups, const long long tiles, const bool even, const int NT, const int sms,
+                   const Resident& resident) {
   const long long slots = att_slots(NT, sms), all = units * groups;
   long long most = slots / all < kMaxCluster ? slots / all : kMaxCluster;
   if (most > tiles / kAttWarps) most = tiles / kAttWarps;
   int S = most < 1 ? 1 : (int)most;
   while (S > 1 && all > resident(S)) --S;
   const long long alone = (tiles + S * kAttWarps - 1) / (S * kAttWarps);     // tiles of a warp
-  if (alone <= (NT == 1 ? kAttFew : kAttFewRows)) return {S, 0};
+  if (alone <= (NT == 1 && all * S * 2 < slots ? kAttFew : even ? kAttEven : kAttMany)) return {S, 0};
   if (units <= kAttUnits && groups < slots && units * tiles <= 0x7fffffffll) {
     const long long want = (units * tiles + kAttWarps * 4 - 1) / (kAttWarps * 4);     // (four tiles to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups)};
@@ -783,6 +852,7 @@ AttShape att_shape(const long long units, const int groups, const long long tile
 struct AttPlan {
   int R, groups, NT, cap, pitch, sms;
   long long tiles;                    // of the longest unit
+  bool even;                          // cut to that number by a window
   size_t part, spans, stats, logits, bytes;   // offsets: sums at 0, (reference, sum) at `part`
 };
 int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, const int32_t max_rows, const int32_t window,
@@ -794,11 +864,12 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
   p->R = (int)R, p->groups = (eights + kAttGroups - 1) / kAttGroups, p->NT = (eights + p->groups - 1) / p->groups;
   if (units * p->groups > 1 << 24) return MIXKV_ERR_UNSUPPORTED;
   const long long room = (long long)c->max_pages * c->page_rows, seen = max_rows < room ? max_rows : room;
-  p->tiles = (seen + kBlockRows - 1) / kBlockRows;
+  p->tiles = (seen + kBlockRows - 1) / kBlockRows, p->even = false;
   if (window > 0) {     // tiles of the sinks, of the window and of the tokens behind the first, each with a ragged end
     const long long some = ((long long)sinks + kBlockRows - 1) / kBlockRows +
                            ((long long)window + q_tokens - 1 + kBlockRows - 2) / kBlockRows + 1;
-    if (some < p->tiles) p->tiles = some;
+    p->even = some < p->tiles;
+    if (p->even) p->tiles = some;
   }
   p->cap = (int)p->tiles, p->pitch = ((int)R + 1) & ~1, p->sms = device_sm_count();
   const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
@@ -815,9 +886,9 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
 
 using namespace mixkv;
 
-extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t eights, int32_t sms,
+extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t even, int32_t eights, int32_t sms,
                                             const int32_t* resident, int32_t* ctas, int32_t* shared) {
-  const AttShape s = att_shape(units, groups, tiles, eights, sms, [&](const int n) { return resident[n]; });
+  const AttShape s = att_shape(units, groups, tiles, even != 0, eights, sms, [&](const int n) { return resident[n]; });
   *ctas = s.S, *shared = s.ctas;
 }
 
@@ -855,7 +926,7 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   const int dev = device_slot(), variant = 4 * p.NT + 2 * e4m3 + bf16;
   const AttKernel kernel = att_kernel(bf16, e4m3, p.NT);
   const size_t smem = att_smem(p.NT);
-  const AttShape shape = att_shape(units, p.groups, p.tiles, p.NT, p.sms, [&](const int size) {
+  const AttShape shape = att_shape(units, p.groups, p.tiles, p.even, p.NT, p.sms, [&](const int size) {
     if (!answered(ensure_smem(kernel, smem, done[variant], dev))) return 0;
     return fits[variant].ask(kernel, 32 * kAttWarps, smem, size, dev);
   });
@@ -870,22 +941,22 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   a.spans = reinterpret_cast<int2*>(ws + p.spans), a.stats = reinterpret_cast<float2*>(ws + p.stats);
   a.logits = accumulate ? reinterpret_cast<float*>(ws + p.logits) : nullptr, a.cap = p.cap, a.pitch = p.pitch;
   a.out = out;
+  a.inside = accumulate && !shape.ctas && p.groups == 1;
   a.per = ((p.R < 8 * p.NT ? p.R : 8 * p.NT) * (kHeadDim / 4) + shape.S - 1) / shape.S;
   const unsigned grid = shape.ctas ? (unsigned)shape.ctas : (unsigned)(units * shape.S);
   const cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = launch_pdl(kernel, dim3(grid, p.groups), dim3(32 * kAttWarps), smem, st, shape.S, a);
-  if (e == cudaSuccess && (shape.ctas || accumulate)) {
+  if (e == cudaSuccess && (shape.ctas || (accumulate && !a.inside))) {
     int per_row = 1;      // warps that go through the shares of one query row
     while (per_row < kEndWarps && per_row * 2 * units < shape.ctas) per_row *= 2;
-    const int at_once = kEndWarps / per_row;
-    long long C = shape.ctas ? (p.R + at_once - 1) / at_once : 1;      // CTAs of a unit
-    if (accumulate) {     // as many as are resident at once, and no fewer than sixteen tiles to one
-      const long long room = kEndPerSm * p.sms / units, some = (p.tiles + 15) / 16;
-      C = room < some ? room : some;
-      if (C < 1) C = 1;
+    const int at_once = kEndWarps / per_row, join = shape.ctas ? (p.R + at_once - 1) / at_once : 0;
+    long long add = 0;
+    if (accumulate && !a.inside) {       // sixty-four tiles to a CTA, where that is no more of them than twice those that are there at once
+      const long long some = (p.tiles + 63) / 64, room = 2 * kEndPerSm * p.sms / units;
+      add = some < room ? some : room < 1 ? 1 : room;
     }
-    e = launch_pdl(bf16 ? k_cache8_finish<__nv_bfloat16> : k_cache8_finish<__half>, dim3((unsigned)(units * C)), dim3(kEndThreads), 0,
-                   st, 1, a, Divider((uint32_t)C), Divider(per_row));
+    e = launch_pdl(bf16 ? k_cache8_finish<__nv_bfloat16> : k_cache8_finish<__half>, dim3((unsigned)(units * (join + add))),
+                   dim3(kEndThreads), 0, st, 1, a, Divider((uint32_t)(join + add)), join, (int)add, Divider(per_row));
   }
   return e == cudaSuccess ? MIXKV_OK : MIXKV_ERR_CUDA;
 }

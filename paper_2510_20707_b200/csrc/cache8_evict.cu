@@ -16,7 +16,7 @@ namespace cg = cooperative_groups;
 namespace mixkv {
 namespace {
 
-constexpr int kPickThreads = 1024, kPickWarps = kPickThreads / 32;
+constexpr int kPickThreads = 1024, kPickWarps = kPickThreads / 32;   // (as many warps as a warp has lanes)
 constexpr int kBins = 2048;
 constexpr int kPickKeys = 40960;       // keys that a CTA keeps in shared memory
 constexpr int kPickRows = 2048;        // rows that a CTA of a cluster should have
@@ -43,6 +43,11 @@ __device__ __forceinline__ uint32_t key_of(const CachePool& p, const int u, cons
   const float m = fresh(p.mass + (long long)id * p.page_rows + (row - page * p.page_rows)) + 0.f;      // (-0 is 0)
   const uint32_t b = __float_as_uint(m);
   return m != m ? 0xffffffffu : b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u);
+}
+
+// Of the numbers that lanes have, one for each warp: the sum of those before warp `warp`'s.
+__device__ __forceinline__ int sum_below(const int x, const int warp, const int lane) {
+  return __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
 }
 
 __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a) {
@@ -79,41 +84,38 @@ __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a)
   const int each = (m + S - 1) / S, lo = min(rank * each, m), hi = min(lo + each, m), mine = hi - lo;
   const bool cached = mine <= a.cached;
   auto key = [&](const int i) { return cached ? keys[i] : key_of(a.p, u, m0 + lo + i); };
-  if (cached) {       // eight rows of a thread on their way: a page, then its mass, are two trips to memory
-    constexpr int kAtOnce = 8;
-    for (int i = tid; i < mine; i += kAtOnce * kPickThreads) {
-      uint32_t x[kAtOnce];
+  for (int i = tid; i < kBins; i += kPickThreads) hist[i] = 0;
+  __syncthreads();
+  // the highest digit is counted as the keys come; eight rows of a thread on their way: a page, then its mass, are two trips to memory
+  constexpr int kAtOnce = 8;
+  for (int i = tid; i < mine; i += kAtOnce * kPickThreads) {
+    uint32_t x[kAtOnce];
 #pragma unroll
-      for (int j = 0; j < kAtOnce; ++j) x[j] = key_of(a.p, u, m0 + lo + min(i + j * kPickThreads, mine - 1));
+    for (int j = 0; j < kAtOnce; ++j) x[j] = key_of(a.p, u, m0 + lo + min(i + j * kPickThreads, mine - 1));
 #pragma unroll
-      for (int j = 0; j < kAtOnce; ++j)
-        if (i + j * kPickThreads < mine) keys[i + j * kPickThreads] = x[j];
-    }
+    for (int j = 0; j < kAtOnce; ++j)
+      if (i + j * kPickThreads < mine) {
+        if (cached) keys[i + j * kPickThreads] = x[j];
+        atomicAdd(&hist[x[j] >> 21], 1);
+      }
   }
 
   uint32_t prefix = 0;       // digits that are known, in place
   int left = k;
   bool exact = false;        // all that have them are taken
-  int shift = 32;
+  int shift = 21;
 #pragma unroll 1
-  for (int pass = 0; pass < 3 && !exact; ++pass) {
-    const int bits = pass == 2 ? 10 : 11;
-    const uint32_t above = pass == 0 ? 0u : 0xffffffffu << shift;
-    shift -= bits;
-    for (int i = tid; i < kBins; i += kPickThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < mine; i += kPickThreads) {
-      const uint32_t x = key(i);
-      if ((x & above) == prefix) atomicAdd(&hist[(x >> shift) & ((1u << bits) - 1u)], 1);
-    }
+  for (int pass = 0;;) {
     cluster.sync();
     // thread t has bins 2047 - 2 t and the next lower one: the sum of what is above them
     const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
     int n1 = 0, n0 = 0;
-    for (int r = 0; r < S; ++r) {
-      const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(&hist[b0], r));
-      n0 += x.x, n1 += x.y;
-    }
+#pragma unroll
+    for (int r = 0; r < kMaxCluster; ++r)
+      if (r < S) {
+        const int2 x = *reinterpret_cast<const int2*>(cluster.map_shared_rank(&hist[b0], r));
+        n0 += x.x, n1 += x.y;
+      }
     int upto = n0 + n1;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -122,14 +124,24 @@ __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a)
     }
     if (lane == 31) warp_sum[warp] = upto;
     __syncthreads();
-    int before = upto - n0 - n1;
-    for (int w = 0; w < warp; ++w) before += warp_sum[w];
+    const int before = upto - n0 - n1 + sum_below(warp_sum[lane], warp, lane);
     if (before < left && before + n1 >= left) found[0] = b1, found[1] = left - before, found[2] = n1;
     else if (before + n1 < left && before + n1 + n0 >= left) found[0] = b0, found[1] = left - before - n1, found[2] = n0;
     cluster.sync();          // (no CTA clears its histogram before all have read it)
     prefix |= (uint32_t)found[0] << shift;
     left = found[1];
     exact = found[1] == found[2];
+    if (exact || ++pass == 3) break;
+    const uint32_t above = 0xffffffffu << shift;
+    const int bits = pass == 2 ? 10 : 11;
+    shift -= bits;
+    for (int i = tid; i < kBins; i += kPickThreads) hist[i] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < mine; i += kPickThreads) {
+      const uint32_t x = key(i);
+      if ((x & above) == prefix) atomicAdd(&hist[(x >> shift) & ((1u << bits) - 1u)], 1);
+    }
   }
   // kept: keys above `top`, and the first `left` of those equal to it
   const uint32_t top = exact ? prefix - 1u : prefix;     // (the lowest digits of a prefix are zero; key 0 alone is never all)
@@ -137,27 +149,29 @@ __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a)
 
   const int run = (((mine + kPickWarps - 1) / kPickWarps) + 31) & ~31, from = min(warp * run, mine), to = min(from + run, mine);
   int above = 0, equal = 0;
-  for (int i = from; i < to; i += 32) {
-    const uint32_t x = i + lane < to ? key(i + lane) : 0u;
-    const bool in = i + lane < to;
-    above += __popc(__ballot_sync(0xffffffffu, in && x > top));
-    equal += __popc(__ballot_sync(0xffffffffu, in && x == top));
+#pragma unroll 4
+  for (int i = from + lane; i - lane < to; i += 32) {
+    const uint32_t x = i < to ? key(i) : 0u;
+    above += i < to && x > top, equal += i < to && x == top;
   }
+  above = __reduce_add_sync(0xffffffffu, above), equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) warp_run[warp] = make_int2(above, equal);
   __syncthreads();
+  const int2 runs = warp_run[lane];
   if (warp == 0) {
-    int2 x = warp_run[lane];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x.x += __shfl_xor_sync(0xffffffffu, x.x, o), x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
-    if (lane == 0) cta_run = x;
+    const int x = __reduce_add_sync(0xffffffffu, runs.x), y = __reduce_add_sync(0xffffffffu, runs.y);
+    if (lane == 0) cta_run = make_int2(x, y);
   }
   cluster.sync();
-  above = equal = 0;         // of all rows before the warp's run
-  for (int r = 0; r < rank; ++r) {
-    const int2 x = *cluster.map_shared_rank(&cta_run, r);
-    above += x.x, equal += x.y;
-  }
-  for (int w = 0; w < warp; ++w) above += warp_run[w].x, equal += warp_run[w].y;
+  // of all rows before the warp's run
+  above = sum_below(runs.x, warp, lane), equal = sum_below(runs.y, warp, lane);
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r)
+    if (r < rank) {
+      const int2 x = *cluster.map_shared_rank(&cta_run, r);
+      above += x.x, equal += x.y;
+    }
+#pragma unroll 2
   for (int i = from; i < to; i += 32) {
     const bool in = i + lane < to;
     const uint32_t x = in ? key(i + lane) : 0u;

@@ -105,7 +105,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) k_cache8_append(const RowArgs 
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = __vmaxu2(most, x[i].w[j] & 0x7fff7fffu);
+    for (int j = 0; j < 8; ++j) most = max_u16x2(most, x[i].w[j] & 0x7fff7fffu);
   most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
   const float scale = larger_scale(was, scale_of_largest<E4M3>(widen2<T>(most).x)), by = by_scale(scale);
   const bool grown = !(scale == was);      // (or NaN: its codes are zero)

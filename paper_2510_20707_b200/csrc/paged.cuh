@@ -71,6 +71,12 @@ __device__ __forceinline__ unsigned char* tile_ptr(const PagePool& p, const int 
   return p.pool + (long long)(id * p.tiles + t) * kTileBytes;
 }
 
+// The larger of two words' halves, as unsigned numbers of 16 bits.
+__device__ __forceinline__ uint32_t max_u16x2(const uint32_t a, const uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // Two adjacent 16-bit values of a word, widened.
 template <typename T>
 __device__ __forceinline__ float2 widen2(uint32_t w);

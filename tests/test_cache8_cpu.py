@@ -204,7 +204,7 @@ def test_the_tiles_of_a_window_hold_all_that_is_seen():
 def test_how_a_call_is_split(lib, units, groups, tiles, eights):
     S, shared = C.c_int32(), C.c_int32()
     resident = (C.c_int32 * 9)(0, 444, 220, 140, 108, 85, 70, 60, 51)
-    lib.mixkv_internal_cache8_shape(C.c_int64(units), groups, C.c_int64(tiles), eights, 148, resident, C.byref(S), C.byref(shared))
+    lib.mixkv_internal_cache8_shape(C.c_int64(units), groups, C.c_int64(tiles), tiles % 2, eights, 148, resident, C.byref(S), C.byref(shared))
     assert 1 <= S.value <= 8 and 0 <= shared.value <= 444
     if shared.value:
         assert S.value == 1 and shared.value * groups <= 444 and units <= 1024
