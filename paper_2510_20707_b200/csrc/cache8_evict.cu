@@ -222,7 +222,8 @@ __global__ void __launch_bounds__(kMoveWarps * 32) k_cache8_move(const EvictArgs
   }
   int block = -1;
   if (row >= 0) {
-    const int from = a.p.by_rows.div(row), old = fresh(a.p.table + (long long)u * a.p.max_pages + from);
+    const int from = a.p.by_rows.div(row);
+    const int old = from < a.p.max_pages ? fresh(a.p.table + (long long)u * a.p.max_pages + from) : -1;
     row -= from * a.p.page_rows;
     if (old >= 0 && old < a.p.num_pages) block = old * a.p.tiles + (row >> 4);
   }
