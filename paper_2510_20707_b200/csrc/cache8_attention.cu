@@ -26,7 +26,7 @@ namespace mixkv {
 namespace {
 
 constexpr int kAttWarps = 4;
-constexpr int kAttDepth = 3;                   // tiles of a warp on their way or in work
+constexpr int kAttDepth = 2;                   // tiles of a warp on their way or in work
 constexpr int kNoRow = 0x3fffffff;             // first row of a tile that is not there: beyond all
 constexpr int kAttPitch = kHeadDim / 2 + 4;    // floats between the query rows of half a warp's sums
 constexpr int kAttGroups = 4;                  // most groups of eight query rows a CTA takes
@@ -45,7 +45,7 @@ __host__ __device__ constexpr size_t att_smem(int NT) {
   return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
          (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
 }
-__host__ __device__ constexpr int att_per_sm(int NT) { return NT <= 2 ? 3 : 2; }
+__host__ __device__ constexpr int att_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
 
 struct AttArgs {
   CachePool p;
@@ -815,18 +815,19 @@ AttKernel att_kernel(const bool bf16, const bool e4m3, const int NT) {
 // to one length.  resident(n): clusters of n CTAs that are resident at once.
 //
 // A cluster per unit, or all tiles dealt out evenly and joined by a second kernel, which costs a call 4 us.  us a call, one token of
-// four query heads, heads of one length (and of lengths from one row to that), cluster / shares:
+// four query heads, heads of one length (and of lengths from one row to that), clusters / shares:
 //     heads x rows    no weights                        weights counted
-//     8 x 4096        11.5 / 10.8  (11.3 / 11.5)        13.5 / 12.2  (13.3 / 13.2)      eight tiles a warp on 64 CTAs
-//     32 x 4096       15.6 / 18.1  (13.4 / 15.5)        18.0 / 20.8  (15.8 / 18.5)      eight on 256
-//     64 x 4096       19.4 / 22.6  (17.0 / 18.5)        23.0 / 26.6  (20.4 / 22.2)      eleven on 384
-//     256 x 1024      19.8 / 22.9  (17.4 / 20.0)        23.9 / 26.8  (20.4 / 23.3)      sixteen on 256
-//     64 x 8192       30.6 / 32.1  (26.5 / 22.9)        36.3 / 37.3  (31.9 / 27.1)      21 on 384
-//     128 x 4096      30.3 / 32.1  (26.9 / 24.9)        36.2 / 38.3  (32.3 / 29.4)      21 on 384
-//     256 x 2048      32.4 / 32.3  (30.1 / 25.0)        42.1 / 38.2  (35.1 / 29.1)      32 on 256
-// So clusters up to sixteen tiles a warp (24 behind a window: 128 heads of a window of 4096 30.7 / 33.7), where they fill half of the GPU
-// at least, and up to six where they do not.  With more query rows a tile takes longer and the join counts for less (32 of them: 64 x
-// 8192 53.5 / 61.1 (50.9 / 46.8), 8 x 4096 17.7 / 16.9).
+//     8 x 2048         8.7 / 10.5   (8.5 / 11.7)                                        four tiles a warp on 64 CTAs (of 592 at once)
+//     8 x 4096        11.8 / 11.0  (11.6 / 11.7)        14.1 / 11.8  (13.8 / 12.5)      eight on 64
+//     32 x 4096       14.8 / 15.7  (13.5 / 14.8)        16.6 / 17.0  (16.5 / 16.3)      eight on 256
+//     32 x 8192       24.6 / 21.6  (20.1 / 18.3)                                        sixteen on 256
+//     64 x 4096       18.6 / 21.8  (16.0 / 17.8)        21.3 / 25.3  (18.9 / 20.8)      eight on 512
+//     256 x 1024      18.5 / 22.1  (16.1 / 19.9)        21.3 / 25.4  (19.0 / 22.7)      eight on 512
+//     64 x 8192       29.0 / 31.3  (24.5 / 22.6)        34.1 / 37.1  (29.5 / 27.3)      sixteen on 512
+//     256 x 2048      28.8 / 31.2  (24.7 / 24.6)        34.1 / 36.9  (29.8 / 29.1)      sixteen on 512
+// So clusters up to sixteen tiles a warp where they fill the GPU, and up to fewer where they do not, but for six; up to 24 where a window
+// cuts the heads to one length (128 heads of a window of 4096 29.8 / 32.8).  More query rows, clusters / shares: 32 of them, 64 x 8192
+// 52 / 60 (50 / 46), 8 x 8192 26.3 / 21.5 (25.9 / 25.8).
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all tiles
 };
@@ -840,7 +841,9 @@ AttShape att_shape(const long long units, const int groups, const long long tile
   int S = most < 1 ? 1 : (int)most;
   while (S > 1 && all > resident(S)) --S;
   const long long alone = (tiles + S * kAttWarps - 1) / (S * kAttWarps);     // tiles of a warp
-  if (alone <= (NT == 1 && all * S * 2 < slots ? kAttFew : even ? kAttEven : kAttMany)) return {S, 0};
+  const long long full = even ? kAttEven : kAttMany, filled = full * all * S * 5 / (slots * 4);     // (0.8 of the slots count as all)
+  const long long limit = filled > full ? full : filled < kAttFew ? kAttFew : filled;
+  if (alone <= limit) return {S, 0};
   if (units <= kAttUnits && groups < slots && units * tiles <= 0x7fffffffll) {
     const long long want = (units * tiles + kAttWarps * 4 - 1) / (kAttWarps * 4);     // (four tiles to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups)};
