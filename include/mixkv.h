@@ -498,7 +498,8 @@ int mixkv_cache_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t 
  *   accumulate      nonzero: adds to the mass of every row that a query row sees the weights it got, of all tokens and heads of
  *                   the group (needs c->mass_opt; sums in one order, the same every time)
  *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned
- * Logits, softmax statistics and sums are fp32, the weights enter the value sum as fp16 and the mass as fp32.  softmax_scale 0 means
+ * Logits, softmax statistics and sums are fp32; the weights enter the value sum as fp16 (for fp16 outputs as two such numbers) and the
+ * mass as fp32.  softmax_scale 0 means
  * 1 / sqrt(128).  A page outside the pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that
  * sees a NaN, is NaN (as is the mass of the rows it sees), and so is what a wait inside the kernel ran out on (there is no status
  * word). */

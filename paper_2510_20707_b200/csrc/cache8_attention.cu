@@ -9,7 +9,9 @@
 // Two rows of V are interleaved by byte moves before they are widened, so that a pair is two rows of one dimension.
 //
 // Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a step instead of
-// a reduction); weights are fp16 times 2^kLift, sums are fp32.
+// a reduction); weights are fp16 times 2^kLift, sums are fp32.  For bf16 outputs a weight is ONE fp16 number: its rounding, 2^-11 of it, is an
+// eighth of the output's own.  For fp16 outputs it would be as large as that (2.9e-4 from 64 bits where the outputs' rounding makes
+// 2.1e-4, up to 1.7 times that where one row has most of the weight): there a weight is two of them, for 4 to 11 % of a call's time.
 //
 // Weights of rows: what a row got is known when the sums are, so the logits go to the workspace as fp32 (R of them for a row of 257
 // bytes) and a second kernel takes the exponentials of one row's in a fixed order and adds their sum to the row's mass.
@@ -45,7 +47,10 @@ __host__ __device__ constexpr size_t att_smem(int NT) {
   return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
          (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
 }
-__host__ __device__ constexpr int att_per_sm(int NT) { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+// CTAs of an SM, which sets the registers of a thread.  One group of query rows: four CTAs of 128 registers, 64 heads of 4096 rows 16.0 us for
+// 16.7 with three, 8 of 16384 16.2 for 17.5, 256 of 8704 on average 133.6 for 131.6.  Two groups: three of 168, with weights in two parts (60
+// bytes spilt) two of 254: 256 heads of 70 to 1639 rows 40.0 us for 41.9, 64 of 2048 16.4 for 18.1, 256 of 1024 on average 34.2 for 33.1.
+__host__ __device__ constexpr int att_per_sm(int NT, bool half) { return NT == 1 ? 4 : NT == 2 && !half ? 3 : 2; }
 
 struct AttArgs {
   CachePool p;
@@ -183,6 +188,7 @@ __device__ __forceinline__ void stage_queries(const AttArgs& a, const int u, con
 template <typename T, int NT, bool E4M3>
 struct AttState {
   static constexpr bool kHeld = att_held(NT);
+  static constexpr int kParts = std::is_same<T, __half>::value ? 2 : 1;      // of a weight
   uint2 q[kHeld ? NT : 1][8];
   const uint2* at;          // this lane's fragments in shared memory
   float f[NT][2];           // products of codes to log2 units, without the block's scale: query rows 2 t, 2 t + 1
@@ -316,13 +322,21 @@ struct AttState {
     const float ratio = scale.y * inverse(vref);
     const bool aside = !(ratio >= kSmallest) && scale.y != 0.f;
     const float by = aside ? 1.f : ratio;
-    uint32_t p[NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+    uint32_t p[kParts][NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[nt][i] = ex2(x[nt][i]), z[nt][i & 1] += x[nt][i];
-      p[nt][0] = transpose8x8(narrow2<__half>(x[nt][0] * by, x[nt][1] * by));
-      p[nt][1] = transpose8x8(narrow2<__half>(x[nt][2] * by, x[nt][3] * by));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float lo = x[nt][2 * j] * by, hi = x[nt][2 * j + 1] * by;
+        const uint32_t w = narrow2<__half>(lo, hi);
+        p[0][nt][j] = transpose8x8(w);
+        if constexpr (kParts > 1) {
+          const float2 rounded = widen2<__half>(w);
+          p[1][nt][j] = transpose8x8(narrow2<__half>(lo - rounded.x, hi - rounded.y));
+        }
+      }
     }
     uint4 v[2][2];       // 16 dimensions of rows 2 t + e + 8 h
 #pragma unroll
@@ -343,7 +357,9 @@ struct AttState {
     if (__builtin_expect(!aside, 1)) {
       fragments([&](const int m, const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_f16(acc[nt][m], a0, a1, a2, a3, p[nt][0], p[nt][1]);
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < kParts; ++e) mma_f16(acc[nt][m], a0, a1, a2, a3, p[e][nt][0], p[e][nt][1]);
       });
     } else {
       bool into[NT][2];
@@ -358,7 +374,8 @@ struct AttState {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float d[4];
-          mma_f16_first(d, a0, a1, a2, a3, p[nt][0], p[nt][1]);
+          mma_f16_first(d, a0, a1, a2, a3, p[0][nt][0], p[0][nt][1]);
+          if constexpr (kParts > 1) mma_f16(d, a0, a1, a2, a3, p[1][nt][0], p[1][nt][1]);
 #pragma unroll
           for (int c = 0; c < 4; ++c)
             if (into[nt][c & 1]) acc[nt][m][c] = fmaf(d[c], ratio, acc[nt][m][c]);
@@ -441,7 +458,7 @@ __device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const
 
 // grid.x: units * S in clusters of S (ctas == 0), or ctas; grid.y: groups of 8 NT query rows
 template <typename T, int NT, bool E4M3>
-__global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT)) k_cache8_attention(const AttArgs a) {
+__global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T, __half>::value)) k_cache8_attention(const AttArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int W = kAttWarps, Q = 8 * NT, kSums = Q * kAttPitch, kThreads = 32 * W, kRing = kAttDepth * kBlockBytes;
   float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its sums where its rings were
@@ -831,11 +848,11 @@ AttKernel att_kernel(const bool bf16, const bool e4m3, const int NT) {
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all tiles
 };
-int att_slots(const int NT, const int sms) { return att_per_sm(NT) * sms; }
+int att_slots(const int NT, const bool half, const int sms) { return att_per_sm(NT, half) * sms; }
 template <typename Resident>
-AttShape att_shape(const long long units, const int groups, const long long tiles, const bool even, const int NT, const int sms,
-                   const Resident& resident) {
-  const long long slots = att_slots(NT, sms), all = units * groups;
+AttShape att_shape(const long long units, const int groups, const long long tiles, const bool even, const int NT, const bool half,
+                   const int sms, const Resident& resident) {
+  const long long slots = att_slots(NT, half, sms), all = units * groups;
   long long most = slots / all < kMaxCluster ? slots / all : kMaxCluster;
   if (most > tiles / kAttWarps) most = tiles / kAttWarps;
   int S = most < 1 ? 1 : (int)most;
@@ -876,8 +893,9 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
   }
   p->cap = (int)p->tiles, p->pitch = ((int)R + 1) & ~1, p->sms = device_sm_count();
   const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
-  p->part = up((size_t)att_slots(p->NT, p->sms) * 2 * R * kHeadDim * 4);
-  p->spans = up(p->part + (size_t)att_slots(p->NT, p->sms) * 2 * R * sizeof(float4));
+  const size_t shares = 2 * (size_t)att_slots(p->NT, false, p->sms);     // (the workspace serves either type)
+  p->part = up(shares * R * kHeadDim * 4);
+  p->spans = up(p->part + shares * R * sizeof(float4));
   p->stats = up(p->spans + kAttUnits * sizeof(int2));
   p->logits = up(p->stats + (accumulate ? (size_t)units * R * sizeof(float2) : 0));
   p->bytes = p->logits + (accumulate ? (size_t)units * p->cap * kBlockRows * p->pitch * 4 : 0);
@@ -889,9 +907,9 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
 
 using namespace mixkv;
 
-extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t even, int32_t eights, int32_t sms,
-                                            const int32_t* resident, int32_t* ctas, int32_t* shared) {
-  const AttShape s = att_shape(units, groups, tiles, even != 0, eights, sms, [&](const int n) { return resident[n]; });
+extern "C" void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t even, int32_t eights, int32_t half,
+                                            int32_t sms, const int32_t* resident, int32_t* ctas, int32_t* shared) {
+  const AttShape s = att_shape(units, groups, tiles, even != 0, eights, half != 0, sms, [&](const int n) { return resident[n]; });
   *ctas = s.S, *shared = s.ctas;
 }
 
@@ -929,7 +947,7 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   const int dev = device_slot(), variant = 4 * p.NT + 2 * e4m3 + bf16;
   const AttKernel kernel = att_kernel(bf16, e4m3, p.NT);
   const size_t smem = att_smem(p.NT);
-  const AttShape shape = att_shape(units, p.groups, p.tiles, p.even, p.NT, p.sms, [&](const int size) {
+  const AttShape shape = att_shape(units, p.groups, p.tiles, p.even, p.NT, !bf16, p.sms, [&](const int size) {
     if (!answered(ensure_smem(kernel, smem, done[variant], dev))) return 0;
     return fits[variant].ask(kernel, 32 * kAttWarps, smem, size, dev);
   });

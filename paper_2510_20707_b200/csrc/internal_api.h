@@ -44,10 +44,10 @@ void mixkv_internal_paged_shape(int64_t units, int32_t groups, int64_t steps, in
                                 const int32_t* wide, int32_t* ctas, int32_t* large, int32_t* shared);
 
 // How an attention over the 8-bit cache is split (cache8_attention.cu): (sequence, head) units, groups of query rows, tiles (16 rows) of
-// the longest unit and whether a window cut it to that, groups of eight query rows of a CTA; resident[n]: clusters of n CTAs held at once.
-// CTAs of a unit's cluster, or the CTAs that share all tiles (0: none do).
-void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t even, int32_t eights, int32_t sms,
-                                 const int32_t* resident, int32_t* ctas, int32_t* shared);
+// the longest unit and whether a window cut it to that, groups of eight query rows of a CTA, whether they are
+// fp16; resident[n]: clusters of n CTAs held at once.  CTAs of a unit's cluster, or the CTAs that share all tiles (0: none do).
+void mixkv_internal_cache8_shape(int64_t units, int32_t groups, int64_t tiles, int32_t even, int32_t eights, int32_t half,
+                                 int32_t sms, const int32_t* resident, int32_t* ctas, int32_t* shared);
 
 // What the 32 lanes of a warp are told by its common wait for an mbarrier: answers[0 .. 31] for a phase that is complete for the even
 // lanes only, where a wait of the CTA has run out before, answers[32 .. 63] for one that is complete (1: complete).

@@ -93,6 +93,15 @@ def test_page_bytes(lib):
         assert e.value.status == -1
 
 
+def fake_attention(fake, batch, heads, rows, T=1, G=4, accumulate=0, window=0, sinks=0, device=20):
+    fake.reset(device=device)
+    c = cache(batch=batch, kv_heads=heads, max_pages=-(-rows // 64), num_pages=1 << 20)
+    rc = fake.lib.mixkv_cache_attention(C.byref(c), ONE, 0, 128 * T * heads * G, 128 * heads * G, T, G, 0.0, rows, window, sinks, accumulate,
+                                        ONE, 1 << 40, ONE, None)
+    assert rc == 0
+    return fake.launches()
+
+
 def cache(**kw):
     d = dict(pool=ONE, mass_opt=ONE, table=ONE, rows=ONE, num_pages=10, max_pages=4, page_rows=64, batch=2, kv_heads=3, head_dim=128, code=0)
     d.update(kw)
@@ -203,10 +212,55 @@ def test_the_tiles_of_a_window_hold_all_that_is_seen():
                                                        (32, 2, 459, 3), (3, 4, 10, 4)])
 def test_how_a_call_is_split(lib, units, groups, tiles, eights):
     S, shared = C.c_int32(), C.c_int32()
-    resident = (C.c_int32 * 9)(0, 444, 220, 140, 108, 85, 70, 60, 51)
-    lib.mixkv_internal_cache8_shape(C.c_int64(units), groups, C.c_int64(tiles), tiles % 2, eights, 148, resident, C.byref(S), C.byref(shared))
-    assert 1 <= S.value <= 8 and 0 <= shared.value <= 444
+    slots = (4 if eights == 1 else 3 if eights == 2 else 2) * 148
+    resident = (C.c_int32 * 9)(0, *[slots // n - (n > 2) for n in range(1, 9)])
+    lib.mixkv_internal_cache8_shape(C.c_int64(units), groups, C.c_int64(tiles), tiles % 2, eights, 0, 148, resident, C.byref(S), C.byref(shared))
+    assert 1 <= S.value <= 8 and 0 <= shared.value <= slots
     if shared.value:
-        assert S.value == 1 and shared.value * groups <= 444 and units <= 1024
+        assert S.value == 1 and shared.value * groups <= slots and units <= 1024
     elif S.value > 1:
         assert units * groups <= resident[S.value] and S.value * 4 <= tiles
+
+
+def test_what_an_attention_enqueues(fake_cuda):
+    names = lambda calls: [x.kernel for x in calls]
+    # a short call is one kernel in clusters, which add up the weights themselves
+    for acc in (0, 1):
+        calls = fake_attention(fake_cuda, 1, 4, 512, accumulate=acc)
+        assert names(calls) == ["k_cache8_attention"] and calls[0].cluster == 8 and calls[0].grid == 32
+    # a long one is dealt out evenly and joined; its weights are added up by the kernel that joins
+    join = fake_attention(fake_cuda, 1, 8, 131072)
+    both = fake_attention(fake_cuda, 1, 8, 131072, accumulate=1)
+    for calls in (join, both):
+        assert names(calls) == ["k_cache8_attention", "k_cache8_finish"]
+        assert all(x.cluster == 1 for x in calls) and calls[0].grid == 4 * 148
+    assert both[1].grid > join[1].grid
+    # query rows of several groups: no cluster has all of them
+    calls = fake_attention(fake_cuda, 1, 2, 200, T=16, G=8, accumulate=1)
+    assert names(calls) == ["k_cache8_attention", "k_cache8_finish"] and calls[0].cluster > 1
+    # more heads than are dealt out; a window that makes long heads short ones
+    assert names(fake_attention(fake_cuda, 64, 32, 4000)) == ["k_cache8_attention"]
+    assert names(fake_attention(fake_cuda, 1, 8, 131072, window=500, sinks=4)) == ["k_cache8_attention"]
+
+
+def test_a_device_that_holds_no_cluster_gets_none(fake_cuda):
+    fake_cuda.reset(device=21, resident={n: 0 for n in range(2, 9)})
+    c = cache(batch=1, kv_heads=4, max_pages=8, num_pages=64)
+    assert fake_cuda.lib.mixkv_cache_attention(C.byref(c), ONE, 0, 512, 512, 1, 1, 0.0, 512, 0, 0, 0, ONE, 1 << 40, ONE, None) == 0
+    assert all(x.cluster == 1 for x in fake_cuda.launches())
+
+
+def test_what_rows_and_evictions_enqueue(fake_cuda):
+    fake_cuda.reset(device=22)
+    c, into = cache(batch=2, kv_heads=3, max_pages=100), cache(batch=2, kv_heads=3, rows=ONE + 64)
+    lib = fake_cuda.lib
+    # K and V of every tile that new rows can touch: two warps a tile, four to a CTA
+    assert lib.mixkv_cache_append(C.byref(c), ONE, ONE, 0, 40, 384, 128, 384, 128, ONE, 0, 18, None, None) == 0
+    assert lib.mixkv_cache_read(C.byref(c), ONE, ONE, 1, 40, ONE, 0, 1, None) == 0
+    assert [(x.kernel, x.grid) for x in fake_cuda.launches()] == [("k_cache8_append", 2 * 3 * 3 * 2 // 4), ("k_cache8_read", 2 * 3 * 2 // 4)]
+    for rows, budget, cluster in ((2048, 64, 1), (2049, 64, 2), (6400, 1000, 4)):
+        fake_cuda.reset(device=22)
+        assert lib.mixkv_cache_evict(C.byref(c), C.byref(into), budget, None, 1, 1, rows, ONE, None, None) == 0
+        calls = fake_cuda.launches()
+        assert [x.kernel for x in calls] == ["k_cache8_pick", "k_cache8_move"] and calls[0].cluster == cluster
+        assert calls[1].grid == -(-6 * -(-budget // 16) // 4)

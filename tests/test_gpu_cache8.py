@@ -620,3 +620,64 @@ def test_what_the_binding_refuses():
             call()
     with pytest.raises(TypeError):
         binding.cache8_read(cc, 1, torch.float32)
+
+
+def test_what_changes_from_step_to_step_is_read_anew():
+    # rows, tables, masses and rows of the pool are written by one kernel and read by the next, which is resident by then: in one loop
+    # without a pause, with outputs in the memory of earlier ones, every step gives what it gives when nothing overlaps
+    B, H, G, page, n = 3, 2, 4, 16, 60
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    k, v = (torch.randn((n, B, H, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((n, B, 1, H * G, 128), generator=gen, device="cuda").bfloat16()
+
+    def steps(wait):
+        here, there = (binding.new_cache8(B, H, 64, page, mass=True) for _ in range(2))
+        outs, rows = [], 0
+        for i in range(n):
+            rows += 1
+            here.rows += 1
+            binding.cache8_append(here, k[i], v[i])
+            out = binding.cache8_attention(here, q[i], accumulate=True)
+            kept = None
+            if rows == 40:
+                kept = binding.cache8_evict(here, there, 24, keep_first=1, keep_last=6)
+                here, there, rows = there, here, 24
+            if wait:
+                torch.cuda.synchronize()
+            outs.append((out, kept, here.mass.clone()))
+            del out, kept
+        torch.cuda.synchronize()
+        return outs, here.rows.tolist()
+
+    (slow, a), (fast, b) = steps(True), steps(False)
+    assert a == b
+    for (o, kept, m), (p, also, w) in zip(slow, fast):
+        assert torch.equal(o, p) and torch.equal(m, w) and (kept is None) == (also is None) and (kept is None or torch.equal(kept, also))
+
+
+@pytest.mark.parametrize("ties", [False, True])
+def test_an_eviction_gives_the_same_every_time(ties):
+    # clusters of eight, keys counted in any order
+    c = Cache(np.full((1, 2), 40000), 64, "int8")
+    c.fill()
+    c.cache.mass.copy_(masses(c.cache.mass.shape, 9, ties))
+    into = [binding.new_cache8(1, 2, 3000, 64, mass=True) for _ in range(2)]
+    for x in into:
+        x.pool.zero_()
+    first = binding.cache8_evict(c.cache, into[0], 3000, keep_last=8)
+    for _ in range(20):
+        assert torch.equal(binding.cache8_evict(c.cache, into[1], 3000, keep_last=8), first)
+    assert torch.equal(into[0].pool, into[1].pool) and torch.equal(into[0].mass, into[1].mass)
+
+
+def test_the_example_runs():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "evicting_decode.py")
+    spec = importlib.util.spec_from_file_location("evicting_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    error, outs, held, evictions = example.main(40)
+    # eight bits with one scale for sixteen rows: rounding is a percent of a value's typical size
+    assert error < 0.05 and evictions >= 2 and max(held) <= example.BUDGET + example.SLACK
+    assert all(o.shape == (1, 1, 28, 128) and torch.isfinite(o.float()).all() for o in outs)
