@@ -736,7 +736,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
 //  - join: outputs of the query rows of units that several CTAs had a part of, `per_row.d` warps, a power of two, taking the shares of a
 //    row in turn, and zeros for units without rows.
 //  - add: what a run of the unit's rows got of the weights goes to their mass.
-// Every CTA works out the statistics of the query rows for itself: the outputs and the masses do not wait for one another, nor either of them for
+// Either works out the statistics of its query rows for itself: the outputs and the masses do not wait for one another, nor either of them for
 // a launch and its first loads, which would cost as much as they do.
 constexpr int kEndWarps = 8, kEndThreads = kEndWarps * 32, kEndPerSm = 3;
 template <typename T>
@@ -744,7 +744,7 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
                                                                          const Divider per_row) {
   __shared__ float4 sums[kEndWarps][32];
   __shared__ float2 stat[MIXKV_CACHE8_MAX_QUERIES];      // (reference, 1 / sum)
-  __shared__ float units[MIXKV_CACHE8_MAX_QUERIES];      // of sums of values
+  __shared__ float4 of_warp[kEndWarps];                  // (reference, sum, unit, -)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int u = by_unit.div(blockIdx.x), c = blockIdx.x - u * (int)by_unit.d;
   pdl_wait();
@@ -758,23 +758,20 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
       while (lanes < 32 && lanes < c1 - c0 + 1) lanes *= 2;
       const int at = lane & (lanes - 1), at_once = 32 / lanes;
       for (int r = warp * at_once + lane / lanes; r - lane / lanes < a.R; r += kEndWarps * at_once) {
-        float M = kNoRef, den = 0.f, unit = FLT_MIN;
+        float M = kNoRef, den = 0.f;
         for (int k = c0 + at; k <= c1 && r < a.R; k += lanes) {
           const float4 mz = __ldcg(a.part_mz + part_row(k, r));
           const float to = fmaxf(M, mz.x);
           den = fmaf(den, ex2(M - to), mz.y * ex2(mz.x - to));
-          M = to, unit = fmaxf(unit, mz.z);
+          M = to;
         }
         float most = M;
-        for (int o = 1; o < lanes; o *= 2) {
-          most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-          unit = fmaxf(unit, __shfl_xor_sync(0xffffffffu, unit, o));
-        }
+        for (int o = 1; o < lanes; o *= 2) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         den *= ex2(M - most);
         for (int o = 1; o < lanes; o *= 2) den += __shfl_xor_sync(0xffffffffu, den, o);
-        if (at == 0 && r < a.R) stat[r] = make_float2(most, one_over(den)), units[r] = unit;
+        if (at == 0 && r < a.R) stat[r] = make_float2(most, one_over(den));
       }
-    } else if (c >= join) {
+    } else {
       for (int r = tid; r < a.R; r += kEndThreads) stat[r] = __ldcg(a.stats + (long long)u * a.R + r);
     }
     __syncthreads();
@@ -786,15 +783,20 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
     return;
   }
   if (!joined) return;
-  statistics();
   const int slot = per_row.div(warp), part = warp - slot * per_row.d, at_once = per_row.div(kEndWarps), r = c * at_once + slot;
   const bool on = r < a.R;
-  const float2 s = stat[on ? r : 0];
-  const float unit = units[on ? r : 0];
+  float M = kNoRef, den = 0.f, unit = FLT_MIN;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int kAtOnce = 4;
+  const auto move = [&](const float to, const float wide) {      // to another reference and another unit
+    const float shrink = ex2(M - to), by = shrink * (unit * inverse(wide));
+    num.x *= by, num.y *= by, num.z *= by, num.w *= by, den *= shrink;
+    M = to, unit = wide;
+  };
+  constexpr int kAtOnce = 4;      // shares whose sums come in one round trip
+#pragma unroll 1
   for (int k = c0 + part; on && k <= c1; k += kAtOnce * per_row.d) {
     float4 x[kAtOnce], mz[kAtOnce];
+    float to = M, wide = unit;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const long long at = part_row(min(k + i * (int)per_row.d, c1), r);
@@ -802,15 +804,31 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
       x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)
-      add_scaled(num, x[i], k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - s.x) * (mz[i].z * inverse(unit)) : 0.f);
+    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x), wide = fmaxf(wide, mz[i].z);
+    move(to, wide);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float sc = k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
+      add_scaled(num, x[i], sc * (mz[i].z * inverse(unit)));
+      den = fmaf(mz[i].y, sc, den);
+    }
   }
   if (per_row.d > 1) {
     sums[warp][lane] = num;
+    if (lane == 0) of_warp[warp] = make_float4(M, den, unit, 0.f);
     __syncthreads();
-    for (int w = 1; w < (int)per_row.d && !part; ++w) add_scaled(num, sums[warp + w][lane], 1.f);
+    if (part) return;
+    float to = M, wide = unit;
+    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, of_warp[warp + w].x), wide = fmaxf(wide, of_warp[warp + w].z);
+    move(to, wide);
+    for (int w = 1; w < (int)per_row.d; ++w) {
+      const float4 mz = of_warp[warp + w];
+      const float sc = ex2(mz.x - M);
+      add_scaled(num, sums[warp + w][lane], sc * (mz.z * inverse(unit)));
+      den = fmaf(mz.y, sc, den);
+    }
   }
-  if (on && !part) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, s.y, unit);
+  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, one_over(den), unit);
 }
 
 using AttKernel = void (*)(AttArgs);
