@@ -58,7 +58,7 @@ __device__ __forceinline__ int sum_below(const int x, const int warp, const int 
 
 __global__ void __launch_bounds__(kPickThreads) k_cache8_pick(const EvictArgs a) {
   extern __shared__ uint32_t keys[];
-  __shared__ int hist[kBins];
+  __shared__ __align__(8) int hist[kBins];
   __shared__ int warp_sum[kPickWarps];
   __shared__ int2 warp_run[kPickWarps];      // of a warp's run: keys above the threshold, keys equal to it
   __shared__ int2 cta_run;
