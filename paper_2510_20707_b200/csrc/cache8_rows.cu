@@ -5,8 +5,8 @@
 // reduction over the warp, on the bits of the 16-bit values (a magnitude's bits are in its order, infinities and NaN above all numbers).
 // Nothing is pipelined: a warp has four rows a lane in flight, and an SM holds enough warps.
 //
-// What bounds it: 32768 rows of four heads are appended in 17.9 us (100 MB, 5.6 TB/s; an instruction issued in 70 % of the clocks: six a
-// value for the product, the rounding and the packing of a code), read back in 14.6 (100 MB, 6.9 TB/s).  One token of a head costs its tile, 4
+// What bounds it: 32768 rows of four heads are appended in 17.9 us (100 MB, 5.6 TB/s; an instruction issued in 70 % of the clocks, and no
+// faster without the search for the largest magnitude), read back in 14.6 (100 MB, 6.9 TB/s).  One token of a head costs its tile, 4
 // KB read and, where the scale grows, written: 512 heads 4.8 us, the call's host time.
 #include "cache8.cuh"
 
