@@ -2,7 +2,7 @@
 // the first rows, and the weight that every row got of it.
 //
 // A warp takes a tile of 16 cache rows per step, brought by a bulk copy into a ring of its own.  Codes become fp16 exactly; the scale
-// of a block is one number for the whole tile, so it multiplies logits and weights, not codes.  The products run as m16n8k16 with the
+// of a block is one number for the whole tile, so it multiplies logits and products, not codes.  The products run as m16n8k16 with the
 // CACHE on the sixteen-row side and the query rows (tokens x heads of the group) on the eight-column side:
 //   S^T[row, query]  = K q^T      A: rows g and g + 8 of the tile, a lane their dimensions 32 t .. 32 t + 31 (k-step s: 4 s .. 4 s + 3)
 //   O^T[dim, query] += V^T P^T    A: dimensions 16 g + 2 m, + 1 of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9; P^T from S^T by a transposing move
@@ -48,7 +48,6 @@ constexpr int kAttGroups = 4;                  // most groups of eight query row
 constexpr int kAttUnits = 1024;                // most units whose tiles are dealt out evenly
 constexpr int kAttFew = 6, kAttMany = 16, kAttEven = 24;   // tiles of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
-constexpr float kSmallest = 1.f / 4096;        // scale of values that goes into weights of fp16, in units of the largest
 constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
 
 // Whether a warp has the queries in registers (with more of them there is no room).
@@ -318,9 +317,9 @@ struct AttState {
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }
     }
-    // The block's scale, in units of the largest so far, goes into the weights before they are rounded.  Where it is far smaller
-    // (weights would leave fp16's range), or NaN (it must not reach, through weights of zero, a query row that sees none of the
-    // block's rows), the tile's products begin at zero and join the sums by a multiply-add.
+    // The block's scale, in units of the largest so far, multiplies the tile's products on their way into the sums.  (In the weights it
+    // would take them out of fp16's range: of 16384 rows with 2^-17 of the heaviest one's weight, beside a block of values 3000 times
+    // as large, a quarter was lost.)  A scale of NaN must not reach, through weights of zero, a query row that sees none of the block's rows.
     if (scale.y > vref) {
       const float to = __uint_as_float(min((__float_as_uint(scale.y) & 0x7f800000u) + 0x00800000u, 253u << 23));
       const float shrink = vref * inverse(to);
@@ -333,8 +332,6 @@ struct AttState {
           for (int c = 0; c < 4; ++c) acc[nt][i][c] *= shrink;
     }
     const float ratio = scale.y * inverse(vref);
-    const bool aside = !(ratio >= kSmallest) && scale.y != 0.f;
-    const float by = aside ? 1.f : ratio;
     uint32_t p[kParts][NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -342,7 +339,7 @@ struct AttState {
       for (int i = 0; i < 4; ++i) x[nt][i] = ex2(x[nt][i]), z[nt][i & 1] += x[nt][i];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const float lo = x[nt][2 * j] * by, hi = x[nt][2 * j + 1] * by;
+        const float lo = x[nt][2 * j], hi = x[nt][2 * j + 1];
         const uint32_t w = narrow2<__half>(lo, hi);
         p[0][nt][j] = transpose8x8(w);
         if constexpr (kParts > 1) {
@@ -356,44 +353,35 @@ struct AttState {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
-    // A fragments of dimensions 16 g + 2 m, + 1, handed to f one by one
-    const auto fragments = [&](const auto& f) {
+    if (__builtin_expect(ratio == ratio, 1)) {
+      const f32x2 by = pack2(ratio, ratio);
 #pragma unroll
-      for (int m = 0; m < 8; ++m) {
+      for (int m = 0; m < 8; ++m) {      // A fragments: dimensions 16 g + 2 m, + 1
         const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
         uint32_t a0, a1, a2, a3;
         codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
         codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
-        f(m, a0, a1, a2, a3);
-      }
-    };
-    if (__builtin_expect(!aside, 1)) {
-      fragments([&](const int m, const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < kParts; ++e) mma_f16(acc[nt][m], a0, a1, a2, a3, p[e][nt][0], p[e][nt][1]);
-      });
-    } else {
-      bool into[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
-          into[nt][c] = row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks);
-        }
-      fragments([&](const int m, const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float d[4];
           mma_f16_first(d, a0, a1, a2, a3, p[0][nt][0], p[0][nt][1]);
           if constexpr (kParts > 1) mma_f16(d, a0, a1, a2, a3, p[1][nt][0], p[1][nt][1]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (into[nt][c & 1]) acc[nt][m][c] = fmaf(d[c], ratio, acc[nt][m][c]);
+          float(&to)[4] = acc[nt][m];
+          unpack2(fma2(pack2(d[0], d[1]), by, pack2(to[0], to[1])), to[0], to[1]);
+          unpack2(fma2(pack2(d[2], d[3]), by, pack2(to[2], to[3])), to[2], to[3]);
         }
-      });
+      }
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
+          if (row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks)) {
+#pragma unroll
+            for (int m = 0; m < 8; ++m) acc[nt][m][c] = acc[nt][m][2 + c] = NAN;
+          }
+        }
     }
   }
 };
