@@ -49,15 +49,19 @@ constexpr int kAttUnits = 1024;                // most units whose tiles are dea
 constexpr int kAttFew = 6, kAttMany = 16, kAttEven = 24;   // tiles of a warp (att_shape)
 constexpr float kLag = 8.f, kLift = 6.f;       // largest weight 2^14
 constexpr float kNoRef = -FLT_MAX;             // reference before the first row: no logit is below, and it is finite
+// Sums of weighted values are kept times 2^8; those of a query row that has got something of a block with a scale above 2^64, times 2^-48:
+// at 2^14 a weight, 2^30 rows and the largest values of either kind fit fp32, and what falls below its range is nothing beside either
+// the smallest values (2^-126) or that block's own rounding.
+constexpr float kWide = 0x1p64f, kFine = 0x1p8f, kCoarse = 0x1p-48f, kBack = 0x1p40f;
 
 // Whether a warp has the queries in registers (with more of them there is no room).
 __host__ __device__ constexpr bool att_held(int NT) { return NT <= 2; }
-// rings of the warps (a cluster's CTA: then its sums); half of the warps' sums; references and sums of the warps, the CTA,
-// the cluster, and units; barriers and rows of the rings; what the queries were divided by, and they (or in
+// rings of the warps (a cluster's CTA: then its averages); half of the warps' sums; references, sums of weights and units of the warps;
+// references and sums of the CTA, the cluster; barriers and rows of the rings; what the queries were divided by, and they (or in
 // the place of the sums)
 __host__ __device__ constexpr size_t att_smem(int NT) {
-  return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (2 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
-         (kAttWarps + 4 + kMaxCluster) * 4 + kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
+  return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (3 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
+         kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
 }
 // CTAs of an SM, which sets the registers of a thread.  One group of query rows: four CTAs of 128 registers, 64 heads of 4096 rows 16.0 us for
 // 16.7 with three, 8 of 16384 16.2 for 17.5, 256 of 8704 on average 133.6 for 131.6.  Two groups: three of 168, with weights in two parts (60
@@ -77,8 +81,8 @@ struct AttArgs {
   int per;                   // fours of outputs of a CTA of such a cluster
   float scale_log2e;
   int2* spans;               // [units]: first CTA with a share of a unit, times two, plus one if its run begins before the unit; last CTA
-  float* part;               // [2 ctas][R][128]: sums of a unit's share, where it is not the whole
-  float4* part_mz;           // [2 ctas][R]: (reference, sum, unit of the sums of values, -)
+  float* part;               // [2 ctas][R][128]: averages of a unit's share, where it is not the whole
+  float2* part_mz;           // [2 ctas][R]: (reference, sum of weights)
   float2* stats;             // [units][R]: (reference, 1 / sum) of a query row
   bool inside;               // the weights are added up by the clusters
   float* logits;             // [units][cap][16][pitch], log2 units; nullptr: weights are not asked for
@@ -130,17 +134,15 @@ __device__ __forceinline__ long long out_row(const AttArgs& a, const int u, cons
   const int b = a.p.by_heads.div(u), h = u - b * a.p.H, token = a.by_group.div(r);
   return ((long long)b * a.T + token) * ((long long)a.p.H * a.G) + h * a.G + (r - token * a.G);
 }
-// One over a power of two from 2^-126 to 2^126.
-__device__ __forceinline__ float inverse(const float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
-// Four outputs: sums of weighted values times one over the sum of weights (zero where there were none), times their unit.
+// Four outputs.
 template <typename T>
-__device__ __forceinline__ void store_row(T* to, const float4& num, const float by, const float unit) {
-  *reinterpret_cast<uint2*>(to) =
-      make_uint2(narrow2<T>(num.x * by * unit, num.y * by * unit), narrow2<T>(num.z * by * unit, num.w * by * unit));
+__device__ __forceinline__ void store_row(T* to, const float4& x) {
+  *reinterpret_cast<uint2*>(to) = make_uint2(narrow2<T>(x.x, x.y), narrow2<T>(x.z, x.w));
 }
+// (zero where there were no weights)
 __device__ __forceinline__ float one_over(const float den) { return den == 0.f ? 0.f : 1.f / den; }
-__device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float den) {
-  if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, one_over(den));
+__device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float by) {
+  if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, by);
 }
 // Token of query row r of a unit (rows of the padding: the last).
 __device__ __forceinline__ int token_of(const AttArgs& a, const int r) { return a.by_group.div(min(r, a.R - 1)); }
@@ -206,12 +208,11 @@ struct AttState {
   float f[NT][2];           // products of codes to log2 units, without the block's scale: query rows 2 t, 2 t + 1
   float acc[NT][8][4];      // dimensions 16 g + 2 m (0, 1), 16 g + 2 m + 1 (2, 3) of query rows 2 t, 2 t + 1
   float ref[NT][2], z[NT][2];   // weights are 2^(logit - ref)
-  float vref;                   // acc is in units of it: a power of two above every scale of values so far
+  float unit[NT][2];            // acc is in units of one over it: kFine or kCoarse
 
   __device__ __forceinline__ void start(const AttArgs& a, const uint2* staged, const float* up, const int lane) {
     const int t = lane & 3;
     at = staged + lane;
-    vref = FLT_MIN;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if constexpr (kHeld) {
@@ -221,7 +222,7 @@ struct AttState {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         f[nt][c] = up[8 * nt + 2 * t + c] * a.scale_log2e;
-        ref[nt][c] = kNoRef, z[nt][c] = 0.f;
+        ref[nt][c] = kNoRef, z[nt][c] = 0.f, unit[nt][c] = kFine;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -316,22 +317,24 @@ struct AttState {
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[nt][i][c] *= shrink, acc[nt][i][2 + c] *= shrink;
         }
+      bool coarse = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) coarse |= unit[nt][0] != kFine || unit[nt][1] != kFine;
+      if (__any_sync(0xffffffffu, coarse)) {      // back to the finer unit where nothing large is left
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float most = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = fmaxf(most, fmaxf(fabsf(acc[nt][i][c]), fabsf(acc[nt][i][2 + c])));
+            const float by = column_max(most) < kBack && unit[nt][c] != kFine ? kFine / kCoarse : 1.f;
+            if (by != 1.f) unit[nt][c] = kFine;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[nt][i][c] *= by, acc[nt][i][2 + c] *= by;
+          }
+      }
     }
-    // The block's scale, in units of the largest so far, multiplies the tile's products on their way into the sums.  (In the weights it
-    // would take them out of fp16's range: of 16384 rows with 2^-17 of the heaviest one's weight, beside a block of values 3000 times
-    // as large, a quarter was lost.)  A scale of NaN must not reach, through weights of zero, a query row that sees none of the block's rows.
-    if (scale.y > vref) {
-      const float to = __uint_as_float(min((__float_as_uint(scale.y) & 0x7f800000u) + 0x00800000u, 253u << 23));
-      const float shrink = vref * inverse(to);
-      vref = to;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) acc[nt][i][c] *= shrink;
-    }
-    const float ratio = scale.y * inverse(vref);
     uint32_t p[kParts][NT][2];   // B fragments: query row g, tile rows 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -348,40 +351,48 @@ struct AttState {
         }
       }
     }
-    uint4 v[2][2];       // 16 dimensions of rows 2 t + e + 8 h
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
-    if (__builtin_expect(ratio == ratio, 1)) {
-      const f32x2 by = pack2(ratio, ratio);
-#pragma unroll
-      for (int m = 0; m < 8; ++m) {      // A fragments: dimensions 16 g + 2 m, + 1
-        const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
-        uint32_t a0, a1, a2, a3;
-        codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
-        codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float d[4];
-          mma_f16_first(d, a0, a1, a2, a3, p[0][nt][0], p[0][nt][1]);
-          if constexpr (kParts > 1) mma_f16(d, a0, a1, a2, a3, p[1][nt][0], p[1][nt][1]);
-          float(&to)[4] = acc[nt][m];
-          unpack2(fma2(pack2(d[0], d[1]), by, pack2(to[0], to[1])), to[0], to[1]);
-          unpack2(fma2(pack2(d[2], d[3]), by, pack2(to[2], to[3])), to[2], to[3]);
-        }
-      }
-    } else {
+    // The block's scale multiplies the tile's products on their way into the sums.  (In the weights it would take them out of fp16's
+    // range: of 16384 rows with 2^-17 of the heaviest one's weight, beside a block of values 3000 times as large, a quarter was lost.)  A
+    // query row's sums are in a unit of their own: with one for all, values that one row sees would push those of the others out of fp32.
+    if (__builtin_expect(!(scale.y <= kWide), 0)) {
+      const bool nan = scale.y != scale.y;      // (it must not reach a query row that sees none of the block's rows)
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
           const Seen see = seen_by(a, n, token_of(a, first + 8 * nt + 2 * t + c));
-          if (row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks)) {
+          const bool sees = row <= see.last && (row + kBlockRows - 1 >= see.low || row < a.sinks);
+          const bool gets = column_max(fmaxf(x[nt][c], x[nt][2 + c])) > 0x1p-25f;      // (of less, fp16 is zero)
+          const float by = nan ? (sees ? NAN : 1.f) : gets ? kCoarse / unit[nt][c] : 1.f;
+          if (!nan && gets) unit[nt][c] = kCoarse;
 #pragma unroll
-            for (int m = 0; m < 8; ++m) acc[nt][m][c] = acc[nt][m][2 + c] = NAN;
-          }
+          for (int m = 0; m < 8; ++m) acc[nt][m][c] *= by, acc[nt][m][2 + c] *= by;
         }
+      if (nan) return;
+    }
+    uint4 v[2][2];       // 16 dimensions of rows 2 t + e + 8 h
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) v[h][e] = *reinterpret_cast<const uint4*>(tile + kBlockV + piece_at(2 * t + e + 8 * h, g));
+    f32x2 by[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) by[nt] = mul2(pack2(scale.y, scale.y), pack2(unit[nt][0], unit[nt][1]));
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {      // A fragments: dimensions 16 g + 2 m, + 1
+      const uint32_t sel = (m & 1) ? 0x7362u : 0x5140u;
+      uint32_t a0, a1, a2, a3;
+      codes_to_half<E4M3>(__byte_perm(word_of(v[0][0], m >> 1), word_of(v[0][1], m >> 1), sel), a0, a1);
+      codes_to_half<E4M3>(__byte_perm(word_of(v[1][0], m >> 1), word_of(v[1][1], m >> 1), sel), a2, a3);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float d[4];
+        mma_f16_first(d, a0, a1, a2, a3, p[0][nt][0], p[0][nt][1]);
+        if constexpr (kParts > 1) mma_f16(d, a0, a1, a2, a3, p[1][nt][0], p[1][nt][1]);
+        float(&to)[4] = acc[nt][m];
+        unpack2(fma2(pack2(d[0], d[1]), by[nt], pack2(to[0], to[1])), to[0], to[1]);
+        unpack2(fma2(pack2(d[2], d[3]), by[nt], pack2(to[2], to[3])), to[2], to[3]);
+      }
     }
   }
 };
@@ -462,20 +473,18 @@ template <typename T, int NT, bool E4M3>
 __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T, __half>::value)) k_cache8_attention(const AttArgs a) {
   extern __shared__ __align__(128) unsigned char smem[];
   constexpr int W = kAttWarps, Q = 8 * NT, kSums = Q * kAttPitch, kThreads = 32 * W, kRing = kAttDepth * kBlockBytes;
-  float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its sums where its rings were
-  static_assert(Q * kHeadDim * 4 <= W * kRing, "sums of a CTA fit the rings");
+  float* xo = reinterpret_cast<float*>(smem);   // [Q][128]: a cluster's CTA has its averages where its rings were
+  static_assert(Q * kHeadDim * 4 <= W * kRing, "averages of a CTA fit the rings");
   static_assert(kBlockBytes % 16 == 0, "tiles in the ring are 16-byte aligned");
   float* sums = reinterpret_cast<float*>(smem + W * kRing);   // [warps][Q][pitch]
   float* wm = sums + W * kSums;      // [warps][Q]
   float* wz = wm + W * Q;            // [warps][Q]
-  float* xm = wz + W * Q;            // [Q]
+  float* wu = wz + W * Q;            // [warps][Q]: what their sums of values are to be multiplied by
+  float* xm = wu + W * Q;            // [Q]
   float* xz = xm + Q;                        // [Q]
   float* allm = xz + Q;                      // [8][Q]
   float* allz = allm + kMaxCluster * Q;      // [8][Q]
-  float* wv = allz + kMaxCluster * Q;        // [warps]: units of their sums of values
-  float* xv = wv + W;                        // of the CTA's; [3] fill up
-  float* allv = xv + 4;                      // [8]
-  uint64_t* bars = reinterpret_cast<uint64_t*>(allv + kMaxCluster);   // [warps][depth]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(allz + kMaxCluster * Q);   // [warps][depth]
   int* rows = reinterpret_cast<int*>(bars + W * kAttDepth);   // [warps][depth]: first rows of the tiles
   int* abort = rows + W * kAttDepth;         // [4]
   float* up = reinterpret_cast<float*>(abort + 4);      // [Q]
@@ -624,7 +633,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
     }
 
     pdl_launch_dependents();      // (the next kernel's CTAs, where this one's have ended)
-    // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others
+    // ---- the warps merge through shared memory, the dimensions 16 g .. 16 g + 7 first and then the others.  What is handed on are averages
+    // of values, with the sum of weights that they stand for: no larger than the values, whatever the units were.
     float* own = sums + warp * kSums;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -633,8 +643,8 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
         const float z = column_sum(st.z[nt][c]);
         const int r = 8 * nt + 2 * t + c;
         if (g == 0) wm[warp * Q + r] = st.ref[nt][c], wz[warp * Q + r] = lost ? NAN : z;
+        if (g == 0) wu[warp * Q + r] = st.unit[nt][c] == kFine ? 1.f / kFine : 1.f / kCoarse;
       }
-    if (lane == 0) wv[warp] = st.vref;
     const bool whole = shares ? lo <= starts[u] && end == starts[u + 1] : S == 1;
     const int share = 2 * blockIdx.x + (shares && lo < starts[u]);   // (the first unit of a CTA, or its last)
 #pragma unroll
@@ -651,28 +661,30 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
       __syncthreads();
       for (int e = tid; e < live * (kHeadDim / 8); e += kThreads) {
         const int r = e / (kHeadDim / 8), x = 4 * (e % (kHeadDim / 8)), dim = 16 * (x >> 3) + 8 * half + (x & 7);
-        float M = kNoRef, unit = FLT_MIN;
+        float M = kNoRef, den = 0.f, sc[W];
 #pragma unroll
-        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]), unit = fmaxf(unit, wv[w]);
-        float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-        float den = 0.f;
+        for (int w = 0; w < W; ++w) M = fmaxf(M, wm[w * Q + r]);
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-          const float sc = ex2(wm[w * Q + r] - M);
-          add_scaled(num, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc * (wv[w] * inverse(unit)));
-          den = fmaf(wz[w * Q + r], sc, den);
+          sc[w] = ex2(wm[w * Q + r] - M);
+          den = fmaf(wz[w * Q + r], sc[w], den);
         }
+        const float by = one_over(den);
+        float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          add_scaled(mean, *reinterpret_cast<const float4*>(sums + w * kSums + r * kAttPitch + x), sc[w] * by * wu[w * Q + r]);
         if (whole) {
-          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
-          if (dim == 0) store_stat(a, u, first + r, M, den);
-          if (dim == 0 && !shares) stat[r] = make_float2(M, one_over(den));
+          store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, mean);
+          if (dim == 0) store_stat(a, u, first + r, M, by);
+          if (dim == 0 && !shares) stat[r] = make_float2(M, by);
         } else if (shares) {
           const long long at = (long long)share * a.R + first + r;
-          *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = num;
-          if (dim == 0) a.part_mz[at] = make_float4(M, den, unit, 0.f);
+          *reinterpret_cast<float4*>(a.part + at * kHeadDim + dim) = mean;
+          if (dim == 0) a.part_mz[at] = make_float2(M, den);
         } else {
-          *reinterpret_cast<float4*>(xo + r * kHeadDim + dim) = num;
-          if (dim == 0) xm[r] = M, xz[r] = den, *xv = unit;      // (the same for every r)
+          *reinterpret_cast<float4*>(xo + r * kHeadDim + dim) = mean;
+          if (dim == 0) xm[r] = M, xz[r] = den;
         }
       }
     }
@@ -701,31 +713,25 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
       const int k = e / Q, r = e % Q;
       allm[e] = *cluster.map_shared_rank(&xm[r], k);
       allz[e] = *cluster.map_shared_rank(&xz[r], k);
-      if (r == 0) allv[k] = *cluster.map_shared_rank(xv, k);
     }
     __syncthreads();
-    if (a.inside) {
-      for (int r = tid; r < live; r += kThreads) {
-        float M = kNoRef, den = 0.f;
-        for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
-        for (int k = 0; k < S; ++k) den = fmaf(allz[k * Q + r], ex2(allm[k * Q + r] - M), den);
-        stat[r] = make_float2(M, one_over(den));
-      }
+    for (int r = tid; r < live; r += kThreads) {
+      float M = kNoRef, den = 0.f;
+      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+      for (int k = 0; k < S; ++k) den = fmaf(allz[k * Q + r], ex2(allm[k * Q + r] - M), den);
+      stat[r] = make_float2(M, one_over(den));
     }
+    __syncthreads();
     for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
       const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
-      float M = kNoRef, unit = FLT_MIN;
-      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]), unit = fmaxf(unit, allv[k]);
-      float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-      float den = 0.f;
+      const float2 of = stat[r];
+      float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-      for (int k = 0; k < S; ++k) {
-        const float sc = ex2(allm[k * Q + r] - M);
-        add_scaled(num, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)), sc * (allv[k] * inverse(unit)));
-        den = fmaf(allz[k * Q + r], sc, den);
-      }
-      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, num, one_over(den), unit);
-      if (dim == 0) store_stat(a, u, first + r, M, den);
+      for (int k = 0; k < S; ++k)
+        add_scaled(mean, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)),
+                   allz[k * Q + r] * ex2(allm[k * Q + r] - of.x) * of.y);
+      store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, mean);
+      if (dim == 0) store_stat(a, u, first + r, of.x, of.y);
     }
     weigh();
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
@@ -745,7 +751,7 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
                                                                          const Divider per_row) {
   __shared__ float4 sums[kEndWarps][32];
   __shared__ float2 stat[MIXKV_CACHE8_MAX_QUERIES];      // (reference, 1 / sum)
-  __shared__ float4 of_warp[kEndWarps];                  // (reference, sum, unit, -)
+  __shared__ float2 of_warp[kEndWarps];                  // (reference, sum)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int u = by_unit.div(blockIdx.x), c = blockIdx.x - u * (int)by_unit.d;
   pdl_wait();
@@ -761,7 +767,7 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
       for (int r = warp * at_once + lane / lanes; r - lane / lanes < a.R; r += kEndWarps * at_once) {
         float M = kNoRef, den = 0.f;
         for (int k = c0 + at; k <= c1 && r < a.R; k += lanes) {
-          const float4 mz = __ldcg(a.part_mz + part_row(k, r));
+          const float2 mz = __ldcg(a.part_mz + part_row(k, r));
           const float to = fmaxf(M, mz.x);
           den = fmaf(den, ex2(M - to), mz.y * ex2(mz.x - to));
           M = to;
@@ -786,18 +792,14 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
   if (!joined) return;
   const int slot = per_row.div(warp), part = warp - slot * per_row.d, at_once = per_row.div(kEndWarps), r = c * at_once + slot;
   const bool on = r < a.R;
-  float M = kNoRef, den = 0.f, unit = FLT_MIN;
-  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
-  const auto move = [&](const float to, const float wide) {      // to another reference and another unit
-    const float shrink = ex2(M - to), by = shrink * (unit * inverse(wide));
-    num.x *= by, num.y *= by, num.z *= by, num.w *= by, den *= shrink;
-    M = to, unit = wide;
-  };
+  float M = kNoRef, den = 0.f;
+  float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
   constexpr int kAtOnce = 4;      // shares whose sums come in one round trip
 #pragma unroll 1
   for (int k = c0 + part; on && k <= c1; k += kAtOnce * per_row.d) {
-    float4 x[kAtOnce], mz[kAtOnce];
-    float to = M, wide = unit;
+    float4 x[kAtOnce];
+    float2 mz[kAtOnce];
+    float to = M;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
       const long long at = part_row(min(k + i * (int)per_row.d, c1), r);
@@ -805,31 +807,35 @@ __global__ void __launch_bounds__(kEndThreads, kEndPerSm) k_cache8_finish(const 
       x[i] = __ldcg(reinterpret_cast<const float4*>(a.part + at * kHeadDim) + lane);
     }
 #pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x), wide = fmaxf(wide, mz[i].z);
-    move(to, wide);
+    for (int i = 0; i < kAtOnce; ++i) to = fmaxf(to, mz[i].x);
+    const float had = den * ex2(M - to);
+    den = had;
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i) {
-      const float sc = k + i * (int)per_row.d <= c1 ? ex2(mz[i].x - M) : 0.f;
-      add_scaled(num, x[i], sc * (mz[i].z * inverse(unit)));
-      den = fmaf(mz[i].y, sc, den);
+      mz[i].y = k + i * (int)per_row.d <= c1 ? mz[i].y * ex2(mz[i].x - to) : 0.f;
+      den += mz[i].y;
     }
+    M = to;
+    const float by = one_over(den), old = had * by;
+    mean.x *= old, mean.y *= old, mean.z *= old, mean.w *= old;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) add_scaled(mean, x[i], mz[i].y * by);
   }
   if (per_row.d > 1) {
-    sums[warp][lane] = num;
-    if (lane == 0) of_warp[warp] = make_float4(M, den, unit, 0.f);
+    sums[warp][lane] = mean;
+    if (lane == 0) of_warp[warp] = make_float2(M, den);
     __syncthreads();
     if (part) return;
-    float to = M, wide = unit;
-    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, of_warp[warp + w].x), wide = fmaxf(wide, of_warp[warp + w].z);
-    move(to, wide);
-    for (int w = 1; w < (int)per_row.d; ++w) {
-      const float4 mz = of_warp[warp + w];
-      const float sc = ex2(mz.x - M);
-      add_scaled(num, sums[warp + w][lane], sc * (mz.z * inverse(unit)));
-      den = fmaf(mz.y, sc, den);
-    }
+    float to = M;
+    for (int w = 1; w < (int)per_row.d; ++w) to = fmaxf(to, of_warp[warp + w].x);
+    const float mine = den * ex2(M - to);
+    den = mine;
+    for (int w = 1; w < (int)per_row.d; ++w) den = fmaf(of_warp[warp + w].y, ex2(of_warp[warp + w].x - to), den);
+    const float by = one_over(den), old = mine * by;
+    mean.x *= old, mean.y *= old, mean.z *= old, mean.w *= old;
+    for (int w = 1; w < (int)per_row.d; ++w) add_scaled(mean, sums[warp + w][lane], of_warp[warp + w].y * ex2(of_warp[warp + w].x - to) * by);
   }
-  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, num, one_over(den), unit);
+  if (on) store_row(static_cast<T*>(a.out) + out_row(a, u, r) * kHeadDim + 4 * lane, mean);
 }
 
 using AttKernel = void (*)(AttArgs);
@@ -914,7 +920,7 @@ int att_plan(const mixkv_cache8* c, const int32_t q_tokens, const int32_t gqa, c
   const auto up = [](const size_t x) { return (x + 127) & ~(size_t)127; };
   const size_t shares = 2 * (size_t)att_slots(p->NT, false, p->sms);     // (the workspace serves either type)
   p->part = up(shares * R * kHeadDim * 4);
-  p->spans = up(p->part + shares * R * sizeof(float4));
+  p->spans = up(p->part + shares * R * sizeof(float2));
   p->stats = up(p->spans + kAttUnits * sizeof(int2));
   p->logits = up(p->stats + (accumulate ? (size_t)units * R * sizeof(float2) : 0));
   p->bytes = p->logits + (accumulate ? (size_t)units * p->cap * kBlockRows * p->pitch * 4 : 0);
@@ -977,7 +983,7 @@ extern "C" int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32
   a.window = window, a.sinks = sinks;
   a.units = (int)units, a.ctas = shape.ctas;
   a.scale_log2e = (softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim)) * kLog2e;
-  a.part = reinterpret_cast<float*>(ws), a.part_mz = reinterpret_cast<float4*>(ws + p.part);
+  a.part = reinterpret_cast<float*>(ws), a.part_mz = reinterpret_cast<float2*>(ws + p.part);
   a.spans = reinterpret_cast<int2*>(ws + p.spans), a.stats = reinterpret_cast<float2*>(ws + p.stats);
   a.logits = accumulate ? reinterpret_cast<float*>(ws + p.logits) : nullptr, a.cap = p.cap, a.pitch = p.pitch;
   a.out = out;

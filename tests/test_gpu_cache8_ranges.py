@@ -1,11 +1,11 @@
-"""The 8-bit attention where a row's weight is far below another's."""
+"""The 8-bit attention where blocks of values are of unlike size, and where a row's weight is far below another's."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import cache8_plain as plain
 from paper_2510_20707_b200 import binding
-from test_gpu_cache8 import TYPES, Cache, dev
+from test_gpu_cache8 import TYPES, Cache, dev, query
 
 pytestmark = pytest.mark.gpu
 
@@ -15,11 +15,17 @@ def attended(q, K, V, scale, window=0, sinks=0):
     - the fp32 logits: 128 products in eight sums, each off by 2^-23 of the products' magnitudes at most, and three products: less than 2^-19 of
       them, twice with the sum of weights;
     - few bits of fp16: weights are 2^6 times as large as the share of the heaviest at least, the smallest step is 2^-24: 2^-31 of the
-      heaviest, and never more than the weight."""
+      heaviest, and never more than the weight;
+    - a block with values above 2^64, of which a row gets something (2^-25 at least, of weights that sum to 2^31 at most for 2^17 rows: 2^-56):
+      the row's sums are kept times 2^-48, so another block's scale s, as 2^-48 s, is off by 2^-150, half of fp32's smallest step, its codes
+      are 448 at most, and the average is off by 448 2^(48 - 150) < 2^-93 (the large block's own rounding: 2^56 and more)."""
     ref, w, aw = plain.attention(q, K, V, scale, window, sinks)
     V = np.abs(np.asarray(V, np.float64))
     size = (np.abs(q) @ np.abs(np.asarray(K, np.float64)).T * scale).max(-1, keepdims=True)
-    return ref, aw, 2.0 ** -18 * size * aw + np.minimum(w, 2.0 ** -31) @ V
+    blocks = np.arange(0, len(V), plain.ROWS)
+    large = np.maximum.reduceat(V.max(-1), blocks) > 2.0 ** 64
+    coarse = (large & (np.add.reduceat(w, blocks, -1) > 2.0 ** -56)).any(-1, keepdims=True)
+    return ref, aw, 2.0 ** -18 * size * aw + np.minimum(w, 2.0 ** -31) @ V + coarse * 2.0 ** -93
 
 
 def close(got, want, dtype):
@@ -60,3 +66,75 @@ def test_a_long_tail_beside_a_block_of_large_values(dtype, tail):
     assert (out == out[:, :, :1]).all()
     want = attended(q.double().cpu().numpy()[0, :, :1], *c.rows_of(0, 0), 1.0)
     close(out[0, :, :1], want, dtype)
+
+
+SIZES = [(1e-20, 1e30), (1e30, 1e-20), (1e-36, 1e37), (1e37, 1e-36), (1.0, 1e20), (1e-30, 1.0)]
+
+
+@pytest.mark.parametrize("n,heads", [(17, 2), (65, 2), (513, 2), (30001, 8), (161, 1100)])
+@pytest.mark.parametrize("here,there", SIZES)
+def test_values_that_a_token_does_not_see_leave_its_outputs_alone(n, heads, here, there):
+    # the newest row, alone in its block, has values of another size: the token before it does not see it
+    c = Cache([[n] * heads], 32, "int8")
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    k, v = (torch.randn((n * heads, 128), generator=gen, device="cuda") for _ in range(2))
+    v.view(heads, n, 128)[:, :-1] *= here
+    v.view(heads, n, 128)[:, -1] *= there
+    put(c, k.bfloat16(), v.bfloat16())
+    q = query(1, 2, 3 * heads, "bf16", seed=n)
+    out = binding.cache8_attention(c.cache, q)
+    for h in range(0, heads, max(1, heads // 3)):
+        close(out[0, :, 3 * h:3 * h + 3], attended(q.double().cpu().numpy()[0, :, 3 * h:3 * h + 3], *c.rows_of(0, h), 128 ** -0.5), "bf16")
+
+
+@pytest.mark.parametrize("here,there", SIZES)
+def test_values_that_have_left_the_window(here, there):
+    # the second token does not see the first block any more, the sinks' block is of the other size again for one of the heads
+    for sinks in (0, 3):
+        c = Cache([[160, 400]], 16, "e4m3")
+        gen = torch.Generator(device="cuda").manual_seed(1)
+        k, v = (torch.randn((560, 128), generator=gen, device="cuda") for _ in range(2))
+        size = torch.full((560, 1), here, device="cuda")
+        size[:16], size[160:320] = there, there
+        v *= size
+        put(c, k.bfloat16(), v.bfloat16())
+        q = query(1, 2, 4, "bf16")
+        out = binding.cache8_attention(c.cache, q, window=240 if sinks else 144, sinks=sinks)
+        for h in range(2):
+            close(out[0, :, 2 * h:2 * h + 2], attended(q.double().cpu().numpy()[0, :, 2 * h:2 * h + 2], *c.rows_of(0, h), 128 ** -0.5,
+                                                      240 if sinks else 144, sinks), "bf16")
+
+
+@pytest.mark.parametrize("n", [64, 257, 5000])
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("here,there", SIZES)
+def test_values_without_weight_leave_the_outputs_alone(n, order, here, there):
+    # rows that are seen and get e^-200 of the weight by one query row, all of it by the other
+    c = Cache([[n]], 64, "int8")
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((n, 128), generator=gen, device="cuda") for _ in range(2))
+    some = (torch.arange(n, device="cuda") // 16) % 2 == 0
+    k[:, 0] = torch.where(some, 10.0, -10.0)
+    v *= torch.where(some, here, there).unsqueeze(1)
+    put(c, (k if order > 0 else k.flip(0)).bfloat16(), (v if order > 0 else v.flip(0)).bfloat16())
+    q = query(1, 1, 2, "bf16", gain=0.1)
+    q[0, 0, :, 0] = torch.tensor([10.0, -10.0])
+    out = binding.cache8_attention(c.cache, q, softmax_scale=1.0)
+    close(out[0], attended(q.double().cpu().numpy()[0], *c.rows_of(0, 0), 1.0), "bf16")
+
+
+def test_blocks_of_every_size():
+    # values from 1e-37 to 3e38, in no order, each seen by a query row that looks for it
+    n = 16 * 76
+    c = Cache([[n]], 64, "int8")
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    size = torch.from_numpy(np.random.default_rng(0).permutation(76) - 37.0).cuda()
+    v = (torch.rand((n, 128), generator=gen, device="cuda", dtype=torch.float64) + 1) * (10.0 ** size).repeat_interleave(16).unsqueeze(1)
+    k = torch.zeros((n, 128), device="cuda")
+    k[torch.arange(n), torch.arange(n) // 16] = 1.0
+    put(c, k.bfloat16(), v.bfloat16())
+    q = torch.zeros((1, 1, 76, 128), device="cuda")
+    q[0, 0, torch.arange(76), torch.arange(76)] = 300.0
+    q = q.bfloat16()
+    out = binding.cache8_attention(c.cache, q, softmax_scale=1.0)
+    close(out[0], attended(q.double().cpu().numpy()[0], *c.rows_of(0, 0), 1.0), "bf16")
