@@ -496,8 +496,9 @@ int mixkv_cache_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t 
  *   max_rows        upper bound on c->rows; rows beyond it do not exist for this call.  It steers how the rows of a head are
  *                   split
  *   accumulate      nonzero: adds to the mass of every row that a query row sees the weights it got, of all tokens and heads of
- *                   the group (needs c->mass_opt; sums in one order, the same every time).  A page that the table names for two heads or
- *                   sequences can lose what one of them gives it
+ *                   the group (needs c->mass_opt; sums in one order, the same every time).  A page that the table names for several heads
+ *                   or sequences (a prompt that they share) gets what each of them gives, one after the other in any order: the last bits
+ *                   of its masses may differ from call to call.  A mass below 2^-126 may become zero
  *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned
  * Logits, softmax statistics and sums are fp32; the weights enter the value sum as fp16 (for fp16 outputs as two such numbers) and the
  * mass as fp32.  softmax_scale 0 means

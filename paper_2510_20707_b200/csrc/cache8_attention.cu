@@ -397,8 +397,10 @@ struct AttState {
   }
 };
 
-// Adds to the mass of a unit's rows what they got, a thread a row at a time: of the tiles number(0 .. n - 1).  stat: (reference, 1 / sum)
-// of the query rows, there once ready() has been called (by the whole CTA), which the first rows' logits do not wait for.
+// Adds to the mass of a unit's rows what they got, a thread a row at a time: of the tiles number(0 .. n - 1) (a page's tiles lie one after
+// the other in the pool and in the masses).  stat: (reference, 1 / sum) of the query rows, there once ready() has been called (by the whole
+// CTA), which the first rows' logits do not wait for.  One addition a row of each unit, atomic since units may share a page: where they
+// do not, there is no order in which it could differ.
 template <int THREADS, typename Number, typename Ready>
 __device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const UnitTiles& ut, const float2* stat, const int n,
                                             const Number& number, const Ready& ready) {
@@ -406,7 +408,6 @@ __device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const
   const int in = threadIdx.x % kBlockRows;
   const bool fours = (a.pitch & 3) == 0;
   int at[kAtOnce];
-  float was[kAtOnce];
   const float* row[kAtOnce];
   float4 y[kAtOnce][2];
   const auto load = [&](const int r0) {
@@ -433,9 +434,6 @@ __device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const
       at[k] = i + k * kStep < n && t.tile >= 0 && t.row + in < ut.n ? t.tile : -1;
       row[k] = a.logits + (((long long)u * a.cap + tile) * kBlockRows + in) * a.pitch;
     }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k)     // (a page's tiles lie one after the other in the pool and in the masses)
-      if (at[k] >= 0) was[k] = fresh(a.p.mass + (long long)at[k] * kBlockRows + in);
     load(0);
   };
   // (what a query row does not see gets nothing of it, if it is NaN either)
@@ -462,7 +460,7 @@ __device__ __forceinline__ void add_weights(const AttArgs& a, const int u, const
     }
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k)
-      if (at[k] >= 0) a.p.mass[(long long)at[k] * kBlockRows + in] = was[k] + sum[k];
+      if (at[k] >= 0) atomicAdd(a.p.mass + (long long)at[k] * kBlockRows + in, sum[k]);
     i += kAtOnce * kStep;
     if (i < n) begin(i);
   }
