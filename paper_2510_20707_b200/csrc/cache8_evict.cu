@@ -303,14 +303,21 @@ extern "C" int mixkv_cache_evict(const mixkv_cache8* c, const mixkv_cache8* into
   a.budget = budget, a.budgets = budgets_opt, a.first = keep_first, a.last = keep_last, a.max_rows = max_rows;
   a.idx = idx, a.status = status_dev, a.slots = (int)slots, a.by_slots = Divider((uint32_t)slots);
   const long long room = (long long)c->max_pages * c->page_rows, rows = max_rows < room ? max_rows : room;
-  // CTAs of a head: as many as its rows are worth, and no more than one to an SM
+  constexpr size_t kMost = (size_t)kPickKeys * 4;
+  static std::atomic<bool> done[kMaxDevices];
+  const int dev = device_slot();
+  if (ensure_smem(k_cache8_pick, kMost, done, dev) != cudaSuccess) return MIXKV_ERR_CUDA;
+  // CTAs of a head: as many as its rows are worth, no more than one to an SM, and in clusters that are all resident at once (asked with
+  // the most shared memory: what is remembered does not depend on the call).  65536 rows, an eighth kept, us a call, with clusters that fit /
+  // with one CTA to every SM, of which some clusters wait: 16 heads 45.9 / 52.4, 18 47.8 / 55.6, 36 80.2 / 84.8.  A device that holds no
+  // cluster of a size would refuse the launch.
   int S = 1;
   while (S < kMaxCluster && S * (long long)kPickRows < rows && units * S * 2 <= device_sm_count()) S *= 2;
+  static ClusterFit fits;
+  while (S > 1 && units > fits.ask(k_cache8_pick, kPickThreads, kMost, S, dev)) S /= 2;
   const long long each = (rows + S - 1) / S;
   a.cached = (int)(each < kPickKeys ? each : kPickKeys);
   const size_t smem = (size_t)a.cached * 4;
-  static std::atomic<bool> done[kMaxDevices];
-  if (ensure_smem(k_cache8_pick, (size_t)kPickKeys * 4, done) != cudaSuccess) return MIXKV_ERR_CUDA;
   const cudaStream_t st = (cudaStream_t)stream;
   cudaError_t e = launch_pdl(k_cache8_pick, dim3((unsigned)(units * S)), dim3(kPickThreads), smem, st, S, a);
   const int tasks = (int)(units * slots);
