@@ -884,7 +884,8 @@ AttShape att_shape(const long long units, const int groups, const long long tile
   const long long full = even ? kAttEven : kAttMany, filled = full * all * S * 5 / (slots * 4);     // (0.8 of the slots count as all)
   const long long limit = filled > full ? full : filled < kAttFew ? kAttFew : filled;
   if (alone <= limit) return {S, 0};
-  if (units <= kAttUnits && groups < slots && units * tiles <= 0x7fffffffll) {
+  // (sums up to tiles + CTAs, and a step of a CTA's warps past the end, are kept in 32 bits)
+  if (units <= kAttUnits && groups < slots && units * tiles <= 0x7fffffffll - slots - kAttWarps) {
     const long long want = (units * tiles + kAttWarps * 4 - 1) / (kAttWarps * 4);     // (four tiles to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups)};
   }
