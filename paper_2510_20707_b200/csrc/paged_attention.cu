@@ -712,7 +712,8 @@ AttShape att_shape(const long long units, const int groups, const long long step
   } else if (NT == 1 && alone <= kAttManySteps) {
     return {S, 0, false};
   }
-  if (units <= kAttUnits && groups < slots && units * most <= 0x7fffffffll) {
+  // (sums up to steps + CTAs, and a step of a CTA's warps past the end, are kept in 32 bits)
+  if (units <= kAttUnits && groups < slots && units * most <= 0x7fffffffll - slots - kAttWide) {
     const long long want = (units * steps + kAttWarps * 2 - 1) / (kAttWarps * 2);     // (two steps to a warp)
     return {1, (int)(want < slots / groups ? want : slots / groups), false};
   }
