@@ -138,3 +138,28 @@ def test_blocks_of_every_size():
     q = q.bfloat16()
     out = binding.cache8_attention(c.cache, q, softmax_scale=1.0)
     close(out[0], attended(q.double().cpu().numpy()[0], *c.rows_of(0, 0), 1.0), "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("heads,n,where", [(2, 129, 128), (8, 20001, 20000), (8, 20001, 9000)])
+def test_a_block_of_nan_reaches_the_rows_that_see_it(dtype, code, heads, n, where):
+    # among the newest rows, where the first token does not see it; or before the window of the second one, block's last row first
+    c = Cache([[n] * heads], 64, code)
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    k, v = (torch.randn((n * heads, 128), generator=gen, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    v.view(heads, n, 128)[::2, where, 5] = float("nan")
+    put(c, k, v)
+    q = query(1, 2, 3 * heads, dtype)
+    last = where | 15                                    # of the block
+    window = 0 if where == n - 1 else n - 1 - last       # the first token sees rows from `last` on, the second from the next
+    c.cache.mass.fill_(0.0)
+    out = binding.cache8_attention(c.cache, q, window=window, accumulate=True).view(2, heads, 3, 128)
+    sees = 1 if where == n - 1 else 0
+    assert torch.isnan(out[sees, ::2]).all() and not torch.isnan(out[1 - sees]).any() and not torch.isnan(out[:, 1::2]).any()
+    assert not torch.isnan(c.cache.mass).any()           # (a value of NaN is in no weight)
+    for h in range(heads):
+        K, V = c.rows_of(0, h)
+        t = np.arange(2) if h % 2 else np.array([1 - sees])
+        ref = attended(q.double().cpu().numpy()[0, :, 3 * h:3 * h + 3], K, np.nan_to_num(V), 128 ** -0.5, window)
+        close(out.transpose(0, 1)[h][torch.from_numpy(t).cuda()], tuple(x[t] for x in ref), dtype)
