@@ -141,6 +141,9 @@ __device__ __forceinline__ void store_row(T* to, const float4& x) {
 }
 // (zero where there were no weights)
 __device__ __forceinline__ float one_over(const float den) { return den == 0.f ? 0.f : 1.f / den; }
+// The same but for two units of the last place (sums of weights are between 1 and 2^44), for the merge of a CTA's warps, which every unit
+// goes through: a division there took 0.9 us of a draft's 41.8, 0.2 of eight heads' of 2048 rows.
+__device__ __forceinline__ float about_one_over(const float den) { return den == 0.f ? 0.f : __fdividef(1.f, den); }
 __device__ __forceinline__ void store_stat(const AttArgs& a, const int u, const int r, const float ref, const float by) {
   if (a.logits) a.stats[(long long)u * a.R + r] = make_float2(ref, by);
 }
@@ -667,7 +670,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
           sc[w] = ex2(wm[w * Q + r] - M);
           den = fmaf(wz[w * Q + r], sc[w], den);
         }
-        const float by = one_over(den);
+        const float by = about_one_over(den);
         float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < W; ++w)
@@ -713,23 +716,37 @@ __global__ void __launch_bounds__(32 * kAttWarps, att_per_sm(NT, std::is_same<T,
       allz[e] = *cluster.map_shared_rank(&xz[r], k);
     }
     __syncthreads();
-    for (int r = tid; r < live; r += kThreads) {
-      float M = kNoRef, den = 0.f;
-      for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
-      for (int k = 0; k < S; ++k) den = fmaf(allz[k * Q + r], ex2(allm[k * Q + r] - M), den);
-      stat[r] = make_float2(M, one_over(den));
+    if (a.inside) {
+      for (int r = tid; r < live; r += kThreads) {
+        float M = kNoRef, den = 0.f;
+        for (int k = 0; k < S; ++k) M = fmaxf(M, allm[k * Q + r]);
+        for (int k = 0; k < S; ++k) den = fmaf(allz[k * Q + r], ex2(allm[k * Q + r] - M), den);
+        stat[r] = make_float2(M, one_over(den));
+      }
     }
-    __syncthreads();
     for (int e = crank * a.per + tid; e < min((crank + 1) * a.per, live * (kHeadDim / 4)); e += kThreads) {
       const int r = e / (kHeadDim / 4), dim = 4 * (e % (kHeadDim / 4));
-      const float2 of = stat[r];
+      float M = kNoRef, den = 0.f, share_z[kMaxCluster];
+      float4 x[kMaxCluster];
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k)
+        if (k < S) {
+          M = fmaxf(M, allm[k * Q + r]);
+          x[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k));
+        }
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k)
+        if (k < S) {
+          const float sc = ex2(allm[k * Q + r] - M);
+          share_z[k] = allz[k * Q + r] * sc, den = fmaf(allz[k * Q + r], sc, den);
+        }
+      const float by = one_over(den);
       float4 mean = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (int k = 0; k < S; ++k)
-        add_scaled(mean, *reinterpret_cast<const float4*>(cluster.map_shared_rank(xo + r * kHeadDim + dim, k)),
-                   allz[k * Q + r] * ex2(allm[k * Q + r] - of.x) * of.y);
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k)
+        if (k < S) add_scaled(mean, x[k], share_z[k] * by);
       store_row(static_cast<T*>(a.out) + out_row(a, u, first + r) * kHeadDim + dim, mean);
-      if (dim == 0) store_stat(a, u, first + r, of.x, of.y);
+      if (dim == 0) store_stat(a, u, first + r, M, by);
     }
     weigh();
     cluster.sync();   // a CTA's shared memory stays alive until its peers have read it
