@@ -63,10 +63,16 @@ __host__ __device__ constexpr size_t att_smem(int NT) {
   return kAttWarps * (kAttDepth * kBlockBytes + 8 * NT * kAttPitch * 4) + (3 * kAttWarps + 2 + 2 * kMaxCluster) * 8 * NT * 4 +
          kAttWarps * kAttDepth * 16 + 16 + 8 * NT * 4 + (att_held(NT) ? 0 : 8 * NT * kHeadDim * 2);
 }
-// CTAs of an SM, which sets the registers of a thread.  One group of query rows: four CTAs of 128 registers, 64 heads of 4096 rows 16.0 us for
-// 16.7 with three, 8 of 16384 16.2 for 17.5, 256 of 8704 on average 133.6 for 131.6.  Two groups: three of 168, with weights in two parts (60
-// bytes spilt) two of 254: 256 heads of 70 to 1639 rows 40.0 us for 41.9, 64 of 2048 16.4 for 18.1, 256 of 1024 on average 34.2 for 33.1.
-__host__ __device__ constexpr int att_per_sm(int NT, bool half) { return NT == 1 ? 4 : NT == 2 && !half ? 3 : 2; }
+// CTAs of an SM, which sets the registers of a thread.  us a call, one token of four query heads unless said.
+// One group of query rows, bf16: four of 128 registers for three, 256 heads of 1024 rows 18.7 for 20.7, of 2048 29.0 for 30.2, 32 of 4096
+// 14.6 for 15.1; but 64 of one to 8192 rows 24.9 for 21.8 (att_shape then deals all tiles out), 8 of 2048 9.3 for 8.7.
+// fp16, whose weights take more registers: three of 168 for four, which spill 28 bytes, 8 heads of 2048 8.8 for 9.7, 256 of 2048 31.4 for 31.7,
+// of 8704 98.6 for 99.8, 64 of one to 8192 22.2 for 27.3; but 256 of 1024 21.3 for 20.0.
+// Two groups (two tokens of seven query heads): two for three, which spill 48 bytes with bf16 and 60 with fp16, bf16 64 heads of 2048 16.1 for
+// 17.5, 256 of 1024 21.9 for 28.3, of 70 to 1639 28.0 for 29.0, of 1639 36.7 for 36.2; fp16 64 of 2048 16.4 for 18.1, 256 of 70 to 1639
+// 40.0 for 41.9, of 1024 34.2 for 33.1.  More groups: 255 registers, the most there are.
+__host__ __device__ constexpr int att_per_sm(int NT, bool half) { return NT > 1 ? 2 : half ? 3 : 4; }
+static_assert(att_per_sm(1, false) >= att_per_sm(1, true), "a workspace has room for the shares of bf16 outputs, whatever the type");
 
 struct AttArgs {
   CachePool p;
@@ -871,20 +877,24 @@ AttKernel att_kernel(const bool bf16, const bool e4m3, const int NT) {
 // How the work is split.  units: (sequence, head) pairs; groups of query rows; tiles of the longest unit; even: a window cuts long units
 // to one length.  resident(n): clusters of n CTAs that are resident at once.
 //
-// A cluster per unit, or all tiles dealt out evenly and joined by a second kernel, which costs a call 4 us.  us a call, one token of
-// four query heads, heads of one length (and of lengths from one row to that), clusters / shares:
+// A cluster per unit, or all tiles dealt out evenly and joined by a second kernel.  us a call, one token of four query heads, bf16, heads of
+// one length (and of lengths from one row to that), clusters / shares:
 //     heads x rows    no weights                        weights counted
-//     8 x 2048         8.7 / 10.5   (8.5 / 11.7)                                        four tiles a warp on 64 CTAs (of 592 at once)
-//     8 x 4096        11.8 / 11.0  (11.6 / 11.7)        14.1 / 11.8  (13.8 / 12.5)      eight on 64
-//     32 x 4096       14.8 / 15.7  (13.5 / 14.8)        16.6 / 17.0  (16.5 / 16.3)      eight on 256
-//     32 x 8192       24.6 / 21.6  (20.1 / 18.3)                                        sixteen on 256
-//     64 x 4096       18.6 / 21.8  (16.0 / 17.8)        21.3 / 25.3  (18.9 / 20.8)      eight on 512
-//     256 x 1024      18.5 / 22.1  (16.1 / 19.9)        21.3 / 25.4  (19.0 / 22.7)      eight on 512
-//     64 x 8192       29.0 / 31.3  (24.5 / 22.6)        34.1 / 37.1  (29.5 / 27.3)      sixteen on 512
-//     256 x 2048      28.8 / 31.2  (24.7 / 24.6)        34.1 / 36.9  (29.8 / 29.1)      sixteen on 512
+//     8 x 2048         8.5 / 10.0   (8.4 / 11.3)                                        four tiles a warp on 64 CTAs (of 592 at once)
+//     8 x 4096        11.7 / 10.4  (11.7 / 11.0)        14.0 / 11.5  (13.9 / 12.2)      eight on 64
+//     32 x 4096       15.7 / 15.0  (13.4 / 14.1)        16.5 / 16.7  (16.2 / 16.0)      eight on 256
+//     32 x 8192       24.5 / 20.8  (20.6 / 17.4)                                        sixteen on 256
+//     64 x 4096       18.2 / 21.0  (15.8 / 17.2)        21.0 / 24.9  (18.6 / 20.5)      eight on 512
+//     256 x 1024      18.3 / 21.4  (16.0 / 19.4)        21.0 / 25.4  (18.9 / 22.9)      eight on 512
+//     64 x 8192       28.7 / 30.6  (24.3 / 21.9)        34.3 / 36.8  (29.7 / 26.8)      sixteen on 512
+//     256 x 2048      28.6 / 30.7  (24.8 / 23.9)        34.3 / 36.6  (30.3 / 28.8)      sixteen on 512
 // So clusters up to sixteen tiles a warp where they fill the GPU, and up to fewer where they do not, but for six; up to 24 where a window
-// cuts the heads to one length (128 heads of a window of 4096 29.8 / 32.8).  More query rows, clusters / shares: 32 of them, 64 x 8192
-// 52 / 60 (50 / 46), 8 x 8192 26.3 / 21.5 (25.9 / 25.8).
+// cuts the heads to one length (4096 rows seen: 128 heads 29.3 / 32.1, 64 heads 18.8 / 22.4; 2048 rows: 256 heads 29.5 / 32.1; 8192 rows:
+// 32 heads, 64 tiles a warp, 25.5 / 22.0).
+// More query rows, and a head's CTAs fewer: 32 of them, 64 x 8192 55.6 / 60.6 (52.2 / 43.9), 64 x 4096 32.9 / 40.0 (30.9 / 32.9), 8 x 8192 26.3 /
+// 19.1 (25.9 / 20.6); fourteen, 256 x 1639 31.3 / 36.2 (29.9 / 27.3), 256 x 1024 21.6 / 27.1 (20.7 / 23.1).  The rule is the same: where it
+// takes shares, heads of one length lose up to a seventh, and heads of unlike length, as budgets of their own leave them, gain as much.
+// fp16, with three CTAs an SM: 256 x 1024 19.6 / 21.0 (17.9 / 18.0), 64 x 8192 30.8 / 31.5 (26.6 / 21.7), 256 x 2048 33.5 / 31.1 (31.6 / 23.1).
 struct AttShape {
   int S, ctas;      // CTAs of a cluster that has a unit; or, not 0, CTAs that share all tiles
 };

@@ -18,7 +18,7 @@ def is_dealt_out(units, R, rows, T, window, sinks, dtype, sms=148):
     eights = -(-R // 8)
     groups = -(-eights // 4)
     NT = -(-eights // groups)
-    slots = (4 if NT == 1 else 3 if NT == 2 and dtype != "fp16" else 2) * sms
+    slots = (2 if NT > 1 else 3 if dtype == "fp16" else 4) * sms
     tiles = -(-rows // 16)
     some = -(-sinks // 16) + (window + T - 1 + 14) // 16 + 1
     even = window > 0 and some < tiles
@@ -75,7 +75,7 @@ def test_all_tiles_dealt_out(dtype, code, T, G, page, B, H, lo, hi):
 # a gap inside units: rows of the window and the sinks numbered one after the other over CTAs' borders
 @pytest.mark.parametrize("dtype,code,T,G,page,lens,window,sinks", [
     ("bf16", "int8", 1, 4, 64, [[20000, 20000, 20000]], 16000, 100), ("fp16", "e4m3", 3, 4, 32, [[30000, 25000, 17000, 40]], 20000, 33),
-    ("bf16", "e4m3", 2, 7, 16, spread(6, 5, 0, 20000, 1), 9000, 4), ("fp16", "int8", 5, 7, 64, spread(8, 4, 1, 9000, 2), 7000, 64),
+    ("bf16", "e4m3", 2, 7, 16, spread(6, 5, 0, 20000, 1), 14000, 4), ("fp16", "int8", 5, 7, 64, spread(8, 4, 1, 9000, 2), 7000, 64),
     ("bf16", "int8", 1, 1, 48, [[50000, 3], [0, 49999]], 30000, 0), ("bf16", "e4m3", 16, 8, 128, spread(3, 3, 10, 20000, 3), 15000, 17)])
 def test_all_tiles_of_windows_dealt_out(dtype, code, T, G, page, lens, window, sinks):
     attend_and_check(lens, page, code, dtype, T, G, window, sinks)
