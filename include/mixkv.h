@@ -467,8 +467,9 @@ int mixkv_cache_page_bytes(int32_t page_rows, size_t* bytes);
  * head.  Strides in elements, multiples of 16; k and v 32-byte aligned.
  * Rows that join a block which has rows: its scale becomes the larger of its own and that of the new rows, and if it grows, the codes of
  * its old rows are rounded again, from fp32(code * old scale).  A block that begins with a new row is set, whatever was there.  The mass
- * of new rows (if there is any) is set to zero.
- * Rows are taken back (a draft's rejected tokens) by counting them out of c->rows; the scale of a block that keeps rows stays.
+ * of new rows (if there is any) is set to zero; a caller who has scores for them writes these behind the call.
+ * Rows are taken back (a draft's rejected tokens) by counting them out of c->rows; the scale of a block that keeps rows stays, and so does
+ * what the rows' queries have added to masses.
  * Of more than max_new new rows of a head the last are written.  These others, and tokens whose place (table entry outside the pool, row
  * beyond the table or below zero, token not in k) does not exist, are not written and give MIXKV_ERR_INVALID_ARG in *status_dev.
  * Pages are written by one call at a time. */
@@ -498,13 +499,16 @@ int mixkv_cache_workspace_size(const mixkv_cache8* c, int32_t q_tokens, int32_t 
  *   accumulate      nonzero: adds to the mass of every row that a query row sees the weights it got, of all tokens and heads of
  *                   the group (needs c->mass_opt; sums in one order, the same every time).  A page that the table names for several heads
  *                   or sequences (a prompt that they share) gets what each of them gives, one after the other in any order: the last bits
- *                   of its masses may differ from call to call.  A mass below 2^-126 may become zero
+ *                   of its masses may differ from call to call.  A mass below 2^-126 may become zero.  What a call has added
+ *                   stays: a draft's tokens that are rejected afterwards leave their weights on the rows they saw (a caller who does
+ *                   not want that checks the draft without, counts the rejected rows out and calls again for the tokens that
+ *                   stay), and a row that has a mass of NaN keeps it, which an eviction ranks above all others
  *   out             device, type `type`, contiguous [batch, q_tokens, kv_heads * gqa_ratio, 128], 16-byte aligned
- * Logits, softmax statistics and sums are fp32; the weights enter the value sum as fp16 (for fp16 outputs as two such numbers) and the
- * mass as fp32.  softmax_scale 0 means
- * 1 / sqrt(128).  A page outside the pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that
- * sees a NaN, is NaN (as is the mass of the rows it sees), and so is what a wait inside the kernel ran out on (there is no status
- * word). */
+ * Logits, softmax statistics and sums are fp32; the weights enter the value sum as fp16 (for fp16 outputs as two such numbers; one below
+ * 2^-31 of its query row's largest may be lost there) and the mass as fp32.  softmax_scale 0 means 1 / sqrt(128).  A page outside the
+ * pool counts as a page without rows.  A query row that holds a NaN or an infinity, or one that sees a block of NaN, is NaN (and, unless
+ * the NaN is among the values, gives NaN to the mass of the rows it sees), and so is what a wait inside the kernel ran out on (there
+ * is no status word). */
 int mixkv_cache_attention(const mixkv_cache8* c, const void* q, int32_t type, int64_t q_batch_stride,
                            int64_t q_token_stride, int32_t q_tokens, int32_t gqa_ratio, float softmax_scale,
                            int32_t max_rows, int32_t window, int32_t sinks, int32_t accumulate, void* workspace,

@@ -521,7 +521,8 @@ def cache8_attention(cache: Cache8, q: torch.Tensor, max_rows: Optional[int] = N
     """mixkv_cache_attention: q [batch, tokens, kv_heads * gqa_ratio, 128] bf16 or fp16, the newest tokens of every sequence
     (append theirs first) -> the same shape and type.  ``max_rows``: upper bound on ``cache.rows`` (default: what the table has room
     for).  ``window`` > 0: a token sees the last ``window`` rows up to its own, and the first ``sinks``.  ``accumulate``: what every
-    row got of the softmax's weight, over tokens and heads of the group, is added to ``cache.mass``."""
+    row got of the softmax's weight, over tokens and heads of the group, is added to ``cache.mass``; it stays there if tokens of a draft
+    are rejected afterwards (check it without, and call again with the tokens that stay)."""
     return (_host_module or _host()).cache8_attention(cache, q, _seen_rows(cache, max_rows), window, sinks, accumulate,
                                                       softmax_scale, workspace, stream)
 

@@ -14,8 +14,9 @@ namespace mixkv {
 namespace {
 
 constexpr int kRowWarps = 4;
-// CTAs of an SM that appends, which sets the registers of a thread: 32768 rows of four heads 17.9 us with ten (48 registers), 20.3 with six
-// (79, what the compiler takes), 21.7 and 22.0 with eight and nine, 22.9 with twelve (40, which spill), 31 with sixteen.
+// CTAs of an SM that appends, which sets the registers of a thread: 32768 rows of four heads 17.9 us with ten (48 registers, 24 bytes
+// spilt), 20.3 with six (79, what the compiler takes), 21.7 and 22.0 with eight and nine (56, 8 bytes), 22.9 with twelve (40, 132 bytes), 31
+// with sixteen.
 constexpr int kAppendPerSm = 10;
 
 struct RowArgs {

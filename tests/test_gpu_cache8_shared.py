@@ -1,4 +1,4 @@
-"""Pages of the 8-bit cache that several sequences share: what each of them gives a row counts."""
+"""Masses of the 8-bit cache: pages that several sequences share get what each of them gives; what a draft has given stays."""
 import numpy as np
 import pytest
 import torch
@@ -64,3 +64,29 @@ def test_a_head_whose_pages_are_all_one():
     K, V = c.rows_of(0, 0)
     w = plain.attention(q.double().cpu().numpy()[0], K, V, 128 ** -0.5)[1].sum((0, 1)).reshape(40, 64).sum(0)
     assert np.allclose(m, w, rtol=1e-4) and abs(m.sum() - 8) < 1e-4
+
+
+def test_weights_of_a_draft():
+    # five tokens are checked, two of them stay
+    c = Cache([[300, 77]], 32, "int8")
+    c.fill()
+    c.cache.mass.fill_(0.0)
+    q = query(1, 5, 8, "bf16")
+    weights = lambda T, n: [plain.attention(q.double().cpu().numpy()[0, :T, 4 * h:4 * h + 4], *(x[:n[h]] for x in c.rows_of(0, h)),
+                                            128 ** -0.5)[1].sum((0, 1)) for h in range(2)]
+    out = binding.cache8_attention(c.cache, q)
+    assert (c.cache.mass == 0).all()
+    c.cache.rows -= 3
+    again = binding.cache8_attention(c.cache, q[:, :2], accumulate=True)
+    # (the same rows for each token; how the work is split may differ, and with it an output's last bit)
+    assert torch.allclose(out[:, :2].float(), again.float(), rtol=2.0 ** -7, atol=1e-5)
+    for h, w in enumerate(weights(2, [297, 74])):
+        m = c.mass_of(0, h)
+        assert np.allclose(m[:len(w)], w, rtol=1e-4, atol=1e-7) and (m[len(w):] == 0).all()
+    # with the weights at once, those of the rejected tokens stay on the rows that stay
+    c.cache.mass.fill_(0.0)
+    c.cache.rows += 3
+    binding.cache8_attention(c.cache, q, accumulate=True)
+    c.cache.rows -= 3
+    for h, w in enumerate(weights(5, [300, 77])):
+        assert np.allclose(c.mass_of(0, h), w, rtol=1e-4, atol=1e-7)
