@@ -10,22 +10,24 @@
 //
 // Softmax: a running reference per query row, moved only when a logit exceeds it by more than 2^kLag (one vote a step instead of
 // a reduction); weights are fp16 times 2^kLift, sums are fp32.  For bf16 outputs a weight is ONE fp16 number: its rounding, 2^-11 of it, is an
-// eighth of the output's own.  For fp16 outputs it would be as large as that (2.9e-4 from 64 bits where the outputs' rounding makes
-// 2.1e-4, up to 1.7 times that where one row has most of the weight): there a weight is two of them, for 4 to 11 % of a call's time.
+// eighth of the output's own (0.0017 from 64 bits as with fp32 weights; two would cost 7 to 10 % of most calls' time, 1 % of one that counts
+// weights over 256 long heads, 23 % with 32 query rows).  For fp16 outputs it would be as large as that (2.9e-4 from 64 bits where the outputs'
+// rounding makes 2.1e-4, up to 1.7 times that where one row has most of the weight): there a weight is two of them, for 2 to 5 % of a call's
+// time with one group of query rows, 12 with 35 rows, 24 with 32 over 64 heads.
 //
 // Weights of rows: what a row got is known when the sums are, so the logits go to the workspace as fp32 (R of them for a row of 257
 // bytes), and the exponentials of one row's, taken in a fixed order, are added to the row's mass once all tiles have been read: by the
 // clusters themselves, or by the kernel that joins the shares.
 //
-// What bounds it.  A row pair is 257 bytes, a tile of 16 costs a warp 390 instructions with int8 and 98 fewer with e4m3 (whose widening needs no
-// subtraction).  256 heads of 1021 to 16384 rows (571 MB) take 104 us in this kernel under the profiler, weights counted: 5.7 TB/s, an instruction
-// issued in 60 % of the clocks, the arithmetic pipe busy in 51, the tensor pipe in 18.  Without weights the call takes 103 us, and 93 with
-// the same copies and no arithmetic; 8 heads of 131072 rows 48.5 and 45.  Few or short heads are bounded by the chain from rows to table to
-// tiles, the merge and the join (8 heads of 2048 rows 8.7 us, 5.2 without arithmetic); drafts by eight warps an SM, which 255 registers leave
-// (35 query rows: issue slots 41 %, tensor pipe 36 %).  Loads that L2 evicts first: 8 heads of 131072 rows 49.6 us for 52.
+// What bounds it.  A row pair is 257 bytes, a tile of 16 costs a warp 426 instructions with int8, all told, and 335 with e4m3 (whose widening
+// needs no subtraction).  256 heads of 1021 to 16384 rows (587 MB) take 104 us in this kernel under the profiler, weights counted: 5.7 TB/s, an
+// instruction issued in 60 % of the clocks, the arithmetic pipe busy in 50, the tensor pipe in 18.  Without weights the call takes 101 us (an earlier
+// build 103, and 93 with the same copies and no arithmetic); 8 heads of 131072 rows 49.2 (48.5 and 45).  Few or short heads are bounded by the chain
+// from rows to table to tiles, the merge and the join (8 heads of 2048 rows 8.5 us; 8.7 and 5.2); drafts by eight warps an SM, which 255
+// registers leave (35 query rows: issue slots 40 %, tensor pipe 33 %).  Loads that L2 evicts first: 8 heads of 131072 rows 49.6 us for 52.
 //
-// Measured and not taken: two tiles a softmax step (256 heads 133 us for 131, 64 of 4096 rows 24.8 for 23.3); four warps in step on four
-// tiles, each with 32 dimensions of all of them, so that warps need no merge (145 for 131, a draft 40 for 38: every warp then prepares every
+// Measured and not taken, of earlier builds: two tiles a softmax step (256 heads 133 us for 131, 64 of 4096 rows 24.8 for 23.3); four warps in step on
+// four tiles, each with 32 dimensions of all of them, so that warps need no merge (145 for 131, a draft 40 for 38: every warp then prepares every
 // tile); forty query rows in one CTA, their queries in shared memory (a draft 42.6 for 36.5); two chains of products for two groups of query rows
 // (nothing); weights in two parts only where a heavy one is among them (a draft 41.3 for 41.7, with 1.2 times the error).
 #include <cfloat>
